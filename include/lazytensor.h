@@ -54,10 +54,13 @@ typedef enum {
     LT_ERR_UNSUPPORTED = 5,   /* op or shape outside what the kernels implement          */
     LT_ERR_OOM = 6,           /* the allocator callback returned NULL                    */
     LT_ERR_CUDA = 7,          /* a CUDA runtime call failed (message has the CUDA text)  */
-    LT_ERR_DEVICE_TIMEOUT = 8 /* a bounded device-side wait gave up: reported by the first blocking call
+    LT_ERR_DEVICE_TIMEOUT = 8, /* a bounded device-side wait gave up: reported by the first blocking call
                                  (lt_barrier with blocking set, lt_fetch) after a long-row kernel ran out
                                  of time waiting for a copy into shared memory, or for the partial results
                                  of the other thread blocks of its cluster                                */
+    LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes:
+                                 reported by the first blocking call after the operator that met it, which left
+                                 out what the index named and did the rest                                */
 } lt_status;
 
 typedef enum { LT_F32 = 0, LT_BF16 = 1, LT_U8 = 2, LT_I32 = 3, LT_U32 = 4 } lt_dtype;
@@ -111,7 +114,45 @@ typedef enum {
        PERMUTE: attrs = {p0, .., p(rank-1)}: result dimension i is input dimension p_i.
        UPDATE_SLICE: 2 inputs (base, update), attrs = {dim, start}: base with the slice of update's extent along
        dim, starting at start, replaced by update -- the inverse of NARROW. */
-    LT_OP_RESHAPE = 60, LT_OP_NARROW = 61, LT_OP_PERMUTE = 62, LT_OP_UPDATE_SLICE = 63
+    LT_OP_RESHAPE = 60, LT_OP_NARROW = 61, LT_OP_PERMUTE = 62, LT_OP_UPDATE_SLICE = 63,
+    /* Transformer operators: each runs as kernels of its own on f32 or bf16 data and computes in binary32 (sums,
+       statistics and rotations), rounding once when a result is stored.  They take up to six inputs.  Where the list
+       ends with [out], one more input may follow: a tensor of the result's shape and dtype whose value is not read;
+       lt_assign the result to it and the barrier writes the result into its buffer.  Binary64 attributes travel as
+       their 64-bit patterns.  Row operands (marked *) may be LT_OP_NARROW slices of materialised data whose rows are
+       single runs -- one third of a packed [tokens, heads, head size] projection, say -- and are read in place.
+
+       ROTARY: inputs (x* [T, .., D], positions i32 [T], frequencies u32 [P, 2], [out]), attrs {interleaved, inverse,
+       scale}.  The first 2 P values of every head turn in pairs by the angle position x frequency: (a, b) becomes
+       scale (a cos - b sin, a sin + b cos); the rest passes through.  A pair is (i, i + P), or (2 i, 2 i + 1) with
+       `interleaved`.  A frequency is a 64-bit fixed-point fraction of a full turn per position (low word, high word):
+       position x frequency modulo 2^64 is the angle without loss at any distance.  `inverse` turns backwards, which
+       is also the gradient.
+
+       CACHE_APPEND: inputs (cache [pages, 2, page, H, D], k* [T, H, D], v* [T, H, D], slots i32 [T] [, positions i32
+       [T], frequencies u32 [P, 2]]), attrs {head_major, interleaved, scale}.  The cache with k (rotated, if positions
+       are given) and v of token t at slot slots[t] = page number x page + place in the page.  With head_major the cache is
+       [pages, 2, H, page, D].  A negative slot drops the token (padding); one beyond the cache is left out and
+       reported as LT_ERR_DEVICE_INDEX.  Slots that are not negative are distinct: of two tokens for one slot, either
+       may end up there, in parts.  lt_assign the result to the cache and only the slots are written.
+
+       PAGED_ATTENTION: inputs (q* [B, Hq, D], cache, page table i32 [B, M], lengths i32 [B], [out]), attrs
+       {head_major, scale} -> [B, Hq, D]: softmax(scale q k) v of one query token per sequence and head over the first
+       lengths[b] tokens, which lie in the pages the table's row b lists in order; Hq is a multiple of the cache's H and
+       D at most 256.  An empty sequence gives zeros.  Entries of the table behind a sequence's last page are not read.
+       A negative length counts as 0; one beyond M pages is cut there and, like a page number outside the cache (its
+       tokens are left out), reported as LT_ERR_DEVICE_INDEX.
+
+       RMS_NORM: inputs (x* [.., C] [, residual* [.., C]], gamma [C] f32 or like x, [out]), attrs {result, has residual,
+       group, eps}.  h = x + residual, y = gamma h / sqrt(mean(h^2) + eps).  result 0: y; 1: h; 2: y in 8 bits, as the
+       codes (u8) of float8 e4m3: round(y / scale); 3: the scales f32 [.., groups] = max|y| / 448 over each `group`
+       columns (32, 64, 128, 256; 0: the whole row; the last group may be shorter).  A group of zeros has scale 0 and
+       codes 0.  Nodes that differ only in `result` (and [out]) are one launch.
+
+       RMS_NORM_GRAD: inputs (dy* [.., C], h* [.., C], gamma [C] [, dh* [.., C]], [out]), attrs {result, has dh, eps}.
+       result 0: the gradient of h (of x and of the residual alike), plus dh, the gradient that reaches h past the
+       norm; 1: the gradient of gamma, in gamma's dtype.  Also one launch for both. */
+    LT_OP_ROTARY = 70, LT_OP_CACHE_APPEND = 71, LT_OP_PAGED_ATTENTION = 72, LT_OP_RMS_NORM = 73, LT_OP_RMS_NORM_GRAD = 74
 } lt_opcode;
 
 /*
@@ -298,12 +339,14 @@ lt_status lt_release_many(lt_ctx *ctx, const lt_tensor *handles, size_t n);
  *                        handle is written to results[k] and belongs to the caller, otherwise the result is a temporary
  *                        of the batch, released when the batch has been recorded (results[k] = 0)
  *   LT_BATCH_ASSIGN      lt_assign(in[0], in[1]); no result
+ *   LT_BATCH_MORE        the fourth to sixth operand (n_in of them) of the entry right after it, whose n_in counts all
  * Exactly equivalent to making the calls one by one in order and then releasing the temporaries in order (the graph,
  * its hash and what trace matching sees are the same).  On an error the entries recorded so far are undone as far as
  * their results go (released) and the status of the failing call is returned; assignments already made stay.
  * `results` has n_ops entries.  Arrays are the caller's and only read during the call.
  */
 #define LT_BATCH_ASSIGN (-1)
+#define LT_BATCH_MORE (-2)
 typedef struct {
     int32_t opcode;
     int32_t n_in;

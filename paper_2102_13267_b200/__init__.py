@@ -11,7 +11,9 @@ callbacks) and for the CUDA stream the kernels are enqueued on.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+import struct
 from pathlib import Path
 
 import numpy as np
@@ -39,9 +41,11 @@ OPCODES = {
     "convert": 40, "iota": 41, "philox_bits": 42, "row_sum": 50, "row_max": 51, "row_min": 52,
     "col_sum": 53, "col_max": 54, "col_min": 55, "all_sum": 56, "all_max": 57, "all_min": 58,
     "reshape": 60, "narrow": 61, "permute": 62, "update_slice": 63,
+    "rotary": 70, "cache_append": 71, "paged_attention": 72, "rms_norm": 73, "rms_norm_grad": 74,
 }
 STATUS_NAMES = ["LT_OK", "LT_ERR_INVALID_ARG", "LT_ERR_SHAPE", "LT_ERR_DTYPE", "LT_ERR_DEVICE",
-                "LT_ERR_UNSUPPORTED", "LT_ERR_OOM", "LT_ERR_CUDA", "LT_ERR_DEVICE_TIMEOUT"]
+                "LT_ERR_UNSUPPORTED", "LT_ERR_OOM", "LT_ERR_CUDA", "LT_ERR_DEVICE_TIMEOUT",
+                "LT_ERR_DEVICE_INDEX"]
 
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
@@ -57,6 +61,8 @@ class lt_batch_op(ctypes.Structure):
 
 
 LT_BATCH_ASSIGN = -1
+LT_BATCH_MORE = -2
+LT_OPERATOR_INPUTS = 6  # the most operands an operation takes (the transformer operators; the others take up to three)
 
 
 class lt_stats(ctypes.Structure):
@@ -219,6 +225,108 @@ class LazyTensor:
         return self.ctx.fetch(self)
 
 
+def rotary_table(rotated: int, base: float = 10000.0, kind: str = "none", factor: float = 1.0, original_length: int = 0,
+                 low: float = 1.0, high: float = 4.0) -> np.ndarray:
+    """Frequencies of rotary positions, as the operators `rotary` and `cache_append` take them: u32 [rotated / 2, 2], each
+    the 64-bit fixed-point fraction of a full turn per position.  Pair i turns by base^(-2i / rotated) radians per position,
+    changed for contexts longer than the trained one by `kind`:
+
+    "none";  "linear": divided by `factor`;  "base": the base is multiplied by factor^(rotated / (rotated - 2));
+    "parts": a pair that makes more than `high` turns within `original_length` positions keeps its frequency, one that
+    makes fewer than `low` is divided by `factor`, in between the two are mixed linearly in the number of turns.
+    """
+    if rotated < 2 or rotated % 2:
+        raise ValueError("rotary positions turn pairs: an even number of values")
+    if not (base > 0 and math.isfinite(base) and factor > 0 and math.isfinite(factor)):
+        raise ValueError("base and factor are positive numbers")
+    if kind not in ("none", "linear", "base", "parts"):
+        raise ValueError(f"unknown kind of scaling {kind!r}")
+    if kind == "parts" and not (original_length > 0 and high > low):
+        raise ValueError("scaling by parts needs the original length, and high above low")
+    if kind == "base":
+        if rotated == 2:
+            raise ValueError("scaling the base needs more than one pair")
+        base = base * factor ** (rotated / (rotated - 2))
+    out = np.empty((rotated // 2, 2), dtype=np.uint32)
+    for i in range(rotated // 2):
+        f = float(base) ** (-2.0 * i / rotated)
+        if kind == "linear":
+            f /= factor
+        elif kind == "parts":
+            keep = min(1.0, max(0.0, (original_length * f / (2 * math.pi) - low) / (high - low)))
+            f *= keep + (1.0 - keep) / factor
+        # (a whole number of turns per position is no turn at all)
+        turns = round(math.ldexp(f / (2 * math.pi), 64)) % (1 << 64)
+        out[i] = turns & 0xFFFFFFFF, turns >> 32
+    return out
+
+
+def _double_bits(value: float) -> int:
+    return struct.unpack("<q", struct.pack("<d", float(value)))[0]
+
+
+class _Operators:
+    """The transformer operators, for a context (recorded at once) and a Batch (recorded wherever the batch is).  What each
+    computes, and which operands it takes, is documented with its opcode in include/lazytensor.h.  With `out`, a tensor of
+    the result's shape and dtype over memory of the caller's, the result is assigned to it and the barrier writes it there."""
+
+    __slots__ = ()
+
+    def _result(self, name, inputs, out, **attrs):
+        if out is None:
+            return self.op(name, *inputs, **attrs)
+        t = self.op(name, *inputs, out, **attrs)
+        self.assign(out, t)
+        return t
+
+    def rotary(self, x, positions, frequencies, *, interleaved: bool = False, inverse: bool = False, scale: float = 1.0, out=None):
+        """x [tokens, .., head size] with the first 2 P values of every head turned by position x frequency
+        (`frequencies`: see rotary_table).  `inverse` gives the gradient of x from the gradient of the result."""
+        return self._result("rotary", (x, positions, frequencies), out, interleaved=interleaved, inverse=inverse, scale=scale)
+
+    def cache_append(self, cache, k, v, slots, positions=None, frequencies=None, *, head_major: bool = False, interleaved: bool = False,
+                     scale: float = 1.0) -> None:
+        """Updates `cache` in place: token t's key (rotated when positions and frequencies are given) and value go to slot
+        slots[t]; negative slots are padding.  Two updates of one cache with no barrier between them go through a copy."""
+        if (positions is None) != (frequencies is None):
+            raise ValueError("positions and frequencies are given together")
+        turned = () if positions is None else (positions, frequencies)
+        self.assign(cache, self.op("cache_append", cache, k, v, slots, *turned, head_major=head_major, interleaved=interleaved, scale=scale))
+
+    def paged_attention(self, q, cache, page_table, lengths, *, scale: float, head_major: bool = False, out=None):
+        """softmax(scale q k) v of one token per sequence over the lengths[b] tokens in the pages that page_table[b] lists."""
+        return self._result("paged_attention", (q, cache, page_table, lengths), out, head_major=head_major, scale=scale)
+
+    def rms_norm(self, x, gamma, *, residual=None, eps: float = 1e-6, eight_bit: bool = False, group: int = 0, out=None) -> tuple:
+        """(y,) or, with eight_bit, (e4m3 codes as u8, scales); followed by x + residual if there is a residual.  `out`: as
+        many buffers (or None in the place of one)."""
+        wanted = ([2, 3] if eight_bit else [0]) + ([1] if residual is not None else [])
+        out = [None] * len(wanted) if out is None else list(out)
+        if len(out) != len(wanted):
+            raise ValueError(f"out: {len(wanted)} results, {len(out)} buffers")
+        inputs = (x, gamma) if residual is None else (x, residual, gamma)
+        made = [self.op("rms_norm", *inputs, *(() if o is None else (o,)), result=w, residual=residual is not None, group=group, eps=eps)
+                for w, o in zip(wanted, out)]
+        for t, o in zip(made, out):  # (after all are recorded: a buffer may be the residual's own)
+            if o is not None:
+                self.assign(o, t)
+        return tuple(made)
+
+    def rms_norm_grad(self, dy, h, gamma, *, residual_grad=None, eps: float = 1e-6, out=None) -> tuple:
+        """(gradient of h, gradient of gamma) for y = rms_norm(h, gamma); `residual_grad`, the gradient that reaches h past the
+        norm, is added to the first.  `out`: two buffers (or None in the place of one)."""
+        out = [None, None] if out is None else list(out)
+        if len(out) != 2:
+            raise ValueError(f"out: 2 results, {len(out)} buffers")
+        inputs = (dy, h, gamma) if residual_grad is None else (dy, h, gamma, residual_grad)
+        made = [self.op("rms_norm_grad", *inputs, *(() if o is None else (o,)), result=w, residual=residual_grad is not None, eps=eps)
+                for w, o in enumerate(out)]
+        for t, o in zip(made, out):
+            if o is not None:
+                self.assign(o, t)
+        return tuple(made)
+
+
 class _BatchRef:
     """An operand inside a Batch: one of its inputs (index >= 0) or the result of one of its entries (< 0)."""
     __slots__ = ("batch", "index")
@@ -227,7 +335,7 @@ class _BatchRef:
         self.batch, self.index = batch, index
 
 
-class Batch:
+class Batch(_Operators):
     """A sequence of operations written once and recorded with one call per use (lt_op_many): what a front end's
     operator expands to, e.g. the thirteen operations and three in-place updates of one Adam parameter update.  It has
     the recording interface of a context (`op`, `assign`), so the same function that traces on a context builds it:
@@ -248,6 +356,8 @@ class Batch:
 
     def op(self, name: str, *inputs, **attrs) -> _BatchRef:
         a = _attr_list(name, attrs)
+        if len(inputs) > 3:  # an entry has room for three: the others come in one ahead of it
+            self._ops.append((LT_BATCH_MORE, [r.index for r in inputs[3:]], 0, 0, 0))
         self._ops.append((OPCODES[name], [r.index for r in inputs], len(self._attrs), len(a), 0))
         self._attrs.extend(a)
         self._c = None
@@ -270,7 +380,7 @@ class Batch:
             ops = (lt_batch_op * max(len(self._ops), 1))()
             for k, (code, ins, off, na, keep) in enumerate(self._ops):
                 ops[k].opcode, ops[k].n_in, ops[k].n_attrs, ops[k].attr_offset, ops[k].keep = code, len(ins), na, off, keep
-                for i, r in enumerate(ins):
+                for i, r in enumerate(ins[:3]):
                     ops[k].in_[i] = r
             attrs = (_i64 * max(len(self._attrs), 1))(*self._attrs)
             self._c = (ops, attrs, (_u64 * max(len(self._ops), 1))(), (_u64 * max(self._n_inputs, 1))())
@@ -291,6 +401,16 @@ def _attr_list(name: str, attrs: dict) -> list:
         return [int(p) for p in attrs["perm"]]
     if name == "update_slice":
         return [int(attrs["dim"]), int(attrs["start"])]
+    if name == "rotary":
+        return [int(bool(attrs["interleaved"])), int(bool(attrs["inverse"])), _double_bits(attrs["scale"])]
+    if name == "cache_append":
+        return [int(bool(attrs["head_major"])), int(bool(attrs["interleaved"])), _double_bits(attrs["scale"])]
+    if name == "paged_attention":
+        return [int(bool(attrs["head_major"])), _double_bits(attrs["scale"])]
+    if name == "rms_norm":
+        return [int(attrs["result"]), int(bool(attrs["residual"])), int(attrs["group"]), _double_bits(attrs["eps"])]
+    if name == "rms_norm_grad":
+        return [int(attrs["result"]), int(bool(attrs["residual"])), _double_bits(attrs["eps"])]
     if name == "iota":
         shp = tuple(attrs["shape"])
         return [int(attrs["dim"]), len(shp), *shp]
@@ -300,7 +420,7 @@ def _attr_list(name: str, attrs: dict) -> list:
     return [seed - (1 << 64) if seed >= (1 << 63) else seed, off - (1 << 64) if off >= (1 << 63) else off, len(shp), *shp]
 
 
-class LazyContext:
+class LazyContext(_Operators):
     """One per device: the liveness arena, IR recorder, compile cache and executor."""
 
     def __init__(self, device: int | None = 0, stream: int | None = None, allocator: str = "torch"):
@@ -325,7 +445,7 @@ class LazyContext:
         self.stream = stream or 0
         self._h = _u64()
         self._hp = ctypes.byref(self._h)
-        self._ins = (_u64 * 3)()
+        self._ins = (_u64 * LT_OPERATOR_INPUTS)()
         self._attrs = (_i64 * (3 + LT_MAX_RANK))()
         self._dead: list[int] = []
         self._keeps: list = []

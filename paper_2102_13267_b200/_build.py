@@ -12,9 +12,12 @@ OBJ = HERE / "_build"
 LIB = HERE / "liblazytensor.so"
 CUDA_HOME = Path(os.environ.get("CUDA_HOME", "/usr/local/cuda"))
 
-CU_SOURCES = ["kernels.cu", "compiled.cu", "static_scratch.cu", "reduce.cu", "views.cu"]
-CPP_SOURCES = ["engine.cpp", "canon.cpp", "planner.cpp", "executor.cpp", "jit.cpp"]
+CU_SOURCES = ["kernels.cu", "compiled.cu", "static_scratch.cu", "reduce.cu", "views.cu", "operators.cu", "attention.cu"]
+CPP_SOURCES = ["engine.cpp", "canon.cpp", "planner.cpp", "executor.cpp", "jit.cpp", "operators.cpp"]
 HEADERS = ["engine.h", "vm.h", "launch.h", "vm_core.inc", "vm_ops.cuh", "compiled.h", "compiled_programs.inc", "pdl.cuh", "compiled_shells.cuh", "jit.h", "../../include/lazytensor.h"]
+
+# read by the host runtime and the operators' kernels only
+OPERATOR_HEADERS = ["operators.h", "operator_device.cuh"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-diag-suppress", "177",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
@@ -61,6 +64,8 @@ def _compile(src: str) -> Path:
     path = CSRC / src
     obj = OBJ / (src + ".o")
     deps = [path] + [CSRC / h for h in HEADERS]
+    if src.endswith(".cpp") or src in ("operators.cu", "attention.cu"):
+        deps += [CSRC / h for h in OPERATOR_HEADERS]
     if _stale(obj, deps):
         if src.endswith(".cu"):
             cmd = [str(CUDA_HOME / "bin" / "nvcc"), *NVCC_FLAGS, *PER_SOURCE_FLAGS.get(src, []), *EXTRA_NVCC, "-c", str(path), "-o", str(obj)]

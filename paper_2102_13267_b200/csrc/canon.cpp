@@ -83,13 +83,15 @@ void canonicalise(lt_ctx *c, const std::vector<uint32_t> &root_tensors, Canonica
         cn.dtype = n.dtype;
         cn.rank = n.rank;
         cn.n_in = n.n_in;
-        for (int i = 0; i < 3; ++i) cn.in[i] = i < n.n_in ? N[n.in[i]].canon : 0;
+        for (int i = 0; i < MAX_INPUTS; ++i) cn.in[i] = i < n.n_in ? N[n.in[i]].canon : 0;
         for (int i = 0; i < LT_MAX_RANK; ++i) cn.dims[i] = i < n.rank ? n.dims[i] : 0;
         cn.param = -1;
         cn.dyn = -1;
         cn.sval = 0.0;
         cn.attr0 = 0;
         cn.attr1 = 0;
+        cn.attr2 = 0;
+        cn.attr3 = 0;
         cn.output = -1;
         cn.arena = id;
         if (n.op == N_DEVICE_DATA) {
@@ -121,6 +123,11 @@ void canonicalise(lt_ctx *c, const std::vector<uint32_t> &root_tensors, Canonica
         } else if (n.op >= LT_OP_RESHAPE && n.op <= LT_OP_UPDATE_SLICE) {
             cn.attr0 = n.attr[0];
             cn.attr1 = n.attr[1];
+        } else if (is_operator(n.op)) {
+            cn.attr0 = n.attr[0];
+            cn.attr1 = n.attr[1];
+            cn.attr2 = n.attr[2];
+            cn.attr3 = n.attr[3];
         }
         cg.nodes.push_back(cn);
     };
@@ -174,7 +181,7 @@ void canonicalise(lt_ctx *c, const std::vector<uint32_t> &root_tensors, Canonica
 
     // serialise (into a buffer sized for the worst case, trimmed afterwards)
     std::vector<uint8_t> &b = cg.bytes;
-    b.resize(cg.nodes.size() * (4 + 8 * LT_MAX_RANK + 1 + 12 + 4 + 16) + cg.outputs.size() * 8 + 64);
+    b.resize(cg.nodes.size() * (4 + 8 * LT_MAX_RANK + 1 + 4 * MAX_INPUTS + 4 + 32) + cg.outputs.size() * 8 + 64);
     uint8_t *w = b.data();
     auto put = [&w](auto v) {
         memcpy(w, &v, sizeof(v));
@@ -204,6 +211,12 @@ void canonicalise(lt_ctx *c, const std::vector<uint32_t> &root_tensors, Canonica
             if (n.op >= LT_OP_RESHAPE && n.op <= LT_OP_UPDATE_SLICE) {
                 put((int64_t)n.attr0);
                 put((int64_t)n.attr1);
+            }
+            if (is_operator(n.op)) {
+                put((int64_t)n.attr0);
+                put((int64_t)n.attr1);
+                put((int64_t)n.attr2);
+                put((int64_t)n.attr3);
             }
         }
     }

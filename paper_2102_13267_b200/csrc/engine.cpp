@@ -231,6 +231,14 @@ void record_replay(lt_ctx *c, Plan *cached, Plan *plan, const Canonical &cg, con
 lt_status sync_and_check(lt_ctx *c) {
     cudaError_t e = cudaStreamSynchronize(c->stream);
     if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("cudaStreamSynchronize: ") + cudaGetErrorString(e));
+    if (c->index_status_pending) {
+        c->index_status_pending = false;
+        unsigned int word = 0;
+        e = lt_operator_status_read(&word);
+        if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("reading the operators' status word: ") + cudaGetErrorString(e));
+        if (word) return fail(c, LT_ERR_DEVICE_INDEX, std::string(word & 1u ? "paged_attention: a page number or a length" : "cache_append: a slot number") +
+                                                          " in device memory lies outside the cache; what it names was left out");
+    }
     if (c->status_pending) {
         c->status_pending = false;
         unsigned int word = 0;
@@ -293,6 +301,9 @@ const char *op_name(int op) {
     case LT_OP_ALL_SUM: return "all_sum"; case LT_OP_ALL_MAX: return "all_max"; case LT_OP_ALL_MIN: return "all_min";
     case LT_OP_RESHAPE: return "reshape"; case LT_OP_NARROW: return "narrow"; case LT_OP_PERMUTE: return "permute";
     case LT_OP_UPDATE_SLICE: return "update_slice";
+    case LT_OP_ROTARY: return "rotary"; case LT_OP_CACHE_APPEND: return "cache_append";
+    case LT_OP_PAGED_ATTENTION: return "paged_attention"; case LT_OP_RMS_NORM: return "rms_norm";
+    case LT_OP_RMS_NORM_GRAD: return "rms_norm_grad";
     case N_DEVICE_DATA: return "device_data"; case N_SCALAR: return "constant";
     default: return "?";
     }
@@ -721,7 +732,7 @@ uint32_t trace_virtual_tensor(lt_ctx *c, uint32_t index) {
 
 bool trace_match_op(lt_ctx *c, int opcode, const lt_tensor *in, int n_in, const int64_t *attrs, int n_attrs, lt_tensor *out) {
     TraceState &T = c->trace;
-    if (T.cursor >= T.script.events.size() || n_in < 0 || n_in > 3 || n_attrs < 0) return false;
+    if (T.cursor >= T.script.events.size() || n_in < 0 || n_in > MAX_INPUTS || n_attrs < 0) return false;
     const TraceEvent &ev = T.script.events[T.cursor];
     if (ev.kind != TE_OP || ev.op != opcode || ev.n_in != n_in || ev.n_attrs != n_attrs || (n_in && !in) || (n_attrs && !attrs)) return false;
     for (int i = 0; i < n_in; ++i) {
@@ -871,7 +882,7 @@ void trace_materialise(lt_ctx *c) {
         const TraceEvent &ev = events[e];
         lt_tensor out = 0;
         if (ev.kind == TE_OP) {
-            lt_tensor in[3] = {0, 0, 0};
+            lt_tensor in[MAX_INPUTS] = {0};
             for (int i = 0; i < ev.n_in; ++i) in[i] = make_handle(c, slot_of(ev.in[i]));
             int64_t a[64];
             for (int i = 0; i < ev.n_attrs; ++i) a[i] = attrs[ev.attr_off + i];
@@ -1593,9 +1604,9 @@ lt_status lt_op(lt_ctx *c, int opcode, const lt_tensor *in, int n_in, const int6
         if (trace_match_op(c, opcode, in, n_in, attrs, n_attrs, out)) return LT_OK;
         trace_materialise(c);
     }
-    if (n_in < 0 || n_in > 3 || (n_in > 0 && !in) || n_attrs < 0 || (n_attrs > 0 && !attrs))
+    if (n_in < 0 || n_in > (is_operator(opcode) ? MAX_INPUTS : 3) || (n_in > 0 && !in) || n_attrs < 0 || (n_attrs > 0 && !attrs))
         return fail(c, LT_ERR_INVALID_ARG, "bad operand or attribute list");
-    uint32_t ids[3] = {NONE, NONE, NONE}, in_slots[3] = {NONE, NONE, NONE};
+    uint32_t ids[MAX_INPUTS], in_slots[MAX_INPUTS];
     for (int i = 0; i < n_in; ++i) {
         uint32_t slot;
         lt_status s = lookup(c, in[i], &slot);
@@ -1603,13 +1614,14 @@ lt_status lt_op(lt_ctx *c, int opcode, const lt_tensor *in, int n_in, const int6
         in_slots[i] = slot;
         ids[i] = c->tensors[slot].node;
     }
-    const Node *ops[3] = {nullptr, nullptr, nullptr};
+    const Node *ops[MAX_INPUTS];
     for (int i = 0; i < n_in; ++i) ops[i] = &c->nodes[ids[i]];
 
     int64_t od[LT_MAX_RANK] = {0};
     int orank = 0;
     int odtype = LT_F32;
-    int64_t a0 = 0, a1 = 0;
+    int64_t a0 = 0, a1 = 0, a2 = 0, a3 = 0;
+    int node_inputs = n_in;
 
     auto common_dtype = [&](int first, int count, int *dt) -> bool {
         int found = -1;
@@ -1762,6 +1774,17 @@ lt_status lt_op(lt_ctx *c, int opcode, const lt_tensor *in, int n_in, const int6
             orank = 0;
         }
         odtype = ops[0]->dtype;
+    } else if (is_operator(opcode)) {
+        const lt_status s = operator_infer(c, opcode, ops, n_in, attrs, n_attrs, od, &orank, &odtype);
+        if (s) return s;
+        a0 = attrs[0];
+        a1 = n_attrs > 1 ? attrs[1] : 0;
+        a2 = n_attrs > 2 ? attrs[2] : 0;
+        a3 = n_attrs > 3 ? attrs[3] : 0;
+        // the buffer meant for the result is an input like the others while it holds data; a computation still pending
+        // under that name will never be looked at and is not kept for it
+        const int core = operator_inputs(opcode, n_in, attrs);
+        if (n_in > core && ops[n_in - 1]->op != N_DEVICE_DATA) node_inputs = core;
     } else {
         return fail(c, LT_ERR_UNSUPPORTED, "unknown opcode " + std::to_string(opcode));
     }
@@ -1771,11 +1794,13 @@ lt_status lt_op(lt_ctx *c, int opcode, const lt_tensor *in, int n_in, const int6
     nd.op = (uint16_t)opcode;
     nd.dtype = (uint8_t)odtype;
     nd.rank = (uint8_t)orank;
-    nd.n_in = (uint8_t)n_in;
+    nd.n_in = (uint8_t)node_inputs;
     for (int i = 0; i < orank; ++i) nd.dims[i] = od[i];
     nd.attr[0] = a0;
     nd.attr[1] = a1;
-    for (int i = 0; i < n_in; ++i) {
+    nd.attr[2] = a2;
+    nd.attr[3] = a3;
+    for (int i = 0; i < node_inputs; ++i) {
         nd.in[i] = ids[i];
         node_ref(c, ids[i]);
     }
@@ -1888,17 +1913,29 @@ lt_status lt_op_many(lt_ctx *c, const lt_batch_op *ops, size_t n_ops, const lt_t
     for (size_t k = 0; k < n_ops; ++k) results[k] = 0;
     lt_status st = LT_OK;
     size_t done = 0;
+    int more = 0;  // operands given ahead by an LT_BATCH_MORE entry
+    int64_t more_in[3] = {0, 0, 0};
     for (; done < n_ops && st == LT_OK; ++done) {
         const lt_batch_op &o = ops[done];
         const int want = o.opcode == LT_BATCH_ASSIGN ? 2 : o.n_in;
-        lt_tensor in[3] = {0, 0, 0};
-        if (want < 0 || want > 3 || o.n_attrs < 0 || (o.n_attrs > 0 && !attrs)) st = fail(c, LT_ERR_INVALID_ARG, "lt_op_many: bad operand or attribute count");
+        lt_tensor in[MAX_INPUTS] = {0};
+        if (o.opcode == LT_BATCH_MORE) {
+            if (o.n_in < 1 || o.n_in > 3 || more || done + 1 >= n_ops || ops[done + 1].opcode < 0 || ops[done + 1].n_in != 3 + o.n_in) {
+                st = fail(c, LT_ERR_INVALID_ARG, "lt_op_many: LT_BATCH_MORE gives the fourth to sixth operand of the operation right after it");
+                break;
+            }
+            more = o.n_in;
+            for (int i = 0; i < more; ++i) more_in[i] = o.in[i];
+            continue;
+        }
+        if (want < 0 || want > 3 + more || o.n_attrs < 0 || (o.n_attrs > 0 && !attrs)) st = fail(c, LT_ERR_INVALID_ARG, "lt_op_many: bad operand or attribute count");
         for (int i = 0; i < want && st == LT_OK; ++i) {
-            const int64_t r = o.in[i];
+            const int64_t r = i < 3 ? o.in[i] : more_in[i - 3];
             if (r >= 0 && (size_t)r < n_inputs) in[i] = inputs[r];
             else if (r < 0 && (size_t)(-(r + 1)) < done && results[-(r + 1)]) in[i] = results[-(r + 1)];
             else st = fail(c, LT_ERR_INVALID_ARG, "lt_op_many: an operand names neither an input nor an earlier result of the batch");
         }
+        more = 0;
         if (st != LT_OK) break;
         if (o.opcode == LT_BATCH_ASSIGN) st = lt_assign(c, in[0], in[1]);
         else st = lt_op(c, o.opcode, in, o.n_in, o.n_attrs ? attrs + o.attr_offset : nullptr, o.n_attrs, &results[done]);

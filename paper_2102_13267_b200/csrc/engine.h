@@ -10,6 +10,7 @@
 
 #include "../../include/lazytensor.h"
 #include "jit.h"
+#include "operators.h"
 #include "vm.h"
 
 namespace lt {
@@ -17,6 +18,7 @@ namespace lt {
 constexpr uint16_t N_DEVICE_DATA = 200;  // leaf over a device buffer (Fig. 1: xla::device_data)
 constexpr uint16_t N_SCALAR = 201;       // rank-0 constant (Fig. 1: prim::Constant)
 constexpr uint32_t NONE = 0xffffffffu;
+constexpr int MAX_INPUTS = LT_OPERATOR_INPUTS;  // operands of one operation (the transformer operators take up to six, all others up to three)
 
 enum : uint8_t { NF_DYNAMIC = 1 };  // scalar is a run-time parameter (not 0/1, or forced)
 
@@ -26,7 +28,7 @@ struct Node {
     uint16_t op = 0;
     uint8_t dtype = 0, rank = 0;
     uint8_t n_in = 0, flags = 0;
-    uint32_t in[3] = {NONE, NONE, NONE};
+    uint32_t in[MAX_INPUTS] = {NONE, NONE, NONE, NONE, NONE, NONE};
     uint32_t refs = 0;         // tensors + consumer nodes holding this node
     uint32_t tensor_refs = 0;  // tensors only
     uint32_t buffer = NONE;    // N_DEVICE_DATA
@@ -34,7 +36,7 @@ struct Node {
     uint32_t canon = 0;        // canonical index within the current traversal
     int64_t dims[LT_MAX_RANK] = {0};
     double sval = 0.0;         // N_SCALAR value
-    int64_t attr[2] = {0, 0};  // CONVERT: dtype; IOTA: dim; PHILOX: seed, offset
+    int64_t attr[4] = {0, 0, 0, 0};  // CONVERT: dtype; IOTA: dim; PHILOX: seed, offset; operators: their attributes as passed
     // trace matching: where the node entered the trace numbered trace_epoch -- the event that made it, or
     // TID_IMPORT | the ordinal among the nodes from before the trace that it has read
     uint32_t trace_ref = 0, trace_epoch = 0;
@@ -71,13 +73,14 @@ struct TensorRec {
 struct CNode {
     uint16_t op;
     uint8_t dtype, rank, n_in;
-    uint32_t in[3];
+    uint32_t in[MAX_INPUTS];
     int64_t dims[LT_MAX_RANK];
     int32_t param;   // N_DEVICE_DATA: parameter ordinal
     int32_t dyn;     // first run-time slot (scalar: 1 slot; philox: 2 slots), else -1
     double sval;     // static scalar value
     int64_t attr0;   // CONVERT dtype / IOTA dim / NARROW, UPDATE_SLICE dim / PERMUTE packed permutation
     int64_t attr1;   // NARROW, UPDATE_SLICE start
+    int64_t attr2, attr3;  // operators: attr0..attr3 are their attributes
     int32_t output;  // index in the output list, else -1
     uint32_t arena;  // arena node (not part of the hashed bytes)
 };
@@ -120,7 +123,9 @@ struct IoRef {
     uint64_t offset = 0;   // elements from the start of the buffer to the operand's first element (a slice read in place)
 };
 
-enum : uint8_t { K_EW = 0, K_ROW = 1, K_MULTI = 2, K_RED = 3, K_VIEW = 4 };  // K_RED: a reduction that runs as a kernel of its own (reduce.cu); K_VIEW: a shape operation (views.cu)
+// K_RED: a reduction that runs as a kernel of its own (reduce.cu); K_VIEW: a shape operation (views.cu); K_OPERATOR: a
+// transformer operator, with all its results that the graph asks for (operators.cu, attention.cu)
+enum : uint8_t { K_EW = 0, K_ROW = 1, K_MULTI = 2, K_RED = 3, K_VIEW = 4, K_OPERATOR = 5 };
 
 struct Group {
     uint8_t kind = K_EW;
@@ -143,6 +148,9 @@ struct Group {
     uint8_t view_rank = 0;
     int64_t view_a0 = 0, view_a1 = 0;
     int64_t view_in_dims[LT_MAX_RANK] = {0}, view_out_dims[LT_MAX_RANK] = {0};  // of the (first) input and of the result
+    LtOperator operation{};         // K_OPERATOR: everything but the addresses; io = the operands shared by its results, then the results and the buffers meant for them
+    std::vector<uint8_t> results;   // K_OPERATOR: per io, which result of the operator it is
+    uint8_t n_operands = 0;         // K_OPERATOR: how many of io are operands the kernel reads
 };
 
 struct Launch {
@@ -247,7 +255,7 @@ struct TraceEvent {
     uint8_t kind = 0, n_in = 0, n_attrs = 0, dtype = 0;
     uint16_t op = 0;
     uint8_t flags = 0, rank = 0;   // scalar: NF_DYNAMIC
-    uint32_t in[3] = {0, 0, 0};    // tensor ids: operands (op), destination and source (assign), the tensor (release)
+    uint32_t in[MAX_INPUTS] = {0, 0, 0, 0, 0, 0};  // tensor ids: operands (op), destination and source (assign), the tensor (release)
     uint32_t attr_off = 0;         // first of n_attrs words in TraceScript::attrs: an op's attributes as passed, a leaf's dimensions
     double sval = 0.0;             // static scalar: its value
 };
@@ -362,6 +370,7 @@ struct lt_ctx {
 
     lt::ReplayRecord replay;
     lt::TraceState trace;
+    bool index_status_pending = false;  // an operator that follows indices in device memory ran since its status word was last read
     bool status_pending = false;      // a kernel with bounded device-side waits ran since the status word was last read
     int64_t wait_limit_ns = 2000000000ll;  // how long such a wait may last
 
@@ -470,6 +479,18 @@ void hash_bytes(const uint8_t *data, size_t n, uint64_t out[2]);
 lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_long_rows = false);
 std::string describe_plan(const Plan &plan);
 int broadcast_class(const int64_t *dims, int rank, uint64_t rows, uint64_t cols);
+
+// transformer operators (operators.cpp)
+inline bool is_operator(int op) { return op >= LT_OP_ROTARY && op <= LT_OP_RMS_NORM_GRAD; }
+lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in, const int64_t *attrs, int n_attrs, int64_t *od, int *orank,
+                         int *odtype);
+int operator_core_inputs(const CNode &n);
+int operator_result(const CNode &n);
+bool operator_same_launch(const CNode &a, const CNode &b);
+uint64_t operator_operand_rows(const CNode &n, int k, const CNode &operand);
+bool operator_in_place(const CNode &n, int k);
+void operator_fill(const Canonical &cg, const CNode &n, LtOperator &out);
+uint64_t operator_bytes(const LtOperator &o);
 
 // executor (executor.cpp)
 lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_split = nullptr);

@@ -259,7 +259,22 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
             ev0 = take_event(c);
             ev1 = take_event(c);
         }
-        if (L.kind == K_VIEW) {
+        if (L.kind == K_OPERATOR) {
+            const Group &g = plan.groups[L.groups[0]];
+            unsigned launched = 1;
+            if (!dry) {
+                LtOperator o = g.operation;
+                for (int k = 0; k < g.n_operands; ++k) o.in[k] = (const void *)(uintptr_t)resolve(g.io[k]);
+                for (size_t q = g.n_operands; q < g.io.size(); ++q)
+                    if (g.io[q].is_store) o.out[g.results[q]] = (void *)(uintptr_t)resolve(g.io[q]);
+                o.scratch = g.scratch_temp >= 0 ? c->temp_ptr[g.scratch_temp] : nullptr;
+                if (ev0) cudaEventRecord(ev0, c->stream);
+                e = lt_launch_operator(o, c->sm_count, c->stream, &launched);
+                if (ev1) cudaEventRecord(ev1, c->stream);
+                if (o.op == LT_OP_PAGED_ATTENTION || o.op == LT_OP_CACHE_APPEND) c->index_status_pending = true;
+            }
+            if (launched > 1) c->stats.kernels_launched += launched - 1;
+        } else if (L.kind == K_VIEW) {
             const Group &g = plan.groups[L.groups[0]];
             unsigned launched = 1;
             if (!dry) {
@@ -685,7 +700,7 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
                 c->stats.launches_row++;
             }
         }
-        if (ev0) c->timed.push_back(TimedLaunch{ev0, ev1, (uint8_t)(L.kind == K_RED ? K_ROW : L.kind == K_VIEW ? K_EW : L.kind), L.bytes});
+        if (ev0) c->timed.push_back(TimedLaunch{ev0, ev1, (uint8_t)(L.kind == K_RED ? K_ROW : L.kind >= K_VIEW ? K_EW : L.kind), L.bytes});
         if (e != cudaSuccess) {
             release_all(true);
             return fail(c, LT_ERR_CUDA, std::string("kernel launch: ") + cudaGetErrorString(e));

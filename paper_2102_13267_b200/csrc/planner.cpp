@@ -731,7 +731,7 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
         domain_of(n, &pn[i].rows, &pn[i].cols, &pn[i].numel);
         pn[i].leaf = n.op == N_DEVICE_DATA || n.op == N_SCALAR;
         pn[i].reduce = is_reduce(n.op);
-        pn[i].foreign = is_col_reduce(n.op) || is_all_reduce(n.op);
+        pn[i].foreign = is_col_reduce(n.op) || is_all_reduce(n.op) || is_operator(n.op);
         for (int k = 0; k < n.n_in; ++k) pn[n.in[k]].consumers.push_back((uint32_t)i);
         if (pn[i].numel == 0) return fail(c, LT_ERR_UNSUPPORTED, "empty tensors cannot be part of a flushed graph");
     }
@@ -744,11 +744,23 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
         pn[i].foreign = !(same_domain && fuse);
         // A slice of materialised data along the last or the first dimension is a block of rows at a fixed pitch (or one
         // contiguous range): consumers that compute over the slice's own [rows, cols] read it in place.
+        // An operator reads a slice in place when each row of its operand (a token's heads, a row to normalise) is one run.
         if (fuse && n.op == LT_OP_NARROW && cg.nodes[n.in[0]].op == N_DEVICE_DATA && n.output < 0 && !pn[i].consumers.empty() &&
-            (n.attr0 == n.rank - 1 || n.attr0 == 0) && src.cols < (1ull << 32)) {
+            src.cols < (1ull << 32)) {
+            uint64_t before = 1;
+            for (int d = 0; d < n.attr0; ++d) before *= (uint64_t)n.dims[d];
             bool all = true;
             for (uint32_t q : pn[i].consumers) {
                 const CNode &qn = cg.nodes[q];
+                if (is_operator(qn.op)) {
+                    for (int k = 0; k < qn.n_in; ++k) {
+                        if (qn.in[k] != i) continue;
+                        const uint64_t r = operator_operand_rows(qn, k, n);
+                        if (r == 0 || !(n.attr0 == 0 || before == r) || src.numel / std::max<uint64_t>(before, 1) >= (1ull << 32)) all = false;
+                    }
+                    continue;
+                }
+                if (n.attr0 != n.rank - 1 && n.attr0 != 0) all = false;
                 const bool elementwise = (qn.op >= LT_OP_ADD && qn.op <= LT_OP_NOT) || qn.op == LT_OP_CONVERT || is_reduce(qn.op);
                 uint64_t qr = pn[q].rows, qc = pn[q].cols;
                 if (is_reduce(qn.op)) qr = pn[i].rows, qc = pn[i].cols;
@@ -822,7 +834,7 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
             dr = pn[n.in[0]].rows;
             dc = pn[n.in[0]].cols;
         }
-        if (p.foreign && !is_shape_op(n.op)) {
+        if (p.foreign && !is_shape_op(n.op) && !is_operator(n.op)) {
             dr = pn[n.in[0]].rows;
             dc = pn[n.in[0]].cols;
         }
@@ -830,7 +842,16 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
         int gmin = -1;
         for (uint32_t d : deps) gmin = std::max(gmin, pn[d].group);
         int target = -1;
-        if (fuse && !p.foreign) {
+        if (is_operator(n.op)) {
+            // another result of an operator that is already in the plan: one launch gives both
+            for (size_t gi = 0; gi < groups.size() && target < 0; ++gi)
+                if (groups[gi].kind == K_OPERATOR && fuse) {
+                    bool same = true;
+                    for (uint32_t m : groups[gi].members)
+                        same = same && operator_same_launch(cg.nodes[m], n) && operator_result(cg.nodes[m]) != operator_result(n);
+                    if (same) target = (int)gi;
+                }
+        } else if (fuse && !p.foreign) {
             auto joinable = [&](int gi) -> bool {
                 const Group &g = groups[gi];
                 if (g.kind >= K_RED || (int)g.members.size() >= MAX_GROUP_NODES) return false;
@@ -910,6 +931,9 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
                 memcpy(g.view_out_dims, n.dims, sizeof(g.view_out_dims));
                 if (n.op == LT_OP_UPDATE_SLICE) memcpy(g.view_out_dims, cg.nodes[n.in[1]].dims, sizeof(g.view_out_dims));  // the slice's extent
                 if (n.op == LT_OP_RESHAPE) g.view_rank = 1, g.view_in_dims[0] = g.view_out_dims[0] = (int64_t)p.numel;
+            } else if (is_operator(n.op)) {
+                groups[target].kind = K_OPERATOR;
+                operator_fill(cg, n, groups[target].operation);
             } else if (p.foreign) {
                 Group &g = groups[target];
                 g.kind = K_RED;
@@ -958,6 +982,56 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
                         else if (pn[q].group != (int)gi) pn[m].needs_store = true;
                     }
                 }
+            }
+            if (g.kind == K_OPERATOR) {
+                // the operands its results share, then per result the result itself and, where there is one, the buffer
+                // meant for it (not read: it only makes that buffer an input, so that the result can be written there)
+                g.ins.clear();
+                g.io.clear();
+                g.imms.clear();
+                auto slot_for = [&](uint32_t v, bool store) {
+                    const CNode &vn = cg.nodes[v];
+                    IoRef io;
+                    io.is_store = store ? 1 : 0;
+                    io.dtype = vn.dtype;
+                    io.cls = LT_CLS_FULL;
+                    io.cnode = v;
+                    if (pn[v].in_place_slice) {
+                        const CNode &base = cg.nodes[vn.in[0]];
+                        uint64_t inner = 1;
+                        for (int d = (int)vn.attr0 + 1; d < vn.rank; ++d) inner *= (uint64_t)vn.dims[d];
+                        io.kind = IO_PARAM;
+                        io.index = (uint32_t)base.param;
+                        io.offset = (uint64_t)vn.attr1 * inner;
+                        if (vn.attr0 > 0) io.pitch = (uint32_t)(inner * (uint64_t)base.dims[vn.attr0]);
+                    } else if (vn.op == N_DEVICE_DATA) {
+                        io.kind = IO_PARAM;
+                        io.index = (uint32_t)vn.param;
+                    } else {
+                        io.kind = vn.output >= 0 ? IO_OUTPUT : IO_TEMP;
+                        io.index = vn.output >= 0 ? (uint32_t)vn.output : 0;
+                    }
+                    g.io.push_back(io);
+                };
+                const CNode &first = cg.nodes[g.members[0]];
+                g.n_operands = (uint8_t)operator_core_inputs(first);
+                g.results.clear();
+                for (int k = 0; k < g.n_operands; ++k) {
+                    slot_for(first.in[k], false);
+                    if (g.io.back().pitch) g.operation.pitch[k] = g.io.back().pitch;
+                }
+                for (uint32_t m : g.members) {
+                    pn[m].needs_store = true;
+                    slot_for(m, true);
+                    g.operation.wanted |= 1u << operator_result(cg.nodes[m]);
+                    g.results.resize(g.io.size(), 0);
+                    g.results.back() = (uint8_t)operator_result(cg.nodes[m]);
+                    if (cg.nodes[m].n_in > g.n_operands) slot_for(cg.nodes[m].in[g.n_operands], false);
+                }
+                g.results.resize(g.io.size(), 0);
+                g.flavour = 1;
+                for (uint32_t nn : emit) in_emit[nn] = 0;
+                break;
             }
             if (g.kind == K_VIEW) {
                 // a copy kernel: the inputs in order, then the result; all dense buffers
@@ -1078,6 +1152,14 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
         if (g.kind == K_VIEW) {
             g.bytes = 0;
             for (const IoRef &io : g.io) g.bytes += pn[io.cnode].numel * dtype_size(io.dtype);
+        }
+        if (g.kind == K_OPERATOR) {
+            g.bytes = operator_bytes(g.operation);
+            const size_t scratch = lt_operator_scratch_bytes(g.operation, c->sm_count);
+            if (scratch) {
+                g.scratch_temp = (int32_t)plan.temp_bytes.size();
+                plan.temp_bytes.push_back(scratch);
+            }
         }
         if (g.kind == K_RED) {
             const size_t scratch = lt_reduce_scratch_bytes(g.red_axis, g.rows, g.cols, c->sm_count);
@@ -1245,7 +1327,13 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
                 bool safe = true;
                 for (auto &rd : readers[p]) {
                     const uint32_t rg = rd.first;
-                    if (rg == gi && g.kind == K_VIEW) {
+                    if (rg == gi && g.kind == K_OPERATOR) {
+                        // the buffer meant for this very result, or an operand of which every element is read before
+                        // the thread that read it overwrites it
+                        const bool meant = rd.second >= g.n_operands;
+                        const IoRef &ld = g.io[rd.second];
+                        if (meant ? rd.second != s + 1 : !(operator_in_place(cg.nodes[st.cnode], (int)rd.second) && !ld.pitch && !ld.offset)) { safe = false; break; }
+                    } else if (rg == gi && g.kind == K_VIEW) {
                         // update_slice rewrites only the slice of its base: in place when the base (slot 0) is the one
                         // read of the buffer; the other shape operations move every element
                         if (g.view_op != LT_OP_UPDATE_SLICE || rd.second != 0) { safe = false; break; }
@@ -1394,7 +1482,7 @@ std::string describe_plan(const Plan &plan) {
             snprintf(buf, sizeof(buf), "  output %zu donated param %d\n", k, plan.outputs[k].donated_param);
             s += buf;
         }
-    static const char *kind[] = {"elementwise", "row", "multi", "reduce", "view"};
+    static const char *kind[] = {"elementwise", "row", "multi", "reduce", "view", "operator"};
     static const char *cls[] = {"full", "colvec", "rowvec", "scalar", "pitched"};
     static const char *reduced[] = {"reduced-over-rows(sum)", "reduced-over-rows(max)", "reduced-over-rows(min)",
                                     "reduced-over-all(sum)",  "reduced-over-all(max)",  "reduced-over-all(min)"};
@@ -1406,7 +1494,10 @@ std::string describe_plan(const Plan &plan) {
                  L.flavour == 0 ? "fast" : (L.flavour == 1 ? "precise" : "ieee"), L.groups.size(), (unsigned long long)g.rows, (unsigned long long)g.cols,
                  g.rowcol ? "rowcol" : "flat", (unsigned long long)L.bytes);
         s += buf;
-        if (L.kind == K_VIEW) {
+        if (L.kind == K_OPERATOR) {
+            snprintf(buf, sizeof(buf), "  operator: %s, results=%zu\n", op_name(g.operation.op), L.groups.size() ? plan.groups[L.groups[0]].members.size() : (size_t)0);
+            s += buf;
+        } else if (L.kind == K_VIEW) {
             snprintf(buf, sizeof(buf), "  copy kernel: %s\n", op_name(g.view_op));
             s += buf;
         } else if (L.kind == K_RED) {
