@@ -5,9 +5,11 @@
 // written, so the bound is the cache's bytes over the memory's rate.
 //
 // Work split: the tokens of all sequences are cut into tiles of TILE; the list of (sequence, head block, tile) is divided
-// evenly over the thread blocks, whatever the sequences' lengths (which only the device knows).  A block walks its part
-// of the list; a (sequence, head block) that lies within one block's part is finished there, one that is spread over
-// several leaves partial results (m, sum, unnormalised out), which a second kernel joins in the list's order.
+// evenly over the thread blocks, whatever the sequences' lengths (which only the device knows).  Every (sequence, head
+// block) counts START tiles more than it has, for what beginning one costs (measured below).  A block walks its part of
+// the list; a (sequence, head block) that lies within one block's part is finished there.  One that is spread over
+// several blocks leaves partial results (maximum, sum, unnormalised output) in scratch memory, and the block that
+// arrives last joins them, always in the list's order, so results do not depend on the arrival.
 #include <atomic>
 
 #include "operator_device.cuh"
@@ -17,13 +19,16 @@ using namespace ltop;
 namespace {
 
 constexpr int TILE = 64;        // tokens
+constexpr int START = 2;        // tiles that beginning a (sequence, head block) counts for
+constexpr int MOST_PARTS = 64;  // blocks one (sequence, head block) is spread over
 constexpr int THREADS = 128;
 
 struct AttendArgs {
     const void *q, *cache;
     const int *table, *lengths;
     void *out;
-    float *partial;             // [2 x blocks][block_heads][dim + 2]; null: every (sequence, head block) has a block of its own
+    float *partial;             // [2 x blocks][block_heads][dim + 2]: outputs, then (maximum, sum) of each head; null: every (sequence, head block) has a block of its own
+    unsigned int *arrivals;     // [blocks], zero between launches: how many of the blocks that share what begins in block i have left their part
     unsigned int *status;
     uint64_t q_pitch, page_stride, value_offset, token_stride, head_stride;
     uint32_t batch, heads, kv_heads, group, block_heads, head_blocks, dim, pages, page, table_width;  // block_heads: query heads a block works on at a time
@@ -42,50 +47,42 @@ __device__ __forceinline__ void check_length(const AttendArgs &a, uint32_t b) {
 
 __device__ __forceinline__ uint32_t tiles_of(const AttendArgs &a, uint32_t b) { return ((uint32_t)length_of(a, b) + TILE - 1) / TILE; }
 
-// Inclusive sums over the block's threads of a 64-bit value each; *all: over the whole block.
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t *part, uint64_t *all) {
+// Length of sequence b's part of the list, per head block.
+__device__ __forceinline__ uint32_t items_of(const AttendArgs &a, uint32_t b) {
+    const uint32_t t = tiles_of(a, b);
+    return t ? t + START : 0;
+}
+
+// Inclusive sums over the block's threads of a 64-bit value each; *all: over the whole block; *most: the largest `w`.
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint32_t w, uint64_t *part, uint64_t *all, uint32_t *most) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const uint64_t o = __shfl_up_sync(0xffffffffu, v, d);
         if (lane >= d) v += o;
     }
+    w = __reduce_max_sync(0xffffffffu, w);
     __syncthreads();  // `part` may still be read from the scan before
-    if (lane == 31) part[warp] = v;
+    if (lane == 31) part[warp] = v, part[THREADS / 32 + warp] = w;
     __syncthreads();
     uint64_t before = 0, sum = 0;
+    uint32_t top = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += part[w];
-        sum += part[w];
+    for (int k = 0; k < THREADS / 32; ++k) {
+        if (k < warp) before += part[k];
+        sum += part[k];
+        top = max(top, (uint32_t)part[THREADS / 32 + k]);
     }
     *all = sum;
+    *most = top;
     return v + before;
-}
-
-// Tiles of all sequences, and of those before `upto`.
-__device__ __forceinline__ void count_tiles(const AttendArgs &a, uint32_t upto, uint64_t *part, uint64_t *before, uint64_t *all) {
-    uint64_t s = 0, t = 0;
-    for (uint32_t b = threadIdx.x; b < a.batch; b += THREADS) {
-        const uint64_t n = tiles_of(a, b);
-        t += n;
-        if (b < upto) s += n;
-    }
-    block_scan(t, part, all);
-    block_scan(s, part, before);
 }
 
 // What a block works on: items [idx, end) of the list, the first in sequence b, whose own first item is `base`.
 struct Share {
-    uint64_t idx, end, base;
+    uint64_t idx, end, base, size;  // size: of a block's share
     uint32_t b;
 };
-
-// A block's share of the list, in tiles.
-__device__ __forceinline__ uint64_t share_of(uint64_t items, unsigned blocks) {
-    const uint64_t s = (items + blocks - 1) / blocks;
-    return s < 1 ? 1 : s;
-}
 
 // The block's part of the list, from the sequences' lengths.  `part`, `found`: shared, 32 and 2 values.
 __device__ __forceinline__ Share my_share(const AttendArgs &a, uint64_t *part, uint64_t *found) {
@@ -93,23 +90,35 @@ __device__ __forceinline__ Share my_share(const AttendArgs &a, uint64_t *part, u
     Share s{};
     if (!a.partial) {  // a block per (sequence, head block)
         s.b = blockIdx.x / per;
-        const uint64_t t = tiles_of(a, s.b);
+        const uint64_t t = items_of(a, s.b);
         s.idx = (uint64_t)(blockIdx.x - s.b * per) * t;
         s.end = s.idx + t;
         return s;
     }
     uint64_t total = 0, sum;
-    uint64_t mine = threadIdx.x < a.batch ? (uint64_t)tiles_of(a, threadIdx.x) * per : 0, upto = block_scan(mine, part, &sum);
+    uint32_t most, more = 0;
+    uint32_t items = threadIdx.x < a.batch ? items_of(a, threadIdx.x) : 0;
+    uint64_t mine = (uint64_t)items * per, upto = block_scan(mine, items, part, &sum, &most);
     if (a.batch > THREADS) {
         uint64_t rest = 0;
-        for (uint32_t b = threadIdx.x + THREADS; b < a.batch; b += THREADS) rest += (uint64_t)tiles_of(a, b) * per;
-        block_scan(rest, part, &total);
+        uint32_t top = 0;
+        for (uint32_t b = threadIdx.x + THREADS; b < a.batch; b += THREADS) {
+            const uint32_t n = items_of(a, b);
+            rest += (uint64_t)n * per;
+            top = max(top, n);
+        }
+        block_scan(rest, top, part, &total, &more);
     }
     total += sum;
-    const uint64_t share = share_of(total, gridDim.x);
-    s.idx = (uint64_t)blockIdx.x * share;
-    s.end = min(s.idx + share, total);
-    if (s.idx >= s.end) return s;
+    most = max(most, more);
+    // an even share, and no (sequence, head block) over more than MOST_PARTS blocks
+    s.size = max((total + gridDim.x - 1) / gridDim.x, (uint64_t)((most + MOST_PARTS - 2) / (MOST_PARTS - 1)));
+    s.idx = (uint64_t)blockIdx.x * s.size;
+    s.end = min(s.idx + s.size, total);
+    if (s.idx >= s.end) {
+        s.idx = s.end = 0;
+        return s;
+    }
     uint64_t before = 0;
     for (uint32_t b0 = 0;;) {
         if (s.idx < before + sum) {
@@ -118,8 +127,8 @@ __device__ __forceinline__ Share my_share(const AttendArgs &a, uint64_t *part, u
         }
         before += sum;
         b0 += THREADS;
-        mine = b0 + threadIdx.x < a.batch ? (uint64_t)tiles_of(a, b0 + threadIdx.x) * per : 0;
-        upto = block_scan(mine, part, &sum);
+        mine = b0 + threadIdx.x < a.batch ? (uint64_t)items_of(a, b0 + threadIdx.x) * per : 0;
+        upto = block_scan(mine, 0, part, &sum, &more);
     }
     __syncthreads();
     s.b = (uint32_t)found[0];
@@ -129,47 +138,135 @@ __device__ __forceinline__ Share my_share(const AttendArgs &a, uint64_t *part, u
 
 // A stretch of tiles of one (sequence, head block).
 struct Stretch {
+    uint64_t first;         // list index of the first item of the (sequence, head block)
     uint32_t b, kv, h0;     // h0: first query head
     int n, heads;           // tokens of the sequence, query heads
     uint32_t t0, t1, tiles;
+    uint32_t items;         // of the list
 };
 
-// The next stretch of the share, or false when it is done; `done`: tiles of the one before.
+// The next stretch of the share, or false when it is done; `done`: items of the one before.
 __device__ __forceinline__ bool next_stretch(const AttendArgs &a, Share &s, Stretch &w, uint32_t done) {
-    s.idx += done;
-    if (s.idx >= s.end) return false;
     const uint32_t per = a.kv_heads * a.head_blocks;
     for (;;) {
-        w.n = length_of(a, s.b);
-        w.tiles = ((uint32_t)w.n + TILE - 1) / TILE;
-        if (s.idx < s.base + (uint64_t)w.tiles * per) break;
-        s.base += (uint64_t)w.tiles * per;
-        ++s.b;
+        s.idx += done;
+        if (s.idx >= s.end) return false;
+        uint32_t all;
+        for (;;) {
+            w.n = length_of(a, s.b);
+            w.tiles = ((uint32_t)w.n + TILE - 1) / TILE;
+            all = w.tiles ? w.tiles + START : 0;
+            if (s.idx < s.base + (uint64_t)all * per) break;
+            s.base += (uint64_t)all * per;
+            ++s.b;
+        }
+        const uint32_t hb = (uint32_t)((s.idx - s.base) / all);
+        w.first = s.base + (uint64_t)hb * all;
+        const uint32_t v0 = (uint32_t)(s.idx - w.first), v1 = (uint32_t)min((uint64_t)all, v0 + (s.end - s.idx));
+        done = w.items = v1 - v0;
+        w.t0 = max(v0, (uint32_t)START) - START;
+        w.t1 = max(v1, (uint32_t)START) - START;
+        if (w.t1 == w.t0) continue;  // only of what beginning counts for
+        w.b = s.b;
+        w.kv = hb / a.head_blocks;
+        const uint32_t first = (hb - w.kv * a.head_blocks) * a.block_heads;
+        w.h0 = w.kv * a.group + first;
+        w.heads = (int)min(a.block_heads, a.group - first);
+        return true;
     }
-    const uint32_t hb = (uint32_t)((s.idx - s.base) / w.tiles);
-    w.t0 = (uint32_t)((s.idx - s.base) - (uint64_t)hb * w.tiles);
-    w.t1 = (uint32_t)min((uint64_t)w.tiles, w.t0 + (s.end - s.idx));
-    w.b = s.b;
-    w.kv = hb / a.head_blocks;
-    const uint32_t first = (hb - w.kv * a.head_blocks) * a.block_heads;
-    w.h0 = w.kv * a.group + first;
-    w.heads = (int)min(a.block_heads, a.group - first);
-    return true;
 }
 
-// Without a list: the zeros of an empty sequence, and the check of its length.
-template <class T>
-__device__ __forceinline__ void finish_alone(const AttendArgs &a, const Share &s, bool empty) {
-    if (a.partial) return;
-    check_length(a, s.b);
-    if (!empty) return;
-    const uint32_t per = a.kv_heads * a.head_blocks, hb = blockIdx.x - s.b * per, kv = hb / a.head_blocks, first = (hb - kv * a.head_blocks) * a.block_heads;
-    const uint32_t count = min(a.block_heads, a.group - first) * a.dim;
-    T *out = (T *)a.out + ((uint64_t)s.b * a.heads + kv * a.group + first) * a.dim;
-    for (uint32_t x = threadIdx.x; x < count; x += THREADS) out[x] = from_float<T>(0.f);
+// Where the block leaves its part of a stretch that others share.
+__device__ __forceinline__ float *part_of(const AttendArgs &a, uint64_t block, bool second) {
+    return a.partial + (2 * block + (second ? 1 : 0)) * a.block_heads * (a.dim + 2);
 }
 
 __device__ __forceinline__ float quotient(float o, float l) { return l > 0.f ? o / l : l == 0.f ? 0.f : l; }
+
+// The block has left its part of stretch w: if it is the last of those that share the (sequence, head block), it joins the
+// parts.  `room`: shared memory for block_heads x MOST_PARTS values; `sums`: for block_heads values.  V values at a time
+// (dim a multiple of V, scratch and output aligned accordingly).
+template <class T, int V>
+__device__ __forceinline__ void join_if_last(const AttendArgs &a, const Share &s, const Stretch &w, float *room, float *sums, uint64_t *flag) {
+    const uint64_t c0 = (w.first + START) / s.size, c1 = (w.first + START + w.tiles - 1) / s.size;
+    const uint32_t count = (uint32_t)(c1 - c0) + 1;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        *flag = atomicAdd(a.arrivals + c0, 1u) == count - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!*flag) return;
+    if (threadIdx.x == 0) a.arrivals[c0] = 0;
+    const uint32_t dim = a.dim;
+    const uint64_t slot = (uint64_t)2 * a.block_heads * (dim + 2);
+    const float *head = part_of(a, c0, c0 * s.size < w.first), *rest = part_of(a, c0, false);  // of the first part; of the others, i x slot on
+    auto of = [&](uint32_t i) { return i ? rest + i * slot : head; };
+    for (uint32_t x = threadIdx.x; x < (uint32_t)w.heads * MOST_PARTS; x += THREADS) {
+        const uint32_t h = x / MOST_PARTS, i = x % MOST_PARTS;
+        if (i < count) room[x] = __ldcg(of(i) + a.block_heads * dim + 2 * h);
+    }
+    __syncthreads();
+    for (int h = threadIdx.x >> 5; h < w.heads; h += THREADS / 32) {  // a warp per head: maxima to weights
+        float top = -INFINITY, sum = 0.f;
+        for (uint32_t i = threadIdx.x & 31; i < count; i += 32) top = fmaxf(top, room[h * MOST_PARTS + i]);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (top == -INFINITY) top = 0.f;
+        for (uint32_t i = threadIdx.x & 31; i < count; i += 32) {
+            const float f = exp2f(room[h * MOST_PARTS + i] - top);
+            room[h * MOST_PARTS + i] = f;
+            sum += f * __ldcg(of(i) + a.block_heads * dim + 2 * h + 1);
+        }
+        sum = warp_sum(sum);
+        if ((threadIdx.x & 31) == 0) sums[h] = sum;
+    }
+    __syncthreads();
+    for (uint32_t x = threadIdx.x; x < (uint32_t)w.heads * (dim / V); x += THREADS) {
+        const uint32_t h = x / (dim / V), d = (x - h * (dim / V)) * V;
+        float o[V] = {};
+#pragma unroll 8
+        for (uint32_t i = 0; i < count; ++i) {
+            const float *p = of(i) + h * dim + d;
+            const float f = room[h * MOST_PARTS + i];
+            if constexpr (V == 4) {
+                const float4 v = __ldcg(reinterpret_cast<const float4 *>(p));
+                o[0] += f * v.x;
+                o[1] += f * v.y;
+                o[2] += f * v.z;
+                o[3] += f * v.w;
+            } else {
+                o[0] += f * __ldcg(p);
+            }
+        }
+        T *out = (T *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * dim + d;
+#pragma unroll
+        for (int k = 0; k < V; ++k) out[k] = from_float<T>(quotient(o[k], sums[h]));
+    }
+    __syncthreads();  // `room` is used again
+}
+
+// The zeros of empty sequences, and the check of the lengths.
+template <class T>
+__device__ __forceinline__ void finish(const AttendArgs &a) {
+    if (!a.partial) {  // the block's own sequence
+        const uint32_t per = a.kv_heads * a.head_blocks, b = blockIdx.x / per;
+        check_length(a, b);
+        if (tiles_of(a, b)) return;
+        const uint32_t hb = blockIdx.x - b * per, kv = hb / a.head_blocks, first = (hb - kv * a.head_blocks) * a.block_heads;
+        const uint32_t count = min(a.block_heads, a.group - first) * a.dim;
+        T *out = (T *)a.out + ((uint64_t)b * a.heads + kv * a.group + first) * a.dim;
+        for (uint32_t x = threadIdx.x; x < count; x += THREADS) out[x] = from_float<T>(0.f);
+        return;
+    }
+    for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
+        check_length(a, b);
+        if (tiles_of(a, b)) continue;
+        T *out = (T *)a.out + (uint64_t)b * a.heads * a.dim;
+        for (uint32_t x = threadIdx.x; x < a.heads * a.dim; x += THREADS) out[x] = from_float<T>(0.f);
+    }
+}
 
 // First element of token i's key in head `kv`; false where its page is no page of the cache.
 __device__ __forceinline__ bool locate(const AttendArgs &a, const int *row, int i, uint32_t kv, uint64_t *at) {
@@ -192,6 +289,8 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
     __shared__ uint64_t part[32], found[2];
     __shared__ float sm_m[4][HEADS], sm_l[4][HEADS];
     __shared__ float sm_o[4][HEADS][NE * 32];
+    float *sm_room = &sm_o[0][0][0];
+    static_assert(4 * NE * 32 >= MOST_PARTS, "the parts' weights fit");
     pdl_release();
     pdl_wait();
     const T *q = (const T *)a.q, *cache = (const T *)a.cache;
@@ -199,7 +298,7 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
     Share s = my_share(a, part, found);
     const uint64_t start = s.idx;
     Stretch w;
-    for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.t1 - w.t0) {
+    for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
         const int *row = a.table + (uint64_t)w.b * a.table_width;
         float qr[HEADS][NE], acc[HEADS][NE], m[HEADS], l[HEADS];
 #pragma unroll
@@ -248,7 +347,7 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
         }
         __syncthreads();
         const bool whole = w.t0 == 0 && w.t1 == w.tiles;
-        float *slot = whole ? nullptr : a.partial + ((uint64_t)2 * blockIdx.x + (s.idx == start ? 0 : 1)) * HEADS * (a.dim + 2);
+        float *slot = whole ? nullptr : part_of(a, blockIdx.x, s.idx != start);
         for (int x = threadIdx.x; x < w.heads * (int)a.dim; x += THREADS) {
             const int h = x / (int)a.dim, d = x - h * (int)a.dim;
             float mm = -INFINITY;
@@ -263,12 +362,13 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
             if (whole) {
                 ((T *)a.out)[((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d] = from_float<T>(quotient(oo, ll));
             } else {
-                slot[h * (a.dim + 2) + d] = oo;
-                if (d == 0) slot[h * (a.dim + 2) + a.dim] = mm, slot[h * (a.dim + 2) + a.dim + 1] = ll;
+                slot[h * a.dim + d] = oo;
+                if (d == 0) slot[HEADS * a.dim + 2 * h] = mm, slot[HEADS * a.dim + 2 * h + 1] = ll;
             }
         }
+        if (!whole) join_if_last<T, 1>(a, s, w, sm_room, &sm_l[0][0], found);
     }
-    finish_alone<T>(a, s, start == s.end);
+    finish<T>(a);
 }
 
 // ------------------------------------------------------------------------------------------- bf16 on the matrix units
@@ -346,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
     Share s = my_share(a, part, found);
     const uint64_t start = s.idx;
     Stretch w;
-    for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.t1 - w.t0) {
+    for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
         // columns from dim to DP stay zero (the memory is also used to join warps)
         if (chunks < CHUNKS)
             for (int x = lane; x < STAGES * 2 * STEP * (CHUNKS - (int)chunks); x += 32) {
@@ -528,7 +628,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
             }
         __syncthreads();
         const bool whole = w.t0 == 0 && w.t1 == w.tiles;
-        float *slot = whole ? nullptr : a.partial + ((uint64_t)2 * blockIdx.x + (s.idx == start ? 0 : 1)) * HEADS * (a.dim + 2);
+        float *slot = whole ? nullptr : part_of(a, blockIdx.x, s.idx != start);
         for (int x = threadIdx.x; x < w.heads * (int)(a.dim / 2); x += THREADS) {
             const int h = x / (int)(a.dim / 2), d = 2 * (x - h * (int)(a.dim / 2));
             float mm = -INFINITY;
@@ -547,70 +647,14 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
             if (whole) {
                 *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d) = pack(quotient(o0, ll), quotient(o1, ll));
             } else {
-                *reinterpret_cast<float2 *>(slot + h * (a.dim + 2) + d) = make_float2(o0, o1);
-                if (d == 0) *reinterpret_cast<float2 *>(slot + h * (a.dim + 2) + a.dim) = make_float2(mm, ll);
+                *reinterpret_cast<float2 *>(slot + h * a.dim + d) = make_float2(o0, o1);
+                if (d == 0) *reinterpret_cast<float2 *>(slot + HEADS * a.dim + 2 * h) = make_float2(mm, ll);
             }
         }
+        if (!whole) join_if_last<__nv_bfloat16, 4>(a, s, w, sm_o, &sm_l[0][0], found);
         __syncthreads();  // the next stretch's copies go where the parts were
     }
-    finish_alone<__nv_bfloat16>(a, s, start == s.end);
-}
-
-// Joins what several blocks left for one query head, in the order of its tiles; writes the zeros of empty sequences.  A
-// thread has one value of the head (two beyond 128); the weights of the parts are computed once for all.
-template <class T>
-__global__ void __launch_bounds__(THREADS) lt_attend_join(const AttendArgs a, const unsigned blocks) {
-    __shared__ uint64_t part[32];
-    __shared__ float weight[THREADS], red[32];
-    pdl_release();
-    pdl_wait();
-    const uint32_t head = blockIdx.x, b = blockIdx.y, blocks_per = a.kv_heads * a.head_blocks;
-    check_length(a, b);
-    uint64_t before, all;
-    count_tiles(a, b, part, &before, &all);
-    const uint32_t tiles = tiles_of(a, b), kv = head / a.group, in_group = head - kv * a.group, h = in_group % a.block_heads;
-    const uint32_t hb = kv * a.head_blocks + in_group / a.block_heads;
-    T *out = (T *)a.out + ((uint64_t)b * a.heads + head) * a.dim;
-    if (tiles == 0) {
-        for (uint32_t d = threadIdx.x; d < a.dim; d += THREADS) out[d] = from_float<T>(0.f);
-        return;
-    }
-    const uint64_t share = share_of(all * blocks_per, blocks), s = before * blocks_per + (uint64_t)hb * tiles, e = s + tiles;
-    const uint32_t c0 = (uint32_t)(s / share), c1 = (uint32_t)((e - 1) / share);
-    if (c0 == c1) return;  // finished by its block
-    const uint32_t stride = a.dim + 2, count = c1 - c0 + 1;
-    // part i of the head: the first one is its block's second unless the head begins where the block does
-    const uint64_t slot = (uint64_t)2 * a.block_heads * stride, at0 = (uint64_t)h * stride + (s != c0 * share ? (uint64_t)a.block_heads * stride : 0);
-    const float *parts = a.partial + c0 * slot + (uint64_t)h * stride;
-    auto of = [&](uint32_t i) -> const float * { return i ? parts + i * slot : a.partial + c0 * slot + at0; };
-    float top = -INFINITY;
-    for (uint32_t i = threadIdx.x; i < count; i += THREADS) top = fmaxf(top, of(i)[a.dim]);
-    top = block_reduce<true>(top, red);
-    if (top == -INFINITY) top = 0.f;
-    const uint32_t d0 = threadIdx.x, d1 = threadIdx.x + THREADS;
-    float o0 = 0.f, o1 = 0.f, sum = 0.f;
-    for (uint32_t i0 = 0; i0 < count; i0 += THREADS) {
-        const uint32_t n = min(count - i0, (uint32_t)THREADS);
-        __syncthreads();
-        if (threadIdx.x < n) {
-            const float *p = of(i0 + threadIdx.x);
-            const float f = exp2f(p[a.dim] - top);
-            weight[threadIdx.x] = f;
-            sum += f * p[a.dim + 1];
-        }
-        __syncthreads();
-        if (d0 < a.dim) {
-#pragma unroll 8
-            for (uint32_t i = 0; i < n; ++i) o0 += weight[i] * of(i0 + i)[d0];
-        }
-        if (d1 < a.dim) {
-#pragma unroll 8
-            for (uint32_t i = 0; i < n; ++i) o1 += weight[i] * of(i0 + i)[d1];
-        }
-    }
-    sum = block_reduce<false>(sum, red);
-    if (d0 < a.dim) out[d0] = from_float<T>(quotient(o0, sum));
-    if (d1 < a.dim) out[d1] = from_float<T>(quotient(o1, sum));
+    finish<__nv_bfloat16>(a);
 }
 
 // A block of its own per (sequence, head block) when no sequence can hold more than a few tiles.
@@ -663,7 +707,7 @@ size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count) {
     return 2 * (size_t)sm_count * (any > tensor ? any : tensor) * (o.dim + 2) * sizeof(float);
 }
 
-cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream, unsigned *launched) {
+cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream) {
     AttendArgs a{};
     a.q = o.in[0];
     a.cache = o.in[1];
@@ -671,6 +715,7 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     a.lengths = (const int *)o.in[3];
     a.out = o.out[0];
     a.partial = split(o) ? (float *)o.scratch : nullptr;
+    a.arrivals = (unsigned int *)o.arrivals;
     a.status = status;
     a.q_pitch = o.pitch[0];
     a.value_offset = (uint64_t)o.page * o.kv_heads * o.dim;
@@ -691,7 +736,6 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     a.head_blocks = (a.group + a.block_heads - 1) / a.block_heads;
     const unsigned per = a.kv_heads * a.head_blocks;
     const unsigned grid = a.partial ? (unsigned)sm_count * (tensor ? tensor_blocks(tensor_width(o.dim), (int)a.block_heads / 8) : ANY_BLOCKS) : a.batch * per;
-    *launched = 1;
     cudaError_t e;
     if (!tensor) {
         e = o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
@@ -704,9 +748,5 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
         default: e = launch_tensor_heads<256>(a, grid, stream); break;
         }
     }
-    if (e != cudaSuccess || !a.partial) return e;
-    *launched = 2;
-    const dim3 g2(a.heads, a.batch);
-    return o.dtype == LT_BF16 ? launch_pdl_grid(lt_attend_join<__nv_bfloat16>, g2, THREADS, stream, a, grid)
-                              : launch_pdl_grid(lt_attend_join<float>, g2, THREADS, stream, a, grid);
+    return e;
 }

@@ -1191,6 +1191,7 @@ lt_status lt_ctx_destroy(lt_ctx *c) {
     for (auto e : c->event_pool) cudaEventDestroy(e);
     for (auto &b : c->buffers)
         if (b.owned && b.ptr && b.refs > 0) ctx_free(c, b.ptr);
+    ctx_free(c, c->arrivals);
     pool_trim(c, 0);
     delete c;
     return LT_OK;

@@ -183,6 +183,7 @@ struct Plan {
     uint64_t hash[2];
     std::vector<uint8_t> canon_bytes;
     uint32_t n_params = 0, n_dyn = 0;
+    bool needs_arrivals = false;  // an operator whose blocks share a result is in it
     std::vector<OutputPlan> outputs;
     std::vector<size_t> temp_bytes;
     std::vector<Group> groups;
@@ -370,6 +371,7 @@ struct lt_ctx {
 
     lt::ReplayRecord replay;
     lt::TraceState trace;
+    void *arrivals = nullptr;           // LT_ARRIVALS counters of operators whose blocks share a result; made at their first flush
     bool index_status_pending = false;  // an operator that follows indices in device memory ran since its status word was last read
     bool status_pending = false;      // a kernel with bounded device-side waits ran since the status word was last read
     int64_t wait_limit_ns = 2000000000ll;  // how long such a wait may last

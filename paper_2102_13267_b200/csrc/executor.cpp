@@ -246,6 +246,30 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
         }
     }
 
+    // counters of operators whose blocks share a result: zero now, and left at zero by every launch that uses them
+    void *arrivals = nullptr;
+    if (plan.needs_arrivals && !dry) {
+        cudaError_t ae = cudaSuccess;
+        if (c->static_mode) {
+            ae = lt_static_arrivals(&arrivals);
+        } else if (!c->arrivals) {
+            arrivals = ctx_alloc(c, LT_ARRIVALS * sizeof(unsigned int));
+            if (!arrivals) {
+                release_all(true);
+                return fail(c, LT_ERR_OOM, "allocator returned null for an operator's counters");
+            }
+            ae = cudaMemsetAsync(arrivals, 0, LT_ARRIVALS * sizeof(unsigned int), c->stream);
+            if (ae == cudaSuccess) c->arrivals = arrivals;
+            else ctx_free(c, arrivals);
+        } else {
+            arrivals = c->arrivals;
+        }
+        if (ae != cudaSuccess) {
+            release_all(true);
+            return fail(c, LT_ERR_CUDA, std::string("an operator's counters: ") + cudaGetErrorString(ae));
+        }
+    }
+
     auto resolve = [&](const IoRef &io) -> uint64_t {
         void *p = io.kind == IO_PARAM ? c->param_ptr[io.index] : io.kind == IO_OUTPUT ? c->out_ptr[io.index] : c->temp_ptr[io.index];
         return (uint64_t)(uintptr_t)p + io.offset * dtype_size(io.dtype);  // (offset: a slice read in place)
@@ -268,6 +292,7 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
                 for (size_t q = g.n_operands; q < g.io.size(); ++q)
                     if (g.io[q].is_store) o.out[g.results[q]] = (void *)(uintptr_t)resolve(g.io[q]);
                 o.scratch = g.scratch_temp >= 0 ? c->temp_ptr[g.scratch_temp] : nullptr;
+                o.arrivals = arrivals;
                 if (ev0) cudaEventRecord(ev0, c->stream);
                 e = lt_launch_operator(o, c->sm_count, c->stream, &launched);
                 if (ev1) cudaEventRecord(ev1, c->stream);

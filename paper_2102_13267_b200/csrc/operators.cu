@@ -10,27 +10,29 @@
 using namespace ltop;
 
 static __device__ unsigned int lt_operator_status = 0;
+static __device__ unsigned int lt_operator_arrivals[LT_ARRIVALS];
 
 namespace {
 
 constexpr int kMaxDevices = 64;
 std::mutex g_lock;
-void *g_status[kMaxDevices];
+void *g_status[kMaxDevices], *g_arrivals[kMaxDevices];
 
-cudaError_t status_address(unsigned int **out) {
+// Address of a device variable on the current device, looked up once per device.
+template <class S>
+cudaError_t address_of(const S &symbol, void **known, void **out) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> hold(g_lock);
-    if (!g_status[device]) {
-        e = cudaGetSymbolAddress(&g_status[device], lt_operator_status);
-        if (e != cudaSuccess) {
-            g_status[device] = nullptr;
-            return e;
-        }
+    if (!known[device]) {
+        void *p = nullptr;
+        e = cudaGetSymbolAddress(&p, symbol);
+        if (e != cudaSuccess) return e;
+        known[device] = p;
     }
-    *out = (unsigned int *)g_status[device];
+    *out = known[device];
     return cudaSuccess;
 }
 
@@ -374,20 +376,23 @@ size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count) {
 
 cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
     *launched = 1;
-    unsigned int *status = nullptr;
+    void *word = nullptr;
     if (o.op == LT_OP_CACHE_APPEND || o.op == LT_OP_PAGED_ATTENTION) {
-        const cudaError_t e = status_address(&status);
+        const cudaError_t e = address_of(lt_operator_status, g_status, &word);
         if (e != cudaSuccess) return e;
     }
+    unsigned int *status = (unsigned int *)word;
     switch (o.op) {
     case LT_OP_ROTARY: return lt_launch_rotary(o, sm_count, stream);
     case LT_OP_CACHE_APPEND: return lt_launch_cache_append(o, status, sm_count, stream, launched);
-    case LT_OP_PAGED_ATTENTION: return lt_launch_paged_attention(o, status, sm_count, stream, launched);
+    case LT_OP_PAGED_ATTENTION: return lt_launch_paged_attention(o, status, sm_count, stream);
     case LT_OP_RMS_NORM: return lt_launch_rms_norm(o, sm_count, stream);
     case LT_OP_RMS_NORM_GRAD: return lt_launch_rms_norm_grad(o, sm_count, stream, launched);
     default: return cudaErrorInvalidValue;
     }
 }
+
+cudaError_t lt_static_arrivals(void **out) { return address_of(lt_operator_arrivals, g_arrivals, out); }
 
 cudaError_t lt_operator_status_read(unsigned int *out) {
     cudaError_t e = cudaMemcpyFromSymbol(out, lt_operator_status, sizeof(*out));

@@ -21,6 +21,7 @@ struct LtOperator {
     void *out[LT_OPERATOR_RESULTS];        // per result; null where the graph does not ask for it
     unsigned wanted;                       // bit k: result k is asked for
     void *scratch;
+    void *arrivals;                        // paged_attention: LT_ARRIVALS counters that are zero between launches
     // sizes (those that the operator has)
     uint64_t rows;                         // tokens, sequences or rows
     uint32_t heads, kv_heads, dim, pairs;  // pairs: rotated pairs of a head
@@ -49,6 +50,10 @@ static inline int operator_inputs(int op, int n_in, const int64_t *attrs) {
 }
 
 size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count);
+// Counters of blocks that have left their part of a result that several share.  A context has its own; flushes that may not
+// allocate share one array per device, like the static scratch.
+#define LT_ARRIVALS 2048
+cudaError_t lt_static_arrivals(void **out);
 // Enqueues the operator on `stream`; *launched receives the number of kernels.
 cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
 // Indices in device memory that lay outside what they index, since the last call (synchronises): bit 0 paged_attention, bit 1 cache_append.
@@ -57,7 +62,7 @@ cudaError_t lt_operator_status_read(unsigned int *out);
 // the operators' own launchers
 cudaError_t lt_launch_rotary(const LtOperator &o, int sm_count, cudaStream_t stream);
 cudaError_t lt_launch_cache_append(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream, unsigned *launched);
-cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream, unsigned *launched);
+cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream);
 size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_rms_norm(const LtOperator &o, int sm_count, cudaStream_t stream);
 cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);

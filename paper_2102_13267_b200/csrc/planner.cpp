@@ -1159,6 +1159,7 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
             if (scratch) {
                 g.scratch_temp = (int32_t)plan.temp_bytes.size();
                 plan.temp_bytes.push_back(scratch);
+                if (g.operation.op == LT_OP_PAGED_ATTENTION) plan.needs_arrivals = true;
             }
         }
         if (g.kind == K_RED) {
