@@ -404,10 +404,6 @@ __device__ __forceinline__ float power2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
 
 constexpr int STEP = 16;        // tokens a warp takes at a time: a quarter of a tile
 constexpr int STAGES = 3;
@@ -588,8 +584,8 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const float x = c[t][2 * i], y = c[t][2 * i + 1];
-                    const uint32_t hi = pack(x, y);
-                    const uint32_t lo = pack(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+                    const uint32_t hi = pack_bf16(x, y);
+                    const uint32_t lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
                     p_hi[t][i] = turned(hi);
                     p_lo[t][i] = turned(lo);
                 }
@@ -645,7 +641,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
                 o1 += v.y * f;
             }
             if (whole) {
-                *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d) = pack(quotient(o0, ll), quotient(o1, ll));
+                *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d) = pack_bf16(quotient(o0, ll), quotient(o1, ll));
             } else {
                 *reinterpret_cast<float2 *>(slot + h * a.dim + d) = make_float2(o0, o1);
                 if (d == 0) *reinterpret_cast<float2 *>(slot + HEADS * a.dim + 2 * h) = make_float2(mm, ll);

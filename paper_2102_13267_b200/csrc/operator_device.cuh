@@ -51,6 +51,56 @@ __device__ __forceinline__ float block_reduce(float v, float *part) {
     return r;
 }
 
+// 16 bytes of T as binary32 and back
+template <class T>
+struct Chunk {
+    static constexpr int N = 16 / (int)sizeof(T);
+};
+
+__device__ __forceinline__ void unpack(const uint4 &v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void unpack(const uint4 &v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// Division of 32-bit numbers by one known on the host (as fastdiv_make does for the row kernels).
+struct Divisor {
+    uint32_t by, mul, sh1, sh2;
+    __host__ static Divisor make(uint32_t d) {
+        Divisor r;
+        r.by = d;
+        uint32_t l = 0;
+        while (l < 32 && (1ull << l) < d) ++l;
+        r.mul = (uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1);
+        r.sh1 = l < 1 ? l : 1;
+        r.sh2 = l < 1 ? 0 : l - 1;
+        return r;
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const {
+        const uint32_t t = __umulhi(mul, n);
+        return (t + ((n - t) >> sh1)) >> sh2;
+    }
+};
+
 // The angle of `position` turns at a frequency given as a 64-bit fraction of a turn: the product modulo 2^64 is the
 // fraction of a turn that is left, exactly, however far the position; its upper 32 bits (rounded) are the angle to
 // 2^-33 of a turn.  Returns scale (cos, sin).

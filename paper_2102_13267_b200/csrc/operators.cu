@@ -3,6 +3,7 @@
 // that reads the cache is in attention.cu.
 #include <cuda_fp8.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "operator_device.cuh"
@@ -114,8 +115,131 @@ __global__ void __launch_bounds__(256) lt_turn_any(const TurnArgs a) {
     }
 }
 
+constexpr int TURN_THREADS = 256, TURN_FLIGHT = 4;
+
+struct TurnShape {
+    uint32_t block_tokens;      // tokens of a block
+    uint32_t turned, passed;    // units of a head that turn and that pass through
+    Divisor per_token, per_head, pairs;
+};
+
+// 16 bytes at a time.  A unit is what a thread reads and writes at once: two chunks whose values form pairs, one chunk of
+// neighbouring pairs (interleaved), one that passes through, or one of the values (cache_append).  The bound is memory; the
+// angles would not be free if every head computed them (a sine and a cosine are some fifty instructions), so a block
+// computes those of its tokens once, into shared memory, while the first loads are on their way.
+// Measured on 8192 tokens x 32 heads x 128 bf16: see the table in the documentation of the operators.
+template <class T, bool APPEND>
+__global__ void __launch_bounds__(TURN_THREADS) lt_turn_chunks(const TurnArgs a, const TurnShape sh) {
+    constexpr int N = Chunk<T>::N;
+    extern __shared__ float turn_mem[];  // cosines, then sines, [block_tokens][pairs]
+    __shared__ uint64_t sm_at[TURN_THREADS];  // where a token goes (all ones: nowhere)
+    const uint64_t t0 = (uint64_t)blockIdx.x * sh.block_tokens;
+    const uint32_t tokens = (uint32_t)min((uint64_t)sh.block_tokens, a.tokens - t0);
+    const uint32_t units = tokens * sh.per_token.by, angles = tokens * a.pairs;
+    float *cosines = turn_mem, *sines = turn_mem + sh.block_tokens * a.pairs;
+    pdl_release();
+    pdl_wait();
+    const T *x = (const T *)a.x, *v = (const T *)a.v;
+    for (uint32_t u0 = 0; u0 < units; u0 += TURN_THREADS * TURN_FLIGHT) {
+        uint4 lo[TURN_FLIGHT], hi[TURN_FLIGHT];
+        uint32_t token[TURN_FLIGHT], head[TURN_FLIGHT], chunk[TURN_FLIGHT];
+#pragma unroll
+        for (int k = 0; k < TURN_FLIGHT; ++k) {
+            const uint32_t u = u0 + k * TURN_THREADS + threadIdx.x;
+            if (u >= units) break;
+            token[k] = sh.per_token.quotient(u);
+            const uint32_t r = u - token[k] * sh.per_token.by;
+            head[k] = sh.per_head.quotient(r);
+            chunk[k] = r - head[k] * sh.per_head.by;
+            if (APPEND && chunk[k] >= sh.turned + sh.passed) {
+                lo[k] = *reinterpret_cast<const uint4 *>(v + (t0 + token[k]) * a.v_pitch + (uint64_t)head[k] * a.dim + (chunk[k] - sh.turned - sh.passed) * N);
+            } else {
+                const T *src = x + (t0 + token[k]) * a.x_pitch + (uint64_t)head[k] * a.dim;
+                const bool turns = chunk[k] < sh.turned;
+                lo[k] = *reinterpret_cast<const uint4 *>(src + (turns ? chunk[k] * N : 2 * a.pairs + (chunk[k] - sh.turned) * N));
+                if (turns && !a.interleaved) hi[k] = *reinterpret_cast<const uint4 *>(src + a.pairs + chunk[k] * N);
+            }
+        }
+        if (u0 == 0) {
+            for (uint32_t i = threadIdx.x; i < angles; i += TURN_THREADS) {
+                const uint32_t t = sh.pairs.quotient(i);
+                const float2 cs = turn(a.positions[t0 + t], a.frequencies[i - t * a.pairs], a.scale, a.inverse != 0);
+                cosines[i] = cs.x;
+                sines[i] = cs.y;
+            }
+            if (threadIdx.x < tokens) {
+                uint64_t at;
+                sm_at[threadIdx.x] = destination<APPEND>(a, t0 + threadIdx.x, &at) ? at : ~0ull;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int k = 0; k < TURN_FLIGHT; ++k) {
+            const uint32_t u = u0 + k * TURN_THREADS + threadIdx.x;
+            if (u >= units) break;
+            const uint64_t at = sm_at[token[k]];
+            if (APPEND && at == ~0ull) continue;
+            T *dst = (T *)a.out + at + (uint64_t)head[k] * (APPEND ? a.head_stride : (uint64_t)a.dim);
+            if (chunk[k] >= sh.turned) {
+                const bool value = APPEND && chunk[k] >= sh.turned + sh.passed;
+                const uint64_t to = value ? a.value_offset + (chunk[k] - sh.turned - sh.passed) * N : 2 * a.pairs + (chunk[k] - sh.turned) * N;
+                *reinterpret_cast<uint4 *>(dst + to) = lo[k];
+                continue;
+            }
+            float p[N], q[N];
+            unpack(lo[k], p);
+            if (a.interleaved) {
+                const float *c = cosines + token[k] * a.pairs + chunk[k] * (N / 2), *s = sines + token[k] * a.pairs + chunk[k] * (N / 2);
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    q[2 * i] = p[2 * i] * c[i] - p[2 * i + 1] * s[i];
+                    q[2 * i + 1] = p[2 * i] * s[i] + p[2 * i + 1] * c[i];
+                }
+                *reinterpret_cast<uint4 *>(dst + chunk[k] * N) = pack(q);
+            } else {
+                const float4 *c = reinterpret_cast<const float4 *>(cosines + token[k] * a.pairs + chunk[k] * N), *s = reinterpret_cast<const float4 *>(sines + token[k] * a.pairs + chunk[k] * N);
+                unpack(hi[k], q);
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) {
+                    const float4 cc = c[i], ss = s[i];
+                    const float co[4] = {cc.x, cc.y, cc.z, cc.w}, si[4] = {ss.x, ss.y, ss.z, ss.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float fp = p[4 * i + j], fq = q[4 * i + j];
+                        p[4 * i + j] = fp * co[j] - fq * si[j];
+                        q[4 * i + j] = fp * si[j] + fq * co[j];
+                    }
+                }
+                *reinterpret_cast<uint4 *>(dst + chunk[k] * N) = pack(p);
+                *reinterpret_cast<uint4 *>(dst + a.pairs + chunk[k] * N) = pack(q);
+            }
+        }
+    }
+}
+
 template <class T, bool APPEND>
 cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
+    constexpr uint32_t N = Chunk<T>::N;
+    const bool chunks = a.dim % N == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % N == 0 && a.x_pitch % N == 0 && is_aligned(a.x, 16) && is_aligned(a.out, 16) &&
+                        (!APPEND || (a.v_pitch % N == 0 && is_aligned(a.v, 16)));
+    const uint32_t turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N, passed = (a.dim - 2 * a.pairs) / N, per_head = turned + passed + (APPEND ? a.dim / N : 0);
+    const uint64_t per_token = (uint64_t)per_head * a.heads;
+    if (chunks && a.pairs <= 2048 && per_token < (1u << 20) && a.tokens < (1ull << 31)) {
+        // enough tokens for a thread to have TURN_FLIGHT units in flight, fewer where that would leave SMs without a block
+        uint64_t n = TURN_THREADS * TURN_FLIGHT / per_token;
+        if (n > a.tokens / (2 * (uint64_t)sm_count)) n = a.tokens / (2 * (uint64_t)sm_count);
+        if (a.pairs && n > 4096 / a.pairs) n = 4096 / a.pairs;  // (32 KB of cosines and sines)
+        if (n > TURN_THREADS) n = TURN_THREADS;
+        if (n < 1) n = 1;
+        TurnShape sh;
+        sh.block_tokens = (uint32_t)n;
+        sh.turned = turned;
+        sh.passed = passed;
+        sh.per_token = Divisor::make((uint32_t)per_token);
+        sh.per_head = Divisor::make(per_head);
+        sh.pairs = Divisor::make(a.pairs ? a.pairs : 1);
+        return launch_pdl(lt_turn_chunks<T, APPEND>, (unsigned)((a.tokens + n - 1) / n), TURN_THREADS, (size_t)n * a.pairs * 8, stream, a, sh);
+    }
     const uint64_t total = a.tokens * (a.dim - a.pairs);
     const uint64_t blocks = (total + 255) / 256, most = (uint64_t)sm_count * 32;
     return launch_pdl(lt_turn_any<T, APPEND>, (unsigned)(blocks < most ? blocks : most), 256, (size_t)0, stream, a);
@@ -196,6 +320,132 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
     }
 }
 
+// N values of gamma from column c on, which is a multiple of N
+template <class T>
+__device__ __forceinline__ void gamma_chunk(const void *gamma, int f32, uint32_t c, float (&g)[Chunk<T>::N]) {
+    constexpr int N = Chunk<T>::N;
+    if (f32 || sizeof(T) == 4) {
+        const float4 *p = reinterpret_cast<const float4 *>((const float *)gamma + c);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 v = p[i];
+            g[4 * i] = v.x;
+            g[4 * i + 1] = v.y;
+            g[4 * i + 2] = v.z;
+            g[4 * i + 3] = v.w;
+        }
+    } else {
+        unpack(*reinterpret_cast<const uint4 *>((const T *)gamma + c), g);
+    }
+}
+
+// Sum or maximum over the RT threads of a row: a warp, or a block of its own.
+template <int RT, bool MAX>
+__device__ __forceinline__ float row_reduce(float v, float *part) {
+    if constexpr (RT == 32) return MAX ? warp_max_nan(v) : warp_sum(v);
+    else return block_reduce<MAX>(v, part);
+}
+
+// 16 bytes at a time, a row in the registers of its RT threads (CH chunks each): every value is read once and every
+// result written once, so the bound is memory.  Threads keep their columns of gamma from row to row and ask for the next
+// row before they reduce this one.
+template <class T, int RT, int CH>
+__global__ void __launch_bounds__(RT == 32 ? 128 : RT) lt_norm_rows(const NormArgs a) {
+    constexpr int N = Chunk<T>::N;
+    __shared__ float part[32];
+    const uint32_t lane = RT == 32 ? (threadIdx.x & 31) : threadIdx.x;
+    const uint32_t chunks = (uint32_t)a.cols / N;
+    const uint64_t step = RT == 32 ? (uint64_t)gridDim.x * 4 : gridDim.x;
+    uint64_t row = RT == 32 ? (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    pdl_release();
+    pdl_wait();
+    float g[CH][N];
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+        if (lane + k * RT < chunks) gamma_chunk<T>(a.gamma, a.gamma_f32, (lane + k * RT) * N, g[k]);
+    uint4 x[CH], r[CH];
+    auto fetch = [&](uint64_t at) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const uint32_t c = lane + k * RT;
+            if (c < chunks && at < a.rows) {
+                x[k] = *reinterpret_cast<const uint4 *>((const T *)a.x + at * a.x_pitch + (uint64_t)c * N);
+                if (a.r) r[k] = *reinterpret_cast<const uint4 *>((const T *)a.r + at * a.r_pitch + (uint64_t)c * N);
+            }
+        }
+    };
+    fetch(row);
+    for (; row < a.rows; row += step) {
+        float h[CH][N], ss = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if (lane + k * RT >= chunks) continue;
+            unpack(x[k], h[k]);
+            if (a.r) {
+                float f[N];
+                unpack(r[k], f);
+#pragma unroll
+                for (int i = 0; i < N; ++i) h[k][i] += f[i];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss += h[k][i] * (h[k][i] * a.down);
+        }
+        fetch(row + step);  // (results of this row go over its own operands only)
+        const float inv = rsqrtf(row_reduce<RT, false>(ss, part) * a.up + a.eps);
+        if (a.sum) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.sum + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(h[k]);
+        }
+        float top[CH], row_top = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            top[k] = 0.f;
+            if (lane + k * RT >= chunks) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                h[k][i] = h[k][i] * inv * g[k][i];
+                top[k] = max_nan(top[k], fabsf(h[k][i]));
+            }
+            row_top = max_nan(row_top, top[k]);
+        }
+        if (a.y) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.y + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(h[k]);
+        }
+        if (a.codes || a.scales) {
+            const uint32_t lanes = a.group / N;  // of a group; 0: the row
+            if (!a.group) {
+                row_top = row_reduce<RT, true>(row_top, part);
+                if (a.scales && lane == 0) a.scales[row] = __fdiv_rn(row_top, 448.f);
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                const uint32_t c = lane + k * RT;
+                float t = row_top;
+                if (a.group) {
+                    t = top[k];
+                    for (uint32_t d = 1; d < lanes; d <<= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, d));
+                    if (a.scales && c < chunks && c % lanes == 0) a.scales[row * a.groups + c / lanes] = __fdiv_rn(t, 448.f);
+                }
+                if (!a.codes || c >= chunks) continue;
+                const float f = code_factor(t);
+                uint32_t w[N / 4];
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) {
+                    const uint32_t p0 = __nv_cvt_float2_to_fp8x2(make_float2(h[k][4 * i] * f, h[k][4 * i + 1] * f), __NV_SATFINITE, __NV_E4M3);
+                    const uint32_t p1 = __nv_cvt_float2_to_fp8x2(make_float2(h[k][4 * i + 2] * f, h[k][4 * i + 3] * f), __NV_SATFINITE, __NV_E4M3);
+                    w[i] = p0 | (p1 << 16);
+                }
+                uint8_t *to = a.codes + row * a.cols + (uint64_t)c * N;
+                if constexpr (N == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<uint32_t *>(to) = w[0];
+            }
+        }
+    }
+}
+
 struct NormGradArgs {
     const void *dy, *h, *gamma, *dh;
     void *dx;
@@ -236,15 +486,138 @@ __global__ void __launch_bounds__(256) lt_norm_grad_any(const NormGradArgs a) {
     }
 }
 
-// The blocks' sums, in their order, in binary64.
-template <class G>
-__global__ void __launch_bounds__(256) lt_norm_grad_join(const float *partial, G *out, uint64_t cols, unsigned blocks) {
+// Sums of two values over the RT threads of a row group inside a block (`group`: which).
+template <int RT>
+__device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int group) {
+    x = warp_sum(x);
+    y = warp_sum(y);
+    if constexpr (RT == 32) return make_float2(x, y);
+    constexpr int W = RT / 32;
+    float2 *mine = part + group * W;
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");  // `mine` may still be read
+    if ((threadIdx.x & 31) == 0) mine[(threadIdx.x % RT) >> 5] = make_float2(x, y);
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");
+    float2 s = mine[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s.x += mine[w].x, s.y += mine[w].y;
+    return s;
+}
+
+// 16 bytes at a time, a row in the registers of its RT threads; a block has several rows at once and goes on to others,
+// the sums for gamma staying in registers.  Bound by memory like lt_norm_rows.
+template <class T, int RT, int CH>
+__global__ void __launch_bounds__(RT > 512 ? RT : 512) lt_norm_grad_rows(const NormGradArgs a) {
+    constexpr int N = Chunk<T>::N, BLOCK = RT > 512 ? RT : 512, GROUPS = BLOCK / RT;
+    __shared__ float2 part[32];
+    extern __shared__ float4 grad_mem[];  // [GROUPS - 1][cols]: the groups' sums for gamma
+    const int group = threadIdx.x / RT;
+    const uint32_t lane = threadIdx.x % RT, chunks = (uint32_t)a.cols / N;
+    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
     pdl_release();
     pdl_wait();
-    for (uint64_t c = (uint64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (uint64_t)gridDim.x * 256) {
+    float g[CH][N], sum[CH][N];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[k][i] = sum[k][i] = 0.f;
+        if (lane + k * RT < chunks) gamma_chunk<T>(a.gamma, a.gamma_f32, (lane + k * RT) * N, g[k]);
+    }
+    uint4 dy[CH], h[CH], dh[CH];
+    auto fetch = [&](uint64_t at) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const uint32_t c = lane + k * RT;
+            dy[k] = h[k] = dh[k] = make_uint4(0, 0, 0, 0);
+            if (c < chunks && at < a.rows) {
+                dy[k] = *reinterpret_cast<const uint4 *>((const T *)a.dy + at * a.dy_pitch + (uint64_t)c * N);
+                h[k] = *reinterpret_cast<const uint4 *>((const T *)a.h + at * a.h_pitch + (uint64_t)c * N);
+                if (a.dh) dh[k] = *reinterpret_cast<const uint4 *>((const T *)a.dh + at * a.dh_pitch + (uint64_t)c * N);
+            }
+        }
+    };
+    uint64_t row = (uint64_t)blockIdx.x * GROUPS + group;
+    fetch(row);
+    for (; row < a.rows; row += step) {
+        float d[CH][N], u[CH][N], e[CH][N], ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            unpack(dy[k], d[k]);
+            unpack(h[k], u[k]);
+            unpack(dh[k], e[k]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ss += u[k][i] * (u[k][i] * a.down);
+                dot += d[k][i] * g[k][i] * (u[k][i] * a.down);
+            }
+        }
+        fetch(row + step);
+        const float2 s = group_sum<RT>(ss, dot, part, group);
+        const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float n = u[k][i] * inv;
+                sum[k][i] += d[k][i] * n;
+                e[k][i] += (d[k][i] * g[k][i] - n * m) * inv;
+            }
+            if (a.dx && lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.dx + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(e[k]);
+        }
+    }
+    if (!a.partial) return;
+    if (GROUPS > 1) {
+        if (group > 0) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (lane + k * RT < chunks) {
+#pragma unroll
+                    for (int i = 0; i < N / 4; ++i)
+                        grad_mem[((uint64_t)(group - 1) * a.cols + (uint64_t)(lane + k * RT) * N) / 4 + i] = make_float4(sum[k][4 * i], sum[k][4 * i + 1], sum[k][4 * i + 2], sum[k][4 * i + 3]);
+                }
+        }
+        __syncthreads();
+        if (group > 0) return;
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const uint32_t c = lane + k * RT;
+        if (c >= chunks) continue;
+        for (int o = 1; o < GROUPS; ++o)
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                const float4 v = grad_mem[((uint64_t)(o - 1) * a.cols + (uint64_t)c * N) / 4 + i];
+                sum[k][4 * i] += v.x;
+                sum[k][4 * i + 1] += v.y;
+                sum[k][4 * i + 2] += v.z;
+                sum[k][4 * i + 3] += v.w;
+            }
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            *reinterpret_cast<float4 *>(a.partial + (uint64_t)blockIdx.x * a.cols + (uint64_t)c * N + 4 * i) = make_float4(sum[k][4 * i], sum[k][4 * i + 1], sum[k][4 * i + 2], sum[k][4 * i + 3]);
+    }
+}
+
+// The blocks' sums, in binary64, always in the same order: a warp's lanes have neighbouring columns, its 32 warps every
+// 32nd block each.
+template <class G>
+__global__ void __launch_bounds__(1024) lt_norm_grad_join(const float *partial, G *out, uint64_t cols, unsigned blocks) {
+    __shared__ double sums[32][33];
+    pdl_release();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (uint64_t c0 = (uint64_t)blockIdx.x * 32; c0 < cols; c0 += (uint64_t)gridDim.x * 32) {
         double s = 0.0;
-        for (unsigned b = 0; b < blocks; ++b) s += (double)partial[(uint64_t)b * cols + c];
-        out[c] = from_float<G>((float)s);
+        if (c0 + lane < cols) {
+#pragma unroll 4
+            for (unsigned b = warp; b < blocks; b += 32) s += (double)partial[(uint64_t)b * cols + c0 + lane];
+        }
+        __syncthreads();
+        sums[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && c0 + lane < cols) {
+            for (int w = 1; w < 32; ++w) s += sums[w][lane];
+            out[c0 + lane] = from_float<G>((float)s);
+        }
     }
 }
 
@@ -256,9 +629,97 @@ void mean_factors(uint64_t cols, float *down, float *up) {
     *up = (float)((double)(1ull << k) / (double)cols);
 }
 
-unsigned norm_grad_blocks(const LtOperator &o, int sm_count) {
-    const uint64_t most = (uint64_t)sm_count * 4;
-    return (unsigned)(o.rows < most ? o.rows : most);
+// Threads per row: enough that a thread has at most `most` chunks.  0: the row does not fit.
+int row_threads(uint64_t chunks, int most) {
+    for (int rt : {32, 128, 256, 512, 1024})
+        if (chunks <= (uint64_t)rt * most) return rt;
+    return 0;
+}
+
+template <class T, int RT, int CH>
+cudaError_t launch_norm_rows(const NormArgs &a, int sm_count, cudaStream_t stream) {
+    const uint64_t blocks = RT == 32 ? (a.rows + 3) / 4 : a.rows;
+    // as many blocks as an SM holds, each going on to further rows
+    static int resident = 0;
+    if (!resident) {
+        int n = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, lt_norm_rows<T, RT, CH>, RT == 32 ? 128 : RT, 0);
+        if (e != cudaSuccess) return e;
+        resident = n < 1 ? 1 : n;
+    }
+    const uint64_t most = (uint64_t)sm_count * resident;
+    return launch_pdl(lt_norm_rows<T, RT, CH>, (unsigned)(blocks < most ? blocks : most), RT == 32 ? 128 : RT, (size_t)0, stream, a);
+}
+
+template <class T, int CH>
+cudaError_t launch_norm_threads(const NormArgs &a, int rt, int sm_count, cudaStream_t stream) {
+    switch (rt) {
+    case 32: return launch_norm_rows<T, 32, CH>(a, sm_count, stream);
+    case 128: return launch_norm_rows<T, 128, CH>(a, sm_count, stream);
+    case 256: return launch_norm_rows<T, 256, CH>(a, sm_count, stream);
+    case 512: return launch_norm_rows<T, 512, CH>(a, sm_count, stream);
+    default: return launch_norm_rows<T, 1024, CH>(a, sm_count, stream);
+    }
+}
+
+template <class T>
+cudaError_t launch_norm(const NormArgs &a, int sm_count, cudaStream_t stream) {
+    constexpr uint64_t N = Chunk<T>::N;
+    const uint64_t chunks = a.cols / N;
+    const bool fits = a.cols % N == 0 && a.x_pitch % N == 0 && (!a.r || (a.r_pitch % N == 0 && is_aligned(a.r, 16))) && is_aligned(a.x, 16) && is_aligned(a.gamma, 16) &&
+                      is_aligned(a.y, 16) && is_aligned(a.sum, 16) && is_aligned(a.codes, 8) && a.group <= 32 * N;
+    // few rows: one chunk per thread, the most threads a row can use; many: four, fewer threads to agree on a sum
+    const int most = a.rows <= 2 * (uint64_t)sm_count ? 1 : 4;
+    const int rt = fits ? row_threads(chunks, most) : 0, rt4 = fits ? row_threads(chunks, 4) : 0;
+    if (rt && most == 1) return launch_norm_threads<T, 1>(a, rt, sm_count, stream);
+    if (rt4) {
+        if (chunks <= (uint64_t)rt4) return launch_norm_threads<T, 1>(a, rt4, sm_count, stream);
+        if (chunks <= 2 * (uint64_t)rt4) return launch_norm_threads<T, 2>(a, rt4, sm_count, stream);
+        return launch_norm_threads<T, 4>(a, rt4, sm_count, stream);
+    }
+    const uint64_t blocks = (uint64_t)sm_count * 8;
+    return launch_pdl(lt_norm_any<T>, (unsigned)(a.rows < blocks ? a.rows : blocks), 256, (size_t)0, stream, a);
+}
+
+// Blocks of the gradient's first kernel, and the threads per row of lt_norm_grad_rows (0: lt_norm_grad_any).  What the
+// scratch holds is planned before the addresses are known: the most either takes.
+unsigned norm_grad_any_blocks(uint64_t rows, int sm_count) { return (unsigned)std::min<uint64_t>(rows, (uint64_t)sm_count * 4); }
+unsigned norm_grad_row_blocks(uint64_t rows, int rt, int sm_count) {
+    const uint64_t groups = rt > 512 ? 1 : 512 / rt, n = (rows + groups - 1) / groups;
+    return (unsigned)std::min<uint64_t>(n, (uint64_t)sm_count * 2);
+}
+
+template <class T, int RT, int CH>
+cudaError_t launch_norm_grad_rows(const NormGradArgs &a, unsigned grid, cudaStream_t stream) {
+    constexpr int BLOCK = RT > 512 ? RT : 512, GROUPS = BLOCK / RT;
+    const size_t mem = a.partial ? (size_t)(GROUPS - 1) * a.cols * 4 : 0;  // (at most 15 groups x 512 columns: 30 KB)
+    return launch_pdl(lt_norm_grad_rows<T, RT, CH>, grid, BLOCK, mem, stream, a);
+}
+
+template <class T, int CH>
+cudaError_t launch_norm_grad_threads(const NormGradArgs &a, int rt, unsigned grid, cudaStream_t stream) {
+    switch (rt) {
+    case 32: return launch_norm_grad_rows<T, 32, CH>(a, grid, stream);
+    case 128: return launch_norm_grad_rows<T, 128, CH>(a, grid, stream);
+    case 256: return launch_norm_grad_rows<T, 256, CH>(a, grid, stream);
+    case 512: return launch_norm_grad_rows<T, 512, CH>(a, grid, stream);
+    default: return launch_norm_grad_rows<T, 1024, CH>(a, grid, stream);
+    }
+}
+
+template <class T>
+cudaError_t launch_norm_grad(const NormGradArgs &a, int sm_count, cudaStream_t stream, unsigned *grid) {
+    constexpr uint64_t N = Chunk<T>::N;
+    const bool fits = a.cols % N == 0 && a.dy_pitch % N == 0 && a.h_pitch % N == 0 && (!a.dh || (a.dh_pitch % N == 0 && is_aligned(a.dh, 16))) && is_aligned(a.dy, 16) &&
+                      is_aligned(a.h, 16) && is_aligned(a.gamma, 16) && is_aligned(a.dx, 16);
+    const int rt = fits ? row_threads(a.cols / N, 2) : 0;
+    if (!rt) {
+        *grid = norm_grad_any_blocks(a.rows, sm_count);
+        return launch_pdl(lt_norm_grad_any<T>, *grid, 256, (size_t)0, stream, a);
+    }
+    *grid = norm_grad_row_blocks(a.rows, rt, sm_count);
+    if (a.cols / N <= (uint64_t)rt) return launch_norm_grad_threads<T, 1>(a, rt, *grid, stream);
+    return launch_norm_grad_threads<T, 2>(a, rt, *grid, stream);
 }
 
 }  // namespace
@@ -331,13 +792,12 @@ cudaError_t lt_launch_rms_norm(const LtOperator &o, int sm_count, cudaStream_t s
     a.eps = (float)lt_attr_double(o.attr[3]);
     mean_factors(o.cols, &a.down, &a.up);
     a.gamma_f32 = o.gamma_dtype == LT_F32;
-    const uint64_t most = (uint64_t)sm_count * 8;
-    const unsigned grid = (unsigned)(o.rows < most ? o.rows : most);
-    return o.dtype == LT_BF16 ? launch_pdl(lt_norm_any<__nv_bfloat16>, grid, 256, (size_t)0, stream, a) : launch_pdl(lt_norm_any<float>, grid, 256, (size_t)0, stream, a);
+    return o.dtype == LT_BF16 ? launch_norm<__nv_bfloat16>(a, sm_count, stream) : launch_norm<float>(a, sm_count, stream);
 }
 
 size_t lt_rms_norm_grad_scratch(const LtOperator &o, int sm_count) {
-    return (o.wanted & 2u) ? (size_t)norm_grad_blocks(o, sm_count) * o.cols * sizeof(float) : 0;
+    const size_t blocks = norm_grad_any_blocks(o.rows, sm_count);  // (never fewer than the other kernel's: it has a row per block at least)
+    return (o.wanted & 2u) ? blocks * o.cols * sizeof(float) : 0;
 }
 
 cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
@@ -356,16 +816,15 @@ cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStrea
     a.eps = (float)lt_attr_double(o.attr[2]);
     mean_factors(o.cols, &a.down, &a.up);
     a.gamma_f32 = o.gamma_dtype == LT_F32;
-    const unsigned grid = norm_grad_blocks(o, sm_count);
+    unsigned grid = 0;
     *launched = 1;
-    cudaError_t e = o.dtype == LT_BF16 ? launch_pdl(lt_norm_grad_any<__nv_bfloat16>, grid, 256, (size_t)0, stream, a)
-                                       : launch_pdl(lt_norm_grad_any<float>, grid, 256, (size_t)0, stream, a);
+    const cudaError_t e = o.dtype == LT_BF16 ? launch_norm_grad<__nv_bfloat16>(a, sm_count, stream, &grid) : launch_norm_grad<float>(a, sm_count, stream, &grid);
     if (e != cudaSuccess || !o.out[1]) return e;
     *launched = 2;
-    const uint64_t blocks = (o.cols + 255) / 256;
+    const uint64_t blocks = (o.cols + 31) / 32;
     const unsigned g2 = (unsigned)(blocks < 4096 ? blocks : 4096);
-    return o.gamma_dtype == LT_F32 ? launch_pdl(lt_norm_grad_join<float>, g2, 256, (size_t)0, stream, (const float *)a.partial, (float *)o.out[1], o.cols, grid)
-                                   : launch_pdl(lt_norm_grad_join<__nv_bfloat16>, g2, 256, (size_t)0, stream, (const float *)a.partial, (__nv_bfloat16 *)o.out[1], o.cols, grid);
+    return o.gamma_dtype == LT_F32 ? launch_pdl(lt_norm_grad_join<float>, g2, 1024, (size_t)0, stream, (const float *)a.partial, (float *)o.out[1], o.cols, grid)
+                                   : launch_pdl(lt_norm_grad_join<__nv_bfloat16>, g2, 1024, (size_t)0, stream, (const float *)a.partial, (__nv_bfloat16 *)o.out[1], o.cols, grid);
 }
 
 size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count) {
