@@ -10,8 +10,6 @@
 // the list; a (sequence, head block) that lies within one block's part is finished there.  One that is spread over
 // several blocks leaves partial results (maximum, sum, unnormalised output) in scratch memory, and the block that
 // arrives last joins them, always in the list's order, so results do not depend on the arrival.
-#include <atomic>
-
 #include "operator_device.cuh"
 
 using namespace ltop;
@@ -373,16 +371,6 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
 
 // ------------------------------------------------------------------------------------------- bf16 on the matrix units
 
-__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {  // 16 zero bytes where there is nothing
-    const int bytes = there ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
@@ -673,15 +661,9 @@ cudaError_t launch_any(const AttendArgs &a, unsigned grid, cudaStream_t stream) 
 
 template <int DP, int NT, bool WHOLE>
 cudaError_t launch_tensor(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
-    static std::atomic<uint64_t> ready{0};  // devices on which the shared memory has been asked for
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(lt_attend_tensor<DP, NT, WHOLE>, tensor_bytes<DP>(), ready);
     if (e != cudaSuccess) return e;
-    if (device > 63 || !((ready.load(std::memory_order_relaxed) >> device) & 1u)) {
-        e = cudaFuncSetAttribute(lt_attend_tensor<DP, NT, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tensor_bytes<DP>());
-        if (e != cudaSuccess) return e;
-        if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
-    }
     return launch_pdl(lt_attend_tensor<DP, NT, WHOLE>, grid, THREADS, tensor_bytes<DP>(), stream, a);
 }
 

@@ -4,10 +4,25 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "operators.h"
 #include "pdl.cuh"
 
 namespace ltop {
+
+// Lets a kernel have `bytes` of dynamic shared memory on the current device; asked once per kernel and device (`ready`).
+template <class K>
+__host__ cudaError_t allow_shared(K kernel, size_t bytes, std::atomic<uint64_t> &ready) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (bit && (ready.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -50,6 +65,17 @@ __device__ __forceinline__ float block_reduce(float v, float *part) {
     for (int w = 1; w < warps; ++w) r = MAX ? max_nan(r, part[w]) : r + part[w];
     return r;
 }
+
+// Asynchronous copies of 16 bytes into shared memory
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {  // 16 zero bytes where there is nothing
+    const int bytes = there ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 
 // 16 bytes of T as binary32 and back
 template <class T>

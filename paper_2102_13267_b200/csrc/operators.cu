@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) lt_turn_any(const TurnArgs a) {
     }
 }
 
-constexpr int TURN_THREADS = 256, TURN_FLIGHT = 4;
+constexpr int TURN_THREADS = 256;
 
 struct TurnShape {
     uint32_t block_tokens;      // tokens of a block
@@ -128,7 +128,7 @@ struct TurnShape {
 // angles would not be free if every head computed them (a sine and a cosine are some fifty instructions), so a block
 // computes those of its tokens once, into shared memory, while the first loads are on their way.
 // Measured on 8192 tokens x 32 heads x 128 bf16: see the table in the documentation of the operators.
-template <class T, bool APPEND>
+template <class T, bool APPEND, int TURN_FLIGHT>
 __global__ void __launch_bounds__(TURN_THREADS) lt_turn_chunks(const TurnArgs a, const TurnShape sh) {
     constexpr int N = Chunk<T>::N;
     extern __shared__ float turn_mem[];  // cosines, then sines, [block_tokens][pairs]
@@ -226,6 +226,7 @@ cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
     const uint64_t per_token = (uint64_t)per_head * a.heads;
     if (chunks && a.pairs <= 2048 && per_token < (1u << 20) && a.tokens < (1ull << 31)) {
         // enough tokens for a thread to have TURN_FLIGHT units in flight, fewer where that would leave SMs without a block
+        constexpr uint32_t TURN_FLIGHT = sizeof(T) == 2 ? 2 : 4;  // (a unit of f32 has half the values)
         uint64_t n = TURN_THREADS * TURN_FLIGHT / per_token;
         if (n > a.tokens / (2 * (uint64_t)sm_count)) n = a.tokens / (2 * (uint64_t)sm_count);
         if (a.pairs && n > 4096 / a.pairs) n = 4096 / a.pairs;  // (32 KB of cosines and sines)
@@ -238,7 +239,7 @@ cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
         sh.per_token = Divisor::make((uint32_t)per_token);
         sh.per_head = Divisor::make(per_head);
         sh.pairs = Divisor::make(a.pairs ? a.pairs : 1);
-        return launch_pdl(lt_turn_chunks<T, APPEND>, (unsigned)((a.tokens + n - 1) / n), TURN_THREADS, (size_t)n * a.pairs * 8, stream, a, sh);
+        return launch_pdl(lt_turn_chunks<T, APPEND, (int)TURN_FLIGHT>, (unsigned)((a.tokens + n - 1) / n), TURN_THREADS, (size_t)n * a.pairs * 8, stream, a, sh);
     }
     const uint64_t total = a.tokens * (a.dim - a.pairs);
     const uint64_t blocks = (total + 255) / 256, most = (uint64_t)sm_count * 32;
@@ -254,6 +255,7 @@ struct NormArgs {
     float *scales;
     uint64_t rows, cols, x_pitch, r_pitch;
     uint32_t group, groups;     // columns of a group (0: the row)
+    uint32_t group_shift;       // lt_norm_rows: log2 of the chunks of a group
     float eps;
     float down, up;             // 2^-k <= 1 / cols and 2^k / cols: a mean of squares is summed as h (h 2^-k), which fits where the mean does
     int gamma_f32;
@@ -264,12 +266,15 @@ __device__ __forceinline__ float gamma_at(const void *gamma, int f32, uint64_t c
     return f32 ? ((const float *)gamma)[c] : to_float(((const T *)gamma)[c]);
 }
 
-// 448 / top, the factor from values to e4m3 codes (0 for a group of zeros; a group so small that the quotient would
-// overflow takes the largest number instead)
+// 448 / top, the factor from values to e4m3 codes, by the reciprocal unit (1 ulp: far below half a step of a code; 0 for a
+// group of zeros; a group so small that the quotient would overflow takes the largest number instead).  A NaN stays.
 __device__ __forceinline__ float code_factor(float top) {
-    if (top == 0.f) return 0.f;
-    return fminf(__fdiv_rn(448.f, top), 3.402823466e38f) + (top != top ? top : 0.f);
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(top));
+    r = r * 448.f;
+    return top == 0.f ? 0.f : r > 3.402823466e38f ? 3.402823466e38f : r;
 }
+__device__ __forceinline__ float scale_of(float top) { return top * (1.f / 448.f); }
 
 // Any shape and alignment: a block per row, which is read once for its mean square, once more for each output.
 template <class T>
@@ -292,7 +297,7 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
                 float top = 0.f;
                 for (uint64_t c = threadIdx.x; c < a.cols; c += 256) top = max_nan(top, fabsf(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c)));
                 top = block_reduce<true>(top, part);
-                if (a.scales && threadIdx.x == 0) a.scales[row] = __fdiv_rn(top, 448.f);
+                if (a.scales && threadIdx.x == 0) a.scales[row] = scale_of(top);
                 const float f = code_factor(top);
                 if (a.codes)
                     for (uint64_t c = threadIdx.x; c < a.cols; c += 256)
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
                     float top = 0.f;
                     for (uint64_t c = c0 + (threadIdx.x & 31); c < c1; c += 32) top = max_nan(top, fabsf(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c)));
                     top = warp_max_nan(top);
-                    if (a.scales && (threadIdx.x & 31) == 0) a.scales[row * a.groups + g] = __fdiv_rn(top, 448.f);
+                    if (a.scales && (threadIdx.x & 31) == 0) a.scales[row * a.groups + g] = scale_of(top);
                     const float f = code_factor(top);
                     if (a.codes)
                         for (uint64_t c = c0 + (threadIdx.x & 31); c < c1; c += 32)
@@ -339,95 +344,126 @@ __device__ __forceinline__ void gamma_chunk(const void *gamma, int f32, uint32_t
     }
 }
 
-// Sum or maximum over the RT threads of a row: a warp, or a block of its own.
+// Sum or maximum over the RT threads of a row: a warp, or a block of its own.  `part`: room for 2 x 32 values, used in turn
+// (`turn` counts the reductions), so that one barrier per reduction is enough: whoever writes a half for the second time
+// has passed the barrier behind everybody's reading of it.
 template <int RT, bool MAX>
-__device__ __forceinline__ float row_reduce(float v, float *part) {
-    if constexpr (RT == 32) return MAX ? warp_max_nan(v) : warp_sum(v);
-    else return block_reduce<MAX>(v, part);
+__device__ __forceinline__ float row_reduce(float v, float *part, int &turn) {
+    v = MAX ? warp_max_nan(v) : warp_sum(v);
+    if constexpr (RT == 32) return v;
+    constexpr int W = RT / 32;
+    float *mine = part + (turn & 1) * 32;
+    ++turn;
+    if ((threadIdx.x & 31) == 0) mine[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = mine[threadIdx.x & (W - 1)];
+#pragma unroll
+    for (int d = W / 2; d > 0; d >>= 1) {
+        const float o = __shfl_xor_sync(0xffffffffu, v, d);
+        v = MAX ? max_nan(v, o) : v + o;
+    }
+    return v;
 }
 
+__host__ __device__ constexpr int norm_block(int rt) { return rt == 32 ? 128 : rt; }
+// Rows on their way while one is worked on: some 130 to 190 KB per SM at the occupancy the registers allow.
+__host__ __device__ constexpr int norm_stages(int ch) { return ch == 1 ? 3 : ch == 2 ? 2 : 1; }
+__host__ __device__ constexpr size_t norm_bytes(int rt, int ch) { return (size_t)norm_stages(ch) * 2 * ch * norm_block(rt) * 16; }
+
 // 16 bytes at a time, a row in the registers of its RT threads (CH chunks each): every value is read once and every
-// result written once, so the bound is memory.  Threads keep their columns of gamma from row to row and ask for the next
-// row before they reduce this one.
-template <class T, int RT, int CH>
-__global__ void __launch_bounds__(RT == 32 ? 128 : RT) lt_norm_rows(const NormArgs a) {
-    constexpr int N = Chunk<T>::N;
-    __shared__ float part[32];
+// result written once, so the bound is memory.  Threads keep their columns of gamma from row to row.  The rows to come
+// travel through shared memory ahead of their turn: a thread copies and reads back only its own chunks, so the ring
+// needs no barrier; registers alone kept too little on its way (8192 x 4096 bf16: 88 us with four chunks per thread and
+// the next row in registers, 52 us with one chunk per thread).
+template <class T, int RT, int CH, bool EIGHT>
+__global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a) {
+    constexpr int N = Chunk<T>::N, BLOCK = norm_block(RT), STAGES = norm_stages(CH);
+    extern __shared__ uint4 ring[];  // [STAGES][x, residual][CH][BLOCK]
+    __shared__ float part[64];
+    int turn = 0;
     const uint32_t lane = RT == 32 ? (threadIdx.x & 31) : threadIdx.x;
     const uint32_t chunks = (uint32_t)a.cols / N;
     const uint64_t step = RT == 32 ? (uint64_t)gridDim.x * 4 : gridDim.x;
     uint64_t row = RT == 32 ? (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
     pdl_release();
     pdl_wait();
+    auto issue = [&](uint64_t at, int stage) {
+        if (at < a.rows) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                const uint32_t c = lane + k * RT;
+                if (c >= chunks) continue;
+                copy16(shared_address(ring + ((stage * 2 + 0) * CH + k) * BLOCK + threadIdx.x), (const T *)a.x + at * a.x_pitch + (uint64_t)c * N, true);
+                if (a.r) copy16(shared_address(ring + ((stage * 2 + 1) * CH + k) * BLOCK + threadIdx.x), (const T *)a.r + at * a.r_pitch + (uint64_t)c * N, true);
+            }
+        }
+        copy_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) issue(row + s * step, s);
     float g[CH][N];
 #pragma unroll
     for (int k = 0; k < CH; ++k)
         if (lane + k * RT < chunks) gamma_chunk<T>(a.gamma, a.gamma_f32, (lane + k * RT) * N, g[k]);
-    uint4 x[CH], r[CH];
-    auto fetch = [&](uint64_t at) {
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const uint32_t c = lane + k * RT;
-            if (c < chunks && at < a.rows) {
-                x[k] = *reinterpret_cast<const uint4 *>((const T *)a.x + at * a.x_pitch + (uint64_t)c * N);
-                if (a.r) r[k] = *reinterpret_cast<const uint4 *>((const T *)a.r + at * a.r_pitch + (uint64_t)c * N);
-            }
-        }
-    };
-    fetch(row);
-    for (; row < a.rows; row += step) {
+    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+        copy_wait<STAGES - 1>();
         float h[CH][N], ss = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             if (lane + k * RT >= chunks) continue;
-            unpack(x[k], h[k]);
+            unpack(ring[((stage * 2 + 0) * CH + k) * BLOCK + threadIdx.x], h[k]);
             if (a.r) {
                 float f[N];
-                unpack(r[k], f);
+                unpack(ring[((stage * 2 + 1) * CH + k) * BLOCK + threadIdx.x], f);
 #pragma unroll
                 for (int i = 0; i < N; ++i) h[k][i] += f[i];
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) ss += h[k][i] * (h[k][i] * a.down);
         }
-        fetch(row + step);  // (results of this row go over its own operands only)
-        const float inv = rsqrtf(row_reduce<RT, false>(ss, part) * a.up + a.eps);
+        issue(row + STAGES * step, stage);  // (results go over the operands of their own row only)
+        const float inv = rsqrtf(row_reduce<RT, false>(ss, part, turn) * a.up + a.eps);
+        const uint64_t at = row * a.cols;
         if (a.sum) {
+            T *to = (T *)a.sum + at;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.sum + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(h[k]);
+                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>(to + (lane + k * RT) * N) = pack(h[k]);
         }
-        float top[CH], row_top = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            top[k] = 0.f;
             if (lane + k * RT >= chunks) continue;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                h[k][i] = h[k][i] * inv * g[k][i];
-                top[k] = max_nan(top[k], fabsf(h[k][i]));
-            }
-            row_top = max_nan(row_top, top[k]);
+            for (int i = 0; i < N; ++i) h[k][i] = h[k][i] * inv * g[k][i];
         }
         if (a.y) {
+            T *to = (T *)a.y + at;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.y + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(h[k]);
+                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>(to + (lane + k * RT) * N) = pack(h[k]);
         }
-        if (a.codes || a.scales) {
-            const uint32_t lanes = a.group / N;  // of a group; 0: the row
+        if constexpr (EIGHT) {
+            float top[CH], row_top = 0.f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                top[k] = 0.f;
+                if (lane + k * RT >= chunks) continue;
+#pragma unroll
+                for (int i = 0; i < N; ++i) top[k] = max_nan(top[k], fabsf(h[k][i]));
+                row_top = max_nan(row_top, top[k]);
+            }
             if (!a.group) {
-                row_top = row_reduce<RT, true>(row_top, part);
-                if (a.scales && lane == 0) a.scales[row] = __fdiv_rn(row_top, 448.f);
+                row_top = row_reduce<RT, true>(row_top, part, turn);
+                if (a.scales && lane == 0) a.scales[row] = scale_of(row_top);
             }
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 const uint32_t c = lane + k * RT;
                 float t = row_top;
-                if (a.group) {
+                if (a.group) {  // a power of two of lanes share a scale
                     t = top[k];
-                    for (uint32_t d = 1; d < lanes; d <<= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, d));
-                    if (a.scales && c < chunks && c % lanes == 0) a.scales[row * a.groups + c / lanes] = __fdiv_rn(t, 448.f);
+                    for (uint32_t d = 1u << a.group_shift >> 1; d > 0; d >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, d));
+                    if (a.scales && c < chunks && (c & ((1u << a.group_shift) - 1)) == 0) a.scales[row * a.groups + (c >> a.group_shift)] = scale_of(t);
                 }
                 if (!a.codes || c >= chunks) continue;
                 const float f = code_factor(t);
@@ -438,7 +474,7 @@ __global__ void __launch_bounds__(RT == 32 ? 128 : RT) lt_norm_rows(const NormAr
                     const uint32_t p1 = __nv_cvt_float2_to_fp8x2(make_float2(h[k][4 * i + 2] * f, h[k][4 * i + 3] * f), __NV_SATFINITE, __NV_E4M3);
                     w[i] = p0 | (p1 << 16);
                 }
-                uint8_t *to = a.codes + row * a.cols + (uint64_t)c * N;
+                uint8_t *to = a.codes + at + c * N;
                 if constexpr (N == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
                 else *reinterpret_cast<uint32_t *>(to) = w[0];
             }
@@ -488,33 +524,60 @@ __global__ void __launch_bounds__(256) lt_norm_grad_any(const NormGradArgs a) {
 
 // Sums of two values over the RT threads of a row group inside a block (`group`: which).
 template <int RT>
-__device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int group) {
+__device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int group, int &turn) {
     x = warp_sum(x);
     y = warp_sum(y);
     if constexpr (RT == 32) return make_float2(x, y);
     constexpr int W = RT / 32;
-    float2 *mine = part + group * W;
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");  // `mine` may still be read
+    float2 *mine = part + (turn & 1) * 32 + group * W;  // (in turn, as in row_reduce)
+    ++turn;
     if ((threadIdx.x & 31) == 0) mine[(threadIdx.x % RT) >> 5] = make_float2(x, y);
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");
-    float2 s = mine[0];
+    float2 s = mine[threadIdx.x & (W - 1)];
 #pragma unroll
-    for (int w = 1; w < W; ++w) s.x += mine[w].x, s.y += mine[w].y;
+    for (int d = W / 2; d > 0; d >>= 1) {
+        s.x += __shfl_xor_sync(0xffffffffu, s.x, d);
+        s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
+    }
     return s;
 }
 
-// 16 bytes at a time, a row in the registers of its RT threads; a block has several rows at once and goes on to others,
-// the sums for gamma staying in registers.  Bound by memory like lt_norm_rows.
+__host__ __device__ constexpr int grad_block(int rt) { return rt > 512 ? rt : 512; }
+__host__ __device__ constexpr int grad_stages(int ch) { return ch == 1 ? 3 : 1; }
+__host__ __device__ constexpr size_t grad_bytes(int rt, int ch) { return (size_t)grad_stages(ch) * 3 * ch * grad_block(rt) * 16; }
+
+// 16 bytes at a time, RT threads per row; a block has several rows at once and goes on to others, the sums for gamma
+// staying in registers.  Bound by memory like lt_norm_rows, and like there the rows to come travel through shared
+// memory, from which a row is read twice: for its sums, and for its results.
 template <class T, int RT, int CH>
-__global__ void __launch_bounds__(RT > 512 ? RT : 512) lt_norm_grad_rows(const NormGradArgs a) {
-    constexpr int N = Chunk<T>::N, BLOCK = RT > 512 ? RT : 512, GROUPS = BLOCK / RT;
-    __shared__ float2 part[32];
-    extern __shared__ float4 grad_mem[];  // [GROUPS - 1][cols]: the groups' sums for gamma
+__global__ void __launch_bounds__(grad_block(RT)) lt_norm_grad_rows(const NormGradArgs a) {
+    constexpr int N = Chunk<T>::N, BLOCK = grad_block(RT), GROUPS = BLOCK / RT, STAGES = grad_stages(CH);
+    __shared__ float2 part[64];
+    int turn = 0;
+    extern __shared__ uint4 ring[];  // [STAGES][dy, h, dh][CH][BLOCK]; at the end [GROUPS - 1][cols]: the groups' sums for gamma
+    float4 *grad_mem = reinterpret_cast<float4 *>(ring);
     const int group = threadIdx.x / RT;
     const uint32_t lane = threadIdx.x % RT, chunks = (uint32_t)a.cols / N;
     const uint64_t step = (uint64_t)gridDim.x * GROUPS;
     pdl_release();
     pdl_wait();
+    auto place = [&](int stage, int which, int k) { return ring + ((stage * 3 + which) * CH + k) * BLOCK + threadIdx.x; };
+    auto issue = [&](uint64_t at, int stage) {
+        if (at < a.rows) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                const uint64_t c = (uint64_t)(lane + k * RT) * N;
+                if (lane + k * RT >= chunks) continue;
+                copy16(shared_address(place(stage, 0, k)), (const T *)a.dy + at * a.dy_pitch + c, true);
+                copy16(shared_address(place(stage, 1, k)), (const T *)a.h + at * a.h_pitch + c, true);
+                if (a.dh) copy16(shared_address(place(stage, 2, k)), (const T *)a.dh + at * a.dh_pitch + c, true);
+            }
+        }
+        copy_commit();
+    };
+    uint64_t row = (uint64_t)blockIdx.x * GROUPS + group;
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) issue(row + s * step, s);
     float g[CH][N], sum[CH][N];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -522,50 +585,45 @@ __global__ void __launch_bounds__(RT > 512 ? RT : 512) lt_norm_grad_rows(const N
         for (int i = 0; i < N; ++i) g[k][i] = sum[k][i] = 0.f;
         if (lane + k * RT < chunks) gamma_chunk<T>(a.gamma, a.gamma_f32, (lane + k * RT) * N, g[k]);
     }
-    uint4 dy[CH], h[CH], dh[CH];
-    auto fetch = [&](uint64_t at) {
+    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+        float ss = 0.f, dot = 0.f;
+        copy_wait<STAGES - 1>();
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const uint32_t c = lane + k * RT;
-            dy[k] = h[k] = dh[k] = make_uint4(0, 0, 0, 0);
-            if (c < chunks && at < a.rows) {
-                dy[k] = *reinterpret_cast<const uint4 *>((const T *)a.dy + at * a.dy_pitch + (uint64_t)c * N);
-                h[k] = *reinterpret_cast<const uint4 *>((const T *)a.h + at * a.h_pitch + (uint64_t)c * N);
-                if (a.dh) dh[k] = *reinterpret_cast<const uint4 *>((const T *)a.dh + at * a.dh_pitch + (uint64_t)c * N);
-            }
-        }
-    };
-    uint64_t row = (uint64_t)blockIdx.x * GROUPS + group;
-    fetch(row);
-    for (; row < a.rows; row += step) {
-        float d[CH][N], u[CH][N], e[CH][N], ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            unpack(dy[k], d[k]);
-            unpack(h[k], u[k]);
-            unpack(dh[k], e[k]);
+            if (lane + k * RT >= chunks) continue;
+            float d[N], u[N];
+            unpack(*place(stage, 0, k), d);
+            unpack(*place(stage, 1, k), u);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                ss += u[k][i] * (u[k][i] * a.down);
-                dot += d[k][i] * g[k][i] * (u[k][i] * a.down);
+                const float v = u[i] * a.down;
+                ss += u[i] * v;
+                dot += d[i] * g[k][i] * v;
             }
         }
-        fetch(row + step);
-        const float2 s = group_sum<RT>(ss, dot, part, group);
+        const float2 s = group_sum<RT>(ss, dot, part, group, turn);
         const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
+            if (lane + k * RT >= chunks) continue;
+            float d[N], u[N], e[N];
+            unpack(*place(stage, 0, k), d);
+            unpack(*place(stage, 1, k), u);
+            if (a.dh) unpack(*place(stage, 2, k), e);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float n = u[k][i] * inv;
-                sum[k][i] += d[k][i] * n;
-                e[k][i] += (d[k][i] * g[k][i] - n * m) * inv;
+                const float n = u[i] * inv;
+                sum[k][i] += d[i] * n;
+                e[i] = (a.dh ? e[i] : 0.f) + (d[i] * g[k][i] - n * m) * inv;
             }
-            if (a.dx && lane + k * RT < chunks) *reinterpret_cast<uint4 *>((T *)a.dx + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(e[k]);
+            if (a.dx) *reinterpret_cast<uint4 *>((T *)a.dx + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(e);
         }
+        issue(row + STAGES * step, stage);
     }
     if (!a.partial) return;
     if (GROUPS > 1) {
+        copy_wait<0>();
+        __syncthreads();  // the other groups' rows are done
         if (group > 0) {
 #pragma unroll
             for (int k = 0; k < CH; ++k)
@@ -614,10 +672,10 @@ __global__ void __launch_bounds__(1024) lt_norm_grad_join(const float *partial, 
         __syncthreads();
         sums[warp][lane] = s;
         __syncthreads();
-        if (warp == 0 && c0 + lane < cols) {
-            for (int w = 1; w < 32; ++w) s += sums[w][lane];
-            out[c0 + lane] = from_float<G>((float)s);
-        }
+        s = sums[lane][warp];  // (a warp per column from here on)
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (lane == 0 && c0 + warp < cols) out[c0 + warp] = from_float<G>((float)s);
     }
 }
 
@@ -636,47 +694,47 @@ int row_threads(uint64_t chunks, int most) {
     return 0;
 }
 
-template <class T, int RT, int CH>
+template <class T, int RT, int CH, bool EIGHT>
 cudaError_t launch_norm_rows(const NormArgs &a, int sm_count, cudaStream_t stream) {
     const uint64_t blocks = RT == 32 ? (a.rows + 3) / 4 : a.rows;
     // as many blocks as an SM holds, each going on to further rows
-    static int resident = 0;
-    if (!resident) {
+    static std::atomic<uint64_t> ready{0};
+    static std::atomic<int> resident{0};
+    cudaError_t e = allow_shared(lt_norm_rows<T, RT, CH, EIGHT>, norm_bytes(RT, CH), ready);
+    if (e != cudaSuccess) return e;
+    if (!resident.load(std::memory_order_relaxed)) {
         int n = 0;
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, lt_norm_rows<T, RT, CH>, RT == 32 ? 128 : RT, 0);
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, lt_norm_rows<T, RT, CH, EIGHT>, norm_block(RT), norm_bytes(RT, CH));
         if (e != cudaSuccess) return e;
-        resident = n < 1 ? 1 : n;
+        resident.store(n < 1 ? 1 : n, std::memory_order_relaxed);
     }
-    const uint64_t most = (uint64_t)sm_count * resident;
-    return launch_pdl(lt_norm_rows<T, RT, CH>, (unsigned)(blocks < most ? blocks : most), RT == 32 ? 128 : RT, (size_t)0, stream, a);
+    const uint64_t most = (uint64_t)sm_count * resident.load(std::memory_order_relaxed);
+    return launch_pdl(lt_norm_rows<T, RT, CH, EIGHT>, (unsigned)(blocks < most ? blocks : most), norm_block(RT), norm_bytes(RT, CH), stream, a);
 }
 
-template <class T, int CH>
-cudaError_t launch_norm_threads(const NormArgs &a, int rt, int sm_count, cudaStream_t stream) {
+template <class T, bool EIGHT>
+cudaError_t launch_norm_threads(const NormArgs &a, int rt, int ch, int sm_count, cudaStream_t stream) {
+    if (ch == 2) return launch_norm_rows<T, 1024, 2, EIGHT>(a, sm_count, stream);
+    if (ch == 4) return launch_norm_rows<T, 1024, 4, EIGHT>(a, sm_count, stream);
     switch (rt) {
-    case 32: return launch_norm_rows<T, 32, CH>(a, sm_count, stream);
-    case 128: return launch_norm_rows<T, 128, CH>(a, sm_count, stream);
-    case 256: return launch_norm_rows<T, 256, CH>(a, sm_count, stream);
-    case 512: return launch_norm_rows<T, 512, CH>(a, sm_count, stream);
-    default: return launch_norm_rows<T, 1024, CH>(a, sm_count, stream);
+    case 32: return launch_norm_rows<T, 32, 1, EIGHT>(a, sm_count, stream);
+    case 128: return launch_norm_rows<T, 128, 1, EIGHT>(a, sm_count, stream);
+    case 256: return launch_norm_rows<T, 256, 1, EIGHT>(a, sm_count, stream);
+    case 512: return launch_norm_rows<T, 512, 1, EIGHT>(a, sm_count, stream);
+    default: return launch_norm_rows<T, 1024, 1, EIGHT>(a, sm_count, stream);
     }
 }
 
 template <class T>
-cudaError_t launch_norm(const NormArgs &a, int sm_count, cudaStream_t stream) {
+cudaError_t launch_norm(NormArgs a, int sm_count, cudaStream_t stream) {
     constexpr uint64_t N = Chunk<T>::N;
+    while (a.group && (N << a.group_shift) < a.group) ++a.group_shift;
     const uint64_t chunks = a.cols / N;
     const bool fits = a.cols % N == 0 && a.x_pitch % N == 0 && (!a.r || (a.r_pitch % N == 0 && is_aligned(a.r, 16))) && is_aligned(a.x, 16) && is_aligned(a.gamma, 16) &&
                       is_aligned(a.y, 16) && is_aligned(a.sum, 16) && is_aligned(a.codes, 8) && a.group <= 32 * N;
-    // few rows: one chunk per thread, the most threads a row can use; many: four, fewer threads to agree on a sum
-    const int most = a.rows <= 2 * (uint64_t)sm_count ? 1 : 4;
-    const int rt = fits ? row_threads(chunks, most) : 0, rt4 = fits ? row_threads(chunks, 4) : 0;
-    if (rt && most == 1) return launch_norm_threads<T, 1>(a, rt, sm_count, stream);
-    if (rt4) {
-        if (chunks <= (uint64_t)rt4) return launch_norm_threads<T, 1>(a, rt4, sm_count, stream);
-        if (chunks <= 2 * (uint64_t)rt4) return launch_norm_threads<T, 2>(a, rt4, sm_count, stream);
-        return launch_norm_threads<T, 4>(a, rt4, sm_count, stream);
-    }
+    // as many threads per row as it has chunks, while a block can have them
+    const int ch = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4, rt = fits ? row_threads(chunks, ch) : 0;
+    if (rt) return a.codes || a.scales ? launch_norm_threads<T, true>(a, rt, ch, sm_count, stream) : launch_norm_threads<T, false>(a, rt, ch, sm_count, stream);
     const uint64_t blocks = (uint64_t)sm_count * 8;
     return launch_pdl(lt_norm_any<T>, (unsigned)(a.rows < blocks ? a.rows : blocks), 256, (size_t)0, stream, a);
 }
@@ -692,8 +750,11 @@ unsigned norm_grad_row_blocks(uint64_t rows, int rt, int sm_count) {
 template <class T, int RT, int CH>
 cudaError_t launch_norm_grad_rows(const NormGradArgs &a, unsigned grid, cudaStream_t stream) {
     constexpr int BLOCK = RT > 512 ? RT : 512, GROUPS = BLOCK / RT;
-    const size_t mem = a.partial ? (size_t)(GROUPS - 1) * a.cols * 4 : 0;  // (at most 15 groups x 512 columns: 30 KB)
-    return launch_pdl(lt_norm_grad_rows<T, RT, CH>, grid, BLOCK, mem, stream, a);
+    static_assert((GROUPS - 1) * RT * CH * Chunk<T>::N * 4 <= (int)grad_bytes(RT, CH), "the groups' sums fit");
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(lt_norm_grad_rows<T, RT, CH>, grad_bytes(RT, CH), ready);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(lt_norm_grad_rows<T, RT, CH>, grid, BLOCK, grad_bytes(RT, CH), stream, a);
 }
 
 template <class T, int CH>
