@@ -89,14 +89,15 @@ _SIGNATURES = {
     "lt_tensor_from_host": [_vp, _vp, _int, _int, _P(_i64), _P(_u64)],
     "lt_scalar": [_vp, ctypes.c_double, _int, _P(_u64)],
     "lt_scalar_dynamic": [_vp, ctypes.c_double, _int, _P(_u64)],
-    "lt_op": [_vp, _int, _P(_u64), _int, _P(_i64), _int, _P(_u64)],
+    # (arrays of the recording calls travel as plain addresses: converting an array to a typed pointer costs more than the call)
+    "lt_op": [_vp, _int, _vp, _int, _vp, _int, _vp],
     "lt_assign": [_vp, _u64, _u64],
     "lt_view_reshape": [_vp, _u64, _int, _P(_i64), _P(_u64)],
     "lt_view_narrow": [_vp, _u64, _int, _i64, _i64, _P(_u64)],
     "lt_view_permute": [_vp, _u64, _P(_int), _P(_u64)],
     "lt_release": [_vp, _u64],
     "lt_release_many": [_vp, _P(_u64), ctypes.c_size_t],
-    "lt_op_many": [_vp, _P(lt_batch_op), ctypes.c_size_t, _P(_u64), ctypes.c_size_t, _P(_i64), _P(_u64)],
+    "lt_op_many": [_vp, _vp, ctypes.c_size_t, _vp, ctypes.c_size_t, _vp, _vp],
     "lt_barrier": [_vp, _int],
     "lt_barrier_static_scratch": [_vp, _int, _int],
     "lt_debug_bounds_violations": [_vp, _P(_u64)],
@@ -383,7 +384,8 @@ class Batch(_Operators):
                 for i, r in enumerate(ins[:3]):
                     ops[k].in_[i] = r
             attrs = (_i64 * max(len(self._attrs), 1))(*self._attrs)
-            self._c = (ops, attrs, (_u64 * max(len(self._ops), 1))(), (_u64 * max(self._n_inputs, 1))())
+            results, ins = (_u64 * max(len(self._ops), 1))(), (_u64 * max(self._n_inputs, 1))()
+            self._c = (results, ins, ctypes.addressof(ops), ctypes.addressof(attrs), ctypes.addressof(results), ctypes.addressof(ins), ops, attrs)
         return self._c
 
 
@@ -444,9 +446,10 @@ class LazyContext(_Operators):
         self._ctx = out
         self.stream = stream or 0
         self._h = _u64()
-        self._hp = ctypes.byref(self._h)
+        self._hp = ctypes.addressof(self._h)
         self._ins = (_u64 * LT_OPERATOR_INPUTS)()
         self._attrs = (_i64 * (3 + LT_MAX_RANK))()
+        self._ins_at, self._attrs_at = ctypes.addressof(self._ins), ctypes.addressof(self._attrs)
         self._dead: list[int] = []
         self._keeps: list = []
 
@@ -528,7 +531,7 @@ class LazyContext(_Operators):
             na = len(a)
             for i in range(na):
                 at[i] = a[i]
-        st = _lib.lt_op(self._ctx, OPCODES[name], ins, n, at, na, self._hp)
+        st = _lib.lt_op(self._ctx, OPCODES[name], self._ins_at, n, self._attrs_at, na, self._hp)
         if st:
             self._check(st)
         return LazyTensor(self, self._h.value)
@@ -562,16 +565,16 @@ class LazyContext(_Operators):
 
     def record(self, batch: Batch, inputs) -> list:
         """lt_op_many: records the operations of `batch` on `inputs` in one call; returns the results it keeps."""
-        ops, attrs, results, ins = batch._compiled()
-        n = 0
-        for t in inputs:
-            ins[n] = t.handle
-            n += 1
+        results, ins, ops_at, attrs_at, results_at, ins_at, _, _ = batch._c or batch._compiled()
+        n = len(inputs)
         if n != batch._n_inputs:
             raise ValueError(f"the batch takes {batch._n_inputs} inputs, {n} given")
-        st = _lib.lt_op_many(self._ctx, ops, len(batch._ops), ins, n, attrs, results)
+        ins[:n] = [t.handle for t in inputs]
+        st = _lib.lt_op_many(self._ctx, ops_at, len(batch._ops), ins_at, n, attrs_at, results_at)
         if st:
             self._check(st)
+        if not batch._kept:
+            return []
         return [LazyTensor(self, results[k]) for k in batch._kept]
 
     def release(self, t: LazyTensor) -> None:
@@ -581,10 +584,13 @@ class LazyContext(_Operators):
     def barrier(self, blocking: bool = False) -> None:
         if self._dead:
             self._flush_dead()
-        keeps, self._keeps = self._keeps, []
+        keeps = self._keeps
+        if keeps:
+            self._keeps = []
         st = _lib.lt_barrier(self._ctx, 1 if blocking else 0)
         if st:
-            self._keeps.extend(keeps)
+            if keeps:
+                self._keeps.extend(keeps)
             self._check(st)
 
     def debug_bounds_violations(self) -> int | None:

@@ -11,6 +11,22 @@
 
 namespace ltop {
 
+// launch_pdl for a grid of two dimensions and dynamic shared memory
+template <class... KArgs, class... Args>
+cudaError_t launch_pdl_shared(void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t bytes, cudaStream_t stream, Args &&...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = LT_PDL;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 // Lets a kernel have `bytes` of dynamic shared memory on the current device; asked once per kernel and device (`ready`).
 template <class K>
 __host__ cudaError_t allow_shared(K kernel, size_t bytes, std::atomic<uint64_t> &ready) {
@@ -46,11 +62,15 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-__device__ __forceinline__ float warp_max_nan(float v) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
+// max(|a|, |b|, |c|), keeping a NaN
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
+
+// Maximum over a warp of values that are not negative (a NaN is larger than all of them, as bits are).
+__device__ __forceinline__ float warp_max_nan(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu)); }
 
 // Over a block of whole warps; `part` has room for 32 values.  Every thread gets the result, the same for all.
 template <bool MAX>
@@ -95,6 +115,20 @@ __device__ __forceinline__ void unpack(const uint4 &v, float (&f)[8]) {
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = __uint_as_float(w[i] << 16);
         f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+// f += the values of a chunk
+__device__ __forceinline__ void add_chunk(const uint4 &v, float (&f)[4]) {
+    f[0] += __uint_as_float(v.x);
+    f[1] += __uint_as_float(v.y);
+    f[2] += __uint_as_float(v.z);
+    f[3] += __uint_as_float(v.w);
+}
+__device__ __forceinline__ void add_chunk(const uint4 &v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; add.f32.bf16 %0, l, %0; add.f32.bf16 %1, h, %1;}" : "+f"(f[2 * i]), "+f"(f[2 * i + 1]) : "r"(w[i]));
     }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

@@ -115,90 +115,123 @@ __global__ void __launch_bounds__(256) lt_turn_any(const TurnArgs a) {
     }
 }
 
-constexpr int TURN_THREADS = 256;
+// (tokens in flight per thread and stages ahead, measured on rotary 8192 x 32 x 128 and append 8192 x 8 x 128, bf16: 4 and 1:
+// 25.7 and 14.4 us; 2 and 2: 25.6 and 15.5; 2 and 3: 26.3 and 16.6; 1 and 4: 25.4 and 18.5; 4 and 2: 27.7 and 16.3)
+constexpr int TURN_THREADS = 256, TURN_FLIGHT = 4, TURN_STAGES = 1;
+constexpr size_t TURN_RING = (size_t)TURN_STAGES * TURN_FLIGHT * 2 * TURN_THREADS * 16;
 
 struct TurnShape {
-    uint32_t block_tokens;      // tokens of a block
+    uint32_t batch;             // tokens a block works on at once
+    uint32_t side;              // of those, tokens side by side
+    uint32_t units, span;       // units of a token, and how many of them a block has (blockIdx.y: which)
     uint32_t turned, passed;    // units of a head that turn and that pass through
-    Divisor per_token, per_head, pairs;
+    Divisor span_by, turned_by, passed_by, value_by, pairs;
 };
 
-// 16 bytes at a time.  A unit is what a thread reads and writes at once: two chunks whose values form pairs, one chunk of
-// neighbouring pairs (interleaved), one that passes through, or one of the values (cache_append).  The bound is memory; the
-// angles would not be free if every head computed them (a sine and a cosine are some fifty instructions), so a block
-// computes those of its tokens once, into shared memory, while the first loads are on their way.
-// Measured on 8192 tokens x 32 heads x 128 bf16: see the table in the documentation of the operators.
-template <class T, bool APPEND, int TURN_FLIGHT>
-__global__ void __launch_bounds__(TURN_THREADS) lt_turn_chunks(const TurnArgs a, const TurnShape sh) {
+// 16 bytes at a time.  A unit is what a thread reads and writes of a token: two chunks whose values form pairs, one chunk
+// of neighbouring pairs (interleaved), one that passes through, or one of the values (cache_append).  A thread keeps its
+// unit and walks over tokens, so what it addresses is found once.  The bound is memory; the angles would not be free if
+// every head computed them (a sine and a cosine are some fifty instructions), so a block computes those of a batch of
+// tokens once, into shared memory, one batch ahead.  The chunks of the next batches are on their way meanwhile: each
+// thread copies its own ahead and reads them back, as in lt_norm_rows.
+template <class T, bool APPEND, bool INTER>
+__global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs a, const TurnShape sh) {
     constexpr int N = Chunk<T>::N;
-    extern __shared__ float turn_mem[];  // cosines, then sines, [block_tokens][pairs]
-    __shared__ uint64_t sm_at[TURN_THREADS];  // where a token goes (all ones: nowhere)
-    const uint64_t t0 = (uint64_t)blockIdx.x * sh.block_tokens;
-    const uint32_t tokens = (uint32_t)min((uint64_t)sh.block_tokens, a.tokens - t0);
-    const uint32_t units = tokens * sh.per_token.by, angles = tokens * a.pairs;
-    float *cosines = turn_mem, *sines = turn_mem + sh.block_tokens * a.pairs;
+    extern __shared__ uint4 turn_mem[];  // the ring [STAGES][FLIGHT][2][threads], then twice cosines and sines [batch][pairs]
+    __shared__ uint64_t sm_at[2][TURN_THREADS];  // where a token goes (all ones: nowhere)
+    float *const angles = reinterpret_cast<float *>(turn_mem + TURN_RING / 16);
+    const uint32_t half = sh.batch * a.pairs;
+    // the block's tokens
+    const uint64_t t0 = a.tokens * blockIdx.x / gridDim.x, t1 = a.tokens * (blockIdx.x + 1) / gridDim.x;
+    const uint32_t tokens = (uint32_t)(t1 - t0);
+    // the thread's unit: first those that turn, head by head, then those that pass, then the values
+    const uint32_t beside = sh.span_by.quotient(threadIdx.x), unit = blockIdx.y * sh.span + threadIdx.x - beside * sh.span;
+    const bool busy = beside < sh.side && unit < sh.units;
+    uint32_t r = unit, head, chunk, from;
+    bool turns = false, value = false;
+    if (r < a.heads * sh.turned) {
+        turns = true;
+        head = sh.turned_by.quotient(r);
+        chunk = r - head * sh.turned;
+        from = chunk * N;
+    } else if ((r -= a.heads * sh.turned) < a.heads * sh.passed) {
+        head = sh.passed_by.quotient(r);
+        chunk = r - head * sh.passed;
+        from = 2 * a.pairs + chunk * N;
+    } else {
+        value = APPEND;
+        r -= a.heads * sh.passed;
+        head = sh.value_by.quotient(r);
+        chunk = r - head * (a.dim / N);
+        from = chunk * N;
+    }
+    const bool two = !INTER && turns;
+    const uint64_t pitch = value ? a.v_pitch : a.x_pitch;
+    const T *src = (const T *)(value ? a.v : a.x) + (t0 + beside) * pitch + (uint64_t)head * a.dim + from;
+    T *const dst = (T *)a.out + (uint64_t)head * (APPEND ? a.head_stride : (uint64_t)a.dim) + (value ? a.value_offset : 0) + from;
+    const uint64_t step = sh.side * pitch;
+    const uint32_t mine = shared_address(turn_mem + threadIdx.x);
+    uint32_t fetched = beside;  // next token to fetch
     pdl_release();
     pdl_wait();
-    const T *x = (const T *)a.x, *v = (const T *)a.v;
-    for (uint32_t u0 = 0; u0 < units; u0 += TURN_THREADS * TURN_FLIGHT) {
-        uint4 lo[TURN_FLIGHT], hi[TURN_FLIGHT];
-        uint32_t token[TURN_FLIGHT], head[TURN_FLIGHT], chunk[TURN_FLIGHT];
+    auto issue = [&](uint32_t stage) {
 #pragma unroll
         for (int k = 0; k < TURN_FLIGHT; ++k) {
-            const uint32_t u = u0 + k * TURN_THREADS + threadIdx.x;
-            if (u >= units) break;
-            token[k] = sh.per_token.quotient(u);
-            const uint32_t r = u - token[k] * sh.per_token.by;
-            head[k] = sh.per_head.quotient(r);
-            chunk[k] = r - head[k] * sh.per_head.by;
-            if (APPEND && chunk[k] >= sh.turned + sh.passed) {
-                lo[k] = *reinterpret_cast<const uint4 *>(v + (t0 + token[k]) * a.v_pitch + (uint64_t)head[k] * a.dim + (chunk[k] - sh.turned - sh.passed) * N);
-            } else {
-                const T *src = x + (t0 + token[k]) * a.x_pitch + (uint64_t)head[k] * a.dim;
-                const bool turns = chunk[k] < sh.turned;
-                lo[k] = *reinterpret_cast<const uint4 *>(src + (turns ? chunk[k] * N : 2 * a.pairs + (chunk[k] - sh.turned) * N));
-                if (turns && !a.interleaved) hi[k] = *reinterpret_cast<const uint4 *>(src + a.pairs + chunk[k] * N);
+            if (busy && fetched < tokens) {
+                copy16(mine + ((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS * 16, src, true);
+                if (two) copy16(mine + ((stage * TURN_FLIGHT + k) * 2 + 1) * TURN_THREADS * 16, src + a.pairs, true);
             }
+            fetched += sh.side;
+            src += step;
         }
-        if (u0 == 0) {
-            for (uint32_t i = threadIdx.x; i < angles; i += TURN_THREADS) {
-                const uint32_t t = sh.pairs.quotient(i);
-                const float2 cs = turn(a.positions[t0 + t], a.frequencies[i - t * a.pairs], a.scale, a.inverse != 0);
-                cosines[i] = cs.x;
-                sines[i] = cs.y;
-            }
-            if (threadIdx.x < tokens) {
-                uint64_t at;
-                sm_at[threadIdx.x] = destination<APPEND>(a, t0 + threadIdx.x, &at) ? at : ~0ull;
-            }
-            __syncthreads();
+        copy_commit();
+    };
+    auto prepare = [&](uint32_t first, uint32_t which) {  // angles and destinations of the tokens from `first` on
+        const uint32_t n = min(sh.batch, tokens - first);
+        float *cosines = angles + which * 2 * half, *sines = cosines + half;
+        for (uint32_t i = threadIdx.x; i < n * a.pairs; i += TURN_THREADS) {
+            const uint32_t t = sh.pairs.quotient(i);
+            const float2 cs = turn(a.positions[t0 + first + t], a.frequencies[i - t * a.pairs], a.scale, a.inverse != 0);
+            cosines[i] = cs.x;
+            sines[i] = cs.y;
         }
+        if (threadIdx.x < n) {
+            uint64_t at;
+            sm_at[which][threadIdx.x] = destination<APPEND>(a, t0 + first + threadIdx.x, &at) ? at : ~0ull;
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < TURN_STAGES; ++s) issue(s);
+    if (tokens) prepare(0, 0);
+    uint32_t stage = 0, which = 0;
+    for (uint32_t first = 0; first < tokens; first += sh.batch, which ^= 1, stage = stage + 1 >= TURN_STAGES ? 0 : stage + 1) {
+        __syncthreads();  // this batch's angles are there, and nobody reads the ones before it any more
+        copy_wait<TURN_STAGES - 1>();
+        const float *cosines = angles + which * 2 * half, *sines = cosines + half;
 #pragma unroll
         for (int k = 0; k < TURN_FLIGHT; ++k) {
-            const uint32_t u = u0 + k * TURN_THREADS + threadIdx.x;
-            if (u >= units) break;
-            const uint64_t at = sm_at[token[k]];
+            const uint32_t token = beside + k * sh.side;
+            if (!busy || first + token >= tokens) break;
+            const uint64_t at = sm_at[which][token];
             if (APPEND && at == ~0ull) continue;
-            T *dst = (T *)a.out + at + (uint64_t)head[k] * (APPEND ? a.head_stride : (uint64_t)a.dim);
-            if (chunk[k] >= sh.turned) {
-                const bool value = APPEND && chunk[k] >= sh.turned + sh.passed;
-                const uint64_t to = value ? a.value_offset + (chunk[k] - sh.turned - sh.passed) * N : 2 * a.pairs + (chunk[k] - sh.turned) * N;
-                *reinterpret_cast<uint4 *>(dst + to) = lo[k];
+            const uint4 lo = turn_mem[((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS + threadIdx.x];
+            if (!turns) {
+                *reinterpret_cast<uint4 *>(dst + at) = lo;
                 continue;
             }
             float p[N], q[N];
-            unpack(lo[k], p);
-            if (a.interleaved) {
-                const float *c = cosines + token[k] * a.pairs + chunk[k] * (N / 2), *s = sines + token[k] * a.pairs + chunk[k] * (N / 2);
+            unpack(lo, p);
+            if constexpr (INTER) {
+                const float *c = cosines + token * a.pairs + chunk * (N / 2), *s = sines + token * a.pairs + chunk * (N / 2);
 #pragma unroll
                 for (int i = 0; i < N / 2; ++i) {
                     q[2 * i] = p[2 * i] * c[i] - p[2 * i + 1] * s[i];
                     q[2 * i + 1] = p[2 * i] * s[i] + p[2 * i + 1] * c[i];
                 }
-                *reinterpret_cast<uint4 *>(dst + chunk[k] * N) = pack(q);
+                *reinterpret_cast<uint4 *>(dst + at) = pack(q);
             } else {
-                const float4 *c = reinterpret_cast<const float4 *>(cosines + token[k] * a.pairs + chunk[k] * N), *s = reinterpret_cast<const float4 *>(sines + token[k] * a.pairs + chunk[k] * N);
-                unpack(hi[k], q);
+                const float4 *c = reinterpret_cast<const float4 *>(cosines + token * a.pairs + chunk * N), *s = reinterpret_cast<const float4 *>(sines + token * a.pairs + chunk * N);
+                unpack(turn_mem[((stage * TURN_FLIGHT + k) * 2 + 1) * TURN_THREADS + threadIdx.x], q);
 #pragma unroll
                 for (int i = 0; i < N / 4; ++i) {
                     const float4 cc = c[i], ss = s[i];
@@ -210,11 +243,27 @@ __global__ void __launch_bounds__(TURN_THREADS) lt_turn_chunks(const TurnArgs a,
                         q[4 * i + j] = fp * si[j] + fq * co[j];
                     }
                 }
-                *reinterpret_cast<uint4 *>(dst + chunk[k] * N) = pack(p);
-                *reinterpret_cast<uint4 *>(dst + a.pairs + chunk[k] * N) = pack(q);
+                *reinterpret_cast<uint4 *>(dst + at) = pack(p);
+                *reinterpret_cast<uint4 *>(dst + at + a.pairs) = pack(q);
             }
         }
+        issue(stage);
+        if (first + sh.batch < tokens) prepare(first + sh.batch, which ^ 1);
     }
+}
+
+template <class T, bool APPEND, bool INTER>
+cudaError_t launch_turn_chunks(const TurnArgs &a, const TurnShape &sh, uint32_t across, int sm_count, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    constexpr size_t most = TURN_RING + 2 * 2048 * 8;
+    const cudaError_t e = allow_shared(lt_turn_chunks<T, APPEND, INTER>, most, ready);
+    if (e != cudaSuccess) return e;
+    // as many blocks as the SMs hold (by threads, by shared memory), each going on to further tokens
+    const size_t mem = TURN_RING + (size_t)2 * sh.batch * a.pairs * 8;
+    const uint64_t per_sm = std::min<uint64_t>(4, 220 * 1024 / (mem + 5 * 1024)), wave = std::max<uint64_t>(1, (uint64_t)sm_count * per_sm / across);
+    const uint64_t batches = (a.tokens + sh.batch - 1) / sh.batch;
+    const dim3 grid((unsigned)std::min(batches, wave), across);
+    return launch_pdl_shared(lt_turn_chunks<T, APPEND, INTER>, grid, TURN_THREADS, mem, stream, a, sh);
 }
 
 template <class T, bool APPEND>
@@ -222,24 +271,26 @@ cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
     constexpr uint32_t N = Chunk<T>::N;
     const bool chunks = a.dim % N == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % N == 0 && a.x_pitch % N == 0 && is_aligned(a.x, 16) && is_aligned(a.out, 16) &&
                         (!APPEND || (a.v_pitch % N == 0 && is_aligned(a.v, 16)));
-    const uint32_t turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N, passed = (a.dim - 2 * a.pairs) / N, per_head = turned + passed + (APPEND ? a.dim / N : 0);
-    const uint64_t per_token = (uint64_t)per_head * a.heads;
-    if (chunks && a.pairs <= 2048 && per_token < (1u << 20) && a.tokens < (1ull << 31)) {
-        // enough tokens for a thread to have TURN_FLIGHT units in flight, fewer where that would leave SMs without a block
-        constexpr uint32_t TURN_FLIGHT = sizeof(T) == 2 ? 2 : 4;  // (a unit of f32 has half the values)
-        uint64_t n = TURN_THREADS * TURN_FLIGHT / per_token;
-        if (n > a.tokens / (2 * (uint64_t)sm_count)) n = a.tokens / (2 * (uint64_t)sm_count);
-        if (a.pairs && n > 4096 / a.pairs) n = 4096 / a.pairs;  // (32 KB of cosines and sines)
-        if (n > TURN_THREADS) n = TURN_THREADS;
-        if (n < 1) n = 1;
+    const uint64_t units = (uint64_t)(a.dim / N - (a.interleaved ? 0 : a.pairs / N) + (APPEND ? a.dim / N : 0)) * a.heads;
+    if (chunks && a.pairs <= 2048 && units < (1u << 20) && a.tokens < (1ull << 31)) {
         TurnShape sh;
-        sh.block_tokens = (uint32_t)n;
-        sh.turned = turned;
-        sh.passed = passed;
-        sh.per_token = Divisor::make((uint32_t)per_token);
-        sh.per_head = Divisor::make(per_head);
+        sh.turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N;
+        sh.passed = (a.dim - 2 * a.pairs) / N;
+        sh.units = (uint32_t)units;
+        // a token's units over as few blocks as hold them, evenly; several tokens side by side where they leave room
+        const uint32_t across = (sh.units + TURN_THREADS - 1) / TURN_THREADS;
+        sh.span = (sh.units + across - 1) / across;
+        sh.side = TURN_THREADS / sh.span;
+        if (a.pairs && sh.side * a.pairs > 2048) sh.side = std::max(1u, 2048 / a.pairs);  // (a batch's angles: at most 32 KB, twice)
+        if (sh.side > TURN_THREADS / TURN_FLIGHT) sh.side = TURN_THREADS / TURN_FLIGHT;
+        sh.batch = sh.side * TURN_FLIGHT;
+        if (a.pairs && sh.batch * a.pairs > 2048) sh.batch = sh.side;
+        sh.span_by = Divisor::make(sh.span);
+        sh.turned_by = Divisor::make(sh.turned ? sh.turned : 1);
+        sh.passed_by = Divisor::make(sh.passed ? sh.passed : 1);
+        sh.value_by = Divisor::make(a.dim / N);
         sh.pairs = Divisor::make(a.pairs ? a.pairs : 1);
-        return launch_pdl(lt_turn_chunks<T, APPEND, (int)TURN_FLIGHT>, (unsigned)((a.tokens + n - 1) / n), TURN_THREADS, (size_t)n * a.pairs * 8, stream, a, sh);
+        return a.interleaved ? launch_turn_chunks<T, APPEND, true>(a, sh, across, sm_count, stream) : launch_turn_chunks<T, APPEND, false>(a, sh, across, sm_count, stream);
     }
     const uint64_t total = a.tokens * (a.dim - a.pairs);
     const uint64_t blocks = (total + 255) / 256, most = (uint64_t)sm_count * 32;
@@ -367,8 +418,8 @@ __device__ __forceinline__ float row_reduce(float v, float *part, int &turn) {
 
 __host__ __device__ constexpr int norm_block(int rt) { return rt == 32 ? 128 : rt; }
 // Rows on their way while one is worked on: some 130 to 190 KB per SM at the occupancy the registers allow.
-__host__ __device__ constexpr int norm_stages(int ch) { return ch == 1 ? 3 : ch == 2 ? 2 : 1; }
-__host__ __device__ constexpr size_t norm_bytes(int rt, int ch) { return (size_t)norm_stages(ch) * 2 * ch * norm_block(rt) * 16; }
+__host__ __device__ constexpr int norm_stages(int rt, int ch) { return ch == 1 ? 3 : norm_block(rt) * ch <= 2048 ? 3 : 1; }
+__host__ __device__ constexpr size_t norm_bytes(int rt, int ch) { return (size_t)norm_stages(rt, ch) * 2 * ch * norm_block(rt) * 16; }
 
 // 16 bytes at a time, a row in the registers of its RT threads (CH chunks each): every value is read once and every
 // result written once, so the bound is memory.  Threads keep their columns of gamma from row to row.  The rows to come
@@ -376,8 +427,8 @@ __host__ __device__ constexpr size_t norm_bytes(int rt, int ch) { return (size_t
 // needs no barrier; registers alone kept too little on its way (8192 x 4096 bf16: 88 us with four chunks per thread and
 // the next row in registers, 52 us with one chunk per thread).
 template <class T, int RT, int CH, bool EIGHT>
-__global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a) {
-    constexpr int N = Chunk<T>::N, BLOCK = norm_block(RT), STAGES = norm_stages(CH);
+__global__ void __launch_bounds__(norm_block(RT), norm_block(RT) == 1024 ? 1 : (CH == 1 ? 1536 : CH == 2 ? 1024 : 512) / norm_block(RT)) lt_norm_rows(const NormArgs a) {
+    constexpr int N = Chunk<T>::N, BLOCK = norm_block(RT), STAGES = norm_stages(RT, CH);
     extern __shared__ uint4 ring[];  // [STAGES][x, residual][CH][BLOCK]
     __shared__ float part[64];
     int turn = 0;
@@ -387,42 +438,57 @@ __global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a)
     uint64_t row = RT == 32 ? (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
     pdl_release();
     pdl_wait();
-    auto issue = [&](uint64_t at, int stage) {
-        if (at < a.rows) {
+    // where the thread's first chunk of the next row to fetch lies, and in the ring
+    const T *next_x = (const T *)a.x + row * a.x_pitch + lane * N, *next_r = (const T *)a.r + (a.r ? row * a.r_pitch + lane * N : 0);
+    const uint64_t x_step = step * a.x_pitch, r_step = step * a.r_pitch;
+    const uint32_t mine = shared_address(ring + threadIdx.x);
+    constexpr uint32_t STAGE_BYTES = 2 * CH * BLOCK * 16;
+    uint64_t fetched = row;
+    auto issue = [&](uint32_t stage) {
+        if (fetched < a.rows) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
-                const uint32_t c = lane + k * RT;
-                if (c >= chunks) continue;
-                copy16(shared_address(ring + ((stage * 2 + 0) * CH + k) * BLOCK + threadIdx.x), (const T *)a.x + at * a.x_pitch + (uint64_t)c * N, true);
-                if (a.r) copy16(shared_address(ring + ((stage * 2 + 1) * CH + k) * BLOCK + threadIdx.x), (const T *)a.r + at * a.r_pitch + (uint64_t)c * N, true);
+                if (lane + k * RT >= chunks) continue;
+                copy16(mine + stage + k * BLOCK * 16, next_x + k * RT * N, true);
+                if (a.r) copy16(mine + stage + (CH + k) * BLOCK * 16, next_r + k * RT * N, true);
             }
         }
         copy_commit();
+        fetched += step;
+        next_x += x_step;
+        next_r += r_step;
     };
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) issue(row + s * step, s);
+    for (int s = 0; s < STAGES; ++s) issue(s * STAGE_BYTES);
     float g[CH][N];
 #pragma unroll
     for (int k = 0; k < CH; ++k)
         if (lane + k * RT < chunks) gamma_chunk<T>(a.gamma, a.gamma_f32, (lane + k * RT) * N, g[k]);
-    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+    for (uint32_t stage = 0; row < a.rows; row += step, stage = stage + STAGE_BYTES == STAGES * STAGE_BYTES ? 0 : stage + STAGE_BYTES) {
         copy_wait<STAGES - 1>();
+        const uint4 *slot = ring + threadIdx.x + stage / 16;
         float h[CH][N], ss = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             if (lane + k * RT >= chunks) continue;
-            unpack(ring[((stage * 2 + 0) * CH + k) * BLOCK + threadIdx.x], h[k]);
-            if (a.r) {
-                float f[N];
-                unpack(ring[((stage * 2 + 1) * CH + k) * BLOCK + threadIdx.x], f);
+            unpack(slot[k * BLOCK], h[k]);
+            if (a.r) add_chunk(slot[(CH + k) * BLOCK], h[k]);
 #pragma unroll
-                for (int i = 0; i < N; ++i) h[k][i] += f[i];
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) ss += h[k][i] * (h[k][i] * a.down);
+            for (int i = 0; i < N; ++i) ss += h[k][i] * h[k][i];
         }
-        issue(row + STAGES * step, stage);  // (results go over the operands of their own row only)
-        const float inv = rsqrtf(row_reduce<RT, false>(ss, part, turn) * a.up + a.eps);
+        issue(stage);  // (results go over the operands of their own row only)
+        float mean = row_reduce<RT, false>(ss, part, turn) * a.down;
+        if (mean > 3.402823466e38f) {  // the sum of the squares does not fit, their mean may
+            ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+                if (lane + k * RT < chunks) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) ss += h[k][i] * (h[k][i] * a.down);
+                }
+            mean = row_reduce<RT, false>(ss, part, turn);
+        }
+        const float inv = rsqrtf(mean * a.up + a.eps);
         const uint64_t at = row * a.cols;
         if (a.sum) {
             T *to = (T *)a.sum + at;
@@ -436,11 +502,11 @@ __global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a)
 #pragma unroll
             for (int i = 0; i < N; ++i) h[k][i] = h[k][i] * inv * g[k][i];
         }
-        if (a.y) {
+        if (!EIGHT || a.y) {
             T *to = (T *)a.y + at;
 #pragma unroll
             for (int k = 0; k < CH; ++k)
-                if (lane + k * RT < chunks) *reinterpret_cast<uint4 *>(to + (lane + k * RT) * N) = pack(h[k]);
+                if (a.y && lane + k * RT < chunks) *reinterpret_cast<uint4 *>(to + (lane + k * RT) * N) = pack(h[k]);
         }
         if constexpr (EIGHT) {
             float top[CH], row_top = 0.f;
@@ -449,7 +515,7 @@ __global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a)
                 top[k] = 0.f;
                 if (lane + k * RT >= chunks) continue;
 #pragma unroll
-                for (int i = 0; i < N; ++i) top[k] = max_nan(top[k], fabsf(h[k][i]));
+                for (int i = 0; i < N; i += 2) top[k] = max_abs(top[k], h[k][i], h[k][i + 1]);
                 row_top = max_nan(row_top, top[k]);
             }
             if (!a.group) {
@@ -462,7 +528,9 @@ __global__ void __launch_bounds__(norm_block(RT)) lt_norm_rows(const NormArgs a)
                 float t = row_top;
                 if (a.group) {  // a power of two of lanes share a scale
                     t = top[k];
-                    for (uint32_t d = 1u << a.group_shift >> 1; d > 0; d >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, d));
+#pragma unroll
+                    for (int d = 0; d < 5; ++d)
+                        if (d < (int)a.group_shift) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, 1 << d));
                     if (a.scales && c < chunks && (c & ((1u << a.group_shift) - 1)) == 0) a.scales[row * a.groups + (c >> a.group_shift)] = scale_of(t);
                 }
                 if (!a.codes || c >= chunks) continue;
@@ -542,16 +610,17 @@ __device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int 
     return s;
 }
 
-__host__ __device__ constexpr int grad_block(int rt) { return rt > 512 ? rt : 512; }
-__host__ __device__ constexpr int grad_stages(int ch) { return ch == 1 ? 3 : 1; }
-__host__ __device__ constexpr size_t grad_bytes(int rt, int ch) { return (size_t)grad_stages(ch) * 3 * ch * grad_block(rt) * 16; }
+__host__ __device__ constexpr int grad_block(int rt) { return rt > 256 ? rt : 256; }
+__host__ __device__ constexpr int grad_stages(int rt, int ch) { return grad_block(rt) * ch <= 512 ? 4 : grad_block(rt) * ch <= 1024 ? 2 : 1; }
+__host__ __device__ constexpr size_t grad_bytes(int rt, int ch) { return (size_t)grad_stages(rt, ch) * 3 * ch * grad_block(rt) * 16; }
+constexpr int GRAD_CHUNKS = 4;  // of a thread, at most
 
 // 16 bytes at a time, RT threads per row; a block has several rows at once and goes on to others, the sums for gamma
 // staying in registers.  Bound by memory like lt_norm_rows, and like there the rows to come travel through shared
 // memory, from which a row is read twice: for its sums, and for its results.
 template <class T, int RT, int CH>
-__global__ void __launch_bounds__(grad_block(RT)) lt_norm_grad_rows(const NormGradArgs a) {
-    constexpr int N = Chunk<T>::N, BLOCK = grad_block(RT), GROUPS = BLOCK / RT, STAGES = grad_stages(CH);
+__global__ void __launch_bounds__(grad_block(RT), RT > 256 ? 1 : 2) lt_norm_grad_rows(const NormGradArgs a) {
+    constexpr int N = Chunk<T>::N, BLOCK = grad_block(RT), GROUPS = BLOCK / RT, STAGES = grad_stages(RT, CH);
     __shared__ float2 part[64];
     int turn = 0;
     extern __shared__ uint4 ring[];  // [STAGES][dy, h, dh][CH][BLOCK]; at the end [GROUPS - 1][cols]: the groups' sums for gamma
@@ -596,12 +665,29 @@ __global__ void __launch_bounds__(grad_block(RT)) lt_norm_grad_rows(const NormGr
             unpack(*place(stage, 1, k), u);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float v = u[i] * a.down;
-                ss += u[i] * v;
-                dot += d[i] * g[k][i] * v;
+                ss += u[i] * u[i];
+                dot += d[i] * g[k][i] * u[i];
             }
         }
-        const float2 s = group_sum<RT>(ss, dot, part, group, turn);
+        float2 s = group_sum<RT>(ss, dot, part, group, turn);
+        s.x *= a.down;
+        s.y *= a.down;
+        if (s.x > 3.402823466e38f) {  // the sum of the squares does not fit, their mean may
+            ss = dot = 0.f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                if (lane + k * RT >= chunks) continue;
+                float d[N], u[N];
+                unpack(*place(stage, 0, k), d);
+                unpack(*place(stage, 1, k), u);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    ss += u[i] * (u[i] * a.down);
+                    dot += d[i] * g[k][i] * (u[i] * a.down);
+                }
+            }
+            s = group_sum<RT>(ss, dot, part, group, turn);
+        }
         const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
@@ -609,13 +695,13 @@ __global__ void __launch_bounds__(grad_block(RT)) lt_norm_grad_rows(const NormGr
             float d[N], u[N], e[N];
             unpack(*place(stage, 0, k), d);
             unpack(*place(stage, 1, k), u);
-            if (a.dh) unpack(*place(stage, 2, k), e);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float n = u[i] * inv;
                 sum[k][i] += d[i] * n;
-                e[i] = (a.dh ? e[i] : 0.f) + (d[i] * g[k][i] - n * m) * inv;
+                e[i] = (d[i] * g[k][i] - n * m) * inv;
             }
+            if (a.dh) add_chunk(*place(stage, 2, k), e);
             if (a.dx) *reinterpret_cast<uint4 *>((T *)a.dx + row * a.cols + (uint64_t)(lane + k * RT) * N) = pack(e);
         }
         issue(row + STAGES * step, stage);
@@ -666,7 +752,7 @@ __global__ void __launch_bounds__(1024) lt_norm_grad_join(const float *partial, 
     for (uint64_t c0 = (uint64_t)blockIdx.x * 32; c0 < cols; c0 += (uint64_t)gridDim.x * 32) {
         double s = 0.0;
         if (c0 + lane < cols) {
-#pragma unroll 4
+#pragma unroll 10
             for (unsigned b = warp; b < blocks; b += 32) s += (double)partial[(uint64_t)b * cols + c0 + lane];
         }
         __syncthreads();
@@ -712,17 +798,26 @@ cudaError_t launch_norm_rows(const NormArgs &a, int sm_count, cudaStream_t strea
     return launch_pdl(lt_norm_rows<T, RT, CH, EIGHT>, (unsigned)(blocks < most ? blocks : most), norm_block(RT), norm_bytes(RT, CH), stream, a);
 }
 
-template <class T, bool EIGHT>
-cudaError_t launch_norm_threads(const NormArgs &a, int rt, int ch, int sm_count, cudaStream_t stream) {
-    if (ch == 2) return launch_norm_rows<T, 1024, 2, EIGHT>(a, sm_count, stream);
-    if (ch == 4) return launch_norm_rows<T, 1024, 4, EIGHT>(a, sm_count, stream);
+template <class T, int CH, bool EIGHT>
+cudaError_t launch_norm_threads(const NormArgs &a, int rt, int sm_count, cudaStream_t stream) {
     switch (rt) {
-    case 32: return launch_norm_rows<T, 32, 1, EIGHT>(a, sm_count, stream);
-    case 128: return launch_norm_rows<T, 128, 1, EIGHT>(a, sm_count, stream);
-    case 256: return launch_norm_rows<T, 256, 1, EIGHT>(a, sm_count, stream);
-    case 512: return launch_norm_rows<T, 512, 1, EIGHT>(a, sm_count, stream);
-    default: return launch_norm_rows<T, 1024, 1, EIGHT>(a, sm_count, stream);
+    case 32: return launch_norm_rows<T, 32, CH, EIGHT>(a, sm_count, stream);
+    case 128: return launch_norm_rows<T, 128, CH, EIGHT>(a, sm_count, stream);
+    case 256: return launch_norm_rows<T, 256, CH, EIGHT>(a, sm_count, stream);
+    case 512: return launch_norm_rows<T, 512, CH, EIGHT>(a, sm_count, stream);
+    default: return launch_norm_rows<T, 1024, CH, EIGHT>(a, sm_count, stream);
     }
+}
+
+template <class T, bool EIGHT>
+cudaError_t launch_norm_chunks(const NormArgs &a, uint64_t chunks, int sm_count, cudaStream_t stream) {
+    // few rows: one chunk per thread, the most threads a row can use; many: four, which halves what a row costs besides its
+    // values (8192 x 4096 bf16 in 8 bits: 42 us against 45 with one chunk per thread and 49 with two)
+    const int rt = row_threads(chunks, a.rows <= 2 * (uint64_t)sm_count && chunks <= 1024 ? 1 : 4);
+    const int ch = chunks <= (uint64_t)rt ? 1 : chunks <= 2 * (uint64_t)rt ? 2 : 4;
+    if (ch == 1) return launch_norm_threads<T, 1, EIGHT>(a, rt, sm_count, stream);
+    if (ch == 2) return launch_norm_threads<T, 2, EIGHT>(a, rt, sm_count, stream);
+    return launch_norm_threads<T, 4, EIGHT>(a, rt, sm_count, stream);
 }
 
 template <class T>
@@ -732,9 +827,7 @@ cudaError_t launch_norm(NormArgs a, int sm_count, cudaStream_t stream) {
     const uint64_t chunks = a.cols / N;
     const bool fits = a.cols % N == 0 && a.x_pitch % N == 0 && (!a.r || (a.r_pitch % N == 0 && is_aligned(a.r, 16))) && is_aligned(a.x, 16) && is_aligned(a.gamma, 16) &&
                       is_aligned(a.y, 16) && is_aligned(a.sum, 16) && is_aligned(a.codes, 8) && a.group <= 32 * N;
-    // as many threads per row as it has chunks, while a block can have them
-    const int ch = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4, rt = fits ? row_threads(chunks, ch) : 0;
-    if (rt) return a.codes || a.scales ? launch_norm_threads<T, true>(a, rt, ch, sm_count, stream) : launch_norm_threads<T, false>(a, rt, ch, sm_count, stream);
+    if (fits && chunks <= 4096) return a.codes || a.scales ? launch_norm_chunks<T, true>(a, chunks, sm_count, stream) : launch_norm_chunks<T, false>(a, chunks, sm_count, stream);
     const uint64_t blocks = (uint64_t)sm_count * 8;
     return launch_pdl(lt_norm_any<T>, (unsigned)(a.rows < blocks ? a.rows : blocks), 256, (size_t)0, stream, a);
 }
@@ -743,13 +836,13 @@ cudaError_t launch_norm(NormArgs a, int sm_count, cudaStream_t stream) {
 // scratch holds is planned before the addresses are known: the most either takes.
 unsigned norm_grad_any_blocks(uint64_t rows, int sm_count) { return (unsigned)std::min<uint64_t>(rows, (uint64_t)sm_count * 4); }
 unsigned norm_grad_row_blocks(uint64_t rows, int rt, int sm_count) {
-    const uint64_t groups = rt > 512 ? 1 : 512 / rt, n = (rows + groups - 1) / groups;
-    return (unsigned)std::min<uint64_t>(n, (uint64_t)sm_count * 2);
+    const uint64_t groups = grad_block(rt) / rt, n = (rows + groups - 1) / groups;
+    return (unsigned)std::min<uint64_t>(n, (uint64_t)sm_count * (rt > 256 ? 1 : 2));
 }
 
 template <class T, int RT, int CH>
 cudaError_t launch_norm_grad_rows(const NormGradArgs &a, unsigned grid, cudaStream_t stream) {
-    constexpr int BLOCK = RT > 512 ? RT : 512, GROUPS = BLOCK / RT;
+    constexpr int BLOCK = grad_block(RT), GROUPS = BLOCK / RT;
     static_assert((GROUPS - 1) * RT * CH * Chunk<T>::N * 4 <= (int)grad_bytes(RT, CH), "the groups' sums fit");
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(lt_norm_grad_rows<T, RT, CH>, grad_bytes(RT, CH), ready);
@@ -763,8 +856,7 @@ cudaError_t launch_norm_grad_threads(const NormGradArgs &a, int rt, unsigned gri
     case 32: return launch_norm_grad_rows<T, 32, CH>(a, grid, stream);
     case 128: return launch_norm_grad_rows<T, 128, CH>(a, grid, stream);
     case 256: return launch_norm_grad_rows<T, 256, CH>(a, grid, stream);
-    case 512: return launch_norm_grad_rows<T, 512, CH>(a, grid, stream);
-    default: return launch_norm_grad_rows<T, 1024, CH>(a, grid, stream);
+    default: return launch_norm_grad_rows<T, 512, CH>(a, grid, stream);
     }
 }
 
@@ -773,14 +865,16 @@ cudaError_t launch_norm_grad(const NormGradArgs &a, int sm_count, cudaStream_t s
     constexpr uint64_t N = Chunk<T>::N;
     const bool fits = a.cols % N == 0 && a.dy_pitch % N == 0 && a.h_pitch % N == 0 && (!a.dh || (a.dh_pitch % N == 0 && is_aligned(a.dh, 16))) && is_aligned(a.dy, 16) &&
                       is_aligned(a.h, 16) && is_aligned(a.gamma, 16) && is_aligned(a.dx, 16);
-    const int rt = fits ? row_threads(a.cols / N, 2) : 0;
-    if (!rt) {
+    const uint64_t chunks = a.cols / N;
+    if (!fits || chunks > 512 * GRAD_CHUNKS) {
         *grid = norm_grad_any_blocks(a.rows, sm_count);
         return launch_pdl(lt_norm_grad_any<T>, *grid, 256, (size_t)0, stream, a);
     }
+    const int rt = row_threads(chunks, a.rows <= 2 * (uint64_t)sm_count && chunks <= 512 ? 1 : GRAD_CHUNKS);
     *grid = norm_grad_row_blocks(a.rows, rt, sm_count);
-    if (a.cols / N <= (uint64_t)rt) return launch_norm_grad_threads<T, 1>(a, rt, *grid, stream);
-    return launch_norm_grad_threads<T, 2>(a, rt, *grid, stream);
+    if (chunks <= (uint64_t)rt) return launch_norm_grad_threads<T, 1>(a, rt, *grid, stream);
+    if (chunks <= 2 * (uint64_t)rt) return launch_norm_grad_threads<T, 2>(a, rt, *grid, stream);
+    return launch_norm_grad_threads<T, 4>(a, rt, *grid, stream);
 }
 
 }  // namespace
