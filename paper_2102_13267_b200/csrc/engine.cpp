@@ -30,7 +30,11 @@ inline uint64_t now_ns() {
 inline uint64_t ticks_now() { return __builtin_ia32_rdtsc(); }
 const uint64_t g_tick0 = ticks_now(), g_ns0 = now_ns();
 inline double ns_per_tick() {
+    static std::atomic<double> known{0.0};  // measured once: the same ticks always read as the same nanoseconds
+    const double k = known.load(std::memory_order_relaxed);
+    if (k > 0.0) return k;
     const uint64_t dt = ticks_now() - g_tick0, dn = now_ns() - g_ns0;
+    if (dt && dn > 10000000) known.store((double)dn / (double)dt, std::memory_order_relaxed);
     return dt && dn > 1000000 ? (double)dn / (double)dt : 0.4;  // (before a millisecond has passed: a nominal 2.5 GHz)
 }
 #else
