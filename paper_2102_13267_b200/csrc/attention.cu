@@ -6,20 +6,23 @@
 //
 // Work split: the tokens of all sequences are cut into tiles of TILE; the list of (sequence, head block, tile) is divided
 // evenly over the thread blocks, whatever the sequences' lengths (which only the device knows).  Every (sequence, head
-// block) counts START tiles more than it has, for what beginning one costs (measured below).  A block walks its part of
-// the list; a (sequence, head block) that lies within one block's part is finished there.  One that is spread over
-// several blocks leaves partial results (maximum, sum, unnormalised output) in scratch memory, and the block that
-// arrives last joins them, always in the list's order, so results do not depend on the arrival.
+// block) counts START tiles more than it has, for what beginning one costs.  A block walks its part of the list; a
+// (sequence, head block) that lies within one block's part is finished there.  One that is spread over several leaves
+// partial results (maximum, sum, unnormalised output) in scratch memory, and the block that arrives last joins them,
+// always in the list's order, so results do not depend on the arrival.
+#include <type_traits>
+
 #include "operator_device.cuh"
 
 using namespace ltop;
 
 namespace {
 
-constexpr int TILE = 64;        // tokens
-constexpr int START = 2;        // tiles that beginning a (sequence, head block) counts for
-constexpr int MOST_PARTS = 64;  // blocks one (sequence, head block) is spread over
+constexpr int TILE = 64;         // tokens
+constexpr int START = 2;         // tiles that beginning a (sequence, head block) counts for
 constexpr int THREADS = 128;
+constexpr int WARPS = THREADS / 32;
+constexpr uint32_t MOST_PARTS = 64;  // blocks that one (sequence, head block) is spread over
 
 struct AttendArgs {
     const void *q, *cache;
@@ -43,104 +46,73 @@ __device__ __forceinline__ void check_length(const AttendArgs &a, uint32_t b) {
     if (threadIdx.x == 0 && a.lengths[b] > 0 && (int64_t)a.lengths[b] > (int64_t)a.table_width * a.page) atomicOr(a.status, 1u);
 }
 
-__device__ __forceinline__ uint32_t tiles_of(const AttendArgs &a, uint32_t b) { return ((uint32_t)length_of(a, b) + TILE - 1) / TILE; }
+__device__ __forceinline__ uint32_t tiles_in(int n) { return ((uint32_t)n + TILE - 1) / TILE; }
 
-// Length of sequence b's part of the list, per head block.
-__device__ __forceinline__ uint32_t items_of(const AttendArgs &a, uint32_t b) {
-    const uint32_t t = tiles_of(a, b);
-    return t ? t + START : 0;
-}
+__device__ __forceinline__ uint32_t items_of(int n) { return n ? tiles_in(n) + START : 0; }
 
-// Inclusive sums over the block's threads of a 64-bit value each; *all: over the whole block; *most: the largest `w`.
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint32_t w, uint64_t *part, uint64_t *all, uint32_t *most) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint64_t o = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v += o;
-    }
-    w = __reduce_max_sync(0xffffffffu, w);
-    __syncthreads();  // `part` may still be read from the scan before
-    if (lane == 31) part[warp] = v, part[THREADS / 32 + warp] = w;
-    __syncthreads();
-    uint64_t before = 0, sum = 0;
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < THREADS / 32; ++k) {
-        if (k < warp) before += part[k];
-        sum += part[k];
-        top = max(top, (uint32_t)part[THREADS / 32 + k]);
-    }
-    *all = sum;
-    *most = top;
-    return v + before;
-}
-
-// What a block works on: items [idx, end) of the list, the first in sequence b, whose own first item is `base`.
+// What a block works on: items [idx, end) of the list.
 struct Share {
-    uint64_t idx, end, base, size;  // size: of a block's share
-    uint32_t b;
+    uint32_t idx, end, size;    // size: of a share
+    uint32_t b, base;           // the sequence it is in, and where that begins in the list
+    int n;                      // its length
 };
 
-// The block's part of the list, from the sequences' lengths.  `part`, `found`: shared, 32 and 2 values.
-__device__ __forceinline__ Share my_share(const AttendArgs &a, uint64_t *part, uint64_t *found) {
+// The block's part of the list, from the sequences' lengths.  Every warp finds it for itself: a lane has a run of
+// sequences, whose sums are added up across lanes, without a barrier.
+__device__ __forceinline__ Share my_share(const AttendArgs &a) {
     const uint32_t per = a.kv_heads * a.head_blocks;
     Share s{};
     if (!a.partial) {  // a block per (sequence, head block)
         s.b = blockIdx.x / per;
-        const uint64_t t = items_of(a, s.b);
-        s.idx = (uint64_t)(blockIdx.x - s.b * per) * t;
+        s.n = length_of(a, s.b);
+        const uint32_t t = items_of(s.n);
+        s.idx = (blockIdx.x - s.b * per) * t;
         s.end = s.idx + t;
         return s;
     }
-    uint64_t total = 0, sum;
-    uint32_t most, more = 0;
-    uint32_t items = threadIdx.x < a.batch ? items_of(a, threadIdx.x) : 0;
-    uint64_t mine = (uint64_t)items * per, upto = block_scan(mine, items, part, &sum, &most);
-    if (a.batch > THREADS) {
-        uint64_t rest = 0;
-        uint32_t top = 0;
-        for (uint32_t b = threadIdx.x + THREADS; b < a.batch; b += THREADS) {
-            const uint32_t n = items_of(a, b);
-            rest += (uint64_t)n * per;
-            top = max(top, n);
-        }
-        block_scan(rest, top, part, &total, &more);
+    const uint32_t lane = threadIdx.x & 31, run = (a.batch + 31) / 32, b0 = lane * run;
+    uint32_t mine = 0, most = 0;
+    int n = 0;
+    for (uint32_t k = 0; k < run; ++k) {
+        const int m = b0 + k < a.batch ? length_of(a, b0 + k) : 0;
+        if (k == 0) n = m;
+        mine += items_of(m);
+        most = max(most, items_of(m));
     }
-    total += sum;
-    most = max(most, more);
+    mine *= per;
+    uint32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= (uint32_t)d) upto += o;
+    }
+    const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+    most = __reduce_max_sync(0xffffffffu, most);
     // an even share, and no (sequence, head block) over more than MOST_PARTS blocks
-    s.size = max((total + gridDim.x - 1) / gridDim.x, (uint64_t)((most + MOST_PARTS - 2) / (MOST_PARTS - 1)));
-    s.idx = (uint64_t)blockIdx.x * s.size;
+    s.size = max((total + gridDim.x - 1) / gridDim.x, (most + MOST_PARTS - 2) / (MOST_PARTS - 1));
+    s.idx = min(blockIdx.x * s.size, total);
     s.end = min(s.idx + s.size, total);
-    if (s.idx >= s.end) {
-        s.idx = s.end = 0;
-        return s;
-    }
-    uint64_t before = 0;
-    for (uint32_t b0 = 0;;) {
-        if (s.idx < before + sum) {
-            if (s.idx >= before + upto - mine && s.idx < before + upto) found[0] = b0 + threadIdx.x, found[1] = before + upto - mine;
-            break;
+    if (s.idx == s.end) return s;
+    uint32_t b = b0, base = upto - mine;
+    const uint32_t holder = __ffs(__ballot_sync(0xffffffffu, s.idx >= base && s.idx < upto)) - 1;
+    if (run > 1 && lane == holder)
+        while (s.idx >= base + items_of(n) * per) {
+            base += items_of(n) * per;
+            n = length_of(a, ++b);
         }
-        before += sum;
-        b0 += THREADS;
-        mine = b0 + threadIdx.x < a.batch ? (uint64_t)items_of(a, b0 + threadIdx.x) * per : 0;
-        upto = block_scan(mine, 0, part, &sum, &more);
-    }
-    __syncthreads();
-    s.b = (uint32_t)found[0];
-    s.base = found[1];
+    s.b = __shfl_sync(0xffffffffu, b, holder);
+    s.base = __shfl_sync(0xffffffffu, base, holder);
+    s.n = __shfl_sync(0xffffffffu, n, holder);
     return s;
 }
 
 // A stretch of tiles of one (sequence, head block).
 struct Stretch {
-    uint64_t first;         // list index of the first item of the (sequence, head block)
-    uint32_t b, kv, h0;     // h0: first query head
-    int n, heads;           // tokens of the sequence, query heads
-    uint32_t t0, t1, tiles;
-    uint32_t items;         // of the list
+    uint32_t first;             // of the (sequence, head block) in the list
+    uint32_t b, kv, h0;         // h0: first query head
+    int n, heads;               // tokens of the sequence, query heads
+    uint32_t t0, t1, tiles;     // tiles: of the sequence
+    uint32_t items;             // of the list
 };
 
 // The next stretch of the share, or false when it is done; `done`: items of the one before.
@@ -149,24 +121,21 @@ __device__ __forceinline__ bool next_stretch(const AttendArgs &a, Share &s, Stre
     for (;;) {
         s.idx += done;
         if (s.idx >= s.end) return false;
-        uint32_t all;
-        for (;;) {
-            w.n = length_of(a, s.b);
-            w.tiles = ((uint32_t)w.n + TILE - 1) / TILE;
-            all = w.tiles ? w.tiles + START : 0;
-            if (s.idx < s.base + (uint64_t)all * per) break;
-            s.base += (uint64_t)all * per;
-            ++s.b;
+        while (s.idx >= s.base + items_of(s.n) * per) {
+            s.base += items_of(s.n) * per;
+            s.n = length_of(a, ++s.b);
         }
-        const uint32_t hb = (uint32_t)((s.idx - s.base) / all);
-        w.first = s.base + (uint64_t)hb * all;
-        const uint32_t v0 = (uint32_t)(s.idx - w.first), v1 = (uint32_t)min((uint64_t)all, v0 + (s.end - s.idx));
+        const uint32_t all = items_of(s.n), hb = (s.idx - s.base) / all;
+        w.tiles = all - START;
+        w.first = s.base + hb * all;
+        const uint32_t v0 = s.idx - w.first, v1 = min(all, v0 + (s.end - s.idx));
         done = w.items = v1 - v0;
         w.t0 = max(v0, (uint32_t)START) - START;
         w.t1 = max(v1, (uint32_t)START) - START;
         if (w.t1 == w.t0) continue;  // only of what beginning counts for
         w.b = s.b;
-        w.kv = hb / a.head_blocks;
+        w.n = s.n;
+        w.kv = a.head_blocks == 1 ? hb : hb / a.head_blocks;
         const uint32_t first = (hb - w.kv * a.head_blocks) * a.block_heads;
         w.h0 = w.kv * a.group + first;
         w.heads = (int)min(a.block_heads, a.group - first);
@@ -174,75 +143,150 @@ __device__ __forceinline__ bool next_stretch(const AttendArgs &a, Share &s, Stre
     }
 }
 
-// Where the block leaves its part of a stretch that others share.
-__device__ __forceinline__ float *part_of(const AttendArgs &a, uint64_t block, bool second) {
-    return a.partial + (2 * block + (second ? 1 : 0)) * a.block_heads * (a.dim + 2);
-}
-
 __device__ __forceinline__ float quotient(float o, float l) { return l > 0.f ? o / l : l == 0.f ? 0.f : l; }
 
-// The block has left its part of stretch w: if it is the last of those that share the (sequence, head block), it joins the
-// parts.  `room`: shared memory for block_heads x MOST_PARTS values; `sums`: for block_heads values.  V values at a time
-// (dim a multiple of V, scratch and output aligned accordingly).
-template <class T, int V>
-__device__ __forceinline__ void join_if_last(const AttendArgs &a, const Share &s, const Stretch &w, float *room, float *sums, uint64_t *flag) {
-    const uint64_t c0 = (w.first + START) / s.size, c1 = (w.first + START + w.tiles - 1) / s.size;
-    const uint32_t count = (uint32_t)(c1 - c0) + 1;
+// Where a block leaves its parts: of the first or the second stretch that it does not finish.
+__device__ __forceinline__ uint64_t part_floats(const AttendArgs &a) { return (uint64_t)a.block_heads * (a.dim + 2); }
+__device__ __forceinline__ float *part_of(const AttendArgs &a, uint32_t block, bool second) { return a.partial + (2 * (uint64_t)block + (second ? 1 : 0)) * part_floats(a); }
+
+// The parts of a stretch's (sequence, head block), in order.
+struct Parts {
+    const float *head, *rest;   // the first part; where the others are `stride` apart, from the second on
+    uint32_t count;
+    uint64_t stride;
+    __device__ __forceinline__ const float *at(uint32_t i) const { return i ? rest + (i - 1) * stride : head; }
+};
+
+// The block has left its part of stretch w; true if that was the last one of the (sequence, head block), whose parts are then `p`.
+__device__ __forceinline__ bool last_of_parts(const AttendArgs &a, const Share &s, const Stretch &w, Parts &p, uint32_t *flag) {
+    const uint32_t i0 = w.first + START, c0 = i0 / s.size, c1 = (i0 + w.tiles - 1) / s.size;
+    p.count = c1 - c0 + 1;
+    p.stride = 2 * part_floats(a);
+    p.head = part_of(a, c0, c0 * s.size < w.first);
+    p.rest = part_of(a, c0 + 1, false);
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
-        *flag = atomicAdd(a.arrivals + c0, 1u) == count - 1;
+        *flag = atomicAdd(a.arrivals + c0, 1u) == p.count - 1;
         __threadfence();
     }
     __syncthreads();
-    if (!*flag) return;
-    if (threadIdx.x == 0) a.arrivals[c0] = 0;
-    const uint32_t dim = a.dim;
-    const uint64_t slot = (uint64_t)2 * a.block_heads * (dim + 2);
-    const float *head = part_of(a, c0, c0 * s.size < w.first), *rest = part_of(a, c0, false);  // of the first part; of the others, i x slot on
-    auto of = [&](uint32_t i) { return i ? rest + i * slot : head; };
-    for (uint32_t x = threadIdx.x; x < (uint32_t)w.heads * MOST_PARTS; x += THREADS) {
-        const uint32_t h = x / MOST_PARTS, i = x % MOST_PARTS;
-        if (i < count) room[x] = __ldcg(of(i) + a.block_heads * dim + 2 * h);
-    }
-    __syncthreads();
-    for (int h = threadIdx.x >> 5; h < w.heads; h += THREADS / 32) {  // a warp per head: maxima to weights
-        float top = -INFINITY, sum = 0.f;
-        for (uint32_t i = threadIdx.x & 31; i < count; i += 32) top = fmaxf(top, room[h * MOST_PARTS + i]);
+    const bool last = *flag != 0;
+    if (last && threadIdx.x == 0) a.arrivals[c0] = 0;
+    return last;
+}
+
+// The parts' weights 2^(maximum - largest maximum) and, in `sums`, the weighted sum of their sums: a warp per head, a lane per part.
+__device__ __forceinline__ void weigh_parts(const AttendArgs &a, const Stretch &w, const Parts &p, float *weights, float *sums) {
+    const uint32_t lane = threadIdx.x & 31;
+    for (int h = threadIdx.x >> 5; h < w.heads; h += WARPS) {
+        float m[MOST_PARTS / 32], l[MOST_PARTS / 32], top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (uint32_t k = 0; k < MOST_PARTS / 32; ++k) {
+            const uint32_t i = lane + 32 * k;
+            const float *ml = p.at(i) + a.block_heads * a.dim + 2 * h;
+            m[k] = i < p.count ? __ldcg(ml) : -INFINITY;
+            l[k] = i < p.count ? __ldcg(ml + 1) : 0.f;
+            top = fmaxf(top, m[k]);
+        }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         if (top == -INFINITY) top = 0.f;
-        for (uint32_t i = threadIdx.x & 31; i < count; i += 32) {
-            const float f = exp2f(room[h * MOST_PARTS + i] - top);
-            room[h * MOST_PARTS + i] = f;
-            sum += f * __ldcg(of(i) + a.block_heads * dim + 2 * h + 1);
+#pragma unroll
+        for (uint32_t k = 0; k < MOST_PARTS / 32; ++k) {
+            const float f = exp2f(m[k] - top);
+            if (lane + 32 * k < p.count) weights[h * MOST_PARTS + lane + 32 * k] = f;
+            sum += f * l[k];
         }
         sum = warp_sum(sum);
-        if ((threadIdx.x & 31) == 0) sums[h] = sum;
+        if (lane == 0) sums[h] = sum;
     }
+}
+
+// Joins parts, one value at a time (any head size).  `room`: shared, block_heads x MOST_PARTS values.
+template <class T>
+__device__ __forceinline__ void join_any(const AttendArgs &a, const Stretch &w, const Parts &p, float *room, float *sums) {
+    const uint32_t dim = a.dim;
+    weigh_parts(a, w, p, room, sums);
     __syncthreads();
-    for (uint32_t x = threadIdx.x; x < (uint32_t)w.heads * (dim / V); x += THREADS) {
-        const uint32_t h = x / (dim / V), d = (x - h * (dim / V)) * V;
-        float o[V] = {};
+    for (uint32_t x = threadIdx.x; x < (uint32_t)w.heads * dim; x += THREADS) {
+        const uint32_t h = x / dim, d = x - h * dim;
+        float o = 0.f;
 #pragma unroll 8
-        for (uint32_t i = 0; i < count; ++i) {
-            const float *p = of(i) + h * dim + d;
-            const float f = room[h * MOST_PARTS + i];
-            if constexpr (V == 4) {
-                const float4 v = __ldcg(reinterpret_cast<const float4 *>(p));
-                o[0] += f * v.x;
-                o[1] += f * v.y;
-                o[2] += f * v.z;
-                o[3] += f * v.w;
-            } else {
-                o[0] += f * __ldcg(p);
-            }
-        }
-        T *out = (T *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * dim + d;
-#pragma unroll
-        for (int k = 0; k < V; ++k) out[k] = from_float<T>(quotient(o[k], sums[h]));
+        for (uint32_t i = 0; i < p.count; ++i) o += room[h * MOST_PARTS + i] * __ldcg(p.at(i) + h * dim + d);
+        ((T *)a.out)[((uint64_t)w.b * a.heads + w.h0 + h) * dim + d] = from_float<T>(quotient(o, sums[h]));
     }
     __syncthreads();  // `room` is used again
+}
+
+template <class T>
+__device__ __forceinline__ void store4(T *to, const float4 &v);
+template <>
+__device__ __forceinline__ void store4<float>(float *to, const float4 &v) { *reinterpret_cast<float4 *>(to) = v; }
+template <>
+__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 *to, const float4 &v) { *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
+
+// Joins parts, four values at a time: as many parts as fit are brought into shared memory at once, while the weights are
+// found (one trip to L2 for both, instead of one for the maxima and one for every few parts after them).
+// `mem`: `bytes` of shared memory; a.dim a multiple of 4; HEADS x WIDTH values at most.
+template <class T, int HEADS, int WIDTH>
+__device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &w, const Parts &p, float *mem, uint32_t bytes) {
+    constexpr int MINE = (HEADS * WIDTH / 4 + THREADS - 1) / THREADS;  // groups of four values of a thread
+    const uint32_t dim = a.dim, quads = (uint32_t)w.heads * dim / 4;
+    float *weights = mem, *sums = weights + HEADS * MOST_PARTS;       // [HEADS][MOST_PARTS], [HEADS]
+    float4 *staged = reinterpret_cast<float4 *>(sums + HEADS);
+    const uint32_t room = (bytes - (HEADS * MOST_PARTS + HEADS) * 4) / (quads * 16);
+    float4 acc[MINE];
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i0 = 0; i0 < p.count; i0 += room) {
+        const uint32_t n = min(room, p.count - i0);
+        if (i0) __syncthreads();  // the parts before have been read
+        for (uint32_t x = threadIdx.x; x < quads; x += THREADS) {
+            uint32_t to = shared_address(staged + x), i = 0;
+            if (i0 == 0) {
+                copy16(to, p.head + 4 * x, true);
+                to += quads * 16;
+                i = 1;
+            }
+            const float *from = p.rest + (i0 + i - 1) * p.stride + 4 * x;
+#pragma unroll 4
+            for (; i < n; ++i) {
+                copy16(to, from, true);
+                to += quads * 16;
+                from += p.stride;
+            }
+        }
+        copy_commit();
+        if (i0 == 0) weigh_parts(a, w, p, weights, sums);
+        copy_wait<0>();
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t x = threadIdx.x + k * THREADS;
+            if (x >= quads) continue;
+            const float *f = weights + (4 * x / dim) * MOST_PARTS + i0;
+            const float4 *from = staged + x;
+            float4 v = acc[k];
+#pragma unroll 4
+            for (uint32_t i = 0; i < n; ++i) {
+                const float4 o = *from;
+                v.x += f[i] * o.x;
+                v.y += f[i] * o.y;
+                v.z += f[i] * o.z;
+                v.w += f[i] * o.w;
+                from += quads;
+            }
+            acc[k] = v;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+        const uint32_t x = threadIdx.x + k * THREADS;
+        if (x >= quads) continue;
+        const float l = sums[4 * x / dim];
+        store4((T *)a.out + ((uint64_t)w.b * a.heads + w.h0) * dim + 4 * x, make_float4(quotient(acc[k].x, l), quotient(acc[k].y, l), quotient(acc[k].z, l), quotient(acc[k].w, l)));
+    }
 }
 
 // The zeros of empty sequences, and the check of the lengths.
@@ -251,7 +295,7 @@ __device__ __forceinline__ void finish(const AttendArgs &a) {
     if (!a.partial) {  // the block's own sequence
         const uint32_t per = a.kv_heads * a.head_blocks, b = blockIdx.x / per;
         check_length(a, b);
-        if (tiles_of(a, b)) return;
+        if (length_of(a, b)) return;
         const uint32_t hb = blockIdx.x - b * per, kv = hb / a.head_blocks, first = (hb - kv * a.head_blocks) * a.block_heads;
         const uint32_t count = min(a.block_heads, a.group - first) * a.dim;
         T *out = (T *)a.out + ((uint64_t)b * a.heads + kv * a.group + first) * a.dim;
@@ -260,7 +304,7 @@ __device__ __forceinline__ void finish(const AttendArgs &a) {
     }
     for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
         check_length(a, b);
-        if (tiles_of(a, b)) continue;
+        if (length_of(a, b)) continue;
         T *out = (T *)a.out + (uint64_t)b * a.heads * a.dim;
         for (uint32_t x = threadIdx.x; x < a.heads * a.dim; x += THREADS) out[x] = from_float<T>(0.f);
     }
@@ -284,17 +328,16 @@ constexpr int ANY_HEADS = 8;    // block_heads of lt_attend_any
 template <class T, int NE>
 __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
     constexpr int HEADS = ANY_HEADS;
-    __shared__ uint64_t part[32], found[2];
+    __shared__ uint32_t flag;
     __shared__ float sm_m[4][HEADS], sm_l[4][HEADS];
     __shared__ float sm_o[4][HEADS][NE * 32];
-    float *sm_room = &sm_o[0][0][0];
-    static_assert(4 * NE * 32 >= MOST_PARTS, "the parts' weights fit");
+    static_assert(4 * NE * 32 >= (int)MOST_PARTS, "the parts' weights fit where the warps' outputs are");
     pdl_release();
     pdl_wait();
     const T *q = (const T *)a.q, *cache = (const T *)a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    Share s = my_share(a, part, found);
-    const uint64_t start = s.idx;
+    Share s = my_share(a);
+    const uint32_t start = s.idx;
     Stretch w;
     for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
         const int *row = a.table + (uint64_t)w.b * a.table_width;
@@ -364,12 +407,15 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
                 if (d == 0) slot[HEADS * a.dim + 2 * h] = mm, slot[HEADS * a.dim + 2 * h + 1] = ll;
             }
         }
-        if (!whole) join_if_last<T, 1>(a, s, w, sm_room, &sm_l[0][0], found);
+        if (!whole) {
+            Parts parts;
+            if (last_of_parts(a, s, w, parts, &flag)) join_any<T>(a, w, parts, &sm_o[0][0][0], &sm_l[0][0]);
+        }
     }
     finish<T>(a);
 }
 
-// ------------------------------------------------------------------------------------------- bf16 on the matrix units
+// ------------------------------------------------------------------------------------------- on the matrix units
 
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -387,6 +433,29 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void multiply_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x as two numbers of 11 significant bits that the matrix units take: what is left out is below 2^-21 of x.  `odd` becomes a
+// NaN when x is one, or an infinity, or rounds to one: then the small part is useless, see halve_any.
+__device__ __forceinline__ void halve(uint32_t x, uint32_t &hi, uint32_t &lo, float &odd) {
+    hi = (x + 0x1000u) & 0xffffe000u;
+    const float rest = __uint_as_float(x) - __uint_as_float(hi);
+    lo = __float_as_uint(rest);
+    odd = fmaf(rest, 0.f, odd);
+}
+// The same for any x: an infinity or a NaN is all in hi, and `finite` is hi without it: what stands beside the other
+// factor's small part, whose sign says nothing.
+__device__ __forceinline__ void halve_any(uint32_t x, uint32_t &hi, uint32_t &lo, uint32_t &finite) {
+    hi = (x + 0x1000u) & 0xffffe000u;
+    const float rest = __uint_as_float(x) - __uint_as_float(hi);
+    const bool fine = fabsf(rest) <= 3.402823466e38f;
+    lo = fine ? __float_as_uint(rest) : 0u;
+    if (!fine) hi = x & 0xffffe000u;
+    finite = fine ? hi : 0u;
+}
 __device__ __forceinline__ float power2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -394,68 +463,56 @@ __device__ __forceinline__ float power2(float x) {
 }
 
 constexpr int STEP = 16;        // tokens a warp takes at a time: a quarter of a tile
-constexpr int STAGES = 3;
 
-// Resident blocks per SM: what the stages leave room for, fewer where 16 or 32 heads of 64 values take the registers.
-constexpr int tensor_blocks(int width, int tiles) { return width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1; }
+// Sizes of the kernel for heads of up to DP values, NT x 8 query heads per block.
+template <class T, int DP>
+struct Shape {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int CHUNKS = DP * (int)sizeof(T) / 16;
+    // rows of keys and values in shared memory, in bytes: padded so that what a matrix load touches falls into different banks
+    static constexpr int K_PITCH = DP * (int)sizeof(T) + 16, V_PITCH = F32 ? DP * 4 + 32 : K_PITCH;
+    static constexpr int STAGE = STEP * (K_PITCH + V_PITCH);
+    static constexpr int STAGES = F32 && DP > 128 ? 2 : 3;
+    static constexpr int BYTES = WARPS * STAGES * STAGE;
+};
+// Resident blocks per SM: what the stages leave room for, fewer where many heads of 64 values take the registers.
+__host__ __device__ constexpr int tensor_blocks(int size, int width, int tiles) {
+    return size == 4 ? (width <= 64 ? 2 : 1) : width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1;
+}
 
-// Shared memory of a block: per warp STAGES steps of keys and values, rows padded by 16 bytes so that eight rows of a
-// matrix fall into different banks.
-template <int DP>
-constexpr size_t tensor_bytes() { return (size_t)(THREADS / 32) * STAGES * 2 * STEP * (DP * 2 + 16); }
-
-// bf16, 16-byte aligned, head sizes that are multiples of 8, filled up to DP with zeros; NT x 8 query heads per block.
+// bf16 and f32, 16-byte aligned rows, head sizes filled up to DP with zeros; NT x 8 query heads per block.
 //
 // The few query heads make the narrow side of the products: scores are K (16 tokens x dims) times q^T (dims x 8 heads),
 // the output is V^T (16 dims x 16 tokens) times the weights (16 tokens x 8 heads), so no matrix row is wasted on
-// padding of the group to 16.  The weights leave the first product with tokens along the rows and enter the second with
-// tokens along the columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps
-// the weights to 2^-17 and costs one more product.  Each warp has steps and a copy pipeline of its own -- no barrier
-// in the loop -- and its own running maximum and sum; warps are joined once per stretch.
-template <int DP, int NT, bool WHOLE_STEPS>
-__global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tensor(const AttendArgs a) {
-    constexpr int HEADS = 8 * NT, PITCH = DP * 2 + 16, KS = DP / 16, CHUNKS = DP / 8;
-    constexpr uint32_t STAGE_BYTES = 2 * STEP * PITCH;
+// padding of the group to 16.  Each warp has steps and a copy pipeline of its own -- no barrier in the loop -- and its own
+// running maximum and sum; warps are joined once per stretch.
+//   bf16: the weights leave the first product with tokens along the rows and enter the second with tokens along the
+//   columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps the
+//   weights to 2^-17 and costs one more product.
+//   f32: every factor as two tf32 parts, three products each (all but the one of the two small parts); the weights are
+//   turned through 512 bytes of shared memory.  (Infinities in keys and values come out as they should; one in q gives a NaN.)
+template <class T, int DP, int NT, bool WHOLE_STEPS>
+__global__ void __launch_bounds__(THREADS, tensor_blocks(sizeof(T), DP, NT)) lt_attend_tensor(const AttendArgs a) {
+    using S = Shape<T, DP>;
+    constexpr bool F32 = S::F32;
+    constexpr int HEADS = 8 * NT, N = 16 / (int)sizeof(T), CHUNKS = S::CHUNKS, STAGES = S::STAGES, KP = S::K_PITCH, VP = S::V_PITCH;
+    constexpr int MT = DP / 16, QK = F32 ? DP / 8 : DP / 16, QR = F32 ? 4 : 2;  // output tiles; steps of the first product and registers of q in each
     extern __shared__ __align__(128) unsigned char stage_mem[];
-    __shared__ uint64_t part[32], found[2];
-    __shared__ float sm_m[4][HEADS], sm_l[4][HEADS];
-    __shared__ uint32_t sm_mask[4][STAGES];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t chunks = a.dim / 8;
-    unsigned char *mine = stage_mem + warp * STAGES * STAGE_BYTES;
+    __shared__ uint32_t flag;
+    __shared__ float sm_m[WARPS][HEADS], sm_l[WARPS][HEADS];
+    __shared__ uint32_t sm_mask[WARPS][STAGES];
+    __shared__ __align__(16) float sm_p[F32 ? WARPS : 1][F32 ? NT * 128 : 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, eighth = lane >> 2;
+    const uint32_t chunks = a.dim / N;
+    unsigned char *mine = stage_mem + warp * STAGES * S::STAGE;
     const uint32_t stages = shared_address(mine);
-    const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q, *cache = (const __nv_bfloat16 *)a.cache;
+    const T *q = (const T *)a.q, *cache = (const T *)a.cache;
     pdl_release();
     pdl_wait();
-    Share s = my_share(a, part, found);
-    const uint64_t start = s.idx;
+    Share s = my_share(a);
+    const uint32_t start = s.idx;
     Stretch w;
     for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
-        // columns from dim to DP stay zero (the memory is also used to join warps)
-        if (chunks < CHUNKS)
-            for (int x = lane; x < STAGES * 2 * STEP * (CHUNKS - (int)chunks); x += 32) {
-                const int r = x / (CHUNKS - (int)chunks), c = x - r * (CHUNKS - (int)chunks);
-                *reinterpret_cast<uint4 *>(mine + r * PITCH + (chunks + c) * 16) = make_uint4(0, 0, 0, 0);
-            }
-        uint32_t qf[NT][KS][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int h = t * 8 + (lane >> 2);
-                    const uint32_t d = k * 16 + i * 8 + (lane & 3) * 2;
-                    qf[t][k][i] = (h < w.heads && d < a.dim) ? *reinterpret_cast<const uint32_t *>(q + (uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim + d) : 0u;
-                }
-        float o[NT][KS][4], m[NT][2], l[NT][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            m[t][0] = m[t][1] = -INFINITY;
-            l[t][0] = l[t][1] = 0.f;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) o[t][k][0] = o[t][k][1] = o[t][k][2] = o[t][k][3] = 0.f;
-        }
         const int *row = a.table + (uint64_t)w.b * a.table_width;
         const int first = (int)(w.t0 * TILE) + warp * STEP;  // first token of this warp's first step
         const int steps = (int)(w.t1 - w.t0);
@@ -467,9 +524,44 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
             const int i = WHOLE_STEPS ? first + (step + lane) * TILE : first + step * TILE + (lane & 15);
             ahead = i < w.n ? row[(uint32_t)i / a.page] : -2;
         };
+        fetch_pages(0);
+        uint32_t qf[NT][QK][QR];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int h = t * 8 + eighth;
+            const T *from = q + (uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim;
+#pragma unroll
+            for (int k = 0; k < QK; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (F32) {
+                        const uint32_t d = k * 8 + i * 4 + quad;
+                        uint32_t finite;
+                        halve_any(h < w.heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(from + d) : 0u, qf[t][k][i], qf[t][k][2 + i], finite);
+                    } else {
+                        const uint32_t d = k * 16 + i * 8 + quad * 2;
+                        qf[t][k][i] = h < w.heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(from + d) : 0u;
+                    }
+                }
+        }
+        // columns from dim to DP stay zero (the memory is also used to join warps)
+        if (chunks < CHUNKS)
+            for (int x = lane; x < STAGES * 2 * STEP * (CHUNKS - (int)chunks); x += 32) {
+                const int r = x / (CHUNKS - (int)chunks), c = x - r * (CHUNKS - (int)chunks), stage = r / (2 * STEP), i = r % (2 * STEP);
+                *reinterpret_cast<uint4 *>(mine + stage * S::STAGE + (i < STEP ? i * KP : STEP * KP + (i - STEP) * VP) + (chunks + c) * 16) = make_uint4(0, 0, 0, 0);
+            }
+        float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            m[t][0] = m[t][1] = -INFINITY;
+            l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+            for (int k = 0; k < MT; ++k) o[t][k][0] = o[t][k][1] = o[t][k][2] = o[t][k][3] = 0.f;
+        }
+
         auto issue = [&](int step) {
             if (step < steps) {
-                const uint32_t to = stages + (uint32_t)(step % STAGES) * STAGE_BYTES;
+                const uint32_t to = stages + (uint32_t)(step % STAGES) * S::STAGE;
                 const int i0 = first + step * TILE, left = w.n - i0;
                 uint32_t mask = left >= STEP ? 0xffffu : left <= 0 ? 0u : (1u << left) - 1u;
                 if (WHOLE_STEPS) {
@@ -480,15 +572,15 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
                         atomicOr(a.status, 1u);
                     }
                     const uint32_t off = (uint32_t)i0 % a.page;
-                    const __nv_bfloat16 *src = cache + (mask ? (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)w.kv * a.head_stride : 0);
+                    const T *src = cache + (mask ? (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)w.kv * a.head_stride : 0);
 #pragma unroll
                     for (int x = 0; x < STEP * CHUNKS; x += 32) {
                         const int r = (x + lane) / CHUNKS, c = (x + lane) % CHUNKS;
                         const bool there = (mask >> r) & 1u;
-                        const __nv_bfloat16 *at = there ? src + (uint64_t)r * a.token_stride + c * 8 : cache;
+                        const T *at = there ? src + (uint64_t)r * a.token_stride + c * N : cache;
                         if (c < (int)chunks) {
-                            copy16(to + r * PITCH + c * 16, at, there);
-                            copy16(to + (STEP + r) * PITCH + c * 16, there ? at + a.value_offset : cache, there);
+                            copy16(to + r * KP + c * 16, at, there);
+                            copy16(to + STEP * KP + r * VP + c * 16, there ? at + a.value_offset : cache, there);
                         }
                     }
                 } else {
@@ -502,10 +594,10 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
                         const int r = (x + lane) / CHUNKS, c = (x + lane) % CHUNKS;
                         const uint64_t from = __shfl_sync(0xffffffffu, off, r);
                         const bool there = (mask >> r) & 1u;
-                        const __nv_bfloat16 *at = there ? cache + from + c * 8 : cache;
+                        const T *at = there ? cache + from + c * N : cache;
                         if (c < (int)chunks) {
-                            copy16(to + r * PITCH + c * 16, at, there);
-                            copy16(to + (STEP + r) * PITCH + c * 16, there ? at + a.value_offset : cache, there);
+                            copy16(to + r * KP + c * 16, at, there);
+                            copy16(to + STEP * KP + r * VP + c * 16, there ? at + a.value_offset : cache, there);
                         }
                     }
                     if (step + 1 < steps) fetch_pages(step + 1);
@@ -514,7 +606,6 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
             }
             copy_commit();
         };
-        if (steps > 0) fetch_pages(0);
 #pragma unroll
         for (int k = 0; k < STAGES - 1; ++k) issue(k);
         for (int step = 0; step < steps; ++step) {
@@ -523,24 +614,63 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
             const uint32_t mask = sm_mask[warp][step % STAGES];  // the tokens that count
             issue(step + STAGES - 1);
             if (mask == 0) continue;
-            const uint32_t from = stages + (uint32_t)(step % STAGES) * STAGE_BYTES;
-            float c[NT][4];
+            const unsigned char *stage = mine + (step % STAGES) * S::STAGE;
+            const uint32_t from = stages + (uint32_t)(step % STAGES) * S::STAGE;
+            // scores, in several sums: so that a product does not wait for the one before it, and (f32) because the matrix units
+            // cut off what does not fit a sum, which would add up
+            float c[NT][4], c2[NT][4];
+            const uint32_t ka = from + (lane & 15) * KP + (lane >> 4) * 16;
+            if constexpr (F32) {
+                float odd = 0.f;
+                auto scores = [&](auto any) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
-            const uint32_t ka = from + (lane & 15) * PITCH + (lane >> 4) * 16;
+                    for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = c2[t][0] = c2[t][1] = c2[t][2] = c2[t][3] = 0.f;
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                uint32_t f[4];
-                load_matrices(f, ka + k * 32);
+                    for (int k0 = 0; k0 < QK; k0 += 2) {
+                        float big[NT][4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) multiply(c[t], f, qf[t][k][0], qf[t][k][1]);
+                        for (int t = 0; t < NT; ++t) big[t][0] = big[t][1] = big[t][2] = big[t][3] = 0.f;
+#pragma unroll
+                        for (int k = k0; k < k0 + 2; ++k) {
+                            uint32_t f[4], hi[4], lo[4], beside[4];
+                            load_matrices(f, ka + k * 32);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if constexpr (decltype(any)::value) halve_any(f[i], hi[i], lo[i], beside[i]);
+                                else halve(f[i], hi[i], lo[i], odd), beside[i] = hi[i];
+                            }
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                multiply_tf32(c2[t], lo, qf[t][k][0], qf[t][k][1]);
+                                multiply_tf32(big[t], hi, qf[t][k][0], qf[t][k][1]);
+                                multiply_tf32(c2[t], beside, qf[t][k][2], qf[t][k][3]);
+                            }
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) c[t][j] += big[t][j];
+                    }
+                };
+                scores(std::false_type());
+                if (__any_sync(0xffffffffu, odd != 0.f)) scores(std::true_type());
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = c2[t][0] = c2[t][1] = c2[t][2] = c2[t][3] = 0.f;
+#pragma unroll
+                for (int k = 0; k < QK; ++k) {
+                    uint32_t f[4];
+                    load_matrices(f, ka + k * 32);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) multiply(k & 1 ? c2[t] : c[t], f, qf[t][k][0], qf[t][k][1]);
+                }
             }
-            const bool in0 = (mask >> (lane >> 2)) & 1u, in1 = (mask >> ((lane >> 2) + 8)) & 1u;
-            uint32_t p_hi[NT][2], p_lo[NT][2];
+            const bool in0 = (mask >> eighth) & 1u, in1 = (mask >> (eighth + 8)) & 1u;
+            uint32_t p_hi[NT][F32 ? 4 : 2], p_lo[NT][F32 ? 4 : 2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) c[t][j] = (j < 2 ? in0 : in1) ? c[t][j] * a.scale : -INFINITY;
+                for (int j = 0; j < 4; ++j) c[t][j] = (j < 2 ? in0 : in1) ? (c[t][j] + c2[t][j]) * a.scale : -INFINITY;
                 float top0 = fmaxf(c[t][0], c[t][2]), top1 = fmaxf(c[t][1], c[t][3]);
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
@@ -555,7 +685,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
                     l[t][0] *= f0;
                     l[t][1] *= f1;
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) {
+                    for (int k = 0; k < MT; ++k) {
                         o[t][k][0] *= f0;
                         o[t][k][1] *= f1;
                         o[t][k][2] *= f0;
@@ -569,43 +699,91 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
                 c[t][3] = power2(c[t][3] - b1);
                 l[t][0] += c[t][0] + c[t][2];
                 l[t][1] += c[t][1] + c[t][3];
+                if constexpr (F32) {
+                    float *turn_p = sm_p[warp] + t * 128;  // [token][head]
+                    __syncwarp();
+                    *reinterpret_cast<float2 *>(turn_p + eighth * 8 + quad * 2) = make_float2(c[t][0], c[t][1]);
+                    *reinterpret_cast<float2 *>(turn_p + (eighth + 8) * 8 + quad * 2) = make_float2(c[t][2], c[t][3]);
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float x = c[t][2 * i], y = c[t][2 * i + 1];
-                    const uint32_t hi = pack_bf16(x, y);
-                    const uint32_t lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
-                    p_hi[t][i] = turned(hi);
-                    p_lo[t][i] = turned(lo);
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t finite;
+                        halve_any(__float_as_uint(turn_p[(quad + 4 * i) * 8 + eighth]), p_hi[t][i], p_lo[t][i], finite);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float x = c[t][2 * i], y = c[t][2 * i + 1];
+                        const uint32_t hi = pack_bf16(x, y);
+                        const uint32_t lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+                        p_hi[t][i] = turned(hi);
+                        p_lo[t][i] = turned(lo);
+                    }
                 }
             }
-            const uint32_t va = from + STEP * PITCH + ((lane & 7) + ((lane >> 4) & 1) * 8) * PITCH + ((lane >> 3) & 1) * 16;
+            if constexpr (F32) {
+                const float *v = reinterpret_cast<const float *>(stage + STEP * KP) + quad * (VP / 4) + eighth;
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                uint32_t f[4];
-                load_matrices_turned(f, va + k * 32);
+                for (int k = 0; k < MT; ++k) {
+                    float sum[NT][4], odd = 0.f;
+                    auto outputs = [&](auto any) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    multiply(o[t][k], f, p_hi[t][0], p_hi[t][1]);
-                    multiply(o[t][k], f, p_lo[t][0], p_lo[t][1]);
+                        for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = sum[t][2] = sum[t][3] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {  // eight tokens
+                            uint32_t hi[4], lo[4], beside[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x = __float_as_uint(v[(e * 8 + (i >> 1) * 4) * (VP / 4) + k * 16 + (i & 1) * 8]);
+                                if constexpr (decltype(any)::value) halve_any(x, hi[i], lo[i], beside[i]);
+                                else halve(x, hi[i], lo[i], odd), beside[i] = hi[i];
+                            }
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                multiply_tf32(sum[t], lo, p_hi[t][2 * e], p_hi[t][2 * e + 1]);
+                                multiply_tf32(sum[t], beside, p_lo[t][2 * e], p_lo[t][2 * e + 1]);
+                                multiply_tf32(sum[t], hi, p_hi[t][2 * e], p_hi[t][2 * e + 1]);
+                            }
+                        }
+                    };
+                    outputs(std::false_type());
+                    if (__any_sync(0xffffffffu, odd != 0.f)) outputs(std::true_type());
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[t][k][j] += sum[t][j];
+                }
+            } else {
+                const uint32_t va = from + STEP * KP + ((lane & 7) + ((lane >> 4) & 1) * 8) * VP + ((lane >> 3) & 1) * 16;
+#pragma unroll
+                for (int k = 0; k < MT; ++k) {
+                    uint32_t f[4];
+                    load_matrices_turned(f, va + k * 32);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        multiply(o[t][k], f, p_hi[t][0], p_hi[t][1]);
+                        multiply(o[t][k], f, p_lo[t][0], p_lo[t][1]);
+                    }
                 }
             }
         }
         // join the warps
         copy_wait<0>();
-        float *sm_o = reinterpret_cast<float *>(stage_mem);  // [4][HEADS][DP + 4]
+        float *sm_o = reinterpret_cast<float *>(stage_mem);  // [WARPS][HEADS][DP + 4]
+        static_assert(WARPS * HEADS * (DP + 4) * 4 <= S::BYTES, "the warps' outputs fit");
         __syncthreads();  // every warp is done with its stages
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int h = t * 8 + (lane & 3) * 2 + j;
+                const int h = t * 8 + quad * 2 + j;
                 float sum = l[t][j];
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
                 if (lane < 4) sm_m[warp][h] = m[t][j], sm_l[warp][h] = sum;
-                float *to = sm_o + (warp * HEADS + h) * (DP + 4) + (lane >> 2);
+                float *to = sm_o + (warp * HEADS + h) * (DP + 4) + eighth;
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
+                for (int k = 0; k < MT; ++k) {
                     to[k * 16] = o[t][k][j];
                     to[k * 16 + 8] = o[t][k][2 + j];
                 }
@@ -613,41 +791,56 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
         __syncthreads();
         const bool whole = w.t0 == 0 && w.t1 == w.tiles;
         float *slot = whole ? nullptr : part_of(a, blockIdx.x, s.idx != start);
-        for (int x = threadIdx.x; x < w.heads * (int)(a.dim / 2); x += THREADS) {
-            const int h = x / (int)(a.dim / 2), d = 2 * (x - h * (int)(a.dim / 2));
+        for (int x = threadIdx.x; x < w.heads * (int)(a.dim / 4); x += THREADS) {
+            const int h = x / (int)(a.dim / 4), d = 4 * (x - h * (int)(a.dim / 4));
             float mm = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mm = fmaxf(mm, sm_m[k][h]);
+            for (int k = 0; k < WARPS; ++k) mm = fmaxf(mm, sm_m[k][h]);
             const float base = mm == -INFINITY ? 0.f : mm;
-            float ll = 0.f, o0 = 0.f, o1 = 0.f;
+            float ll = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < WARPS; ++k) {
                 const float f = power2(sm_m[k][h] - base);
-                const float2 v = *reinterpret_cast<const float2 *>(sm_o + (k * HEADS + h) * (DP + 4) + d);
+                const float4 u = *reinterpret_cast<const float4 *>(sm_o + (k * HEADS + h) * (DP + 4) + d);
                 ll += sm_l[k][h] * f;
-                o0 += v.x * f;
-                o1 += v.y * f;
+                v.x += u.x * f;
+                v.y += u.y * f;
+                v.z += u.z * f;
+                v.w += u.w * f;
             }
             if (whole) {
-                *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d) = pack_bf16(quotient(o0, ll), quotient(o1, ll));
+                store4((T *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d, make_float4(quotient(v.x, ll), quotient(v.y, ll), quotient(v.z, ll), quotient(v.w, ll)));
             } else {
-                *reinterpret_cast<float2 *>(slot + h * a.dim + d) = make_float2(o0, o1);
+                *reinterpret_cast<float4 *>(slot + h * a.dim + d) = v;
                 if (d == 0) *reinterpret_cast<float2 *>(slot + HEADS * a.dim + 2 * h) = make_float2(mm, ll);
             }
         }
-        if (!whole) join_if_last<__nv_bfloat16, 4>(a, s, w, sm_o, &sm_l[0][0], found);
+        if (!whole) {
+            Parts parts;
+            if (last_of_parts(a, s, w, parts, &flag)) join_staged<T, HEADS, DP>(a, w, parts, sm_o, S::BYTES);
+        }
         __syncthreads();  // the next stretch's copies go where the parts were
     }
-    finish<__nv_bfloat16>(a);
+    finish<T>(a);
 }
 
 // A block of its own per (sequence, head block) when no sequence can hold more than a few tiles.
 bool split(const LtOperator &o) { return (uint64_t)o.table_width * o.page > 2 * TILE; }
 
-// Query heads per block of lt_attend_tensor: as many heads as share a key, while queries and
-// output fit the registers (32 heads of 128 values, 16 of 256).
-int tensor_width(uint32_t dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256; }
-int tensor_tiles(uint32_t dim, uint32_t group) { return group <= 8 ? 1 : group <= 16 || dim > 128 ? 2 : 4; }
+// lt_attend_tensor: widths it is built for (0: none), and query heads per block in eights -- as many as share a key, while
+// queries and output fit the registers.
+int tensor_width(int dtype, uint32_t dim) {
+    const int w = dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
+    if (dtype == LT_BF16) return dim % 8 == 0 ? w : 0;
+    return dim % 4 == 0 && w <= 192 ? w : 0;
+}
+int tensor_tiles(int dtype, int width, uint32_t group) {
+    if (group <= 8) return 1;
+    if (dtype == LT_F32) return width <= 64 ? 2 : 1;
+    return group <= 16 || width > 128 ? 2 : 4;
+}
+int element_size(int dtype) { return dtype == LT_BF16 ? 2 : 4; }
 constexpr int ANY_BLOCKS = 4;  // resident blocks per SM of lt_attend_any
 
 inline bool is_aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -659,30 +852,57 @@ cudaError_t launch_any(const AttendArgs &a, unsigned grid, cudaStream_t stream) 
     return launch_pdl(lt_attend_any<T, 8>, grid, THREADS, (size_t)0, stream, a);
 }
 
-template <int DP, int NT, bool WHOLE>
+template <class T, int DP, int NT, bool WHOLE>
 cudaError_t launch_tensor(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(lt_attend_tensor<DP, NT, WHOLE>, tensor_bytes<DP>(), ready);
+    constexpr size_t bytes = Shape<T, DP>::BYTES;
+    const cudaError_t e = allow_shared(lt_attend_tensor<T, DP, NT, WHOLE>, bytes, ready);
     if (e != cudaSuccess) return e;
-    return launch_pdl(lt_attend_tensor<DP, NT, WHOLE>, grid, THREADS, tensor_bytes<DP>(), stream, a);
+    return launch_pdl(lt_attend_tensor<T, DP, NT, WHOLE>, grid, THREADS, bytes, stream, a);
 }
 
-template <int DP>
+template <class T, int DP>
 cudaError_t launch_tensor_heads(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     const bool whole = a.page % STEP == 0;
-    if (a.block_heads == 8) return whole ? launch_tensor<DP, 1, true>(a, grid, stream) : launch_tensor<DP, 1, false>(a, grid, stream);
-    if (a.block_heads == 16) return whole ? launch_tensor<DP, 2, true>(a, grid, stream) : launch_tensor<DP, 2, false>(a, grid, stream);
-    if constexpr (DP <= 128) return whole ? launch_tensor<DP, 4, true>(a, grid, stream) : launch_tensor<DP, 4, false>(a, grid, stream);
+    if (a.block_heads == 8) return whole ? launch_tensor<T, DP, 1, true>(a, grid, stream) : launch_tensor<T, DP, 1, false>(a, grid, stream);
+    if constexpr (sizeof(T) == 2 || DP <= 64)
+        if (a.block_heads == 16) return whole ? launch_tensor<T, DP, 2, true>(a, grid, stream) : launch_tensor<T, DP, 2, false>(a, grid, stream);
+    if constexpr (sizeof(T) == 2 && DP <= 128)
+        if (a.block_heads == 32) return whole ? launch_tensor<T, DP, 4, true>(a, grid, stream) : launch_tensor<T, DP, 4, false>(a, grid, stream);
     return cudaErrorInvalidValue;
+}
+
+template <class T>
+cudaError_t launch_tensor_width(const AttendArgs &a, int width, unsigned grid, cudaStream_t stream) {
+    switch (width) {
+    case 64: return launch_tensor_heads<T, 64>(a, grid, stream);
+    case 96: return launch_tensor_heads<T, 96>(a, grid, stream);
+    case 128: return launch_tensor_heads<T, 128>(a, grid, stream);
+    case 192: return launch_tensor_heads<T, 192>(a, grid, stream);
+    default:
+        if constexpr (sizeof(T) == 2) return launch_tensor_heads<T, 256>(a, grid, stream);
+        return cudaErrorInvalidValue;
+    }
+}
+
+// blocks of a launch that splits sequences: what the SMs hold, and what the counters suffice for
+unsigned split_blocks(int sm_count, int per_sm) {
+    const unsigned n = (unsigned)sm_count * (unsigned)per_sm;
+    return n < LT_ARRIVALS ? n : LT_ARRIVALS;
 }
 
 }  // namespace
 
 size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count) {
     if (!split(o)) return 0;
-    const size_t any = (size_t)ANY_BLOCKS * ANY_HEADS, tiles = (size_t)tensor_tiles(o.dim, o.heads / o.kv_heads),
-                 tensor = (size_t)tensor_blocks(tensor_width(o.dim), (int)tiles) * 8 * tiles;
-    return 2 * (size_t)sm_count * (any > tensor ? any : tensor) * (o.dim + 2) * sizeof(float);
+    // (whether the addresses are aligned is not known yet: room for either kernel)
+    const size_t any = (size_t)split_blocks(sm_count, ANY_BLOCKS) * ANY_HEADS;
+    size_t tensor = 0;
+    if (const int width = tensor_width(o.dtype, o.dim)) {
+        const int tiles = tensor_tiles(o.dtype, width, o.heads / o.kv_heads);
+        tensor = (size_t)split_blocks(sm_count, tensor_blocks(element_size(o.dtype), width, tiles)) * 8 * tiles;
+    }
+    return 2 * (any > tensor ? any : tensor) * (o.dim + 2) * sizeof(float);
 }
 
 cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream) {
@@ -709,22 +929,12 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     a.page = o.page;
     a.table_width = o.table_width;
     a.scale = (float)(lt_attr_double(o.attr[1]) * 1.4426950408889634);
-    const bool tensor = o.dtype == LT_BF16 && o.dim % 8 == 0 && is_aligned(a.cache, 16) && is_aligned(a.q, 4) && a.q_pitch % 2 == 0 && is_aligned(a.out, 4);
-    a.block_heads = tensor ? 8 * tensor_tiles(o.dim, a.group) : ANY_HEADS;
+    const int width = tensor_width(o.dtype, o.dim);
+    const bool tensor = width && is_aligned(a.cache, 16) && is_aligned(a.q, 4) && (o.dtype == LT_F32 || a.q_pitch % 2 == 0) && is_aligned(a.out, 16);
+    const int tiles = tensor ? tensor_tiles(o.dtype, width, a.group) : ANY_HEADS / 8;
+    a.block_heads = 8 * tiles;
     a.head_blocks = (a.group + a.block_heads - 1) / a.block_heads;
-    const unsigned per = a.kv_heads * a.head_blocks;
-    const unsigned grid = a.partial ? (unsigned)sm_count * (tensor ? tensor_blocks(tensor_width(o.dim), (int)a.block_heads / 8) : ANY_BLOCKS) : a.batch * per;
-    cudaError_t e;
-    if (!tensor) {
-        e = o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
-    } else {
-        switch (tensor_width(o.dim)) {
-        case 64: e = launch_tensor_heads<64>(a, grid, stream); break;
-        case 96: e = launch_tensor_heads<96>(a, grid, stream); break;
-        case 128: e = launch_tensor_heads<128>(a, grid, stream); break;
-        case 192: e = launch_tensor_heads<192>(a, grid, stream); break;
-        default: e = launch_tensor_heads<256>(a, grid, stream); break;
-        }
-    }
-    return e;
+    const unsigned grid = !a.partial ? a.batch * a.kv_heads * a.head_blocks : split_blocks(sm_count, tensor ? tensor_blocks(element_size(o.dtype), width, tiles) : ANY_BLOCKS);
+    if (tensor) return o.dtype == LT_BF16 ? launch_tensor_width<__nv_bfloat16>(a, width, grid, stream) : launch_tensor_width<float>(a, width, grid, stream);
+    return o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
 }
