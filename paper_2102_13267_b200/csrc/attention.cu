@@ -10,8 +10,6 @@
 // (sequence, head block) that lies within one block's part is finished there.  One that is spread over several leaves
 // partial results (maximum, sum, unnormalised output) in scratch memory, and the block that arrives last joins them,
 // always in the list's order, so results do not depend on the arrival.
-#include <type_traits>
-
 #include "operator_device.cuh"
 
 using namespace ltop;
@@ -146,7 +144,9 @@ __device__ __forceinline__ bool next_stretch(const AttendArgs &a, Share &s, Stre
 __device__ __forceinline__ float quotient(float o, float l) { return l > 0.f ? o / l : l == 0.f ? 0.f : l; }
 
 // Where a block leaves its parts: of the first or the second stretch that it does not finish.
-__device__ __forceinline__ uint64_t part_floats(const AttendArgs &a) { return (uint64_t)a.block_heads * (a.dim + 2); }
+// (an even number of heads each, so that parts of four-value rows start on 16 bytes)
+__host__ __device__ constexpr int part_heads(int heads) { return heads + (heads & 1); }
+__device__ __forceinline__ uint64_t part_floats(const AttendArgs &a) { return (uint64_t)part_heads((int)a.block_heads) * (a.dim + 2); }
 __device__ __forceinline__ float *part_of(const AttendArgs &a, uint32_t block, bool second) { return a.partial + (2 * (uint64_t)block + (second ? 1 : 0)) * part_floats(a); }
 
 // The parts of a stretch's (sequence, head block), in order.
@@ -234,8 +234,9 @@ __device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &
     constexpr int MINE = (HEADS * WIDTH / 4 + THREADS - 1) / THREADS;  // groups of four values of a thread
     const uint32_t dim = a.dim, quads = (uint32_t)w.heads * dim / 4;
     float *weights = mem, *sums = weights + HEADS * MOST_PARTS;       // [HEADS][MOST_PARTS], [HEADS]
-    float4 *staged = reinterpret_cast<float4 *>(sums + HEADS);
-    const uint32_t room = (bytes - (HEADS * MOST_PARTS + HEADS) * 4) / (quads * 16);
+    constexpr int PADDED = (HEADS + 3) / 4 * 4;
+    float4 *staged = reinterpret_cast<float4 *>(sums + PADDED);
+    const uint32_t room = (bytes - (HEADS * MOST_PARTS + PADDED) * 4) / (quads * 16);
     float4 acc[MINE];
 #pragma unroll
     for (int k = 0; k < MINE; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -433,29 +434,6 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void multiply_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// x as two numbers of 11 significant bits that the matrix units take: what is left out is below 2^-21 of x.  `odd` becomes a
-// NaN when x is one, or an infinity, or rounds to one: then the small part is useless, see halve_any.
-__device__ __forceinline__ void halve(uint32_t x, uint32_t &hi, uint32_t &lo, float &odd) {
-    hi = (x + 0x1000u) & 0xffffe000u;
-    const float rest = __uint_as_float(x) - __uint_as_float(hi);
-    lo = __float_as_uint(rest);
-    odd = fmaf(rest, 0.f, odd);
-}
-// The same for any x: an infinity or a NaN is all in hi, and `finite` is hi without it: what stands beside the other
-// factor's small part, whose sign says nothing.
-__device__ __forceinline__ void halve_any(uint32_t x, uint32_t &hi, uint32_t &lo, uint32_t &finite) {
-    hi = (x + 0x1000u) & 0xffffe000u;
-    const float rest = __uint_as_float(x) - __uint_as_float(hi);
-    const bool fine = fabsf(rest) <= 3.402823466e38f;
-    lo = fine ? __float_as_uint(rest) : 0u;
-    if (!fine) hi = x & 0xffffe000u;
-    finite = fine ? hi : 0u;
-}
 __device__ __forceinline__ float power2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -464,209 +442,338 @@ __device__ __forceinline__ float power2(float x) {
 
 constexpr int STEP = 16;        // tokens a warp takes at a time: a quarter of a tile
 
-// Sizes of the kernel for heads of up to DP values, NT x 8 query heads per block.
+// Sizes of the kernels for heads of up to DP values.  Rows of keys and values in shared memory are padded so that what is
+// read at once falls into different banks: eight rows of a matrix (bf16), four tokens by two chunks (f32).
 template <class T, int DP>
 struct Shape {
-    static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int CHUNKS = DP * (int)sizeof(T) / 16;
-    // rows of keys and values in shared memory, in bytes: padded so that what a matrix load touches falls into different banks
-    static constexpr int K_PITCH = DP * (int)sizeof(T) + 16, V_PITCH = F32 ? DP * 4 + 32 : K_PITCH;
-    static constexpr int STAGE = STEP * (K_PITCH + V_PITCH);
-    static constexpr int STAGES = F32 && DP > 128 ? 2 : 3;
+    static constexpr int PITCH = DP * (int)sizeof(T) + (sizeof(T) == 4 ? 32 : 16);
+    static constexpr int STAGE = 2 * STEP * PITCH;
+    static constexpr int STAGES = sizeof(T) == 2 ? 3 : DP == 64 ? 2 : DP == 128 ? 3 : DP == 192 ? 2 : 1;
     static constexpr int BYTES = WARPS * STAGES * STAGE;
 };
 // Resident blocks per SM: what the stages leave room for, fewer where many heads of 64 values take the registers.
-__host__ __device__ constexpr int tensor_blocks(int size, int width, int tiles) {
-    return size == 4 ? (width <= 64 ? 2 : 1) : width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1;
+__host__ __device__ constexpr int tensor_blocks(int width, int tiles) { return width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1; }
+__host__ __device__ constexpr int single_blocks(int width, int heads) { return width <= 64 ? (heads <= 4 ? 3 : 2) : 1; }
+
+// A warp's copies of one stretch: steps of STEP tokens, every WARPS-th of the stretch's quarter tiles, into its stages.
+//
+// Page numbers are fetched ahead of the copies they address.  Where a step never crosses a page (WHOLE_STEPS) one number
+// serves a step, and the lanes hold those of the next 32 steps; otherwise lane i has the number of token i.
+template <class T, int DP, bool WHOLE_STEPS>
+struct Stages {
+    using S = Shape<T, DP>;
+    static constexpr int N = 16 / (int)sizeof(T);
+    const AttendArgs &a;
+    const Stretch &w;
+    const int *row;
+    unsigned char *mine;
+    uint32_t at, *masks;        // shared address of the stages; which tokens of the step in a stage count
+    int lane, first, steps, ahead;
+
+    __device__ __forceinline__ Stages(const AttendArgs &a_, const Stretch &w_, unsigned char *mine_, uint32_t *masks_)
+        : a(a_), w(w_), row(a_.table + (uint64_t)w_.b * a_.table_width), mine(mine_), at(shared_address(mine_)), masks(masks_), lane(threadIdx.x & 31),
+          first((int)(w_.t0 * TILE) + (int)(threadIdx.x >> 5) * STEP), steps((int)(w_.t1 - w_.t0)), ahead(-1) {
+        fetch_pages(0);
+    }
+    __device__ __forceinline__ void fetch_pages(int step) {
+        const int i = WHOLE_STEPS ? first + (step + lane) * TILE : first + step * TILE + (lane & 15);
+        ahead = i < w.n ? row[(uint32_t)i / a.page] : -2;
+    }
+    // columns from dim to DP stay zero (the memory is also used to join warps)
+    __device__ __forceinline__ void clear_rest() {
+        const int chunks = (int)a.dim / N, rest = S::CHUNKS - chunks;
+        if (rest == 0) return;
+        for (int x = lane; x < S::STAGES * 2 * STEP * rest; x += 32) {
+            const int r = x / rest, c = x - r * rest;
+            *reinterpret_cast<uint4 *>(mine + r * S::PITCH + (chunks + c) * 16) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    // The copies of a step, committed as one group (an empty one behind the last step).
+    __device__ __forceinline__ void issue(int step) {
+        const T *cache = (const T *)a.cache;
+        const int chunks = (int)a.dim / N;
+        if (step < steps) {
+            const uint32_t to = at + (uint32_t)(step % S::STAGES) * S::STAGE;
+            const int i0 = first + step * TILE, left = w.n - i0;
+            uint32_t mask = left >= STEP ? 0xffffu : left <= 0 ? 0u : (1u << left) - 1u;
+            if (WHOLE_STEPS) {
+                if (step > 0 && (step & 31) == 0) fetch_pages(step);
+                const int p = __shfl_sync(0xffffffffu, ahead, step & 31);
+                if (mask && (uint32_t)p >= a.pages) {
+                    mask = 0;
+                    atomicOr(a.status, 1u);
+                }
+                const uint32_t off = (uint32_t)i0 % a.page;
+                const T *src = cache + (mask ? (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)w.kv * a.head_stride : 0);
+#pragma unroll
+                for (int x = 0; x < STEP * S::CHUNKS; x += 32) {
+                    const int r = (x + lane) / S::CHUNKS, c = (x + lane) % S::CHUNKS;
+                    const bool there = (mask >> r) & 1u;
+                    const T *from = there ? src + (uint64_t)r * a.token_stride + c * N : cache;
+                    if (c < chunks) {
+                        copy16(to + r * S::PITCH + c * 16, from, there);
+                        copy16(to + (STEP + r) * S::PITCH + c * 16, there ? from + a.value_offset : cache, there);
+                    }
+                }
+            } else {
+                const int i = i0 + (lane & 15), p = ahead;
+                const bool known = i < w.n && (uint32_t)p < a.pages;
+                if (i < w.n && !known) atomicOr(a.status, 1u);
+                mask = __ballot_sync(0xffffffffu, known) & 0xffffu;
+                const uint64_t off = known ? (uint64_t)p * a.page_stride + (uint64_t)((uint32_t)i % a.page) * a.token_stride + (uint64_t)w.kv * a.head_stride : 0;
+#pragma unroll
+                for (int x = 0; x < STEP * S::CHUNKS; x += 32) {
+                    const int r = (x + lane) / S::CHUNKS, c = (x + lane) % S::CHUNKS;
+                    const uint64_t o = __shfl_sync(0xffffffffu, off, r);
+                    const bool there = (mask >> r) & 1u;
+                    const T *from = there ? cache + o + c * N : cache;
+                    if (c < chunks) {
+                        copy16(to + r * S::PITCH + c * 16, from, there);
+                        copy16(to + (STEP + r) * S::PITCH + c * 16, there ? from + a.value_offset : cache, there);
+                    }
+                }
+                if (step + 1 < steps) fetch_pages(step + 1);
+            }
+            if (lane == 0) masks[step % S::STAGES] = mask;
+        }
+        copy_commit();
+    }
+};
+
+// Joins the warps' outputs in `sm_o` [WARPS][HEADS][DP + 4], with their maxima and sums, into the result or a part; then,
+// if the block's part was the last one, the parts.
+template <class T, int HEADS, int DP>
+__device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &s, const Stretch &w, bool first_stretch, float *sm_o, const float (*sm_m)[HEADS],
+                                              const float (*sm_l)[HEADS], uint32_t bytes, uint32_t *flag) {
+    const bool whole = w.t0 == 0 && w.t1 == w.tiles;
+    float *slot = whole ? nullptr : part_of(a, blockIdx.x, !first_stretch);
+    for (int x = threadIdx.x; x < w.heads * (int)(a.dim / 4); x += THREADS) {
+        const int h = x / (int)(a.dim / 4), d = 4 * (x - h * (int)(a.dim / 4));
+        float mm = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) mm = fmaxf(mm, sm_m[k][h]);
+        const float base = mm == -INFINITY ? 0.f : mm;
+        float ll = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {
+            const float f = exp2f(sm_m[k][h] - base);
+            const float4 u = *reinterpret_cast<const float4 *>(sm_o + (k * HEADS + h) * (DP + 4) + d);
+            ll += sm_l[k][h] * f;
+            v.x += u.x * f;
+            v.y += u.y * f;
+            v.z += u.z * f;
+            v.w += u.w * f;
+        }
+        if (whole) {
+            store4((T *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d, make_float4(quotient(v.x, ll), quotient(v.y, ll), quotient(v.z, ll), quotient(v.w, ll)));
+        } else {
+            *reinterpret_cast<float4 *>(slot + h * a.dim + d) = v;
+            if (d == 0) *reinterpret_cast<float2 *>(slot + a.block_heads * a.dim + 2 * h) = make_float2(mm, ll);
+        }
+    }
+    if (!whole) {
+        Parts parts;
+        if (last_of_parts(a, s, w, parts, flag)) join_staged<T, HEADS, DP>(a, w, parts, sm_o, bytes);
+    }
+    __syncthreads();  // the next stretch's copies go where the parts were
 }
 
-// bf16 and f32, 16-byte aligned rows, head sizes filled up to DP with zeros; NT x 8 query heads per block.
+// f32, 16-byte aligned rows, head sizes filled up to DP with zeros; up to NH query heads per block.
 //
-// The few query heads make the narrow side of the products: scores are K (16 tokens x dims) times q^T (dims x 8 heads),
-// the output is V^T (16 dims x 16 tokens) times the weights (16 tokens x 8 heads), so no matrix row is wasted on
-// padding of the group to 16.  Each warp has steps and a copy pipeline of its own -- no barrier in the loop -- and its own
-// running maximum and sum; warps are joined once per stretch.
-//   bf16: the weights leave the first product with tokens along the rows and enter the second with tokens along the
-//   columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps the
-//   weights to 2^-17 and costs one more product.
-//   f32: every factor as two tf32 parts, three products each (all but the one of the two small parts); the weights are
-//   turned through 512 bytes of shared memory.  (Infinities in keys and values come out as they should; one in q gives a NaN.)
-template <class T, int DP, int NT, bool WHOLE_STEPS>
-__global__ void __launch_bounds__(THREADS, tensor_blocks(sizeof(T), DP, NT)) lt_attend_tensor(const AttendArgs a) {
-    using S = Shape<T, DP>;
-    constexpr bool F32 = S::F32;
-    constexpr int HEADS = 8 * NT, N = 16 / (int)sizeof(T), CHUNKS = S::CHUNKS, STAGES = S::STAGES, KP = S::K_PITCH, VP = S::V_PITCH;
-    constexpr int MT = DP / 16, QK = F32 ? DP / 8 : DP / 16, QR = F32 ? 4 : 2;  // output tiles; steps of the first product and registers of q in each
+// Full binary32 products rule the matrix units out (in two tf32 parts each, taking the numbers apart cost more than these
+// products: 40 us against 30 on 16 sequences of 16 heads of 64 values), and memory is slow enough for the others.  Two
+// lanes share a token's key, every other chunk each; the weights go through shared memory to all lanes, which have the
+// output's values between them, two neighbouring ones of every 64.  Warps, stages and joins as in lt_attend_tensor.
+template <int DP, int NH, bool WHOLE_STEPS>
+__global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_single(const AttendArgs a) {
+    using S = Shape<float, DP>;
+    constexpr int J = DP / 64;
     extern __shared__ __align__(128) unsigned char stage_mem[];
     __shared__ uint32_t flag;
-    __shared__ float sm_m[WARPS][HEADS], sm_l[WARPS][HEADS];
-    __shared__ uint32_t sm_mask[WARPS][STAGES];
-    __shared__ __align__(16) float sm_p[F32 ? WARPS : 1][F32 ? NT * 128 : 1];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, eighth = lane >> 2;
-    const uint32_t chunks = a.dim / N;
-    unsigned char *mine = stage_mem + warp * STAGES * S::STAGE;
-    const uint32_t stages = shared_address(mine);
-    const T *q = (const T *)a.q, *cache = (const T *)a.cache;
+    __shared__ float sm_m[WARPS][NH], sm_l[WARPS][NH];
+    __shared__ uint32_t sm_mask[WARPS][S::STAGES];
+    __shared__ __align__(16) float sm_p[WARPS][NH][STEP], sm_q[NH][DP];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, token = lane >> 1, half = lane & 1;
+    unsigned char *mine = stage_mem + warp * S::STAGES * S::STAGE;
     pdl_release();
     pdl_wait();
     Share s = my_share(a);
     const uint32_t start = s.idx;
     Stretch w;
     for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
-        const int *row = a.table + (uint64_t)w.b * a.table_width;
-        const int first = (int)(w.t0 * TILE) + warp * STEP;  // first token of this warp's first step
-        const int steps = (int)(w.t1 - w.t0);
+        Stages<float, DP, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
+        for (int x = threadIdx.x; x < NH * DP; x += THREADS) {  // (the stretch before has ended with a barrier)
+            const int h = x / DP, d = x % DP;
+            sm_q[h][d] = h < w.heads && d < (int)a.dim ? ((const float *)a.q)[(uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim + d] * a.scale : 0.f;
+        }
+        stages.clear_rest();
+        float o[NH][J][2], m[NH], l[NH];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            m[h] = -INFINITY;
+            l[h] = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[h][j][0] = o[h][j][1] = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < S::STAGES; ++k) stages.issue(k);
+        __syncthreads();  // q is there
+        for (int step = 0; step < stages.steps; ++step) {
+            copy_wait<S::STAGES - 1>();
+            __syncwarp();  // the step's copies of all lanes are there
+            const uint32_t mask = stages.masks[step % S::STAGES];  // the tokens that count
+            if (mask) {
+                const unsigned char *stage = mine + (step % S::STAGES) * S::STAGE;
+                float c[NH];
+#pragma unroll
+                for (int h = 0; h < NH; ++h) c[h] = 0.f;
+                const float4 *key = reinterpret_cast<const float4 *>(stage + token * S::PITCH) + half;
+                const float4 *query = reinterpret_cast<const float4 *>(&sm_q[0][0]) + half;
+#pragma unroll 8
+                for (int k = 0; k < DP / 8; ++k) {
+                    const float4 x = key[2 * k];
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) {
+                        const float4 y = query[h * (DP / 4) + 2 * k];
+                        c[h] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, c[h]))));
+                    }
+                }
+                const bool in = (mask >> token) & 1u;
+#pragma unroll
+                for (int h = 0; h < NH; ++h) {
+                    float v = c[h] + __shfl_xor_sync(0xffffffffu, c[h], 1);
+                    v = in ? v : -INFINITY;
+                    float top = v;
+#pragma unroll
+                    for (int d = 2; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    if (top > m[h]) {  // (the same in all lanes)
+                        const float f = exp2f(m[h] - top);
+                        m[h] = top;
+                        l[h] *= f;
+#pragma unroll
+                        for (int j = 0; j < J; ++j) {
+                            o[h][j][0] *= f;
+                            o[h][j][1] *= f;
+                        }
+                    }
+                    const float p = exp2f(v - (m[h] == -INFINITY ? 0.f : m[h]));
+                    l[h] += p;  // (twice, once in each of the token's lanes)
+                    if (half == 0) sm_p[warp][h][token] = p;
+                }
+                __syncwarp();
+                const float2 *value = reinterpret_cast<const float2 *>(stage + STEP * S::PITCH) + lane;
+#pragma unroll
+                for (int t0 = 0; t0 < STEP; t0 += 4) {
+                    float4 p[NH];
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) p[h] = *reinterpret_cast<const float4 *>(&sm_p[warp][h][t0]);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int j = 0; j < J; ++j) {
+                            const float2 v = value[(t0 + t) * (S::PITCH / 8) + j * 32];
+#pragma unroll
+                            for (int h = 0; h < NH; ++h) {
+                                const float f = t == 0 ? p[h].x : t == 1 ? p[h].y : t == 2 ? p[h].z : p[h].w;
+                                o[h][j][0] = fmaf(f, v.x, o[h][j][0]);
+                                o[h][j][1] = fmaf(f, v.y, o[h][j][1]);
+                            }
+                        }
+                }
+            }
+            __syncwarp();  // everybody is done with the stage, and with the weights
+            stages.issue(step + S::STAGES);
+        }
+        copy_wait<0>();
+        float *sm_o = reinterpret_cast<float *>(stage_mem);  // [WARPS][NH][DP + 4]
+        static_assert(WARPS * NH * (DP + 4) * 4 <= S::BYTES, "the warps' outputs fit");
+        __syncthreads();  // every warp is done with its stages
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const float sum = warp_sum(l[h]) * 0.5f;
+            if (lane == 0) sm_m[warp][h] = m[h], sm_l[warp][h] = sum;
+#pragma unroll
+            for (int j = 0; j < J; ++j) *reinterpret_cast<float2 *>(sm_o + (warp * NH + h) * (DP + 4) + j * 64 + lane * 2) = make_float2(o[h][j][0], o[h][j][1]);
+        }
+        __syncthreads();
+        leave_stretch<float, NH, DP>(a, s, w, s.idx == start, sm_o, sm_m, sm_l, S::BYTES, &flag);
+    }
+    finish<float>(a);
+}
 
-        // Page numbers are fetched ahead of the copies they address.  Where a step never crosses a page (WHOLE_STEPS) one
-        // number serves a step, and the lanes hold those of the next 32 steps; otherwise lane i has the number of token i.
-        int ahead = -1;
-        auto fetch_pages = [&](int step) {
-            const int i = WHOLE_STEPS ? first + (step + lane) * TILE : first + step * TILE + (lane & 15);
-            ahead = i < w.n ? row[(uint32_t)i / a.page] : -2;
-        };
-        fetch_pages(0);
-        uint32_t qf[NT][QK][QR];
+// bf16, 16-byte aligned rows, head sizes filled up to DP with zeros; NT x 8 query heads per block.
+//
+// The few query heads make the narrow side of the products: scores are K (16 tokens x dims) times q^T (dims x 8 heads),
+// the output is V^T (16 dims x 16 tokens) times the weights (16 tokens x 8 heads), so no matrix row is wasted on
+// padding of the group to 16.  The weights leave the first product with tokens along the rows and enter the second with
+// tokens along the columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps
+// the weights to 2^-17 and costs one more product.  Each warp has steps and a copy pipeline of its own -- no barrier
+// in the loop -- and its own running maximum and sum; warps are joined once per stretch.
+template <int DP, int NT, bool WHOLE_STEPS>
+__global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tensor(const AttendArgs a) {
+    using S = Shape<__nv_bfloat16, DP>;
+    constexpr int HEADS = 8 * NT, STAGES = S::STAGES, KS = DP / 16;
+    extern __shared__ __align__(128) unsigned char stage_mem[];
+    __shared__ uint32_t flag;
+    __shared__ float sm_m[WARPS][HEADS], sm_l[WARPS][HEADS];
+    __shared__ uint32_t sm_mask[WARPS][STAGES];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, eighth = lane >> 2;
+    unsigned char *mine = stage_mem + warp * STAGES * S::STAGE;
+    const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q;
+    pdl_release();
+    pdl_wait();
+    Share s = my_share(a);
+    const uint32_t start = s.idx;
+    Stretch w;
+    for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
+        Stages<__nv_bfloat16, DP, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
+        uint32_t qf[NT][KS][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int h = t * 8 + eighth;
-            const T *from = q + (uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim;
+            const __nv_bfloat16 *from = q + (uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim;
 #pragma unroll
-            for (int k = 0; k < QK; ++k)
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if constexpr (F32) {
-                        const uint32_t d = k * 8 + i * 4 + quad;
-                        uint32_t finite;
-                        halve_any(h < w.heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(from + d) : 0u, qf[t][k][i], qf[t][k][2 + i], finite);
-                    } else {
-                        const uint32_t d = k * 16 + i * 8 + quad * 2;
-                        qf[t][k][i] = h < w.heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(from + d) : 0u;
-                    }
+                    const uint32_t d = k * 16 + i * 8 + quad * 2;
+                    qf[t][k][i] = h < w.heads && d < a.dim ? *reinterpret_cast<const uint32_t *>(from + d) : 0u;
                 }
         }
-        // columns from dim to DP stay zero (the memory is also used to join warps)
-        if (chunks < CHUNKS)
-            for (int x = lane; x < STAGES * 2 * STEP * (CHUNKS - (int)chunks); x += 32) {
-                const int r = x / (CHUNKS - (int)chunks), c = x - r * (CHUNKS - (int)chunks), stage = r / (2 * STEP), i = r % (2 * STEP);
-                *reinterpret_cast<uint4 *>(mine + stage * S::STAGE + (i < STEP ? i * KP : STEP * KP + (i - STEP) * VP) + (chunks + c) * 16) = make_uint4(0, 0, 0, 0);
-            }
-        float o[NT][MT][4], m[NT][2], l[NT][2];
+        stages.clear_rest();
+        float o[NT][KS][4], m[NT][2], l[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             m[t][0] = m[t][1] = -INFINITY;
             l[t][0] = l[t][1] = 0.f;
 #pragma unroll
-            for (int k = 0; k < MT; ++k) o[t][k][0] = o[t][k][1] = o[t][k][2] = o[t][k][3] = 0.f;
+            for (int k = 0; k < KS; ++k) o[t][k][0] = o[t][k][1] = o[t][k][2] = o[t][k][3] = 0.f;
         }
-
-        auto issue = [&](int step) {
-            if (step < steps) {
-                const uint32_t to = stages + (uint32_t)(step % STAGES) * S::STAGE;
-                const int i0 = first + step * TILE, left = w.n - i0;
-                uint32_t mask = left >= STEP ? 0xffffu : left <= 0 ? 0u : (1u << left) - 1u;
-                if (WHOLE_STEPS) {
-                    if (step > 0 && (step & 31) == 0) fetch_pages(step);
-                    const int p = __shfl_sync(0xffffffffu, ahead, step & 31);
-                    if (mask && (uint32_t)p >= a.pages) {
-                        mask = 0;
-                        atomicOr(a.status, 1u);
-                    }
-                    const uint32_t off = (uint32_t)i0 % a.page;
-                    const T *src = cache + (mask ? (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)w.kv * a.head_stride : 0);
 #pragma unroll
-                    for (int x = 0; x < STEP * CHUNKS; x += 32) {
-                        const int r = (x + lane) / CHUNKS, c = (x + lane) % CHUNKS;
-                        const bool there = (mask >> r) & 1u;
-                        const T *at = there ? src + (uint64_t)r * a.token_stride + c * N : cache;
-                        if (c < (int)chunks) {
-                            copy16(to + r * KP + c * 16, at, there);
-                            copy16(to + STEP * KP + r * VP + c * 16, there ? at + a.value_offset : cache, there);
-                        }
-                    }
-                } else {
-                    const int i = i0 + (lane & 15), p = ahead;
-                    const bool known = i < w.n && (uint32_t)p < a.pages;
-                    if (i < w.n && !known) atomicOr(a.status, 1u);
-                    mask = __ballot_sync(0xffffffffu, known) & 0xffffu;
-                    const uint64_t off = known ? (uint64_t)p * a.page_stride + (uint64_t)((uint32_t)i % a.page) * a.token_stride + (uint64_t)w.kv * a.head_stride : 0;
-#pragma unroll
-                    for (int x = 0; x < STEP * CHUNKS; x += 32) {
-                        const int r = (x + lane) / CHUNKS, c = (x + lane) % CHUNKS;
-                        const uint64_t from = __shfl_sync(0xffffffffu, off, r);
-                        const bool there = (mask >> r) & 1u;
-                        const T *at = there ? cache + from + c * N : cache;
-                        if (c < (int)chunks) {
-                            copy16(to + r * KP + c * 16, at, there);
-                            copy16(to + STEP * KP + r * VP + c * 16, there ? at + a.value_offset : cache, there);
-                        }
-                    }
-                    if (step + 1 < steps) fetch_pages(step + 1);
-                }
-                if (lane == 0) sm_mask[warp][step % STAGES] = mask;
-            }
-            copy_commit();
-        };
-#pragma unroll
-        for (int k = 0; k < STAGES - 1; ++k) issue(k);
-        for (int step = 0; step < steps; ++step) {
+        for (int k = 0; k < STAGES - 1; ++k) stages.issue(k);
+        for (int step = 0; step < stages.steps; ++step) {
             copy_wait<STAGES - 2>();
             __syncwarp();  // the step's copies of all lanes are there, and everybody is done with the stage that the next ones fill
-            const uint32_t mask = sm_mask[warp][step % STAGES];  // the tokens that count
-            issue(step + STAGES - 1);
+            const uint32_t mask = stages.masks[step % STAGES];  // the tokens that count
+            stages.issue(step + STAGES - 1);
             if (mask == 0) continue;
-            const unsigned char *stage = mine + (step % STAGES) * S::STAGE;
-            const uint32_t from = stages + (uint32_t)(step % STAGES) * S::STAGE;
-            // scores, in several sums: so that a product does not wait for the one before it, and (f32) because the matrix units
-            // cut off what does not fit a sum, which would add up
+            const uint32_t from = stages.at + (uint32_t)(step % STAGES) * S::STAGE;
+            // scores, in two sums, so that a product does not wait for the one before it
             float c[NT][4], c2[NT][4];
-            const uint32_t ka = from + (lane & 15) * KP + (lane >> 4) * 16;
-            if constexpr (F32) {
-                float odd = 0.f;
-                auto scores = [&](auto any) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = c2[t][0] = c2[t][1] = c2[t][2] = c2[t][3] = 0.f;
+            for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = c2[t][0] = c2[t][1] = c2[t][2] = c2[t][3] = 0.f;
+            const uint32_t ka = from + (lane & 15) * S::PITCH + (lane >> 4) * 16;
 #pragma unroll
-                    for (int k0 = 0; k0 < QK; k0 += 2) {
-                        float big[NT][4];
+            for (int k = 0; k < KS; ++k) {
+                uint32_t f[4];
+                load_matrices(f, ka + k * 32);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) big[t][0] = big[t][1] = big[t][2] = big[t][3] = 0.f;
-#pragma unroll
-                        for (int k = k0; k < k0 + 2; ++k) {
-                            uint32_t f[4], hi[4], lo[4], beside[4];
-                            load_matrices(f, ka + k * 32);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if constexpr (decltype(any)::value) halve_any(f[i], hi[i], lo[i], beside[i]);
-                                else halve(f[i], hi[i], lo[i], odd), beside[i] = hi[i];
-                            }
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                multiply_tf32(c2[t], lo, qf[t][k][0], qf[t][k][1]);
-                                multiply_tf32(big[t], hi, qf[t][k][0], qf[t][k][1]);
-                                multiply_tf32(c2[t], beside, qf[t][k][2], qf[t][k][3]);
-                            }
-                        }
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) c[t][j] += big[t][j];
-                    }
-                };
-                scores(std::false_type());
-                if (__any_sync(0xffffffffu, odd != 0.f)) scores(std::true_type());
-            } else {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = c2[t][0] = c2[t][1] = c2[t][2] = c2[t][3] = 0.f;
-#pragma unroll
-                for (int k = 0; k < QK; ++k) {
-                    uint32_t f[4];
-                    load_matrices(f, ka + k * 32);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) multiply(k & 1 ? c2[t] : c[t], f, qf[t][k][0], qf[t][k][1]);
-                }
+                for (int t = 0; t < NT; ++t) multiply(k & 1 ? c2[t] : c[t], f, qf[t][k][0], qf[t][k][1]);
             }
             const bool in0 = (mask >> eighth) & 1u, in1 = (mask >> (eighth + 8)) & 1u;
-            uint32_t p_hi[NT][F32 ? 4 : 2], p_lo[NT][F32 ? 4 : 2];
+            uint32_t p_hi[NT][2], p_lo[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -685,7 +792,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(sizeof(T), DP, NT)) lt_
                     l[t][0] *= f0;
                     l[t][1] *= f1;
 #pragma unroll
-                    for (int k = 0; k < MT; ++k) {
+                    for (int k = 0; k < KS; ++k) {
                         o[t][k][0] *= f0;
                         o[t][k][1] *= f1;
                         o[t][k][2] *= f0;
@@ -699,75 +806,27 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(sizeof(T), DP, NT)) lt_
                 c[t][3] = power2(c[t][3] - b1);
                 l[t][0] += c[t][0] + c[t][2];
                 l[t][1] += c[t][1] + c[t][3];
-                if constexpr (F32) {
-                    float *turn_p = sm_p[warp] + t * 128;  // [token][head]
-                    __syncwarp();
-                    *reinterpret_cast<float2 *>(turn_p + eighth * 8 + quad * 2) = make_float2(c[t][0], c[t][1]);
-                    *reinterpret_cast<float2 *>(turn_p + (eighth + 8) * 8 + quad * 2) = make_float2(c[t][2], c[t][3]);
-                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t finite;
-                        halve_any(__float_as_uint(turn_p[(quad + 4 * i) * 8 + eighth]), p_hi[t][i], p_lo[t][i], finite);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float x = c[t][2 * i], y = c[t][2 * i + 1];
-                        const uint32_t hi = pack_bf16(x, y);
-                        const uint32_t lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
-                        p_hi[t][i] = turned(hi);
-                        p_lo[t][i] = turned(lo);
-                    }
+                for (int i = 0; i < 2; ++i) {
+                    const float x = c[t][2 * i], y = c[t][2 * i + 1];
+                    const uint32_t hi = pack_bf16(x, y);
+                    const uint32_t lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+                    p_hi[t][i] = turned(hi);
+                    p_lo[t][i] = turned(lo);
                 }
             }
-            if constexpr (F32) {
-                const float *v = reinterpret_cast<const float *>(stage + STEP * KP) + quad * (VP / 4) + eighth;
+            const uint32_t va = from + STEP * S::PITCH + ((lane & 7) + ((lane >> 4) & 1) * 8) * S::PITCH + ((lane >> 3) & 1) * 16;
 #pragma unroll
-                for (int k = 0; k < MT; ++k) {
-                    float sum[NT][4], odd = 0.f;
-                    auto outputs = [&](auto any) {
+            for (int k = 0; k < KS; ++k) {
+                uint32_t f[4];
+                load_matrices_turned(f, va + k * 32);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = sum[t][2] = sum[t][3] = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {  // eight tokens
-                            uint32_t hi[4], lo[4], beside[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t x = __float_as_uint(v[(e * 8 + (i >> 1) * 4) * (VP / 4) + k * 16 + (i & 1) * 8]);
-                                if constexpr (decltype(any)::value) halve_any(x, hi[i], lo[i], beside[i]);
-                                else halve(x, hi[i], lo[i], odd), beside[i] = hi[i];
-                            }
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                multiply_tf32(sum[t], lo, p_hi[t][2 * e], p_hi[t][2 * e + 1]);
-                                multiply_tf32(sum[t], beside, p_lo[t][2 * e], p_lo[t][2 * e + 1]);
-                                multiply_tf32(sum[t], hi, p_hi[t][2 * e], p_hi[t][2 * e + 1]);
-                            }
-                        }
-                    };
-                    outputs(std::false_type());
-                    if (__any_sync(0xffffffffu, odd != 0.f)) outputs(std::true_type());
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) o[t][k][j] += sum[t][j];
-                }
-            } else {
-                const uint32_t va = from + STEP * KP + ((lane & 7) + ((lane >> 4) & 1) * 8) * VP + ((lane >> 3) & 1) * 16;
-#pragma unroll
-                for (int k = 0; k < MT; ++k) {
-                    uint32_t f[4];
-                    load_matrices_turned(f, va + k * 32);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        multiply(o[t][k], f, p_hi[t][0], p_hi[t][1]);
-                        multiply(o[t][k], f, p_lo[t][0], p_lo[t][1]);
-                    }
+                for (int t = 0; t < NT; ++t) {
+                    multiply(o[t][k], f, p_hi[t][0], p_hi[t][1]);
+                    multiply(o[t][k], f, p_lo[t][0], p_lo[t][1]);
                 }
             }
         }
-        // join the warps
         copy_wait<0>();
         float *sm_o = reinterpret_cast<float *>(stage_mem);  // [WARPS][HEADS][DP + 4]
         static_assert(WARPS * HEADS * (DP + 4) * 4 <= S::BYTES, "the warps' outputs fit");
@@ -783,64 +842,31 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(sizeof(T), DP, NT)) lt_
                 if (lane < 4) sm_m[warp][h] = m[t][j], sm_l[warp][h] = sum;
                 float *to = sm_o + (warp * HEADS + h) * (DP + 4) + eighth;
 #pragma unroll
-                for (int k = 0; k < MT; ++k) {
+                for (int k = 0; k < KS; ++k) {
                     to[k * 16] = o[t][k][j];
                     to[k * 16 + 8] = o[t][k][2 + j];
                 }
             }
         __syncthreads();
-        const bool whole = w.t0 == 0 && w.t1 == w.tiles;
-        float *slot = whole ? nullptr : part_of(a, blockIdx.x, s.idx != start);
-        for (int x = threadIdx.x; x < w.heads * (int)(a.dim / 4); x += THREADS) {
-            const int h = x / (int)(a.dim / 4), d = 4 * (x - h * (int)(a.dim / 4));
-            float mm = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < WARPS; ++k) mm = fmaxf(mm, sm_m[k][h]);
-            const float base = mm == -INFINITY ? 0.f : mm;
-            float ll = 0.f;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < WARPS; ++k) {
-                const float f = power2(sm_m[k][h] - base);
-                const float4 u = *reinterpret_cast<const float4 *>(sm_o + (k * HEADS + h) * (DP + 4) + d);
-                ll += sm_l[k][h] * f;
-                v.x += u.x * f;
-                v.y += u.y * f;
-                v.z += u.z * f;
-                v.w += u.w * f;
-            }
-            if (whole) {
-                store4((T *)a.out + ((uint64_t)w.b * a.heads + w.h0 + h) * a.dim + d, make_float4(quotient(v.x, ll), quotient(v.y, ll), quotient(v.z, ll), quotient(v.w, ll)));
-            } else {
-                *reinterpret_cast<float4 *>(slot + h * a.dim + d) = v;
-                if (d == 0) *reinterpret_cast<float2 *>(slot + HEADS * a.dim + 2 * h) = make_float2(mm, ll);
-            }
-        }
-        if (!whole) {
-            Parts parts;
-            if (last_of_parts(a, s, w, parts, &flag)) join_staged<T, HEADS, DP>(a, w, parts, sm_o, S::BYTES);
-        }
-        __syncthreads();  // the next stretch's copies go where the parts were
+        leave_stretch<__nv_bfloat16, HEADS, DP>(a, s, w, s.idx == start, sm_o, sm_m, sm_l, S::BYTES, &flag);
     }
-    finish<T>(a);
+    finish<__nv_bfloat16>(a);
 }
 
 // A block of its own per (sequence, head block) when no sequence can hold more than a few tiles.
 bool split(const LtOperator &o) { return (uint64_t)o.table_width * o.page > 2 * TILE; }
 
-// lt_attend_tensor: widths it is built for (0: none), and query heads per block in eights -- as many as share a key, while
-// queries and output fit the registers.
-int tensor_width(int dtype, uint32_t dim) {
-    const int w = dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
-    if (dtype == LT_BF16) return dim % 8 == 0 ? w : 0;
-    return dim % 4 == 0 && w <= 192 ? w : 0;
+// lt_attend_tensor and lt_attend_single: widths they are built for (0: none), and query heads per block -- as many as share
+// a key, while queries and output fit the registers.
+int row_width(int dtype, uint32_t dim) {
+    const int w = dim <= 64 ? 64 : dim <= 96 && dtype == LT_BF16 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
+    return dim % (dtype == LT_BF16 ? 8 : 4) == 0 ? w : 0;
 }
-int tensor_tiles(int dtype, int width, uint32_t group) {
-    if (group <= 8) return 1;
-    if (dtype == LT_F32) return width <= 64 ? 2 : 1;
-    return group <= 16 || width > 128 ? 2 : 4;
+int row_heads(int dtype, int width, uint32_t group) {
+    if (dtype == LT_F32) return group <= 1 ? 1 : group <= 2 ? 2 : group <= 4 ? 4 : 8;
+    return group <= 8 ? 8 : group <= 16 || width > 128 ? 16 : 32;
 }
-int element_size(int dtype) { return dtype == LT_BF16 ? 2 : 4; }
+int row_blocks(int dtype, int width, int heads) { return dtype == LT_F32 ? single_blocks(width, heads) : tensor_blocks(width, heads / 8); }
 constexpr int ANY_BLOCKS = 4;  // resident blocks per SM of lt_attend_any
 
 inline bool is_aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -852,36 +878,42 @@ cudaError_t launch_any(const AttendArgs &a, unsigned grid, cudaStream_t stream) 
     return launch_pdl(lt_attend_any<T, 8>, grid, THREADS, (size_t)0, stream, a);
 }
 
-template <class T, int DP, int NT, bool WHOLE>
+template <int DP, int NT, bool WHOLE>
 cudaError_t launch_tensor(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    constexpr size_t bytes = Shape<T, DP>::BYTES;
-    const cudaError_t e = allow_shared(lt_attend_tensor<T, DP, NT, WHOLE>, bytes, ready);
+    constexpr size_t bytes = Shape<__nv_bfloat16, DP>::BYTES;
+    const cudaError_t e = allow_shared(lt_attend_tensor<DP, NT, WHOLE>, bytes, ready);
     if (e != cudaSuccess) return e;
-    return launch_pdl(lt_attend_tensor<T, DP, NT, WHOLE>, grid, THREADS, bytes, stream, a);
+    return launch_pdl(lt_attend_tensor<DP, NT, WHOLE>, grid, THREADS, bytes, stream, a);
 }
 
-template <class T, int DP>
+template <int DP>
 cudaError_t launch_tensor_heads(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     const bool whole = a.page % STEP == 0;
-    if (a.block_heads == 8) return whole ? launch_tensor<T, DP, 1, true>(a, grid, stream) : launch_tensor<T, DP, 1, false>(a, grid, stream);
-    if constexpr (sizeof(T) == 2 || DP <= 64)
-        if (a.block_heads == 16) return whole ? launch_tensor<T, DP, 2, true>(a, grid, stream) : launch_tensor<T, DP, 2, false>(a, grid, stream);
-    if constexpr (sizeof(T) == 2 && DP <= 128)
-        if (a.block_heads == 32) return whole ? launch_tensor<T, DP, 4, true>(a, grid, stream) : launch_tensor<T, DP, 4, false>(a, grid, stream);
+    if (a.block_heads == 8) return whole ? launch_tensor<DP, 1, true>(a, grid, stream) : launch_tensor<DP, 1, false>(a, grid, stream);
+    if (a.block_heads == 16) return whole ? launch_tensor<DP, 2, true>(a, grid, stream) : launch_tensor<DP, 2, false>(a, grid, stream);
+    if constexpr (DP <= 128)
+        if (a.block_heads == 32) return whole ? launch_tensor<DP, 4, true>(a, grid, stream) : launch_tensor<DP, 4, false>(a, grid, stream);
     return cudaErrorInvalidValue;
 }
 
-template <class T>
-cudaError_t launch_tensor_width(const AttendArgs &a, int width, unsigned grid, cudaStream_t stream) {
-    switch (width) {
-    case 64: return launch_tensor_heads<T, 64>(a, grid, stream);
-    case 96: return launch_tensor_heads<T, 96>(a, grid, stream);
-    case 128: return launch_tensor_heads<T, 128>(a, grid, stream);
-    case 192: return launch_tensor_heads<T, 192>(a, grid, stream);
-    default:
-        if constexpr (sizeof(T) == 2) return launch_tensor_heads<T, 256>(a, grid, stream);
-        return cudaErrorInvalidValue;
+template <int DP, int NH, bool WHOLE>
+cudaError_t launch_single(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    constexpr size_t bytes = Shape<float, DP>::BYTES;
+    const cudaError_t e = allow_shared(lt_attend_single<DP, NH, WHOLE>, bytes, ready);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(lt_attend_single<DP, NH, WHOLE>, grid, THREADS, bytes, stream, a);
+}
+
+template <int DP>
+cudaError_t launch_single_heads(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
+    const bool whole = a.page % STEP == 0;
+    switch (a.block_heads) {
+    case 1: return whole ? launch_single<DP, 1, true>(a, grid, stream) : launch_single<DP, 1, false>(a, grid, stream);
+    case 2: return whole ? launch_single<DP, 2, true>(a, grid, stream) : launch_single<DP, 2, false>(a, grid, stream);
+    case 4: return whole ? launch_single<DP, 4, true>(a, grid, stream) : launch_single<DP, 4, false>(a, grid, stream);
+    default: return whole ? launch_single<DP, 8, true>(a, grid, stream) : launch_single<DP, 8, false>(a, grid, stream);
     }
 }
 
@@ -897,12 +929,12 @@ size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count) {
     if (!split(o)) return 0;
     // (whether the addresses are aligned is not known yet: room for either kernel)
     const size_t any = (size_t)split_blocks(sm_count, ANY_BLOCKS) * ANY_HEADS;
-    size_t tensor = 0;
-    if (const int width = tensor_width(o.dtype, o.dim)) {
-        const int tiles = tensor_tiles(o.dtype, width, o.heads / o.kv_heads);
-        tensor = (size_t)split_blocks(sm_count, tensor_blocks(element_size(o.dtype), width, tiles)) * 8 * tiles;
+    size_t rows = 0;
+    if (const int width = row_width(o.dtype, o.dim)) {
+        const int heads = row_heads(o.dtype, width, o.heads / o.kv_heads);
+        rows = (size_t)split_blocks(sm_count, row_blocks(o.dtype, width, heads)) * part_heads(heads);
     }
-    return 2 * (any > tensor ? any : tensor) * (o.dim + 2) * sizeof(float);
+    return 2 * (any > rows ? any : rows) * (o.dim + 2) * sizeof(float);
 }
 
 cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream) {
@@ -929,12 +961,25 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     a.page = o.page;
     a.table_width = o.table_width;
     a.scale = (float)(lt_attr_double(o.attr[1]) * 1.4426950408889634);
-    const int width = tensor_width(o.dtype, o.dim);
-    const bool tensor = width && is_aligned(a.cache, 16) && is_aligned(a.q, 4) && (o.dtype == LT_F32 || a.q_pitch % 2 == 0) && is_aligned(a.out, 16);
-    const int tiles = tensor ? tensor_tiles(o.dtype, width, a.group) : ANY_HEADS / 8;
-    a.block_heads = 8 * tiles;
+    const int width = row_width(o.dtype, o.dim);
+    const bool rows = width && is_aligned(a.cache, 16) && is_aligned(a.q, 4) && (o.dtype == LT_F32 || a.q_pitch % 2 == 0) && is_aligned(a.out, 16);
+    a.block_heads = rows ? row_heads(o.dtype, width, a.group) : ANY_HEADS;
     a.head_blocks = (a.group + a.block_heads - 1) / a.block_heads;
-    const unsigned grid = !a.partial ? a.batch * a.kv_heads * a.head_blocks : split_blocks(sm_count, tensor ? tensor_blocks(element_size(o.dtype), width, tiles) : ANY_BLOCKS);
-    if (tensor) return o.dtype == LT_BF16 ? launch_tensor_width<__nv_bfloat16>(a, width, grid, stream) : launch_tensor_width<float>(a, width, grid, stream);
-    return o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
+    const unsigned grid = !a.partial ? a.batch * a.kv_heads * a.head_blocks : split_blocks(sm_count, rows ? row_blocks(o.dtype, width, (int)a.block_heads) : ANY_BLOCKS);
+    if (!rows) return o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
+    if (o.dtype == LT_F32) {
+        switch (width) {
+        case 64: return launch_single_heads<64>(a, grid, stream);
+        case 128: return launch_single_heads<128>(a, grid, stream);
+        case 192: return launch_single_heads<192>(a, grid, stream);
+        default: return launch_single_heads<256>(a, grid, stream);
+        }
+    }
+    switch (width) {
+    case 64: return launch_tensor_heads<64>(a, grid, stream);
+    case 96: return launch_tensor_heads<96>(a, grid, stream);
+    case 128: return launch_tensor_heads<128>(a, grid, stream);
+    case 192: return launch_tensor_heads<192>(a, grid, stream);
+    default: return launch_tensor_heads<256>(a, grid, stream);
+    }
 }
