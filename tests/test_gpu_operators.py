@@ -281,6 +281,28 @@ def test_paged_attention_many_sequences(ctx, dtype):
     close(fetch(ctx, y), want, bound)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page,lengths", [
+    (8, 1, 128, 64, [20000]), (4, 1, 256, 16, [9001, 0, 12]), (16, 2, 64, 48, [300, 7000, 64, 1]), (3, 3, 72, 16, [4097, 129]), (32, 1, 128, 16, [5000, 3000]),
+    (8, 2, 128, 16, [1500, 17, 900, 2100, 64, 65, 0, 1300, 800, 1999, 33, 1024])])
+def test_paged_attention_spread_over_blocks(ctx, dtype, heads, kv_heads, dim, page, lengths):
+    """Sequences that many blocks share (up to as many as one may be spread over), beside short ones; unaligned as well,
+    where the kernel for any shape shares them out."""
+    t, g = TYPES[dtype], gen(heads + dim + page)
+    cache, table = paged(g, lengths, page, kv_heads, dim, True, t)
+    q = normal(g, len(lengths), heads, dim, dtype=t, std=1.5)
+    want, bound = ref.attention(q, cache, table, lengths, dim ** -0.5, True)
+    rest = [ctx.from_torch(table), ctx.from_torch(torch.tensor(lengths, dtype=torch.int32, device="cuda"))]
+    lq, first = ctx.from_torch(q), None
+    for lc in (ctx.from_torch(cache), unaligned(ctx, cache, dtype)):
+        for again in range(3):
+            y = fetch(ctx, ctx.paged_attention(lq, lc, *rest, scale=dim ** -0.5, head_major=True))
+            if again == 0:
+                close(y, want, bound)
+                first = y
+            assert torch.equal(y, first)  # whichever block comes last
+
+
 @pytest.mark.parametrize("by", [1, 2, 4])
 def test_paged_attention_unaligned_and_sliced(ctx, by):
     g, n = gen(13), [70, 1, 200]
