@@ -60,7 +60,8 @@ typedef enum {
                                  of the other thread blocks of its cluster                                */
     LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes:
                                  reported by the first blocking call after the operator that met it, which left
-                                 out what the index named and did the rest                                */
+                                 out what the index named and did the rest (one word per device holds it: of
+                                 several contexts there, the first that used such an operator and looks)   */
 } lt_status;
 
 typedef enum { LT_F32 = 0, LT_BF16 = 1, LT_U8 = 2, LT_I32 = 3, LT_U32 = 4 } lt_dtype;

@@ -126,6 +126,10 @@ _lib.lt_last_error.restype = ctypes.c_char_p
 _lib.lt_version.argtypes = []
 _lib.lt_version.restype = ctypes.c_char_p
 
+# The recording call of a Batch, for arguments that are ctypes values already (made once per batch): converting them anew
+# costs more than the call.  It records and returns, so the interpreter lock is kept.
+_op_many = ctypes.PyDLL(str(LIB_PATH)).lt_op_many
+
 EXPORTED_SYMBOLS = sorted(list(_SIGNATURES) + ["lt_last_error", "lt_version"])
 
 
@@ -353,6 +357,7 @@ class Batch(_Operators):
 
     def input(self) -> _BatchRef:
         self._n_inputs += 1
+        self._c = None
         return _BatchRef(self, self._n_inputs - 1)
 
     def op(self, name: str, *inputs, **attrs) -> _BatchRef:
@@ -384,8 +389,10 @@ class Batch(_Operators):
                 for i, r in enumerate(ins[:3]):
                     ops[k].in_[i] = r
             attrs = (_i64 * max(len(self._attrs), 1))(*self._attrs)
-            results, ins = (_u64 * max(len(self._ops), 1))(), (_u64 * max(self._n_inputs, 1))()
-            self._c = (results, ins, ctypes.addressof(ops), ctypes.addressof(attrs), ctypes.addressof(results), ctypes.addressof(ins), ops, attrs)
+            n = self._n_inputs
+            results = (_u64 * max(len(self._ops), 1))()
+            # (the inputs' handles travel as bytes, packed anew every time)
+            self._c = (struct.Struct(f"={n}Q").pack, results, ops, ctypes.c_size_t(len(self._ops)), ctypes.c_size_t(n), attrs)
         return self._c
 
 
@@ -565,12 +572,11 @@ class LazyContext(_Operators):
 
     def record(self, batch: Batch, inputs) -> list:
         """lt_op_many: records the operations of `batch` on `inputs` in one call; returns the results it keeps."""
-        results, ins, ops_at, attrs_at, results_at, ins_at, _, _ = batch._c or batch._compiled()
-        n = len(inputs)
-        if n != batch._n_inputs:
-            raise ValueError(f"the batch takes {batch._n_inputs} inputs, {n} given")
-        ins[:n] = [t.handle for t in inputs]
-        st = _lib.lt_op_many(self._ctx, ops_at, len(batch._ops), ins_at, n, attrs_at, results_at)
+        pack, results, ops, n_ops, n_inputs, attrs = batch._c or batch._compiled()
+        handles = [t.handle for t in inputs]
+        if len(handles) != batch._n_inputs:
+            raise ValueError(f"the batch takes {batch._n_inputs} inputs, {len(handles)} given")
+        st = _op_many(self._ctx, ops, n_ops, pack(*handles), n_inputs, attrs, results)
         if st:
             self._check(st)
         if not batch._kept:

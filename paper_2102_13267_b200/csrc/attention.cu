@@ -55,10 +55,11 @@ struct Share {
     int n;                      // its length
 };
 
-// The block's part of the list, from the sequences' lengths.  Every warp finds it for itself: a lane has a run of
-// sequences, whose sums are added up across lanes, without a barrier.
+// The block's part of the list, from the sequences' lengths.  Every warp finds it for itself, without a barrier: the lanes
+// have a run of sequences each, whose sums are added up across lanes; the run that holds the block's first item is divided
+// among the lanes again, until it is one sequence.
 __device__ __forceinline__ Share my_share(const AttendArgs &a) {
-    const uint32_t per = a.kv_heads * a.head_blocks;
+    const uint32_t per = a.kv_heads * a.head_blocks, lane = threadIdx.x & 31;
     Share s{};
     if (!a.partial) {  // a block per (sequence, head block)
         s.b = blockIdx.x / per;
@@ -68,40 +69,39 @@ __device__ __forceinline__ Share my_share(const AttendArgs &a) {
         s.end = s.idx + t;
         return s;
     }
-    const uint32_t lane = threadIdx.x & 31, run = (a.batch + 31) / 32, b0 = lane * run;
-    uint32_t mine = 0, most = 0;
-    int n = 0;
-    for (uint32_t k = 0; k < run; ++k) {
-        const int m = b0 + k < a.batch ? length_of(a, b0 + k) : 0;
-        if (k == 0) n = m;
-        mine += items_of(m);
-        most = max(most, items_of(m));
-    }
-    mine *= per;
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= (uint32_t)d) upto += o;
-    }
-    const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
-    most = __reduce_max_sync(0xffffffffu, most);
-    // an even share, and no (sequence, head block) over more than MOST_PARTS blocks
-    s.size = max((total + gridDim.x - 1) / gridDim.x, (most + MOST_PARTS - 2) / (MOST_PARTS - 1));
-    s.idx = min(blockIdx.x * s.size, total);
-    s.end = min(s.idx + s.size, total);
-    if (s.idx == s.end) return s;
-    uint32_t b = b0, base = upto - mine;
-    const uint32_t holder = __ffs(__ballot_sync(0xffffffffu, s.idx >= base && s.idx < upto)) - 1;
-    if (run > 1 && lane == holder)
-        while (s.idx >= base + items_of(n) * per) {
-            base += items_of(n) * per;
-            n = length_of(a, ++b);
+    for (uint32_t count = a.batch; ; ) {
+        const uint32_t run = (count + 31) / 32, b0 = s.b + lane * run, b1 = s.b + min(count, (lane + 1) * run);
+        uint32_t mine = 0, most = 0;
+        int n = 0;
+#pragma unroll 8
+        for (uint32_t b = b0; b < b1; ++b) {
+            n = length_of(a, b);
+            mine += items_of(n);
+            most = max(most, items_of(n));
         }
-    s.b = __shfl_sync(0xffffffffu, b, holder);
-    s.base = __shfl_sync(0xffffffffu, base, holder);
-    s.n = __shfl_sync(0xffffffffu, n, holder);
-    return s;
+        mine *= per;
+        uint32_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= (uint32_t)d) upto += o;
+        }
+        if (s.size == 0) {  // all sequences: an even share, and no (sequence, head block) over more than MOST_PARTS blocks
+            const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+            most = __reduce_max_sync(0xffffffffu, most);
+            s.size = max(max((total + gridDim.x - 1) / gridDim.x, (most + MOST_PARTS - 2) / (MOST_PARTS - 1)), 1u);
+            s.idx = min(blockIdx.x * s.size, total);
+            s.end = min(s.idx + s.size, total);
+            if (s.idx == s.end) return s;
+        }
+        const uint32_t base = s.base + upto - mine;
+        const uint32_t holder = __ffs(__ballot_sync(0xffffffffu, s.idx >= base && s.idx < base + mine)) - 1;
+        s.base = __shfl_sync(0xffffffffu, base, holder);
+        s.n = __shfl_sync(0xffffffffu, n, holder);
+        s.b += holder * run;
+        if (run == 1) return s;
+        count = min(run, count - holder * run);
+    }
 }
 
 // A stretch of tiles of one (sequence, head block).

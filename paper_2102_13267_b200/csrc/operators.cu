@@ -834,7 +834,7 @@ cudaError_t launch_norm(NormArgs a, int sm_count, cudaStream_t stream) {
 
 // Blocks of the gradient's first kernel, and the threads per row of lt_norm_grad_rows (0: lt_norm_grad_any).  What the
 // scratch holds is planned before the addresses are known: the most either takes.
-unsigned norm_grad_any_blocks(uint64_t rows, int sm_count) { return (unsigned)std::min<uint64_t>(rows, (uint64_t)sm_count * 4); }
+unsigned norm_grad_any_blocks(uint64_t rows, int sm_count) { return (unsigned)std::min<uint64_t>(rows, (uint64_t)sm_count * 2); }
 unsigned norm_grad_row_blocks(uint64_t rows, int rt, int sm_count) {
     const uint64_t groups = grad_block(rt) / rt, n = (rows + groups - 1) / groups;
     return (unsigned)std::min<uint64_t>(n, (uint64_t)sm_count * (rt > 256 ? 1 : 2));

@@ -268,14 +268,16 @@ def test_paged_attention(ctx, dtype, head_major, heads, kv_heads, dim, page, len
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_paged_attention_many_sequences(ctx, dtype):
+@pytest.mark.parametrize("batch", [33, 300, 1025, 2100])
+def test_paged_attention_many_sequences(ctx, dtype, batch):
     """More sequences than a block has threads, most of them empty, and a table far wider than any sequence."""
     t, g = TYPES[dtype], gen(12)
-    n = [0] * 300
-    for b, x in ((0, 3), (127, 200), (128, 1), (129, 65), (250, 0), (299, 331)):
-        n[b] = x
+    n = [0] * batch
+    for b, x in ((0, 3), (31, 130), (32, 5), (127, 200), (128, 1), (129, 65), (250, 0), (1023, 64), (1024, 66), (2047, 9), (batch - 1, 331)):
+        if b < batch:
+            n[b] = x
     cache, table = paged(g, n, 16, 2, 64, True, t, width=500)
-    q = normal(g, 300, 8, 64, dtype=t)
+    q = normal(g, batch, 8, 64, dtype=t)
     want, bound = ref.attention(q, cache, table, n, 0.2, True)
     y = ctx.paged_attention(*(ctx.from_torch(a) for a in (q, cache, table, torch.tensor(n, dtype=torch.int32, device="cuda"))), scale=0.2, head_major=True)
     close(fetch(ctx, y), want, bound)
