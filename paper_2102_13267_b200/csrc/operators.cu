@@ -376,6 +376,115 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
     }
 }
 
+// Rows of up to NARROW_COLS values at any alignment, where 16 bytes at a time are not to be had: RT threads per row (32, 64
+// or 128, the fewest that hold the row with eight values of each in registers -- values t, t + RT, ..), so that every value
+// is still read once.  The largest values of 32 columns each go through shared memory to whoever needs them.  Bound by its
+// instructions, one or two dozen per value; against lt_norm_any and lt_norm_grad_any, which read a row up to three times:
+// 8000 x 999 bf16 to eight bits 49 us against 55, the gradient of 8000 x 999 bf16 41 against 118, of 30000 x 131 f32 24
+// against 48.
+constexpr int NARROW_COLS = 1024, NARROW_VALUES = 8, NARROW_BLOCKS = 4;  // blocks that share an SM
+constexpr int narrow_threads(uint64_t cols) { return cols <= 32 * NARROW_VALUES ? 32 : cols <= 64 * NARROW_VALUES ? 64 : 128; }
+
+unsigned narrow_blocks(uint64_t rows, uint64_t cols, int sm_count) {
+    const uint64_t at_once = 256 / narrow_threads(cols);
+    return (unsigned)std::min<uint64_t>((rows + at_once - 1) / at_once, (uint64_t)sm_count * NARROW_BLOCKS);
+}
+
+// Both sums over the RT threads of a row group inside a block (`group`: which).  `part`: room for 2 x 32 values, used in
+// turn, as in row_reduce below.
+template <int RT>
+__device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int group, int &turn) {
+    x = warp_sum(x);
+    y = warp_sum(y);
+    if constexpr (RT == 32) return make_float2(x, y);
+    constexpr int W = RT / 32;
+    float2 *mine = part + (turn & 1) * 32 + group * W;
+    ++turn;
+    if ((threadIdx.x & 31) == 0) mine[(threadIdx.x % RT) >> 5] = make_float2(x, y);
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");
+    float2 s = mine[threadIdx.x & (W - 1)];
+#pragma unroll
+    for (int d = W / 2; d > 0; d >>= 1) {
+        s.x += __shfl_xor_sync(0xffffffffu, s.x, d);
+        s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
+    }
+    return s;
+}
+
+// `n` values of a row from `row` on, RT apart; zeros after them.  All are read before the first is used.
+template <class T, int RT>
+__device__ __forceinline__ void load_narrow(float *v, const T *row, int n) {
+    T raw[NARROW_VALUES];
+#pragma unroll
+    for (int k = 0; k < NARROW_VALUES; ++k) {
+        raw[k] = from_float<T>(0.f);
+        if (k < n) raw[k] = row[RT * k];
+    }
+#pragma unroll
+    for (int k = 0; k < NARROW_VALUES; ++k) v[k] = to_float(raw[k]);
+}
+
+template <class T, int RT>
+__global__ void __launch_bounds__(256, NARROW_BLOCKS) lt_norm_narrow(const NormArgs a) {
+    constexpr int E = NARROW_VALUES, GROUPS = 256 / RT, W = RT / 32;
+    __shared__ float2 part[64];
+    __shared__ float tops[GROUPS][E * W];  // of 32 columns each
+    pdl_release();
+    pdl_wait();
+    const uint32_t lane = threadIdx.x % RT, group = threadIdx.x / RT, cols = (uint32_t)a.cols;
+    const uint32_t steps = a.group ? a.group / 32 : E * W;  // of 32 columns, in a group of the output
+    const int n = lane < cols ? (int)((cols - lane + RT - 1) / RT) : 0;  // values of a row that are this thread's
+    int turn = 0;
+    float g[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) g[k] = k < n ? gamma_at<T>(a.gamma, a.gamma_f32, lane + RT * k) : 0.f;
+    for (uint64_t row = (uint64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (uint64_t)gridDim.x * GROUPS) {
+        float h[E], ss = 0.f;
+        load_narrow<T, RT>(h, (const T *)a.x + row * a.x_pitch + lane, n);
+        if (a.r) {
+            float r[E];
+            load_narrow<T, RT>(r, (const T *)a.r + row * a.r_pitch + lane, n);
+#pragma unroll
+            for (int k = 0; k < E; ++k) h[k] += r[k];
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k) ss += h[k] * (h[k] * a.down);
+        const float inv = rsqrtf(group_sum<RT>(ss, 0.f, part, (int)group, turn).x * a.up + a.eps);
+        const uint64_t at = row * cols + lane;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (a.sum && k < n) ((T *)a.sum)[at + RT * k] = from_float<T>(h[k]);
+            h[k] = h[k] * inv * g[k];
+            if (k >= n) h[k] = 0.f;  // (not infinity times nothing)
+            if (a.y && k < n) ((T *)a.y)[at + RT * k] = from_float<T>(h[k]);
+        }
+        if (!a.codes && !a.scales) continue;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            float t = 0.f;
+            if (RT * k + (lane & ~31u) < cols) t = warp_max_nan(fabsf(h[k]));  // (the same in all lanes)
+            if ((lane & 31) == 0) tops[group][k * W + (lane >> 5)] = t;
+        }
+        if constexpr (RT == 32) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");
+        float t = 0.f;
+        uint32_t known = 0;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (RT * k + (lane & ~31u) >= cols) break;
+            const uint32_t mine = k * W + (lane >> 5), first = mine & ~(steps - 1);
+            if (k == 0 || first != known) {  // (the same in all lanes)
+                t = 0.f;
+                for (uint32_t i = 0; i < steps; ++i) t = max_nan(t, tops[group][first + i]);
+                known = first;
+            }
+            if (a.scales && (lane & 31) == 0 && mine == first) a.scales[row * a.groups + (a.group ? mine * 32 / a.group : 0)] = scale_of(t);
+            if (a.codes && k < n) a.codes[at + RT * k] = __nv_cvt_float_to_fp8(h[k] * code_factor(t), __NV_SATFINITE, __NV_E4M3);
+        }
+        if constexpr (RT == 32) __syncwarp();  // (128 threads: the next row's sums have a barrier before `tops` is written again)
+    }
+}
+
 // N values of gamma from column c on, which is a multiple of N
 template <class T>
 __device__ __forceinline__ void gamma_chunk(const void *gamma, int f32, uint32_t c, float (&g)[Chunk<T>::N]) {
@@ -590,24 +699,53 @@ __global__ void __launch_bounds__(256) lt_norm_grad_any(const NormGradArgs a) {
     }
 }
 
-// Sums of two values over the RT threads of a row group inside a block (`group`: which).
-template <int RT>
-__device__ __forceinline__ float2 group_sum(float x, float y, float2 *part, int group, int &turn) {
-    x = warp_sum(x);
-    y = warp_sum(y);
-    if constexpr (RT == 32) return make_float2(x, y);
-    constexpr int W = RT / 32;
-    float2 *mine = part + (turn & 1) * 32 + group * W;  // (in turn, as in row_reduce)
-    ++turn;
-    if ((threadIdx.x & 31) == 0) mine[(threadIdx.x % RT) >> 5] = make_float2(x, y);
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(RT) : "memory");
-    float2 s = mine[threadIdx.x & (W - 1)];
+// The gradient for rows as in lt_norm_narrow; a thread keeps its columns' sums for gamma.
+template <class T, int RT>
+__global__ void __launch_bounds__(256, NARROW_BLOCKS) lt_norm_grad_narrow(const NormGradArgs a) {
+    constexpr int E = NARROW_VALUES, GROUPS = 256 / RT;
+    __shared__ float2 part[64];
+    __shared__ float sums[GROUPS][RT * E];
+    pdl_release();
+    pdl_wait();
+    const uint32_t lane = threadIdx.x % RT, group = threadIdx.x / RT, cols = (uint32_t)a.cols;
+    const int n = lane < cols ? (int)((cols - lane + RT - 1) / RT) : 0;  // values of a row that are this thread's
+    int turn = 0;
+    float g[E], sum[E];
 #pragma unroll
-    for (int d = W / 2; d > 0; d >>= 1) {
-        s.x += __shfl_xor_sync(0xffffffffu, s.x, d);
-        s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
+    for (int k = 0; k < E; ++k) {
+        g[k] = k < n ? gamma_at<T>(a.gamma, a.gamma_f32, lane + RT * k) : 0.f;
+        sum[k] = 0.f;
     }
-    return s;
+    for (uint64_t row = (uint64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (uint64_t)gridDim.x * GROUPS) {
+        float d[E], u[E], e[E] = {}, ss = 0.f, dot = 0.f;
+        if (a.dh) load_narrow<T, RT>(e, (const T *)a.dh + row * a.dh_pitch + lane, n);
+        load_narrow<T, RT>(d, (const T *)a.dy + row * a.dy_pitch + lane, n);
+        load_narrow<T, RT>(u, (const T *)a.h + row * a.h_pitch + lane, n);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            ss += u[k] * (u[k] * a.down);
+            dot += d[k] * g[k] * (u[k] * a.down);
+        }
+        const float2 s = group_sum<RT>(ss, dot, part, (int)group, turn);
+        const uint64_t at = row * cols + lane;
+        const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const float v = u[k] * inv;
+            sum[k] += d[k] * v;
+            if (a.dx && k < n) ((T *)a.dx)[at + RT * k] = from_float<T>((d[k] * g[k] - v * m) * inv + e[k]);
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int k = 0; k < E; ++k) sums[group][lane + RT * k] = sum[k];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < cols; c += 256) {
+        float t = sums[0][c];
+#pragma unroll
+        for (int w = 1; w < GROUPS; ++w) t += sums[w][c];
+        a.partial[(uint64_t)blockIdx.x * cols + c] = t;
+    }
 }
 
 __host__ __device__ constexpr int grad_block(int rt) { return rt > 256 ? rt : 256; }
@@ -829,6 +967,13 @@ cudaError_t launch_norm(NormArgs a, int sm_count, cudaStream_t stream) {
                       is_aligned(a.y, 16) && is_aligned(a.sum, 16) && is_aligned(a.codes, 8) && a.group <= 32 * N;
     if (fits && chunks <= 4096) return a.codes || a.scales ? launch_norm_chunks<T, true>(a, chunks, sm_count, stream) : launch_norm_chunks<T, false>(a, chunks, sm_count, stream);
     const uint64_t blocks = (uint64_t)sm_count * 8;
+    if (a.cols <= NARROW_COLS) {
+        const int threads = narrow_threads(a.cols);
+        const unsigned grid = narrow_blocks(a.rows, a.cols, sm_count);
+        if (threads == 32) return launch_pdl(lt_norm_narrow<T, 32>, grid, 256, (size_t)0, stream, a);
+        if (threads == 64) return launch_pdl(lt_norm_narrow<T, 64>, grid, 256, (size_t)0, stream, a);
+        return launch_pdl(lt_norm_narrow<T, 128>, grid, 256, (size_t)0, stream, a);
+    }
     return launch_pdl(lt_norm_any<T>, (unsigned)(a.rows < blocks ? a.rows : blocks), 256, (size_t)0, stream, a);
 }
 
@@ -868,6 +1013,13 @@ cudaError_t launch_norm_grad(const NormGradArgs &a, int sm_count, cudaStream_t s
     const uint64_t chunks = a.cols / N;
     if (!fits || chunks > 512 * GRAD_CHUNKS) {
         *grid = norm_grad_any_blocks(a.rows, sm_count);
+        if (a.cols <= NARROW_COLS) {
+            const int threads = narrow_threads(a.cols);
+            *grid = narrow_blocks(a.rows, a.cols, sm_count);
+            if (threads == 32) return launch_pdl(lt_norm_grad_narrow<T, 32>, *grid, 256, (size_t)0, stream, a);
+            if (threads == 64) return launch_pdl(lt_norm_grad_narrow<T, 64>, *grid, 256, (size_t)0, stream, a);
+            return launch_pdl(lt_norm_grad_narrow<T, 128>, *grid, 256, (size_t)0, stream, a);
+        }
         return launch_pdl(lt_norm_grad_any<T>, *grid, 256, (size_t)0, stream, a);
     }
     const int rt = row_threads(chunks, a.rows <= 2 * (uint64_t)sm_count && chunks <= 512 ? 1 : GRAD_CHUNKS);
@@ -951,7 +1103,7 @@ cudaError_t lt_launch_rms_norm(const LtOperator &o, int sm_count, cudaStream_t s
 }
 
 size_t lt_rms_norm_grad_scratch(const LtOperator &o, int sm_count) {
-    const size_t blocks = norm_grad_any_blocks(o.rows, sm_count);  // (never fewer than the other kernel's: it has a row per block at least)
+    const size_t blocks = o.cols <= NARROW_COLS ? std::max(norm_grad_any_blocks(o.rows, sm_count), narrow_blocks(o.rows, o.cols, sm_count)) : norm_grad_any_blocks(o.rows, sm_count);
     return (o.wanted & 2u) ? blocks * o.cols * sizeof(float) : 0;
 }
 
