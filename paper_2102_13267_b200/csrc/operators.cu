@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(256) lt_turn_any(const TurnArgs a) {
 // (tokens in flight per thread and stages ahead, measured on rotary 8192 x 32 x 128 and append 8192 x 8 x 128, bf16: 4 and 1:
 // 25.7 and 14.4 us; 2 and 2: 25.6 and 15.5; 2 and 3: 26.3 and 16.6; 1 and 4: 25.4 and 18.5; 4 and 2: 27.7 and 16.3)
 constexpr int TURN_THREADS = 256, TURN_FLIGHT = 4, TURN_STAGES = 1;
+constexpr uint32_t TURN_ANGLES = 2048;  // of a batch, at most: 16 KB, twice
 constexpr size_t TURN_RING = (size_t)TURN_STAGES * TURN_FLIGHT * 2 * TURN_THREADS * 16;
 
 struct TurnShape {
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
 template <class T, bool APPEND, bool INTER>
 cudaError_t launch_turn_chunks(const TurnArgs &a, const TurnShape &sh, uint32_t across, int sm_count, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    constexpr size_t most = TURN_RING + 2 * 2048 * 8;
+    constexpr size_t most = TURN_RING + 2 * TURN_ANGLES * 8;
     const cudaError_t e = allow_shared(lt_turn_chunks<T, APPEND, INTER>, most, ready);
     if (e != cudaSuccess) return e;
     // as many blocks as the SMs hold (by threads, by shared memory), each going on to further tokens
@@ -272,7 +273,7 @@ cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
     const bool chunks = a.dim % N == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % N == 0 && a.x_pitch % N == 0 && is_aligned(a.x, 16) && is_aligned(a.out, 16) &&
                         (!APPEND || (a.v_pitch % N == 0 && is_aligned(a.v, 16)));
     const uint64_t units = (uint64_t)(a.dim / N - (a.interleaved ? 0 : a.pairs / N) + (APPEND ? a.dim / N : 0)) * a.heads;
-    if (chunks && a.pairs <= 2048 && units < (1u << 20) && a.tokens < (1ull << 31)) {
+    if (chunks && TURN_FLIGHT * a.pairs <= TURN_ANGLES && units < (1u << 20) && a.tokens < (1ull << 31)) {
         TurnShape sh;
         sh.turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N;
         sh.passed = (a.dim - 2 * a.pairs) / N;
@@ -281,10 +282,9 @@ cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
         const uint32_t across = (sh.units + TURN_THREADS - 1) / TURN_THREADS;
         sh.span = (sh.units + across - 1) / across;
         sh.side = TURN_THREADS / sh.span;
-        if (a.pairs && sh.side * a.pairs > 2048) sh.side = std::max(1u, 2048 / a.pairs);  // (a batch's angles: at most 32 KB, twice)
-        if (sh.side > TURN_THREADS / TURN_FLIGHT) sh.side = TURN_THREADS / TURN_FLIGHT;
+        if (a.pairs) sh.side = std::min(sh.side, TURN_ANGLES / (TURN_FLIGHT * a.pairs));
+        sh.side = std::min<uint32_t>(sh.side, TURN_THREADS / TURN_FLIGHT);
         sh.batch = sh.side * TURN_FLIGHT;
-        if (a.pairs && sh.batch * a.pairs > 2048) sh.batch = sh.side;
         sh.span_by = Divisor::make(sh.span);
         sh.turned_by = Divisor::make(sh.turned ? sh.turned : 1);
         sh.passed_by = Divisor::make(sh.passed ? sh.passed : 1);

@@ -80,6 +80,17 @@ def test_rotary_gradient_is_the_transposed_rotation(ctx, lt):
         assert abs(float(d) - float(dx[at])) < 64 * ULP * float(dy.abs().max())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,dim,rotated", [(50001, 1, 64, 64), (60000, 1, 16, 8), (20000, 1, 256, 256), (3001, 1, 1024, 1024), (700, 1, 2048, 2048), (9000, 3, 128, 128)])
+def test_rotary_more_tokens_than_the_blocks_have_at_once(ctx, lt, dtype, interleaved, tokens, heads, dim, rotated):
+    t, g = TYPES[dtype], gen(tokens)
+    x = normal(g, tokens, heads, dim, dtype=t)
+    pos = torch.randint(0, 1 << 20, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    y = ctx.rotary(ctx.from_torch(x), ctx.from_torch(pos), ctx.leaf(lt.rotary_table(rotated), "u32"), interleaved=interleaved)
+    close(fetch(ctx, y), *ref.rotary(x, pos, ref.frequencies(rotated), interleaved))
+
+
 def _rot64(x, pos, f, scale):
     z = torch.polar(torch.full((), scale, dtype=torch.float64), pos.double().cpu()[:, None, None] * f)
     p = f.numel()
@@ -133,6 +144,7 @@ def token_view(cache, head_major):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("head_major", [False, True])
 @pytest.mark.parametrize("tokens,heads,dim,rotated,interleaved,page,pages", [
+    (30001, 1, 64, 64, False, 32, 960), (20001, 1, 128, 128, True, 16, 1300),
     (1, 1, 8, 8, False, 1, 3), (1, 8, 128, 128, False, 16, 4), (33, 2, 80, 40, True, 7, 9), (64, 8, 64, 0, False, 16, 40), (300, 4, 256, 256, False, 48, 8),
     (5, 3, 33, 16, True, 5, 5), (90, 1, 96, 32, False, 64, 2)])
 def test_cache_append(ctx, lt, dtype, head_major, tokens, heads, dim, rotated, interleaved, page, pages):
