@@ -139,8 +139,9 @@ typedef enum {
 
        PAGED_ATTENTION: inputs (q* [B, Hq, D], cache, page table i32 [B, M], lengths i32 [B], [out]), attrs
        {head_major, scale} -> [B, Hq, D]: softmax(scale q k) v of one query token per sequence and head over the first
-       lengths[b] tokens, which lie in the pages the table's row b lists in order; Hq is a multiple of the cache's H and
-       D at most 256.  An empty sequence gives zeros.  Entries of the table behind a sequence's last page are not read.
+       lengths[b] tokens, which lie in the pages the table's row b lists in order; Hq is a multiple of the cache's H, D at
+       most 256, and M pages hold at most 2^30 tokens.  An empty sequence gives zeros.  Entries of the table behind a
+       sequence's last page are not read.
        A negative length counts as 0; one beyond M pages is cut there and, like a page number outside the cache (its
        tokens are left out), reported as LT_ERR_DEVICE_INDEX.
 
@@ -424,9 +425,9 @@ lt_status lt_replay_set_slot(lt_ctx *ctx, uint32_t slot, int as_integer, double 
  * A refused call leaves the pending graph in place, so lt_barrier can still flush it.
  * The first call on a device looks up the array's device address (cudaGetSymbolAddress, with
  * that device current); make that first call before starting any stream capture.
- * All calls, from all contexts on a device, share the one array, which keeps the previous call's
- * contents: two flushes that may overlap on the GPU (different streams, no ordering) race on it
- * and must be ordered by the caller.  No kernel of the library reads a temporary before writing
+ * All calls, from all contexts on a device, share the one array (and the counters of
+ * LT_OP_PAGED_ATTENTION), which keeps the previous call's contents: two flushes that may overlap
+ * on the GPU (different streams, no ordering) race on it and must be ordered by the caller.  No kernel of the library reads a temporary before writing
  * it; `clear_first` non-zero zero-fills the array on the stream before the flush all the same.
  */
 #define LT_STATIC_SCRATCH_MAX_BYTES (32u << 20)

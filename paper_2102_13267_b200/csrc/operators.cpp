@@ -88,7 +88,7 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         if (tb.dtype != LT_I32 || ln.dtype != LT_I32) return bad(LT_ERR_DTYPE, "page table and lengths are i32");
         if (tb.rank != 2 || tb.dims[0] != q.dims[0] || ln.rank != 1 || ln.dims[0] != q.dims[0])
             return bad(LT_ERR_SHAPE, "the page table is [sequences, most pages of one], lengths [sequences]");
-        if (ca.dims[0] > 0x7fffffffll || tb.dims[1] > 0x7fffffffll / page) return bad(LT_ERR_UNSUPPORTED, "more tokens per sequence than an i32 numbers");
+        if (ca.dims[0] > 0x7fffffffll || tb.dims[1] > (1ll << 30) / page) return bad(LT_ERR_UNSUPPORTED, "more than 2^30 tokens per sequence");  // (so that a step beyond the last token has a number too)
         if (q.dims[0] > 65535 || q.dims[0] * q.dims[1] >= (1ll << 31)) return bad(LT_ERR_UNSUPPORTED, "more than 65535 sequences, or more heads than the kernel counts");
         // (tiles of 64 tokens, two more for each beginning: the kernel numbers them in 31 bits)
         if ((double)q.dims[0] * (double)q.dims[1] * ((double)(tb.dims[1] * page) / 64.0 + 3.0) >= 2147483648.0)

@@ -1158,7 +1158,11 @@ cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t s
     }
 }
 
-cudaError_t lt_static_arrivals(void **out) { return address_of(lt_operator_arrivals, g_arrivals, out); }
+cudaError_t lt_static_arrivals(void **out) {
+    void *word = nullptr;
+    const cudaError_t e = address_of(lt_operator_status, g_status, &word);  // (nothing is looked up when a flush is captured)
+    return e == cudaSuccess ? address_of(lt_operator_arrivals, g_arrivals, out) : e;
+}
 
 cudaError_t lt_operator_status_read(unsigned int *out) {
     cudaError_t e = cudaMemcpyFromSymbol(out, lt_operator_status, sizeof(*out));

@@ -43,6 +43,8 @@ cudaError_t scratch_address(int device, void **out) {
         if (e == cudaSuccess && previous != device) e = cudaSetDevice(device);
         void *p = nullptr;
         if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, lt_static_scratch);
+        void *counters = nullptr;
+        if (e == cudaSuccess) e = lt_static_arrivals(&counters);
         if (previous >= 0 && previous != device) cudaSetDevice(previous);
         if (e != cudaSuccess) return e;
         g_scratch_addr[device] = p;

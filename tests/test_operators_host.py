@@ -96,7 +96,7 @@ Q, TB, LN = ((7, 6, 32), "bf16"), ((7, 3), "i32"), ((7,), "i32")
     ("SHAPE", [Q, CA, ((6, 3), "i32"), LN], ATT), ("SHAPE", [Q, CA, TB, ((6,), "i32")], ATT), ("DTYPE", [Q, CA, ((7, 3), "u32"), LN], ATT), ("DTYPE", [Q, CA, TB, ((7,), "f32")], ATT),
     ("SHAPE", [Q, ((4, 2, 16, 2, 32, 1), "bf16"), TB, LN], ATT), ("SHAPE", [Q, CA, TB, LN, ((7, 6, 31), "bf16")], ATT), ("UNSUPPORTED", [((7, 6, 264), "bf16"), ((4, 2, 16, 2, 264), "bf16"), TB, LN], ATT),
     ("UNSUPPORTED", [((70000, 6, 32), "bf16"), CA, ((70000, 3), "i32"), ((70000,), "i32")], ATT), ("UNSUPPORTED", [Q, CA, ((7, 1 << 28), "i32"), LN], ATT),
-    ("INVALID_ARG", [Q, CA, TB, LN], dict(ATT, scale=math.inf))])
+    ("UNSUPPORTED", [((1, 2, 32), "bf16"), CA, ((1, (1 << 26) + 1), "i32"), ((1,), "i32")], ATT), ("INVALID_ARG", [Q, CA, TB, LN], dict(ATT, scale=math.inf))])
 def test_paged_attention_refusals(ctx, status, shapes, attrs):
     refused(ctx, status, "paged_attention", shapes, **attrs)
 
