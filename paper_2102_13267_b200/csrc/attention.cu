@@ -20,14 +20,16 @@ constexpr int TILE = 64;         // tokens
 constexpr int START = 2;         // tiles that beginning a (sequence, head block) counts for
 constexpr int THREADS = 128;
 constexpr int WARPS = THREADS / 32;
-constexpr uint32_t MOST_PARTS = 64;  // blocks that one (sequence, head block) is spread over
+constexpr uint32_t JOIN = 32;    // parts that are joined at once
+constexpr uint32_t GROUP = 16;   // more are joined in groups of as many, and then the groups
+constexpr uint32_t MOST_PARTS = GROUP * JOIN;  // blocks that one (sequence, head block) is spread over
 
 struct AttendArgs {
     const void *q, *cache;
     const int *table, *lengths;
     void *out;
     float *partial;             // [2 x blocks][block_heads][dim + 2]: outputs, then (maximum, sum) of each head; null: every (sequence, head block) has a block of its own
-    unsigned int *arrivals;     // [blocks], zero between launches: how many of the blocks that share what begins in block i have left their part
+    unsigned int *arrivals;     // [2][LT_ARRIVALS / 2], zero between launches: how many groups (or all parts) of what begins in block i are there; and how many parts of its groups (i, i + 1, ..)
     unsigned int *status;
     uint64_t q_pitch, page_stride, value_offset, token_stride, head_stride;
     uint32_t batch, heads, kv_heads, group, block_heads, head_blocks, dim, pages, page, table_width;  // block_heads: query heads a block works on at a time
@@ -157,55 +159,68 @@ struct Parts {
     __device__ __forceinline__ const float *at(uint32_t i) const { return i ? rest + (i - 1) * stride : head; }
 };
 
-// The block has left its part of stretch w; true if that was the last one of the (sequence, head block), whose parts are then `p`.
-__device__ __forceinline__ bool last_of_parts(const AttendArgs &a, const Share &s, const Stretch &w, Parts &p, uint32_t *flag) {
-    const uint32_t i0 = w.first + START, c0 = i0 / s.size, c1 = (i0 + w.tiles - 1) / s.size;
-    p.count = c1 - c0 + 1;
-    p.stride = 2 * part_floats(a);
-    p.head = part_of(a, c0, c0 * s.size < w.first);
-    p.rest = part_of(a, c0 + 1, false);
+// One more of `count` has arrived; true if that was the last.  What the block wrote before is then seen by whoever that is.
+__device__ __forceinline__ bool last_arrival(unsigned int *arrived, uint32_t count, uint32_t *flag) {
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
-        *flag = atomicAdd(a.arrivals + c0, 1u) == p.count - 1;
+        *flag = atomicAdd(arrived, 1u) == count - 1;
         __threadfence();
     }
     __syncthreads();
     const bool last = *flag != 0;
-    if (last && threadIdx.x == 0) a.arrivals[c0] = 0;
+    if (last && threadIdx.x == 0) *arrived = 0;
     return last;
 }
 
-// The parts' weights 2^(maximum - largest maximum) and, in `sums`, the weighted sum of their sums: a warp per head, a lane per part.
-__device__ __forceinline__ void weigh_parts(const AttendArgs &a, const Stretch &w, const Parts &p, float *weights, float *sums) {
+// The block has left its part of stretch w.  Joins the parts if it was the last one of the (sequence, head block).  Many
+// parts are joined in two steps, groups first, so that several blocks work on them (one sequence of 100000 tokens with one
+// key head of 128 values, bf16: 24 us over all blocks, 44 over up to 64 or 256 whose parts are joined at once).
+// join(parts, to): into the result, or (`to` not null) into one part.
+template <class F>
+__device__ __forceinline__ void leave_part(const AttendArgs &a, const Share &s, const Stretch &w, uint32_t *flag, F join) {
+    const uint32_t i0 = w.first + START, c0 = i0 / s.size, c1 = (i0 + w.tiles - 1) / s.size;
+    Parts p;
+    p.count = c1 - c0 + 1;
+    p.stride = 2 * part_floats(a);
+    p.head = part_of(a, c0, c0 * s.size < w.first);
+    p.rest = part_of(a, c0 + 1, false);
+    if (p.count > JOIN) {
+        const uint32_t g = (blockIdx.x - c0) / GROUP;
+        Parts some;
+        some.count = min(GROUP, p.count - g * GROUP);
+        some.stride = p.stride;
+        some.head = p.at(g * GROUP);
+        some.rest = p.at(g * GROUP + 1);
+        if (!last_arrival(a.arrivals + LT_ARRIVALS / 2 + c0 + g, some.count, flag)) return;
+        join(some, const_cast<float *>(some.head));
+        p.count = (p.count + GROUP - 1) / GROUP;
+        p.rest = p.at(GROUP);
+        p.stride *= GROUP;
+    }
+    if (last_arrival(a.arrivals + c0, p.count, flag)) join(p, nullptr);
+}
+
+// The parts' weights 2^(maximum - largest maximum) and, of each head, in `sums` the largest maximum and the weighted sum of
+// their sums: a warp per head, a lane per part.
+__device__ __forceinline__ void weigh_parts(const AttendArgs &a, const Stretch &w, const Parts &p, float *weights, float2 *sums) {
     const uint32_t lane = threadIdx.x & 31;
     for (int h = threadIdx.x >> 5; h < w.heads; h += WARPS) {
-        float m[MOST_PARTS / 32], l[MOST_PARTS / 32], top = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (uint32_t k = 0; k < MOST_PARTS / 32; ++k) {
-            const uint32_t i = lane + 32 * k;
-            const float *ml = p.at(i) + a.block_heads * a.dim + 2 * h;
-            m[k] = i < p.count ? __ldcg(ml) : -INFINITY;
-            l[k] = i < p.count ? __ldcg(ml + 1) : 0.f;
-            top = fmaxf(top, m[k]);
-        }
+        const float *ml = p.at(lane) + a.block_heads * a.dim + 2 * h;
+        const float m = lane < p.count ? __ldcg(ml) : -INFINITY, l = lane < p.count ? __ldcg(ml + 1) : 0.f;
+        float top = m;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        if (top == -INFINITY) top = 0.f;
-#pragma unroll
-        for (uint32_t k = 0; k < MOST_PARTS / 32; ++k) {
-            const float f = exp2f(m[k] - top);
-            if (lane + 32 * k < p.count) weights[h * MOST_PARTS + lane + 32 * k] = f;
-            sum += f * l[k];
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) sums[h] = sum;
+        const float f = exp2f(m - (top == -INFINITY ? 0.f : top));
+        weights[h * JOIN + lane] = f;
+        const float sum = warp_sum(f * l);
+        if (lane == 0) sums[h] = make_float2(top, sum);
     }
 }
 
-// Joins parts, one value at a time (any head size).  `room`: shared, block_heads x MOST_PARTS values.
+// Joins parts, one value at a time (any head size).  `room`: shared, block_heads x JOIN values.
 template <class T>
-__device__ __forceinline__ void join_any(const AttendArgs &a, const Stretch &w, const Parts &p, float *room, float *sums) {
+__device__ __forceinline__ void join_any(const AttendArgs &a, const Stretch &w, const Parts &p, float *to, float *room, float2 *sums) {
     const uint32_t dim = a.dim;
     weigh_parts(a, w, p, room, sums);
     __syncthreads();
@@ -213,8 +228,13 @@ __device__ __forceinline__ void join_any(const AttendArgs &a, const Stretch &w, 
         const uint32_t h = x / dim, d = x - h * dim;
         float o = 0.f;
 #pragma unroll 8
-        for (uint32_t i = 0; i < p.count; ++i) o += room[h * MOST_PARTS + i] * __ldcg(p.at(i) + h * dim + d);
-        ((T *)a.out)[((uint64_t)w.b * a.heads + w.h0 + h) * dim + d] = from_float<T>(quotient(o, sums[h]));
+        for (uint32_t i = 0; i < p.count; ++i) o += room[h * JOIN + i] * __ldcg(p.at(i) + h * dim + d);
+        if (to) to[x] = o;
+        else ((T *)a.out)[((uint64_t)w.b * a.heads + w.h0 + h) * dim + d] = from_float<T>(quotient(o, sums[h].y));
+    }
+    if (to && threadIdx.x < w.heads) {
+        to[a.block_heads * dim + 2 * threadIdx.x] = sums[threadIdx.x].x;
+        to[a.block_heads * dim + 2 * threadIdx.x + 1] = sums[threadIdx.x].y;
     }
     __syncthreads();  // `room` is used again
 }
@@ -230,13 +250,14 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 *to, const f
 // found (one trip to L2 for both, instead of one for the maxima and one for every few parts after them).
 // `mem`: `bytes` of shared memory; a.dim a multiple of 4; HEADS x WIDTH values at most.
 template <class T, int HEADS, int WIDTH>
-__device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &w, const Parts &p, float *mem, uint32_t bytes) {
+__device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &w, const Parts &p, float *to, float *mem, uint32_t bytes) {
     constexpr int MINE = (HEADS * WIDTH / 4 + THREADS - 1) / THREADS;  // groups of four values of a thread
     const uint32_t dim = a.dim, quads = (uint32_t)w.heads * dim / 4;
-    float *weights = mem, *sums = weights + HEADS * MOST_PARTS;       // [HEADS][MOST_PARTS], [HEADS]
-    constexpr int PADDED = (HEADS + 3) / 4 * 4;
+    float *weights = mem;                                             // [HEADS][JOIN]
+    float2 *sums = reinterpret_cast<float2 *>(weights + HEADS * JOIN);
+    constexpr int PADDED = (HEADS + 1) / 2 * 2;
     float4 *staged = reinterpret_cast<float4 *>(sums + PADDED);
-    const uint32_t room = (bytes - (HEADS * MOST_PARTS + PADDED) * 4) / (quads * 16);
+    const uint32_t room = (bytes - (HEADS * JOIN + 2 * PADDED) * 4) / (quads * 16);
     float4 acc[MINE];
 #pragma unroll
     for (int k = 0; k < MINE; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -244,17 +265,17 @@ __device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &
         const uint32_t n = min(room, p.count - i0);
         if (i0) __syncthreads();  // the parts before have been read
         for (uint32_t x = threadIdx.x; x < quads; x += THREADS) {
-            uint32_t to = shared_address(staged + x), i = 0;
+            uint32_t at = shared_address(staged + x), i = 0;
             if (i0 == 0) {
-                copy16(to, p.head + 4 * x, true);
-                to += quads * 16;
+                copy16(at, p.head + 4 * x, true);
+                at += quads * 16;
                 i = 1;
             }
             const float *from = p.rest + (i0 + i - 1) * p.stride + 4 * x;
 #pragma unroll 4
             for (; i < n; ++i) {
-                copy16(to, from, true);
-                to += quads * 16;
+                copy16(at, from, true);
+                at += quads * 16;
                 from += p.stride;
             }
         }
@@ -266,7 +287,7 @@ __device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &
         for (int k = 0; k < MINE; ++k) {
             const uint32_t x = threadIdx.x + k * THREADS;
             if (x >= quads) continue;
-            const float *f = weights + (4 * x / dim) * MOST_PARTS + i0;
+            const float *f = weights + (4 * x / dim) * JOIN + i0;
             const float4 *from = staged + x;
             float4 v = acc[k];
 #pragma unroll 4
@@ -285,9 +306,14 @@ __device__ __forceinline__ void join_staged(const AttendArgs &a, const Stretch &
     for (int k = 0; k < MINE; ++k) {
         const uint32_t x = threadIdx.x + k * THREADS;
         if (x >= quads) continue;
-        const float l = sums[4 * x / dim];
+        if (to) {
+            reinterpret_cast<float4 *>(to)[x] = acc[k];
+            continue;
+        }
+        const float l = sums[4 * x / dim].y;
         store4((T *)a.out + ((uint64_t)w.b * a.heads + w.h0) * dim + 4 * x, make_float4(quotient(acc[k].x, l), quotient(acc[k].y, l), quotient(acc[k].z, l), quotient(acc[k].w, l)));
     }
+    if (to && threadIdx.x < w.heads) *reinterpret_cast<float2 *>(to + a.block_heads * dim + 2 * threadIdx.x) = sums[threadIdx.x];
 }
 
 // The zeros of empty sequences, and the check of the lengths.
@@ -331,8 +357,9 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
     constexpr int HEADS = ANY_HEADS;
     __shared__ uint32_t flag;
     __shared__ float sm_m[4][HEADS], sm_l[4][HEADS];
+    __shared__ float2 sums[HEADS];
     __shared__ float sm_o[4][HEADS][NE * 32];
-    static_assert(4 * NE * 32 >= (int)MOST_PARTS, "the parts' weights fit where the warps' outputs are");
+    static_assert(4 * NE * 32 >= (int)JOIN, "the parts' weights fit where the warps' outputs are");
     pdl_release();
     pdl_wait();
     const T *q = (const T *)a.q, *cache = (const T *)a.cache;
@@ -408,10 +435,7 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
                 if (d == 0) slot[HEADS * a.dim + 2 * h] = mm, slot[HEADS * a.dim + 2 * h + 1] = ll;
             }
         }
-        if (!whole) {
-            Parts parts;
-            if (last_of_parts(a, s, w, parts, &flag)) join_any<T>(a, w, parts, &sm_o[0][0][0], &sm_l[0][0]);
-        }
+        if (!whole) leave_part(a, s, w, &flag, [&](const Parts &p, float *to) { join_any<T>(a, w, p, to, &sm_o[0][0][0], sums); });
     }
     finish<T>(a);
 }
@@ -449,12 +473,12 @@ struct Shape {
     static constexpr int CHUNKS = DP * (int)sizeof(T) / 16;
     static constexpr int PITCH = DP * (int)sizeof(T) + (sizeof(T) == 4 ? 32 : 16);
     static constexpr int STAGE = 2 * STEP * PITCH;
-    static constexpr int STAGES = sizeof(T) == 2 ? 3 : DP == 64 ? 2 : DP == 128 ? 3 : DP == 192 ? 2 : 1;
+    static constexpr int STAGES = sizeof(T) == 2 ? 3 : DP == 64 ? 2 : 1;
     static constexpr int BYTES = WARPS * STAGES * STAGE;
 };
 // Resident blocks per SM: what the stages leave room for, fewer where many heads of 64 values take the registers.
 __host__ __device__ constexpr int tensor_blocks(int width, int tiles) { return width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1; }
-__host__ __device__ constexpr int single_blocks(int width, int heads) { return width <= 64 ? (heads <= 4 ? 3 : 2) : 1; }
+__host__ __device__ constexpr int single_blocks(int width, int heads) { return width <= 64 ? (heads <= 4 ? 3 : 2) : width <= 128 ? 3 : width <= 192 ? 2 : 1; }
 
 // A warp's copies of one stretch: steps of STEP tokens, every WARPS-th of the stretch's quarter tiles, into its stages.
 //
@@ -573,10 +597,8 @@ __device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &
             if (d == 0) *reinterpret_cast<float2 *>(slot + a.block_heads * a.dim + 2 * h) = make_float2(mm, ll);
         }
     }
-    if (!whole) {
-        Parts parts;
-        if (last_of_parts(a, s, w, parts, flag)) join_staged<T, HEADS, DP>(a, w, parts, sm_o, bytes);
-    }
+    static_assert((HEADS * (JOIN + 3) + HEADS * DP) * 4 <= Shape<T, DP>::BYTES, "the parts' weights and one part fit");
+    if (!whole) leave_part(a, s, w, flag, [&](const Parts &p, float *to) { join_staged<T, HEADS, DP>(a, w, p, to, sm_o, bytes); });
     __syncthreads();  // the next stretch's copies go where the parts were
 }
 
@@ -920,7 +942,7 @@ cudaError_t launch_single_heads(const AttendArgs &a, unsigned grid, cudaStream_t
 // blocks of a launch that splits sequences: what the SMs hold, and what the counters suffice for
 unsigned split_blocks(int sm_count, int per_sm) {
     const unsigned n = (unsigned)sm_count * (unsigned)per_sm;
-    return n < LT_ARRIVALS ? n : LT_ARRIVALS;
+    return n < LT_ARRIVALS / 2 ? n : LT_ARRIVALS / 2;
 }
 
 }  // namespace

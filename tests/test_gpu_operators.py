@@ -317,6 +317,13 @@ def test_paged_attention_spread_over_blocks(ctx, dtype, heads, kv_heads, dim, pa
             assert torch.equal(y, first)  # whichever block comes last
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page,lengths", [(8, 1, 128, 16, [100000]), (5, 1, 64, 24, [31000, 70000, 40]), (40, 1, 64, 64, [40000]), (2, 1, 36, 16, [50000]), (6, 2, 256, 32, [33, 30000])])
+def test_paged_attention_joined_in_two_steps(ctx, dtype, heads, kv_heads, dim, page, lengths):
+    """So few and so long sequences that hundreds of blocks share each."""
+    test_paged_attention_spread_over_blocks(ctx, dtype, heads, kv_heads, dim, page, lengths)
+
+
 @pytest.mark.parametrize("by", [1, 2, 4])
 def test_paged_attention_unaligned_and_sliced(ctx, by):
     g, n = gen(13), [70, 1, 200]
