@@ -10,6 +10,12 @@
 // (sequence, head block) that lies within one block's part is finished there.  One that is spread over several leaves
 // partial results (maximum, sum, unnormalised output) in scratch memory, and the block that arrives last joins them,
 // always in the list's order, so results do not depend on the arrival.
+//
+// The kernels let the next one on the stream begin late, when their own work is done: blocks that wait beside them for
+// their end cost more than an early launch gains (one sequence of 1013 tokens, 8 key heads of 128 values: 7.8 us against
+// 9.3; four of 7001 to 32768: 61.5 against 62.7).
+#include <algorithm>
+
 #include "operator_device.cuh"
 
 using namespace ltop;
@@ -20,7 +26,7 @@ constexpr int TILE = 64;         // tokens
 constexpr int START = 2;         // tiles that beginning a (sequence, head block) counts for
 constexpr int THREADS = 128;
 constexpr int WARPS = THREADS / 32;
-constexpr uint32_t JOIN = 32;    // parts that are joined at once
+constexpr uint32_t JOIN = 32;    // parts that are joined at once: a lane each
 constexpr uint32_t GROUP = 16;   // more are joined in groups of as many, and then the groups
 constexpr uint32_t MOST_PARTS = GROUP * JOIN;  // blocks that one (sequence, head block) is spread over
 
@@ -360,7 +366,6 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
     __shared__ float2 sums[HEADS];
     __shared__ float sm_o[4][HEADS][NE * 32];
     static_assert(4 * NE * 32 >= (int)JOIN, "the parts' weights fit where the warps' outputs are");
-    pdl_release();
     pdl_wait();
     const T *q = (const T *)a.q, *cache = (const T *)a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -437,6 +442,7 @@ __global__ void __launch_bounds__(THREADS) lt_attend_any(const AttendArgs a) {
         }
         if (!whole) leave_part(a, s, w, &flag, [&](const Parts &p, float *to) { join_any<T>(a, w, p, to, &sm_o[0][0][0], sums); });
     }
+    pdl_release();
     finish<T>(a);
 }
 
@@ -468,25 +474,33 @@ constexpr int STEP = 16;        // tokens a warp takes at a time: a quarter of a
 
 // Sizes of the kernels for heads of up to DP values.  Rows of keys and values in shared memory are padded so that what is
 // read at once falls into different banks: eight rows of a matrix (bf16), four tokens by two chunks (f32).
-template <class T, int DP>
+template <class T, int DP, int HEADS>
 struct Shape {
     static constexpr int CHUNKS = DP * (int)sizeof(T) / 16;
     static constexpr int PITCH = DP * (int)sizeof(T) + (sizeof(T) == 4 ? 32 : 16);
     static constexpr int STAGE = 2 * STEP * PITCH;
-    static constexpr int STAGES = sizeof(T) == 2 ? 3 : DP == 64 ? 2 : 1;
-    static constexpr int BYTES = WARPS * STAGES * STAGE;
+    static constexpr int STAGES = sizeof(T) == 2 ? (DP == 256 ? 3 : 2) : DP == 64 && HEADS <= 4 ? 2 : 1;
+    static constexpr int OUTPUTS = HEADS * (DP + 4) * 4;  // of a warp
+    static constexpr int BYTES = WARPS * (STAGES * STAGE > OUTPUTS ? STAGES * STAGE : OUTPUTS);
 };
-// Resident blocks per SM: what the stages leave room for, fewer where many heads of 64 values take the registers.
-__host__ __device__ constexpr int tensor_blocks(int width, int tiles) { return width <= 64 ? (tiles == 1 ? 4 : tiles == 2 ? 3 : 2) : width <= 128 ? 2 : 1; }
-__host__ __device__ constexpr int single_blocks(int width, int heads) { return width <= 64 ? (heads <= 4 ? 3 : 2) : width <= 128 ? 3 : width <= 192 ? 2 : 1; }
+// Resident blocks per SM: what the stages and the registers leave room for.  More blocks with fewer stages each carry more
+// than the other way round, until the registers run short (us, bf16, 16 sequences of 2000 to 3000 tokens, 16 heads of 64:
+// 36.4 with two stages and five blocks, 39.7 with three and four, 38.0 with two and six, 36.6 with one and six; 8 of them,
+// 8 heads of 128: 21.3 with two and three, 23.4 with three and two, 21.9 with one and four; 8 heads of 192: 30.7 with two
+// and two, 37.2 with three and one; f32, 28 of them, 8 key heads of 64 shared by 16 each: 106 with one and four, 134 with
+// two and two; 28 of 300 to 500 tokens, 32 heads of 128: 64 with one and three, 84 with three and one).
+__host__ __device__ constexpr int tensor_blocks(int width, int tiles) {
+    return width <= 64 ? (tiles == 1 ? 5 : tiles == 2 ? 4 : 2) : width <= 128 ? (tiles == 1 ? 3 : 2) : width <= 192 ? 2 : 1;
+}
+__host__ __device__ constexpr int single_blocks(int width, int heads) { return width <= 64 ? (heads <= 4 ? 3 : 4) : width <= 128 ? 3 : width <= 192 ? 2 : 1; }
 
 // A warp's copies of one stretch: steps of STEP tokens, every WARPS-th of the stretch's quarter tiles, into its stages.
 //
 // Page numbers are fetched ahead of the copies they address.  Where a step never crosses a page (WHOLE_STEPS) one number
 // serves a step, and the lanes hold those of the next 32 steps; otherwise lane i has the number of token i.
-template <class T, int DP, bool WHOLE_STEPS>
+template <class T, int DP, int HEADS, bool WHOLE_STEPS>
 struct Stages {
-    using S = Shape<T, DP>;
+    using S = Shape<T, DP, HEADS>;
     static constexpr int N = 16 / (int)sizeof(T);
     const AttendArgs &a;
     const Stretch &w;
@@ -597,7 +611,7 @@ __device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &
             if (d == 0) *reinterpret_cast<float2 *>(slot + a.block_heads * a.dim + 2 * h) = make_float2(mm, ll);
         }
     }
-    static_assert((HEADS * (JOIN + 3) + HEADS * DP) * 4 <= Shape<T, DP>::BYTES, "the parts' weights and one part fit");
+    static_assert((HEADS * (JOIN + 3) + HEADS * DP) * 4 <= Shape<T, DP, HEADS>::BYTES, "the parts' weights and one part fit");
     if (!whole) leave_part(a, s, w, flag, [&](const Parts &p, float *to) { join_staged<T, HEADS, DP>(a, w, p, to, sm_o, bytes); });
     __syncthreads();  // the next stretch's copies go where the parts were
 }
@@ -605,12 +619,12 @@ __device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &
 // f32, 16-byte aligned rows, head sizes filled up to DP with zeros; up to NH query heads per block.
 //
 // Full binary32 products rule the matrix units out (in two tf32 parts each, taking the numbers apart cost more than these
-// products: 40 us against 30 on 16 sequences of 16 heads of 64 values), and memory is slow enough for the others.  Two
+// products: 40 us against 32 on 16 sequences of 16 heads of 64 values), and memory is slow enough for the others.  Two
 // lanes share a token's key, every other chunk each; the weights go through shared memory to all lanes, which have the
 // output's values between them, two neighbouring ones of every 64.  Warps, stages and joins as in lt_attend_tensor.
 template <int DP, int NH, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_single(const AttendArgs a) {
-    using S = Shape<float, DP>;
+    using S = Shape<float, DP, NH>;
     constexpr int J = DP / 64;
     extern __shared__ __align__(128) unsigned char stage_mem[];
     __shared__ uint32_t flag;
@@ -619,13 +633,12 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
     __shared__ __align__(16) float sm_p[WARPS][NH][STEP], sm_q[NH][DP];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, token = lane >> 1, half = lane & 1;
     unsigned char *mine = stage_mem + warp * S::STAGES * S::STAGE;
-    pdl_release();
     pdl_wait();
     Share s = my_share(a);
     const uint32_t start = s.idx;
     Stretch w;
     for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
-        Stages<float, DP, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
+        Stages<float, DP, NH, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
         for (int x = threadIdx.x; x < NH * DP; x += THREADS) {  // (the stretch before has ended with a barrier)
             const int h = x / DP, d = x % DP;
             sm_q[h][d] = h < w.heads && d < (int)a.dim ? ((const float *)a.q)[(uint64_t)w.b * a.q_pitch + (uint64_t)(w.h0 + h) * a.dim + d] * a.scale : 0.f;
@@ -710,7 +723,6 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
         }
         copy_wait<0>();
         float *sm_o = reinterpret_cast<float *>(stage_mem);  // [WARPS][NH][DP + 4]
-        static_assert(WARPS * NH * (DP + 4) * 4 <= S::BYTES, "the warps' outputs fit");
         __syncthreads();  // every warp is done with its stages
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
@@ -722,6 +734,7 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
         __syncthreads();
         leave_stretch<float, NH, DP>(a, s, w, s.idx == start, sm_o, sm_m, sm_l, S::BYTES, &flag);
     }
+    pdl_release();
     finish<float>(a);
 }
 
@@ -735,8 +748,9 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
 // in the loop -- and its own running maximum and sum; warps are joined once per stretch.
 template <int DP, int NT, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tensor(const AttendArgs a) {
-    using S = Shape<__nv_bfloat16, DP>;
-    constexpr int HEADS = 8 * NT, STAGES = S::STAGES, KS = DP / 16;
+    constexpr int HEADS = 8 * NT;
+    using S = Shape<__nv_bfloat16, DP, HEADS>;
+    constexpr int STAGES = S::STAGES, KS = DP / 16;
     extern __shared__ __align__(128) unsigned char stage_mem[];
     __shared__ uint32_t flag;
     __shared__ float sm_m[WARPS][HEADS], sm_l[WARPS][HEADS];
@@ -744,13 +758,12 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, eighth = lane >> 2;
     unsigned char *mine = stage_mem + warp * STAGES * S::STAGE;
     const __nv_bfloat16 *q = (const __nv_bfloat16 *)a.q;
-    pdl_release();
     pdl_wait();
     Share s = my_share(a);
     const uint32_t start = s.idx;
     Stretch w;
     for (uint32_t done = 0; next_stretch(a, s, w, done); done = w.items) {
-        Stages<__nv_bfloat16, DP, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
+        Stages<__nv_bfloat16, DP, HEADS, WHOLE_STEPS> stages(a, w, mine, sm_mask[warp]);
         uint32_t qf[NT][KS][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -851,7 +864,6 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
         }
         copy_wait<0>();
         float *sm_o = reinterpret_cast<float *>(stage_mem);  // [WARPS][HEADS][DP + 4]
-        static_assert(WARPS * HEADS * (DP + 4) * 4 <= S::BYTES, "the warps' outputs fit");
         __syncthreads();  // every warp is done with its stages
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -872,6 +884,7 @@ __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tens
         __syncthreads();
         leave_stretch<__nv_bfloat16, HEADS, DP>(a, s, w, s.idx == start, sm_o, sm_m, sm_l, S::BYTES, &flag);
     }
+    pdl_release();
     finish<__nv_bfloat16>(a);
 }
 
@@ -903,7 +916,7 @@ cudaError_t launch_any(const AttendArgs &a, unsigned grid, cudaStream_t stream) 
 template <int DP, int NT, bool WHOLE>
 cudaError_t launch_tensor(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    constexpr size_t bytes = Shape<__nv_bfloat16, DP>::BYTES;
+    constexpr size_t bytes = Shape<__nv_bfloat16, DP, 8 * NT>::BYTES;
     const cudaError_t e = allow_shared(lt_attend_tensor<DP, NT, WHOLE>, bytes, ready);
     if (e != cudaSuccess) return e;
     return launch_pdl(lt_attend_tensor<DP, NT, WHOLE>, grid, THREADS, bytes, stream, a);
@@ -922,7 +935,7 @@ cudaError_t launch_tensor_heads(const AttendArgs &a, unsigned grid, cudaStream_t
 template <int DP, int NH, bool WHOLE>
 cudaError_t launch_single(const AttendArgs &a, unsigned grid, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    constexpr size_t bytes = Shape<float, DP>::BYTES;
+    constexpr size_t bytes = Shape<float, DP, NH>::BYTES;
     const cudaError_t e = allow_shared(lt_attend_single<DP, NH, WHOLE>, bytes, ready);
     if (e != cudaSuccess) return e;
     return launch_pdl(lt_attend_single<DP, NH, WHOLE>, grid, THREADS, bytes, stream, a);
@@ -987,7 +1000,11 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     const bool rows = width && is_aligned(a.cache, 16) && is_aligned(a.q, 4) && (o.dtype == LT_F32 || a.q_pitch % 2 == 0) && is_aligned(a.out, 16);
     a.block_heads = rows ? row_heads(o.dtype, width, a.group) : ANY_HEADS;
     a.head_blocks = (a.group + a.block_heads - 1) / a.block_heads;
-    const unsigned grid = !a.partial ? a.batch * a.kv_heads * a.head_blocks : split_blocks(sm_count, rows ? row_blocks(o.dtype, width, (int)a.block_heads) : ANY_BLOCKS);
+    unsigned grid = a.batch * a.kv_heads * a.head_blocks;
+    if (a.partial) {  // (no more blocks than the page table has room for items)
+        const uint64_t items = (uint64_t)grid * (((uint64_t)a.table_width * a.page + TILE - 1) / TILE + START);
+        grid = (unsigned)std::min<uint64_t>(items, split_blocks(sm_count, rows ? row_blocks(o.dtype, width, (int)a.block_heads) : ANY_BLOCKS));
+    }
     if (!rows) return o.dtype == LT_BF16 ? launch_any<__nv_bfloat16>(a, grid, stream) : launch_any<float>(a, grid, stream);
     if (o.dtype == LT_F32) {
         switch (width) {
