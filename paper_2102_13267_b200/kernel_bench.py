@@ -1,6 +1,6 @@
 """Kernel-only timing of the benchmark configurations and of the common fusion groups (also the driver for ncu captures).
 
-    python -m paper_2102_13267_b200.kernel_bench [c1,c2,c2p,c3,c4,c5,idioms,long,reduce,reduced] [--iters N] [--sets K] [key=value ...]
+    python -m paper_2102_13267_b200.kernel_bench [c1,c2,c2p,c3,c4,c5,idioms,long,reduce,reduced,operators] [--iters N] [--sets K] [key=value ...]
 
 For each configuration: traces the graph and flushes it `iters` times over rotating buffer sets (larger than L2
 together), queued behind a busy stream so that the GPU, not the host, sets the pace.  Two figures are printed:
@@ -31,7 +31,7 @@ def main() -> None:
     ap.add_argument("--iters", type=int, default=40)
     ap.add_argument("--sets", type=int, default=0, help="buffer sets to rotate through (0 = enough for 1 GB)")
     ap.add_argument("--long-shapes", default="8192x16384,2048x65536", help="rows x columns of the `long` case")
-    ap.add_argument("--only", default="", help="of the idioms / long / reduce cases, run those whose name contains this")
+    ap.add_argument("--only", default="", help="of the idioms / long / reduce / operators cases, run those whose name contains this")
     ap.add_argument("options", nargs="*")
     args = ap.parse_args()
     which = args.configs.split(",")
@@ -240,6 +240,39 @@ def main() -> None:
                 return out
 
             generic(iname, nbytes, make, lambda c, s_, trace=trace: trace(c, s_, 4096))
+    if "operators" in which:  # the transformer operators at serving and training sizes
+        def ints(values):
+            return torch.tensor(values, dtype=torch.int32, device=dev)
+
+        tokens, heads, kv, dim, page = 8192, 32, 8, 128, 16
+        table = lt.rotary_table(dim)
+
+        def positions(c):
+            return [c.from_torch(torch.arange(tokens, dtype=torch.int32, device=dev)), c.leaf(table, "u32")]
+
+        generic("rotary 8192x32x128", 4 * tokens * heads * dim, lambda c: [c.from_torch(bf16((tokens, heads, dim))), *positions(c)],
+                lambda c, s_: c.rotary(*s_))
+        generic("append 8192x8x128", 8 * tokens * kv * dim,
+                lambda c: [c.from_torch(bf16((tokens // page, 2, page, kv, dim))), c.from_torch(bf16((tokens, kv, dim))), c.from_torch(bf16((tokens, kv, dim))),
+                           c.from_torch(torch.randperm(tokens, device=dev).to(torch.int32)), *positions(c)],
+                lambda c, s_: c.cache_append(*s_))
+        for name, sequences, shortest, longest in (("attend 1x1000", 1, 1000, 1000), ("attend 64x17..4096", 64, 17, 4096), ("attend 1x100000", 1, 100000, 100000)):
+            lengths = [shortest + (longest - shortest) * i // max(1, sequences - 1) for i in range(sequences)]
+            pages = [(n + page - 1) // page for n in lengths]
+
+            def make(c, lengths=lengths, pages=pages):
+                order = torch.randperm(sum(pages)).to(torch.int32)
+                rows = torch.zeros((len(pages), max(pages)), dtype=torch.int32)
+                for i, n in enumerate(pages):
+                    rows[i, :n] = order[sum(pages[:i]):sum(pages[:i + 1])]
+                return [c.from_torch(bf16((len(lengths), heads, dim))), c.from_torch(bf16((sum(pages), 2, page, kv, dim))), c.from_torch(rows.to(dev)), c.from_torch(ints(lengths))]
+
+            generic(name, 4 * kv * dim * sum(lengths), make, lambda c, s_: c.paged_attention(*s_, scale=dim ** -0.5))
+        generic("rms_norm 8 bit", (3 * 2 + 1) * 8192 * 4096, lambda c: [c.from_torch(bf16((8192, 4096))), c.from_torch(torch.ones(4096, device=dev)), c.from_torch(bf16((8192, 4096)))],
+                lambda c, s_: c.rms_norm(s_[0], s_[1], residual=s_[2], eight_bit=True, group=128))
+        generic("rms_norm_grad", 4 * 2 * 16384 * 1024,
+                lambda c: [c.from_torch(bf16((16384, 1024))), c.from_torch(bf16((16384, 1024))), c.from_torch(torch.ones(1024, device=dev)), c.from_torch(bf16((16384, 1024)))],
+                lambda c, s_: c.rms_norm_grad(*s_[:3], residual_grad=s_[3]))
     if "c5" in which:
         shapes = parameter_shapes()
         ctx = context()
