@@ -748,7 +748,7 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
 // tokens along the columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps
 // the weights to 2^-17 and costs one more product.  Each warp has steps and a copy pipeline of its own -- no barrier
 // in the loop -- and its own running maximum and sum; warps are joined once per stretch.  64 sequences of 17 to 4096
-// tokens, 32 heads on 8 key heads of 128: 92.6 us, 5.8 TB/s; the tensor and issue units are a third busy, what is left is
+// tokens, 32 heads on 8 key heads of 128: 92.6 us, 5.8 TB/s; issue slots are 34 % busy, the tensor units 13 %, what is left is
 // latency: beginning stretches, joining parts, and SMs that reach memory more slowly than others.
 template <int DP, int NT, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tensor(const AttendArgs a) {

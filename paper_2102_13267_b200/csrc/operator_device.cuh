@@ -92,6 +92,11 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
     const int bytes = there ? 16 : 0;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+template <int BYTES>
+__device__ __forceinline__ void copy_piece(uint32_t dst, const void *src) {  // of 8 or 16 bytes
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -113,6 +118,14 @@ __device__ __forceinline__ void unpack(const uint4 &v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint2 &v, float (&f)[4]) {
+    const uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
         f[2 * i] = __uint_as_float(w[i] << 16);
         f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
@@ -140,6 +153,13 @@ __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
 }
 __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
     return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// N values as the piece of memory V that holds them
+template <class V, int N>
+__device__ __forceinline__ V packed(const float (&f)[N]) {
+    if constexpr (sizeof(V) == 8) return make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    else return pack(f);
 }
 
 // Division of 32-bit numbers by one known on the host (as fastdiv_make does for the row kernels).

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "operator_device.cuh"
 
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(256) lt_turn_any(const TurnArgs a) {
 // 25.7 and 14.4 us; 2 and 2: 25.6 and 15.5; 2 and 3: 26.3 and 16.6; 1 and 4: 25.4 and 18.5; 4 and 2: 27.7 and 16.3)
 constexpr int TURN_THREADS = 256, TURN_FLIGHT = 4, TURN_STAGES = 1;
 constexpr uint32_t TURN_ANGLES = 2048;  // of a batch, at most: 16 KB, twice
-constexpr size_t TURN_RING = (size_t)TURN_STAGES * TURN_FLIGHT * 2 * TURN_THREADS * 16;
+__host__ __device__ constexpr size_t turn_ring(int bytes) { return (size_t)TURN_STAGES * TURN_FLIGHT * 2 * TURN_THREADS * bytes; }
 
 struct TurnShape {
     uint32_t batch;             // tokens a block works on at once
@@ -130,19 +131,22 @@ struct TurnShape {
     Divisor span_by, turned_by, passed_by, value_by, pairs;
 };
 
-// 16 bytes at a time.  A unit is what a thread reads and writes of a token: two chunks whose values form pairs, one chunk
+// BYTES (16, or 8 where 16 do not fit the pairs) at a time.  A unit is what a thread reads and writes of a token: two chunks whose values form pairs, one chunk
 // of neighbouring pairs (interleaved), one that passes through, or one of the values (cache_append).  A thread keeps its
 // unit and walks over tokens, so what it addresses is found once.  The bound is memory; the angles would not be free if
 // every head computed them (a sine and a cosine are some fifty instructions), so a block computes those of a batch of
 // tokens once, into shared memory, one batch ahead.  The chunks of the next batches are on their way meanwhile: each
 // thread copies its own ahead and reads them back, as in lt_norm_rows.  Rotary 8192 x 32 x 128 bf16: 24.1 us, 5.6 TB/s;
 // append 8192 x 8 x 128 bf16: 14.5 us, 4.6 TB/s.
-template <class T, bool APPEND, bool INTER>
+// With 8 bytes, rotary 8192 x 32 x 80 bf16, 40 turned in halves of 20: 19.5 us, against 43 with lt_turn_any.
+template <class T, bool APPEND, bool INTER, int BYTES>
 __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs a, const TurnShape sh) {
-    constexpr int N = Chunk<T>::N;
-    extern __shared__ uint4 turn_mem[];  // the ring [STAGES][FLIGHT][2][threads], then twice cosines and sines [batch][pairs]
+    constexpr int N = BYTES / (int)sizeof(T);
+    using V = typename std::conditional<BYTES == 16, uint4, uint2>::type;
+    extern __shared__ uint4 turn_room[];
+    V *const turn_mem = reinterpret_cast<V *>(turn_room);  // the ring [STAGES][FLIGHT][2][threads], then twice cosines and sines [batch][pairs]
     __shared__ uint64_t sm_at[2][TURN_THREADS];  // where a token goes (all ones: nowhere)
-    float *const angles = reinterpret_cast<float *>(turn_mem + TURN_RING / 16);
+    float *const angles = reinterpret_cast<float *>(turn_room + turn_ring(BYTES) / 16);
     const uint32_t half = sh.batch * a.pairs;
     // the block's tokens
     const uint64_t t0 = a.tokens * blockIdx.x / gridDim.x, t1 = a.tokens * (blockIdx.x + 1) / gridDim.x;
@@ -182,8 +186,8 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
 #pragma unroll
         for (int k = 0; k < TURN_FLIGHT; ++k) {
             if (busy && fetched < tokens) {
-                copy16(mine + ((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS * 16, src, true);
-                if (two) copy16(mine + ((stage * TURN_FLIGHT + k) * 2 + 1) * TURN_THREADS * 16, src + a.pairs, true);
+                copy_piece<BYTES>(mine + ((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS * BYTES, src);
+                if (two) copy_piece<BYTES>(mine + ((stage * TURN_FLIGHT + k) * 2 + 1) * TURN_THREADS * BYTES, src + a.pairs);
             }
             fetched += sh.side;
             src += step;
@@ -218,9 +222,9 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
             if (!busy || first + token >= tokens) break;
             const uint64_t at = sm_at[which][token];
             if (APPEND && at == ~0ull) continue;
-            const uint4 lo = turn_mem[((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS + threadIdx.x];
+            const V lo = turn_mem[((stage * TURN_FLIGHT + k) * 2) * TURN_THREADS + threadIdx.x];
             if (!turns) {
-                *reinterpret_cast<uint4 *>(dst + at) = lo;
+                *reinterpret_cast<V *>(dst + at) = lo;
                 continue;
             }
             float p[N], q[N];
@@ -232,7 +236,7 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
                     q[2 * i] = p[2 * i] * c[i] - p[2 * i + 1] * s[i];
                     q[2 * i + 1] = p[2 * i] * s[i] + p[2 * i + 1] * c[i];
                 }
-                *reinterpret_cast<uint4 *>(dst + at) = pack(q);
+                *reinterpret_cast<V *>(dst + at) = packed<V>(q);
             } else {
                 const float4 *c = reinterpret_cast<const float4 *>(cosines + token * a.pairs + chunk * N), *s = reinterpret_cast<const float4 *>(sines + token * a.pairs + chunk * N);
                 unpack(turn_mem[((stage * TURN_FLIGHT + k) * 2 + 1) * TURN_THREADS + threadIdx.x], q);
@@ -247,8 +251,8 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
                         q[4 * i + j] = fp * si[j] + fq * co[j];
                     }
                 }
-                *reinterpret_cast<uint4 *>(dst + at) = pack(p);
-                *reinterpret_cast<uint4 *>(dst + at + a.pairs) = pack(q);
+                *reinterpret_cast<V *>(dst + at) = packed<V>(p);
+                *reinterpret_cast<V *>(dst + at + a.pairs) = packed<V>(q);
             }
         }
         issue(stage);
@@ -256,45 +260,54 @@ __global__ void __launch_bounds__(TURN_THREADS, 4) lt_turn_chunks(const TurnArgs
     }
 }
 
-template <class T, bool APPEND, bool INTER>
+template <class T, bool APPEND, bool INTER, int BYTES>
 cudaError_t launch_turn_chunks(const TurnArgs &a, const TurnShape &sh, uint32_t across, int sm_count, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    constexpr size_t most = TURN_RING + 2 * TURN_ANGLES * 8;
-    const cudaError_t e = allow_shared(lt_turn_chunks<T, APPEND, INTER>, most, ready);
+    constexpr size_t most = turn_ring(BYTES) + 2 * TURN_ANGLES * 8;
+    const cudaError_t e = allow_shared(lt_turn_chunks<T, APPEND, INTER, BYTES>, most, ready);
     if (e != cudaSuccess) return e;
     // as many blocks as the SMs hold (by threads, by shared memory), each going on to further tokens
-    const size_t mem = TURN_RING + (size_t)2 * sh.batch * a.pairs * 8;
+    const size_t mem = turn_ring(BYTES) + (size_t)2 * sh.batch * a.pairs * 8;
     const uint64_t per_sm = std::min<uint64_t>(4, 220 * 1024 / (mem + 5 * 1024)), wave = std::max<uint64_t>(1, (uint64_t)sm_count * per_sm / across);
     const uint64_t batches = (a.tokens + sh.batch - 1) / sh.batch;
     const dim3 grid((unsigned)std::min(batches, wave), across);
-    return launch_pdl_shared(lt_turn_chunks<T, APPEND, INTER>, grid, TURN_THREADS, mem, stream, a, sh);
+    return launch_pdl_shared(lt_turn_chunks<T, APPEND, INTER, BYTES>, grid, TURN_THREADS, mem, stream, a, sh);
+}
+
+// lt_turn_chunks, if pieces of BYTES fit the shape and the addresses.
+template <class T, bool APPEND, int BYTES>
+bool launch_turn_pieces(const TurnArgs &a, int sm_count, cudaStream_t stream, cudaError_t *e) {
+    constexpr uint32_t N = BYTES / sizeof(T);
+    const bool fits = a.dim % N == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % N == 0 && a.x_pitch % N == 0 && is_aligned(a.x, BYTES) && is_aligned(a.out, BYTES) &&
+                      (!APPEND || (a.v_pitch % N == 0 && is_aligned(a.v, BYTES)));
+    const uint64_t units = (uint64_t)(a.dim / N - (a.interleaved ? 0 : a.pairs / N) + (APPEND ? a.dim / N : 0)) * a.heads;
+    if (!fits || TURN_FLIGHT * a.pairs > TURN_ANGLES || units >= (1u << 20) || a.tokens >= (1ull << 31)) return false;
+    TurnShape sh;
+    sh.turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N;
+    sh.passed = (a.dim - 2 * a.pairs) / N;
+    sh.units = (uint32_t)units;
+    // a token's units over as few blocks as hold them, evenly; several tokens side by side where they leave room
+    const uint32_t across = (sh.units + TURN_THREADS - 1) / TURN_THREADS;
+    sh.span = (sh.units + across - 1) / across;
+    sh.side = TURN_THREADS / sh.span;
+    if (a.pairs) sh.side = std::min(sh.side, TURN_ANGLES / (TURN_FLIGHT * a.pairs));
+    sh.side = std::min<uint32_t>(sh.side, TURN_THREADS / TURN_FLIGHT);
+    sh.batch = sh.side * TURN_FLIGHT;
+    sh.span_by = Divisor::make(sh.span);
+    sh.turned_by = Divisor::make(sh.turned ? sh.turned : 1);
+    sh.passed_by = Divisor::make(sh.passed ? sh.passed : 1);
+    sh.value_by = Divisor::make(a.dim / N);
+    sh.pairs = Divisor::make(a.pairs ? a.pairs : 1);
+    *e = a.interleaved ? launch_turn_chunks<T, APPEND, true, BYTES>(a, sh, across, sm_count, stream) : launch_turn_chunks<T, APPEND, false, BYTES>(a, sh, across, sm_count, stream);
+    return true;
 }
 
 template <class T, bool APPEND>
 cudaError_t launch_turn(const TurnArgs &a, int sm_count, cudaStream_t stream) {
-    constexpr uint32_t N = Chunk<T>::N;
-    const bool chunks = a.dim % N == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % N == 0 && a.x_pitch % N == 0 && is_aligned(a.x, 16) && is_aligned(a.out, 16) &&
-                        (!APPEND || (a.v_pitch % N == 0 && is_aligned(a.v, 16)));
-    const uint64_t units = (uint64_t)(a.dim / N - (a.interleaved ? 0 : a.pairs / N) + (APPEND ? a.dim / N : 0)) * a.heads;
-    if (chunks && TURN_FLIGHT * a.pairs <= TURN_ANGLES && units < (1u << 20) && a.tokens < (1ull << 31)) {
-        TurnShape sh;
-        sh.turned = (a.interleaved ? 2 * a.pairs : a.pairs) / N;
-        sh.passed = (a.dim - 2 * a.pairs) / N;
-        sh.units = (uint32_t)units;
-        // a token's units over as few blocks as hold them, evenly; several tokens side by side where they leave room
-        const uint32_t across = (sh.units + TURN_THREADS - 1) / TURN_THREADS;
-        sh.span = (sh.units + across - 1) / across;
-        sh.side = TURN_THREADS / sh.span;
-        if (a.pairs) sh.side = std::min(sh.side, TURN_ANGLES / (TURN_FLIGHT * a.pairs));
-        sh.side = std::min<uint32_t>(sh.side, TURN_THREADS / TURN_FLIGHT);
-        sh.batch = sh.side * TURN_FLIGHT;
-        sh.span_by = Divisor::make(sh.span);
-        sh.turned_by = Divisor::make(sh.turned ? sh.turned : 1);
-        sh.passed_by = Divisor::make(sh.passed ? sh.passed : 1);
-        sh.value_by = Divisor::make(a.dim / N);
-        sh.pairs = Divisor::make(a.pairs ? a.pairs : 1);
-        return a.interleaved ? launch_turn_chunks<T, APPEND, true>(a, sh, across, sm_count, stream) : launch_turn_chunks<T, APPEND, false>(a, sh, across, sm_count, stream);
-    }
+    cudaError_t e = cudaSuccess;
+    if (launch_turn_pieces<T, APPEND, 16>(a, sm_count, stream, &e)) return e;
+    if constexpr (sizeof(T) == 2)
+        if (launch_turn_pieces<T, APPEND, 8>(a, sm_count, stream, &e)) return e;
     const uint64_t total = a.tokens * (a.dim - a.pairs);
     const uint64_t blocks = (total + 255) / 256, most = (uint64_t)sm_count * 32;
     return launch_pdl(lt_turn_any<T, APPEND>, (unsigned)(blocks < most ? blocks : most), 256, (size_t)0, stream, a);

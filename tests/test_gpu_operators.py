@@ -65,6 +65,28 @@ def test_rotary(ctx, lt, dtype, tokens, heads, dim, rotated, interleaved, invers
     close(fetch(ctx, y), want, bound)
 
 
+@pytest.mark.parametrize("tokens,heads,dim,rotated,interleaved", [
+    (1, 3, 80, 40, False), (40, 6, 80, 40, False), (9000, 3, 100, 24, False), (70, 5, 20, 16, True), (33, 2, 12, 8, False), (300, 40, 36, 36, True), (5000, 33, 68, 56, False)])
+def test_rotary_and_append_in_pieces_of_eight_bytes(ctx, lt, tokens, heads, dim, rotated, interleaved):
+    """bf16 heads whose pairs do not come in eights."""
+    g, t = gen(tokens + dim), torch.bfloat16
+    k, v = normal(g, tokens, heads, dim, dtype=t), normal(g, tokens, heads, dim, dtype=t)
+    pos = torch.randint(0, 1 << 20, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    want, bound = ref.rotary(k, pos, ref.frequencies(rotated), interleaved)
+    turned = (ctx.from_torch(pos), ctx.leaf(lt.rotary_table(rotated), "u32"))
+    close(fetch(ctx, ctx.rotary(ctx.from_torch(k), *turned, interleaved=interleaved)), want, bound)
+    pages = (tokens + 15) // 16
+    cache = empty_cache(g, pages, 16, heads, dim, True, t)
+    slots = torch.randperm(pages * 16, generator=g, device="cuda")[:tokens].to(torch.int32)
+    lc = ctx.from_torch(cache)
+    ctx.cache_append(lc, ctx.from_torch(k), ctx.from_torch(v), ctx.from_torch(slots), *turned, head_major=True, interleaved=interleaved)
+    ctx.barrier(blocking=True)
+    assert ctx.device_ptr(lc) == cache.data_ptr()
+    after, at = token_view(cache, True).cpu(), slots.cpu().long()
+    close(after[0][at], want, bound, "keys")
+    assert torch.equal(after[1][at], v.cpu())
+
+
 def test_rotary_gradient_is_the_transposed_rotation(ctx, lt):
     """<dy, rotary(x)> differentiated: the inverse applied to dy is the gradient, checked against differences in 64 bits."""
     g = gen(5)
