@@ -250,9 +250,12 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
     void *arrivals = nullptr;
     if (plan.needs_arrivals && !dry) {
         cudaError_t ae = cudaSuccess;
-        if (c->static_mode) {
+        // (a stream that is being captured would set a new context's counters to zero only when the graph runs)
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        if (!c->static_mode && !c->arrivals) ae = cudaStreamIsCapturing(c->stream, &capture);
+        if (ae == cudaSuccess && (c->static_mode || capture != cudaStreamCaptureStatusNone)) {
             ae = lt_static_arrivals(&arrivals);
-        } else if (!c->arrivals) {
+        } else if (ae == cudaSuccess && !c->arrivals) {
             arrivals = ctx_alloc(c, LT_ARRIVALS * sizeof(unsigned int));
             if (!arrivals) {
                 release_all(true);

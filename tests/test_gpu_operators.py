@@ -746,6 +746,42 @@ def test_captured_flushes(lt):
         c.close()
 
 
+def test_first_attention_of_a_context_is_captured(lt):
+    """An ordinary barrier under capture, in a context that has flushed no attention yet: the graph and the flushes after
+    it do not depend on counters that only the graph sets."""
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        warm, c = lt.LazyContext(device=0, stream=s.cuda_stream), lt.LazyContext(device=0, stream=s.cuda_stream)
+        g = gen(47)
+        n = [5000, 300]
+        cache, table = paged(g, n, 16, 2, 64, False, torch.bfloat16)
+        q, out, ln = normal(g, 2, 8, 64, dtype=torch.bfloat16), torch.zeros(2, 8, 64, device="cuda", dtype=torch.bfloat16), torch.tensor(n, dtype=torch.int32, device="cuda")
+
+        def step(ctx):
+            handles = [ctx.from_torch(t) for t in (q, cache, table, ln, out)]
+            ctx.paged_attention(*handles[:4], scale=0.125, out=handles[4])
+            ctx.barrier()
+            return handles
+
+        kept = [step(warm)]
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            kept.append(step(c))
+        kept.append(step(c))
+        s.synchronize()
+        want = ref.attention(q, cache, table, n, 0.125, False)
+        close(out, *want)
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            s.synchronize()
+            close(out, *want)
+        del graph, kept
+        warm.close(), c.close()
+
+
 def test_replay(ctx, lt):
     """lt_replay runs the step again on the tensors' current values."""
     g = gen(44)
