@@ -464,6 +464,7 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// (2 ulp; a weight below 2^-126 of the largest counts nothing)
 __device__ __forceinline__ float power2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -623,7 +624,7 @@ __device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &
 // lanes share a token's key, every other chunk each; the weights go through shared memory to all lanes, which have the
 // output's values between them, two neighbouring ones of every 64.  Warps, stages and joins as in lt_attend_tensor.
 // 28 sequences of 300 to 500 tokens, 32 heads of 128: 64 us, 5.7 TB/s; with 16 query heads per key head the products bound
-// it (28 of 1500 to 2000, 8 key heads of 64: 106 us, 1.9 TB/s).
+// it (28 of 1500 to 2000, 8 key heads of 64: 92 us, 2.2 TB/s; 106 when each head's maximum was followed at once).
 template <int DP, int NH, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_single(const AttendArgs a) {
     using S = Shape<float, DP, NH>;
@@ -678,16 +679,24 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
                     }
                 }
                 const bool in = (mask >> token) & 1u;
+                float top[NH];
+                bool larger = false;
 #pragma unroll
                 for (int h = 0; h < NH; ++h) {
-                    float v = c[h] + __shfl_xor_sync(0xffffffffu, c[h], 1);
-                    v = in ? v : -INFINITY;
-                    float top = v;
+                    const float v = c[h] + __shfl_xor_sync(0xffffffffu, c[h], 1);
+                    top[h] = c[h] = in ? v : -INFINITY;
+                }
 #pragma unroll
-                    for (int d = 2; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    if (top > m[h]) {  // (the same in all lanes)
-                        const float f = exp2f(m[h] - top);
-                        m[h] = top;
+                for (int d = 2; d < 32; d <<= 1)
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], d));
+#pragma unroll
+                for (int h = 0; h < NH; ++h) larger |= top[h] > m[h];
+                if (larger) {  // (the same in all lanes)
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) {
+                        const float n = fmaxf(m[h], top[h]), f = power2(m[h] - (n == -INFINITY ? 0.f : n));
+                        m[h] = n;
                         l[h] *= f;
 #pragma unroll
                         for (int j = 0; j < J; ++j) {
@@ -695,7 +704,10 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
                             o[h][j][1] *= f;
                         }
                     }
-                    const float p = exp2f(v - (m[h] == -INFINITY ? 0.f : m[h]));
+                }
+#pragma unroll
+                for (int h = 0; h < NH; ++h) {
+                    const float p = power2(c[h] - (m[h] == -INFINITY ? 0.f : m[h]));
                     l[h] += p;  // (twice, once in each of the token's lanes)
                     if (half == 0) sm_p[warp][h][token] = p;
                 }
