@@ -429,6 +429,10 @@ lt_status lt_replay_set_slot(lt_ctx *ctx, uint32_t slot, int as_integer, double 
  * LT_OP_PAGED_ATTENTION), which keeps the previous call's contents: two flushes that may overlap
  * on the GPU (different streams, no ordering) race on it and must be ordered by the caller.  No kernel of the library reads a temporary before writing
  * it; `clear_first` non-zero zero-fills the array on the stream before the flush all the same.
+ * Graphs that captured such flushes are flushes here, replay by replay.  A captured lt_barrier that runs
+ * transformer operators does not share: its graph has temporaries, counters and (with allocator
+ * callbacks) results of its own, obtained during the capture, so such graphs may replay side by
+ * side, and after their context is destroyed, as long as the memory they were given lives.
  */
 #define LT_STATIC_SCRATCH_MAX_BYTES (32u << 20)
 lt_status lt_barrier_static_scratch(lt_ctx *ctx, int blocking, int clear_first);

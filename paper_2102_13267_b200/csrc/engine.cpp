@@ -439,6 +439,9 @@ void *ctx_alloc(lt_ctx *c, size_t bytes) {
     return p;
 }
 
+// A block that never enters the pool: it comes from the allocator and goes back there when it is freed (ctx_free).
+void *ctx_alloc_unpooled(lt_ctx *c, size_t bytes) { return raw_alloc(c, (std::max<size_t>(bytes, 16) + 511u) & ~(size_t)511u); }
+
 void ctx_free(lt_ctx *c, void *p) {
     if (!p) return;
     auto it = c->block_size.find(p);

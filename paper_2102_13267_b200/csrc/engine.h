@@ -183,6 +183,7 @@ struct Plan {
     uint64_t hash[2];
     std::vector<uint8_t> canon_bytes;
     uint32_t n_params = 0, n_dyn = 0;
+    bool has_operators = false;
     bool needs_arrivals = false;  // an operator whose blocks share a result is in it
     std::vector<OutputPlan> outputs;
     std::vector<size_t> temp_bytes;
@@ -408,6 +409,7 @@ const char *op_name(int op);
 int64_t shape_numel(const int64_t *dims, int rank);
 lt_status fail(lt_ctx *c, lt_status s, const std::string &msg);
 void *ctx_alloc(lt_ctx *c, size_t bytes);
+void *ctx_alloc_unpooled(lt_ctx *c, size_t bytes);
 void pool_trim(lt_ctx *c, size_t keep_bytes);
 void ctx_free(lt_ctx *c, void *p);
 

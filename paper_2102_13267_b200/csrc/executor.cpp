@@ -180,12 +180,15 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
     }
     c->out_ptr.assign(n_out, nullptr);
     c->temp_ptr.assign(plan.temp_bytes.size(), nullptr);
+    void *captured_arrivals = nullptr;
 
     auto release_all = [&](bool outputs_too) {
         for (void *&p : c->temp_ptr) {
             if (p && !c->static_mode) ctx_free(c, p);
             p = nullptr;
         }
+        ctx_free(c, captured_arrivals);
+        captured_arrivals = nullptr;
         if (outputs_too)
             for (size_t k = 0; k < n_out; ++k)
                 if (c->out_ptr[k] && plan.outputs[k].donated_param < 0) {
@@ -217,6 +220,22 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
             if (ce != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("clearing the static scratch: ") + cudaGetErrorString(ce));
         }
     }
+    // A graph that captures this flush outlives it, and may outlive the context: what its kernels write lies in memory that the
+    // allocator hands out during the capture -- not in the context's pool, from which later flushes and other graphs are
+    // served, and which goes with the context.  (Results too, where the allocator is the caller's: cudaMallocAsync under capture
+    // gives memory that has to be freed before the graph can be launched again.)
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    bool obtains = !plan.temp_bytes.empty();
+    for (size_t k = 0; k < n_out; ++k) obtains = obtains || plan.outputs[k].donated_param < 0;
+    if (plan.has_operators && obtains && !dry) {  // (asking costs half a microsecond)
+        const cudaError_t ce = cudaStreamIsCapturing(c->stream, &capture);
+        if (ce != cudaSuccess) {
+            release_all(true);
+            return fail(c, LT_ERR_CUDA, std::string("cudaStreamIsCapturing: ") + cudaGetErrorString(ce));
+        }
+    }
+    const bool captured = capture != cudaStreamCaptureStatusNone;
+
     uint64_t donated = 0, allocated = 0;
     for (size_t k = 0; k < n_out; ++k) {
         const OutputPlan &o = plan.outputs[k];
@@ -224,7 +243,7 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
             c->out_ptr[k] = c->param_ptr[o.donated_param];
             ++donated;
         } else {
-            c->out_ptr[k] = ctx_alloc(c, o.bytes);
+            c->out_ptr[k] = captured && c->has_alloc ? ctx_alloc_unpooled(c, o.bytes) : ctx_alloc(c, o.bytes);
             if (!c->out_ptr[k]) {
                 release_all(true);
                 return fail(c, LT_ERR_OOM, "allocator returned null for an output");
@@ -239,33 +258,37 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
             static_used += (plan.temp_bytes[t] + 255u) & ~(size_t)255u;
             continue;
         }
-        c->temp_ptr[t] = ctx_alloc(c, plan.temp_bytes[t]);
+        c->temp_ptr[t] = captured ? ctx_alloc_unpooled(c, plan.temp_bytes[t]) : ctx_alloc(c, plan.temp_bytes[t]);
         if (!c->temp_ptr[t]) {
             release_all(true);
             return fail(c, LT_ERR_OOM, "allocator returned null for a temporary");
         }
     }
 
-    // counters of operators whose blocks share a result: zero now, and left at zero by every launch that uses them
+    // Counters of operators whose blocks share a result: every launch that uses them finds them at zero and leaves them so.
     void *arrivals = nullptr;
     if (plan.needs_arrivals && !dry) {
+        const size_t bytes = LT_ARRIVALS * sizeof(unsigned int);
         cudaError_t ae = cudaSuccess;
-        // (a stream that is being captured would set a new context's counters to zero only when the graph runs)
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        if (!c->static_mode && !c->arrivals) ae = cudaStreamIsCapturing(c->stream, &capture);
-        if (ae == cudaSuccess && (c->static_mode || capture != cudaStreamCaptureStatusNone)) {
-            ae = lt_static_arrivals(&arrivals);
-        } else if (ae == cudaSuccess && !c->arrivals) {
-            arrivals = ctx_alloc(c, LT_ARRIVALS * sizeof(unsigned int));
-            if (!arrivals) {
-                release_all(true);
-                return fail(c, LT_ERR_OOM, "allocator returned null for an operator's counters");
-            }
-            ae = cudaMemsetAsync(arrivals, 0, LT_ARRIVALS * sizeof(unsigned int), c->stream);
-            if (ae == cudaSuccess) c->arrivals = arrivals;
-            else ctx_free(c, arrivals);
+        bool zero = true;
+        if (c->static_mode) {
+            ae = lt_static_arrivals(&arrivals);  // (zeroed at every flush: what two flushes that overlapped left does not stay)
+        } else if (captured) {
+            arrivals = captured_arrivals = ctx_alloc_unpooled(c, bytes);  // the graph's own, zeroed by every replay
+        } else if (!c->arrivals) {
+            arrivals = ctx_alloc(c, bytes);
         } else {
             arrivals = c->arrivals;
+            zero = false;
+        }
+        if (ae == cudaSuccess && !arrivals) {
+            release_all(true);
+            return fail(c, LT_ERR_OOM, "allocator returned null for an operator's counters");
+        }
+        if (ae == cudaSuccess && zero) ae = cudaMemsetAsync(arrivals, 0, bytes, c->stream);
+        if (!c->static_mode && !captured && zero) {
+            if (ae == cudaSuccess) c->arrivals = arrivals;
+            else ctx_free(c, arrivals);
         }
         if (ae != cudaSuccess) {
             release_all(true);

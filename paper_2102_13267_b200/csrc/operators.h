@@ -50,8 +50,9 @@ static inline int operator_inputs(int op, int n_in, const int64_t *attrs) {
 }
 
 size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count);
-// Counters of blocks that have left their part of a result that several share.  A context has its own; flushes that may not
-// allocate share one array per device, like the static scratch.
+// Counters of blocks that have left their part of a result that several share.  A context has its own for its flushes, a
+// graph that captures one has its own in the graph's memory; flushes that may not allocate share one array per device, like
+// the static scratch.
 #define LT_ARRIVALS 2048
 cudaError_t lt_static_arrivals(void **out);
 // Enqueues the operator on `stream`; *launched receives the number of kernels.

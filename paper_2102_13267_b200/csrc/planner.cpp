@@ -1154,6 +1154,7 @@ lt_status build_plan(lt_ctx *c, const Canonical &cg, Plan &plan, bool isolate_lo
             for (const IoRef &io : g.io) g.bytes += pn[io.cnode].numel * dtype_size(io.dtype);
         }
         if (g.kind == K_OPERATOR) {
+            plan.has_operators = true;
             g.bytes = operator_bytes(g.operation);
             const size_t scratch = lt_operator_scratch_bytes(g.operation, c->sm_count);
             if (scratch) {

@@ -782,6 +782,84 @@ def test_first_attention_of_a_context_is_captured(lt):
         warm.close(), c.close()
 
 
+def captured_attention(lt, seed, stream, n, warm, allocator="torch"):
+    """(graph of one ordinary barrier with an attention, context, tensors, what it has to give) on `stream`."""
+    with torch.cuda.stream(stream):
+        c, g = lt.LazyContext(device=0, stream=stream.cuda_stream, allocator=allocator), gen(seed)
+        cache, table = paged(g, n, 16, 2, 64, False, torch.bfloat16)
+        q, ln = normal(g, len(n), 8, 64, dtype=torch.bfloat16), torch.tensor(n, dtype=torch.int32, device="cuda")
+        out = torch.zeros_like(q)
+        handles = [c.from_torch(t) for t in (q, cache, table, ln, out)]
+
+        def step():
+            c.paged_attention(*handles[:4], scale=0.125, out=handles[4])
+            c.barrier()
+
+        if warm:
+            step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        stream.synchronize()
+    return graph, c, (q, cache, table, ln, out, handles), ref.attention(q, cache, table, n, 0.125, False)
+
+
+def test_captured_barriers_share_nothing_and_outlive_their_contexts(lt):
+    """Graphs of ordinary barriers, of contexts that have flushed an attention before and of new ones, replayed side by side on
+    their streams; then once more when the contexts are closed and what they gave back is somebody else's."""
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    lengths = ([5000, 300], [9000], [40, 3000, 2000])
+    made = [captured_attention(lt, 60 + i, s, n, warm) for i, (s, n, warm) in enumerate(zip(streams, lengths, (False, False, True)))]
+
+    def replay():
+        for _, _, t, _ in made:
+            t[4].zero_()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (graph, *_), s in zip(made, streams):
+                with torch.cuda.stream(s):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for _, _, t, want in made:
+            close(t[4], *want)
+
+    replay()
+    for _, c, t, _ in made:
+        t[5].clear()
+        c.close()
+    torch.cuda.synchronize()
+    taken = []
+    for s in streams:  # what the contexts held goes to whoever asks on their streams
+        with torch.cuda.stream(s):
+            taken += [torch.full((size,), 0x7fc07fc0, dtype=torch.int32, device="cuda") for size in [2048] * 64 + [1 << 17] * 16 + [1 << 20] * 8]
+    torch.cuda.synchronize()
+    replay()
+    for t in taken:
+        assert bool((t == 0x7fc07fc0).all())
+
+
+def test_captured_barrier_without_allocator_callbacks(lt):
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for warm in (False, True):
+        graph, c, t, want = captured_attention(lt, 70, s, [5000, 300], warm, allocator="none")
+        for _ in range(3):
+            with torch.cuda.stream(s):
+                t[4].zero_()
+                graph.replay()
+            s.synchronize()
+            close(t[4], *want)
+        with torch.cuda.stream(s):
+            t[4].zero_()
+            c.paged_attention(*t[5][:4], scale=0.125, out=t[5][4])
+            c.barrier(blocking=True)
+        close(t[4], *want)
+        t[5].clear()
+        c.close()
+
+
 def test_replay(ctx, lt):
     """lt_replay runs the step again on the tensors' current values."""
     g = gen(44)
