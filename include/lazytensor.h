@@ -59,9 +59,10 @@ typedef enum {
                                  of time waiting for a copy into shared memory, or for the partial results
                                  of the other thread blocks of its cluster                                */
     LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes:
-                                 reported by the first blocking call after the operator that met it, which left
-                                 out what the index named and did the rest (one word per device holds it: of
-                                 several contexts there, the first that used such an operator and looks)   */
+                                 reported by the context's first blocking call after the operator that met it, or
+                                 after the replay of a graph that captured it (call once the replay is done); the
+                                 operator left out what the index named and did the rest.  Up to 4095 contexts at
+                                 a time look separately, any more together.                                */
 } lt_status;
 
 typedef enum { LT_F32 = 0, LT_BF16 = 1, LT_U8 = 2, LT_I32 = 3, LT_U32 = 4 } lt_dtype;

@@ -36,7 +36,7 @@ struct AttendArgs {
     void *out;
     float *partial;             // [2 x blocks][block_heads][dim + 2]: outputs, then (maximum, sum) of each head; null: every (sequence, head block) has a block of its own
     unsigned int *arrivals;     // [2][LT_ARRIVALS / 2], zero between launches: how many groups (or all parts) of what begins in block i are there; and how many parts of its groups (i, i + 1, ..)
-    unsigned int *status;
+    unsigned int *status;       // set to 1 (by whoever finds it) where an index lies outside what it indexes
     uint64_t q_pitch, page_stride, value_offset, token_stride, head_stride;
     uint32_t batch, heads, kv_heads, group, block_heads, head_blocks, dim, pages, page, table_width;  // block_heads: query heads a block works on at a time
     float scale;                // times log2(e): weights are powers of two
@@ -49,7 +49,7 @@ __device__ __forceinline__ int length_of(const AttendArgs &a, uint32_t b) {
 }
 
 __device__ __forceinline__ void check_length(const AttendArgs &a, uint32_t b) {
-    if (threadIdx.x == 0 && a.lengths[b] > 0 && (int64_t)a.lengths[b] > (int64_t)a.table_width * a.page) atomicOr(a.status, 1u);
+    if (threadIdx.x == 0 && a.lengths[b] > 0 && (int64_t)a.lengths[b] > (int64_t)a.table_width * a.page) report(a.status);
 }
 
 __device__ __forceinline__ uint32_t tiles_in(int n) { return ((uint32_t)n + TILE - 1) / TILE; }
@@ -348,7 +348,7 @@ __device__ __forceinline__ bool locate(const AttendArgs &a, const int *row, int 
     const uint32_t e = (uint32_t)i / a.page, off = (uint32_t)i - e * a.page;
     const int p = row[e];
     if ((uint32_t)p >= a.pages) {
-        atomicOr(a.status, 1u);
+        report(a.status);
         return false;
     }
     *at = (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)kv * a.head_stride;
@@ -541,7 +541,7 @@ struct Stages {
                 const int p = __shfl_sync(0xffffffffu, ahead, step & 31);
                 if (mask && (uint32_t)p >= a.pages) {
                     mask = 0;
-                    atomicOr(a.status, 1u);
+                    report(a.status);
                 }
                 const uint32_t off = (uint32_t)i0 % a.page;
                 const T *src = cache + (mask ? (uint64_t)p * a.page_stride + (uint64_t)off * a.token_stride + (uint64_t)w.kv * a.head_stride : 0);
@@ -558,7 +558,7 @@ struct Stages {
             } else {
                 const int i = i0 + (lane & 15), p = ahead;
                 const bool known = i < w.n && (uint32_t)p < a.pages;
-                if (i < w.n && !known) atomicOr(a.status, 1u);
+                if (i < w.n && !known) report(a.status);
                 mask = __ballot_sync(0xffffffffu, known) & 0xffffu;
                 const uint64_t off = known ? (uint64_t)p * a.page_stride + (uint64_t)((uint32_t)i % a.page) * a.token_stride + (uint64_t)w.kv * a.head_stride : 0;
 #pragma unroll
@@ -988,7 +988,7 @@ size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count) {
     return 2 * (any > rows ? any : rows) * (o.dim + 2) * sizeof(float);
 }
 
-cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream) {
+cudaError_t lt_launch_paged_attention(const LtOperator &o, int sm_count, cudaStream_t stream) {
     AttendArgs a{};
     a.q = o.in[0];
     a.cache = o.in[1];
@@ -997,7 +997,7 @@ cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status,
     a.out = o.out[0];
     a.partial = split(o) ? (float *)o.scratch : nullptr;
     a.arrivals = (unsigned int *)o.arrivals;
-    a.status = status;
+    a.status = &o.status->attention;
     a.q_pitch = o.pitch[0];
     a.value_offset = (uint64_t)o.page * o.kv_heads * o.dim;
     a.page_stride = 2 * a.value_offset;

@@ -230,19 +230,16 @@ void record_replay(lt_ctx *c, Plan *cached, Plan *plan, const Canonical &cg, con
     by_node.clear();
 }
 
-// Drains the stream; afterwards, if a kernel with bounded device-side waits has run since the last look, reads the
-// device status word: a wait that gave up is reported (and the word cleared) here.
+// Drains the stream; afterwards looks where operators leave word of indices outside what they index and, if a kernel with
+// bounded device-side waits has run since the last look, reads the device status word: what is found there (a wait that gave
+// up) is reported, and cleared, here.
 lt_status sync_and_check(lt_ctx *c) {
     cudaError_t e = cudaStreamSynchronize(c->stream);
     if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("cudaStreamSynchronize: ") + cudaGetErrorString(e));
-    if (c->index_status_pending) {
-        c->index_status_pending = false;
-        unsigned int word = 0;
-        e = lt_operator_status_read(&word);
-        if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("reading the operators' status word: ") + cudaGetErrorString(e));
-        if (word) return fail(c, LT_ERR_DEVICE_INDEX, std::string(word & 1u ? "paged_attention: a page number or a length" : "cache_append: a slot number") +
-                                                          " in device memory lies outside the cache; what it names was left out");
-    }
+    const LtOperatorStatus found = lt_operator_status_take(c->operator_status);
+    if (found.attention || found.append)
+        return fail(c, LT_ERR_DEVICE_INDEX, std::string(found.attention ? "paged_attention: a page number or a length" : "") + (found.attention && found.append ? "; " : "") +
+                                                (found.append ? "cache_append: a slot number" : "") + " in device memory lies outside the cache; what it names was left out");
     if (c->status_pending) {
         c->status_pending = false;
         unsigned int word = 0;
@@ -1171,6 +1168,7 @@ lt_status lt_ctx_create(int device, void *cuda_stream, const lt_allocator *alloc
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
         if (e == cudaSuccess) e = lt_kernel_setup(LT_MAX_STAGE_BYTES);
         if (e == cudaSuccess) e = lt_kernel_occupancy(&c->occ_ew, &c->occ_row, &c->occ_multi);
+        if (e == cudaSuccess) e = lt_operator_status_claim(&c->operator_status);
         if (e != cudaSuccess) {
             // no usable device: report instead of falling back to anything
             fprintf(stderr, "lt_ctx_create: CUDA device %d unusable: %s\n", device, cudaGetErrorString(e));
@@ -1199,6 +1197,7 @@ lt_status lt_ctx_destroy(lt_ctx *c) {
     for (auto &b : c->buffers)
         if (b.owned && b.ptr && b.refs > 0) ctx_free(c, b.ptr);
     ctx_free(c, c->arrivals);
+    lt_operator_status_return(c->operator_status);
     pool_trim(c, 0);
     delete c;
     return LT_OK;

@@ -373,7 +373,7 @@ struct lt_ctx {
     lt::ReplayRecord replay;
     lt::TraceState trace;
     void *arrivals = nullptr;           // LT_ARRIVALS counters of operators whose blocks share a result; made at their first flush
-    bool index_status_pending = false;  // an operator that follows indices in device memory ran since its status word was last read
+    LtOperatorStatus *operator_status = nullptr;  // where operators that follow indices in device memory leave word of bad ones
     bool status_pending = false;      // a kernel with bounded device-side waits ran since the status word was last read
     int64_t wait_limit_ns = 2000000000ll;  // how long such a wait may last
 

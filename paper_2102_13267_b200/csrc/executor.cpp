@@ -319,10 +319,10 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
                     if (g.io[q].is_store) o.out[g.results[q]] = (void *)(uintptr_t)resolve(g.io[q]);
                 o.scratch = g.scratch_temp >= 0 ? c->temp_ptr[g.scratch_temp] : nullptr;
                 o.arrivals = arrivals;
+                o.status = c->operator_status;
                 if (ev0) cudaEventRecord(ev0, c->stream);
                 e = lt_launch_operator(o, c->sm_count, c->stream, &launched);
                 if (ev1) cudaEventRecord(ev1, c->stream);
-                if (o.op == LT_OP_PAGED_ATTENTION || o.op == LT_OP_CACHE_APPEND) c->index_status_pending = true;
             }
             if (launched > 1) c->stats.kernels_launched += launched - 1;
         } else if (L.kind == K_VIEW) {

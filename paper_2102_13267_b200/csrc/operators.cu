@@ -4,6 +4,8 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <cstring>
+#include <deque>
 #include <mutex>
 #include <type_traits>
 
@@ -11,14 +13,20 @@
 
 using namespace ltop;
 
-static __device__ unsigned int lt_operator_status = 0;
 static __device__ unsigned int lt_operator_arrivals[LT_ARRIVALS];
 
 namespace {
 
 constexpr int kMaxDevices = 64;
 std::mutex g_lock;
-void *g_status[kMaxDevices], *g_arrivals[kMaxDevices];
+void *g_arrivals[kMaxDevices];
+
+// Status words of contexts, in host memory that every device writes to and that lasts as long as the process: a graph may
+// still report to the word of a context that is gone.  So a word that is given back waits until all others have been used.
+// The first one is shared by contexts that find no free one.
+constexpr size_t kStatusWords = 4096;
+LtOperatorStatus *g_status;
+std::deque<LtOperatorStatus *> g_status_free;
 
 // Address of a device variable on the current device, looked up once per device.
 template <class S>
@@ -66,7 +74,7 @@ __device__ __forceinline__ bool destination(const TurnArgs &a, uint64_t t, uint6
     const int slot = a.slots[t];
     if (slot < 0) return false;
     if ((uint64_t)slot >= a.n_slots) {
-        atomicOr(a.status, 2u);
+        report(a.status);
         return false;
     }
     const uint32_t p = (uint32_t)slot / a.page, off = (uint32_t)slot - p * a.page;
@@ -1067,7 +1075,7 @@ cudaError_t lt_launch_rotary(const LtOperator &o, int sm_count, cudaStream_t str
     return o.dtype == LT_BF16 ? launch_turn<__nv_bfloat16, false>(a, sm_count, stream) : launch_turn<float, false>(a, sm_count, stream);
 }
 
-cudaError_t lt_launch_cache_append(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream, unsigned *launched) {
+cudaError_t lt_launch_cache_append(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
     const size_t es = o.dtype == LT_BF16 ? 2 : 4;
     *launched = 1;
     if (o.out[0] != o.in[0]) {
@@ -1080,7 +1088,7 @@ cudaError_t lt_launch_cache_append(const LtOperator &o, unsigned int *status, in
     a.slots = (const int *)o.in[3];
     a.positions = (const int *)o.in[4];
     a.frequencies = (const uint2 *)o.in[5];
-    a.status = status;
+    a.status = &o.status->append;
     a.out = o.out[0];
     a.tokens = o.rows;
     a.x_pitch = o.pitch[1];
@@ -1161,33 +1169,44 @@ size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count) {
 
 cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
     *launched = 1;
-    void *word = nullptr;
-    if (o.op == LT_OP_CACHE_APPEND || o.op == LT_OP_PAGED_ATTENTION) {
-        const cudaError_t e = address_of(lt_operator_status, g_status, &word);
-        if (e != cudaSuccess) return e;
-    }
-    unsigned int *status = (unsigned int *)word;
     switch (o.op) {
     case LT_OP_ROTARY: return lt_launch_rotary(o, sm_count, stream);
-    case LT_OP_CACHE_APPEND: return lt_launch_cache_append(o, status, sm_count, stream, launched);
-    case LT_OP_PAGED_ATTENTION: return lt_launch_paged_attention(o, status, sm_count, stream);
+    case LT_OP_CACHE_APPEND: return lt_launch_cache_append(o, sm_count, stream, launched);
+    case LT_OP_PAGED_ATTENTION: return lt_launch_paged_attention(o, sm_count, stream);
     case LT_OP_RMS_NORM: return lt_launch_rms_norm(o, sm_count, stream);
     case LT_OP_RMS_NORM_GRAD: return lt_launch_rms_norm_grad(o, sm_count, stream, launched);
     default: return cudaErrorInvalidValue;
     }
 }
 
-cudaError_t lt_static_arrivals(void **out) {
-    void *word = nullptr;
-    const cudaError_t e = address_of(lt_operator_status, g_status, &word);  // (nothing is looked up when a flush is captured)
-    return e == cudaSuccess ? address_of(lt_operator_arrivals, g_arrivals, out) : e;
+cudaError_t lt_static_arrivals(void **out) { return address_of(lt_operator_arrivals, g_arrivals, out); }
+
+cudaError_t lt_operator_status_claim(LtOperatorStatus **out) {
+    std::lock_guard<std::mutex> hold(g_lock);
+    if (!g_status) {
+        void *p = nullptr;
+        const cudaError_t e = cudaHostAlloc(&p, kStatusWords * sizeof(LtOperatorStatus), cudaHostAllocPortable | cudaHostAllocMapped);
+        if (e != cudaSuccess) return e;
+        memset(p, 0, kStatusWords * sizeof(LtOperatorStatus));
+        g_status = (LtOperatorStatus *)p;
+        for (size_t i = 1; i < kStatusWords; ++i) g_status_free.push_back(g_status + i);
+    }
+    *out = g_status;
+    if (g_status_free.empty()) return cudaSuccess;
+    *out = g_status_free.front();
+    g_status_free.pop_front();
+    lt_operator_status_take(*out);
+    return cudaSuccess;
 }
 
-cudaError_t lt_operator_status_read(unsigned int *out) {
-    cudaError_t e = cudaMemcpyFromSymbol(out, lt_operator_status, sizeof(*out));
-    if (e == cudaSuccess && *out) {
-        const unsigned int zero = 0;
-        e = cudaMemcpyToSymbol(lt_operator_status, &zero, sizeof(zero));
-    }
-    return e;
+void lt_operator_status_return(LtOperatorStatus *status) {
+    std::lock_guard<std::mutex> hold(g_lock);
+    if (status && status != g_status) g_status_free.push_back(status);
+}
+
+LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status) {
+    LtOperatorStatus s;
+    s.attention = __atomic_exchange_n(&status->attention, 0u, __ATOMIC_ACQ_REL);
+    s.append = __atomic_exchange_n(&status->append, 0u, __ATOMIC_ACQ_REL);
+    return s;
 }

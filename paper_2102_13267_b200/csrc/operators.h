@@ -9,6 +9,11 @@
 #define LT_OPERATOR_INPUTS 6
 #define LT_OPERATOR_RESULTS 4
 
+// Where a context's operators leave word that an index in device memory lay outside what it indexes.
+struct LtOperatorStatus {
+    unsigned int attention, append;
+};
+
 // One launch of an operator.  Everything but the addresses is known when the graph is planned.
 struct LtOperator {
     int op;
@@ -21,6 +26,7 @@ struct LtOperator {
     void *out[LT_OPERATOR_RESULTS];        // per result; null where the graph does not ask for it
     unsigned wanted;                       // bit k: result k is asked for
     void *scratch;
+    LtOperatorStatus *status;              // paged_attention, cache_append
     void *arrivals;                        // paged_attention: LT_ARRIVALS counters that are zero between launches
     // sizes (those that the operator has)
     uint64_t rows;                         // tokens, sequences or rows
@@ -57,13 +63,16 @@ size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count);
 cudaError_t lt_static_arrivals(void **out);
 // Enqueues the operator on `stream`; *launched receives the number of kernels.
 cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
-// Indices in device memory that lay outside what they index, since the last call (synchronises): bit 0 paged_attention, bit 1 cache_append.
-cudaError_t lt_operator_status_read(unsigned int *out);
+// A status for a context, which gives it back when it is destroyed.
+cudaError_t lt_operator_status_claim(LtOperatorStatus **out);
+void lt_operator_status_return(LtOperatorStatus *status);
+// What was left there since the last call (by kernels that have completed), and is from now on not.
+LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status);
 
 // the operators' own launchers
 cudaError_t lt_launch_rotary(const LtOperator &o, int sm_count, cudaStream_t stream);
-cudaError_t lt_launch_cache_append(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream, unsigned *launched);
-cudaError_t lt_launch_paged_attention(const LtOperator &o, unsigned int *status, int sm_count, cudaStream_t stream);
+cudaError_t lt_launch_cache_append(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
+cudaError_t lt_launch_paged_attention(const LtOperator &o, int sm_count, cudaStream_t stream);
 size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_rms_norm(const LtOperator &o, int sm_count, cudaStream_t stream);
 cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);

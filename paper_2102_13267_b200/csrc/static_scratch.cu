@@ -44,7 +44,7 @@ cudaError_t scratch_address(int device, void **out) {
         void *p = nullptr;
         if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, lt_static_scratch);
         void *counters = nullptr;
-        if (e == cudaSuccess) e = lt_static_arrivals(&counters);
+        if (e == cudaSuccess) e = lt_static_arrivals(&counters);  // (so that nothing is looked up when a flush is captured)
         if (previous >= 0 && previous != device) cudaSetDevice(previous);
         if (e != cudaSuccess) return e;
         g_scratch_addr[device] = p;

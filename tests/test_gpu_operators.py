@@ -251,6 +251,31 @@ def test_slots_beyond_the_cache_are_left_out_and_reported(ctx, lt):
     ctx.barrier(blocking=True)  # reported once
 
 
+def test_a_bad_slot_is_reported_to_the_context_that_met_it(lt):
+    g = gen(7)
+    a, b = lt.LazyContext(device=0), lt.LazyContext(device=0)
+    k = normal(g, 2, 1, 8)
+    kept = []
+
+    def append(c, slots):
+        cache = torch.zeros(2, 2, 4, 1, 8, device="cuda")
+        hs = [c.from_torch(t) for t in (cache, k, k, torch.tensor(slots, dtype=torch.int32, device="cuda"))]
+        kept.append(hs)
+        c.cache_append(*hs)
+
+    append(a, [8, 1]), append(b, [0, 1])
+    a.barrier()
+    torch.cuda.synchronize()
+    b.barrier(blocking=True)
+    append(b, [2, 3])
+    b.barrier(blocking=True)
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE_INDEX.*slot"):
+        a.barrier(blocking=True)
+    a.barrier(blocking=True)  # reported once
+    kept.clear()
+    a.close(), b.close()
+
+
 # ------------------------------------------------------------------------------------------------ paged_attention
 def paged(g, lengths, page, kv_heads, dim, head_major, dtype, spare=2, width=None):
     """(cache, page table): pages in random order, everything that no token lies in being NaN, entries behind the last page invalid."""
@@ -858,6 +883,27 @@ def test_captured_barrier_without_allocator_callbacks(lt):
         close(t[4], *want)
         t[5].clear()
         c.close()
+
+
+def test_bad_pages_in_a_replayed_graph_are_reported(lt):
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph, c, (q, cache, table, ln, out, handles), want = captured_attention(lt, 75, s, [300, 500], True)
+    with torch.cuda.stream(s):
+        c.barrier(blocking=True)
+        for i in range(3):
+            good = table.clone()
+            graph.replay()
+            c.barrier(blocking=True)
+            close(out, *want)
+            table[1, i] = cache.shape[0] + i
+            graph.replay()
+            with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE_INDEX.*page"):
+                c.barrier(blocking=True)
+            close(out, *ref.attention(q, cache, table, [300, 500], 0.125, False))
+            table.copy_(good)
+    handles.clear()
+    c.close()
 
 
 def test_replay(ctx, lt):
