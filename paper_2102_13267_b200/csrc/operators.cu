@@ -693,6 +693,18 @@ struct NormGradArgs {
     int gamma_f32;
 };
 
+// The gradient's kernels sum gamma dy h first and scale it afterwards, as the norm is not known before.  Where that sum does not
+// fit (or is no number), they sum gamma dy u over the row a second time.
+__device__ __forceinline__ bool finite_sum(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// (not inlined: the loops of lt_norm_grad_any take 4 to 20 % longer beside it)
+template <class T>
+__device__ __noinline__ float dot_again(const NormGradArgs &a, const T *dy, const T *h, float inv) {
+    float dot = 0.f;
+    for (uint64_t c = threadIdx.x; c < a.cols; c += 256) dot += to_float(dy[c]) * gamma_at<T>(a.gamma, a.gamma_f32, c) * (to_float(h[c]) * inv * a.down);
+    return dot;
+}
+
 // u = h / rms.  dx = dh + (gamma dy - u mean(gamma dy u)) / rms; a block adds up dy u over its rows in its own row of
 // `partial`.
 template <class T>
@@ -714,7 +726,9 @@ __global__ void __launch_bounds__(256) lt_norm_grad_any(const NormGradArgs a) {
         }
         ss = block_reduce<false>(ss, part);
         dot = block_reduce<false>(dot, part);
-        const float inv = rsqrtf(ss * a.up + a.eps), m = dot * inv * a.up;
+        const float inv = rsqrtf(ss * a.up + a.eps);
+        float m = dot * inv * a.up;
+        if (!finite_sum(dot)) m = block_reduce<false>(dot_again<T>(a, dy, h, inv), part) * a.up;
         for (uint64_t c = threadIdx.x; c < a.cols; c += 256) {
             const float d = to_float(dy[c]), u = to_float(h[c]) * inv;
             const float g = (d * gamma_at<T>(a.gamma, a.gamma_f32, c) - u * m) * inv + (dh ? to_float(dh[c]) : 0.f);
@@ -753,7 +767,14 @@ __global__ void __launch_bounds__(256, NARROW_BLOCKS) lt_norm_grad_narrow(const 
         }
         const float2 s = group_sum<RT>(ss, dot, part, (int)group, turn);
         const uint64_t at = row * cols + lane;
-        const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
+        const float inv = rsqrtf(s.x * a.up + a.eps);
+        float m = s.y * inv * a.up;
+        if (!finite_sum(s.y)) {
+            dot = 0.f;
+#pragma unroll
+            for (int k = 0; k < E; ++k) dot += d[k] * g[k] * (u[k] * inv * a.down);
+            m = group_sum<RT>(dot, 0.f, part, (int)group, turn).x * a.up;
+        }
 #pragma unroll
         for (int k = 0; k < E; ++k) {
             const float v = u[k] * inv;
@@ -836,9 +857,22 @@ __global__ void __launch_bounds__(grad_block(RT), RT > 256 ? 1 : 2) lt_norm_grad
         }
         float2 s = group_sum<RT>(ss, dot, part, group, turn);
         s.x *= a.down;
-        s.y *= a.down;
         if (s.x > 3.402823466e38f) {  // the sum of the squares does not fit, their mean may
-            ss = dot = 0.f;
+            ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                if (lane + k * RT >= chunks) continue;
+                float u[N];
+                unpack(*place(stage, 1, k), u);
+#pragma unroll
+                for (int i = 0; i < N; ++i) ss += u[i] * (u[i] * a.down);
+            }
+            s.x = group_sum<RT>(ss, 0.f, part, group, turn).x;
+        }
+        const float inv = rsqrtf(s.x * a.up + a.eps);
+        float m = s.y * a.down * inv * a.up;
+        if (!finite_sum(s.y)) {
+            dot = 0.f;
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 if (lane + k * RT >= chunks) continue;
@@ -846,14 +880,10 @@ __global__ void __launch_bounds__(grad_block(RT), RT > 256 ? 1 : 2) lt_norm_grad
                 unpack(*place(stage, 0, k), d);
                 unpack(*place(stage, 1, k), u);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    ss += u[i] * (u[i] * a.down);
-                    dot += d[i] * g[k][i] * (u[i] * a.down);
-                }
+                for (int i = 0; i < N; ++i) dot += d[i] * g[k][i] * (u[i] * inv * a.down);
             }
-            s = group_sum<RT>(ss, dot, part, group, turn);
+            m = group_sum<RT>(dot, 0.f, part, group, turn).x * a.up;
         }
-        const float inv = rsqrtf(s.x * a.up + a.eps), m = s.y * inv * a.up;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             if (lane + k * RT >= chunks) continue;

@@ -606,6 +606,19 @@ def test_rms_norm_grad_against_differences(ctx):
         assert abs((loss(h64, g64 + e) - loss(h64, g64 - e)) / (2 * step) - float(dg[c])) < 1e-5
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(3, 64), (400, 1024), (2, 16384), (5, 33), (40, 999), (3, 2001), (2, 40000)])
+def test_rms_norm_grad_of_large_values(ctx, dtype, rows, cols):
+    """The sum of dy gamma h does not fit into binary32; the mean of dy gamma h / rms does, and so do the gradients."""
+    t, g = TYPES[dtype], gen(rows + cols)
+    dy, h = normal(g, rows, cols, dtype=t, std=1e24), normal(g, rows, cols, dtype=t, std=1e18)
+    gamma = 1 + normal(g, cols, std=0.2)
+    dx, bx, dg, bg = ref.rms_norm_grad(dy, h, gamma, None, 1e-6)
+    got = ctx.rms_norm_grad(*(ctx.from_torch(a) for a in (dy, h, gamma)))
+    close(fetch(ctx, got[0]), dx, bx, "dx")
+    close(fetch(ctx, got[1]), dg, bg + dg.abs() * ULP, "dgamma")
+
+
 def test_rms_norm_grad_slices_and_in_place(ctx):
     g = gen(33)
     for dtype, t in TYPES.items():
