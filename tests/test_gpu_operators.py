@@ -113,6 +113,25 @@ def test_rotary_more_tokens_than_the_blocks_have_at_once(ctx, lt, dtype, interle
     close(fetch(ctx, y), *ref.rotary(x, pos, ref.frequencies(rotated), interleaved))
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rotated", [128, 6])
+def test_rotary_angles(ctx, lt, interleaved, rotated):
+    """Pairs (1, 0) turn into the cosine and the sine themselves.  The angle is taken to 2^-28 of a turn, which moves neither by
+    more than 2 pi 2^-28 sqrt(1/2); the functions themselves are good to one unit in the last place, 2^-24 at most."""
+    tokens, p = 40000, rotated // 2
+    table = lt.rotary_table(rotated)
+    pos = torch.randint(-(1 << 31), 1 << 31, (tokens,), generator=gen(rotated), device="cuda").to(torch.int32)
+    x = torch.zeros(tokens, 1, rotated, device="cuda")
+    (x[..., ::2] if interleaved else x[..., :p]).fill_(1.0)
+    y = fetch(ctx, ctx.rotary(ctx.from_torch(x), ctx.from_torch(pos), ctx.leaf(table, "u32"), interleaved=interleaved))[:, 0].double().numpy()
+    c, s = (y[:, ::2], y[:, 1::2]) if interleaved else (y[:, :p], y[:, p:])
+    f = table[:, 0].astype(np.uint64) | (table[:, 1].astype(np.uint64) << np.uint64(32))
+    turns = (pos.cpu().numpy().astype(np.int64).view(np.uint64)[:, None] * f[None, :]).view(np.int64) / 2.0 ** 64
+    most = 2.0 ** -24 + 2 * math.pi * 2.0 ** -28 * math.sqrt(0.5)
+    for got, want in ((c, np.cos(2 * math.pi * turns)), (s, np.sin(2 * math.pi * turns))):
+        assert np.abs(got - want).max() <= most
+
+
 def _rot64(x, pos, f, scale):
     z = torch.polar(torch.full((), scale, dtype=torch.float64), pos.double().cpu()[:, None, None] * f)
     p = f.numel()
