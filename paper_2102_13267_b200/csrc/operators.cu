@@ -342,12 +342,14 @@ __device__ __forceinline__ float gamma_at(const void *gamma, int f32, uint64_t c
 }
 
 // 448 / top, the factor from values to e4m3 codes, by the reciprocal unit (1 ulp: far below half a step of a code; 0 for a
-// group of zeros; a group so small that the quotient would overflow takes the largest number instead).  A NaN stays.
+// group of zeros).  A NaN stays.  So small a group that the quotient might overflow is raised by a power of two first, the
+// values and their maximum alike.
+constexpr float SMALL = 0x1p-100f, RAISE = 0x1p100f;
+__device__ __forceinline__ float raise_of(float top) { return top < SMALL ? RAISE : 1.f; }
 __device__ __forceinline__ float code_factor(float top) {
     float r;
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(top));
-    r = r * 448.f;
-    return top == 0.f ? 0.f : r > 3.402823466e38f ? 3.402823466e38f : r;
+    return top == 0.f ? 0.f : r * 448.f;
 }
 __device__ __forceinline__ float scale_of(float top) { return top * (1.f / 448.f); }
 
@@ -373,10 +375,10 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
                 for (uint64_t c = threadIdx.x; c < a.cols; c += 256) top = max_nan(top, fabsf(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c)));
                 top = block_reduce<true>(top, part);
                 if (a.scales && threadIdx.x == 0) a.scales[row] = scale_of(top);
-                const float f = code_factor(top);
+                const float up = raise_of(top), f = code_factor(top * up);
                 if (a.codes)
                     for (uint64_t c = threadIdx.x; c < a.cols; c += 256)
-                        a.codes[row * a.cols + c] = __nv_cvt_float_to_fp8(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c) * f, __NV_SATFINITE, __NV_E4M3);
+                        a.codes[row * a.cols + c] = __nv_cvt_float_to_fp8(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c) * up * f, __NV_SATFINITE, __NV_E4M3);
             } else {
                 for (uint32_t g = threadIdx.x >> 5; g < a.groups; g += 8) {  // a warp per group
                     const uint64_t c0 = (uint64_t)g * a.group, c1 = min(c0 + a.group, a.cols);
@@ -384,10 +386,10 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
                     for (uint64_t c = c0 + (threadIdx.x & 31); c < c1; c += 32) top = max_nan(top, fabsf(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c)));
                     top = warp_max_nan(top);
                     if (a.scales && (threadIdx.x & 31) == 0) a.scales[row * a.groups + g] = scale_of(top);
-                    const float f = code_factor(top);
+                    const float up = raise_of(top), f = code_factor(top * up);
                     if (a.codes)
                         for (uint64_t c = c0 + (threadIdx.x & 31); c < c1; c += 32)
-                            a.codes[row * a.cols + c] = __nv_cvt_float_to_fp8(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c) * f, __NV_SATFINITE, __NV_E4M3);
+                            a.codes[row * a.cols + c] = __nv_cvt_float_to_fp8(h_at(c) * inv * gamma_at<T>(a.gamma, a.gamma_f32, c) * up * f, __NV_SATFINITE, __NV_E4M3);
                 }
                 __syncthreads();  // (y or the sum may overwrite x or the residual)
             }
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(256, NARROW_BLOCKS) lt_norm_narrow(const NormA
                 known = first;
             }
             if (a.scales && (lane & 31) == 0 && mine == first) a.scales[row * a.groups + (a.group ? mine * 32 / a.group : 0)] = scale_of(t);
-            if (a.codes && k < n) a.codes[at + RT * k] = __nv_cvt_float_to_fp8(h[k] * code_factor(t), __NV_SATFINITE, __NV_E4M3);
+            if (a.codes && k < n) a.codes[at + RT * k] = __nv_cvt_float_to_fp8(h[k] * raise_of(t) * code_factor(t * raise_of(t)), __NV_SATFINITE, __NV_E4M3);
         }
         if constexpr (RT == 32) __syncwarp();  // (128 threads: the next row's sums have a barrier before `tops` is written again)
     }
@@ -668,6 +670,11 @@ __global__ void __launch_bounds__(norm_block(RT), norm_block(RT) == 1024 ? 1 : (
                     if (a.scales && c < chunks && (c & ((1u << a.group_shift) - 1)) == 0) a.scales[row * a.groups + (c >> a.group_shift)] = scale_of(t);
                 }
                 if (!a.codes || c >= chunks) continue;
+                if (t < SMALL) {
+                    t *= RAISE;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) h[k][i] *= RAISE;
+                }
                 const float f = code_factor(t);
                 uint32_t w[N / 4];
 #pragma unroll

@@ -558,6 +558,22 @@ def test_rms_norm_with_nan_infinity_and_tiny_values(ctx):
     assert (codes[3:] == 448).all()
 
 
+@pytest.mark.parametrize("top", [1e-35, 1e-36, 1e-37, 1e-38, 1e-40])
+@pytest.mark.parametrize("cols", [512, 500, 499, 8195])
+def test_rms_norm_in_8_bits_of_groups_next_to_nothing(ctx, cols, top):
+    """y / scale, however small the largest y of a group is: 448, 224 and 112 for it, its half and its quarter."""
+    x = torch.ones(3, cols, device="cuda")
+    x[:, 1::3] *= 0.5
+    x[:, 2::3] *= -0.25
+    gamma = torch.full((cols,), top * math.sqrt(0.4375), device="cuda")  # (the mean of the squares is about 0.4375)
+    for group in (0, 128):
+        codes, scales = ctx.rms_norm(ctx.from_torch(x), ctx.from_torch(gamma), eight_bit=True, group=group)
+        assert torch.equal(decoded(fetch(ctx, codes)), (448 * x).cpu().double())
+        y = ref.rms_norm(x, gamma, None, 1e-6)[0].abs().amax()
+        # what y loses where its last bit is worth 2^-149, and the scale
+        assert float((fetch(ctx, scales).double() - y / 448).abs().max()) <= float(y / 448) * 600 * ULP + 2 * 2.0 ** -149
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rms_norm_slices_unaligned_and_in_place(ctx, dtype):
     t, g = TYPES[dtype], gen(21)
