@@ -390,9 +390,9 @@ class Batch(_Operators):
                     ops[k].in_[i] = r
             attrs = (_i64 * max(len(self._attrs), 1))(*self._attrs)
             n = self._n_inputs
-            results = (_u64 * max(len(self._ops), 1))()
-            # (the inputs' handles travel as bytes, packed anew every time)
-            self._c = (struct.Struct(f"={n}Q").pack, results, ops, ctypes.c_size_t(len(self._ops)), ctypes.c_size_t(n), attrs)
+            # (the inputs' handles travel as bytes, packed anew every time; arrays for the results are taken from a list and
+            # given back, so that threads that record at the same time have one each)
+            self._c = (struct.Struct(f"={n}Q").pack, [], _u64 * max(len(self._ops), 1), ops, ctypes.c_size_t(len(self._ops)), ctypes.c_size_t(n), attrs)
         return self._c
 
 
@@ -572,16 +572,20 @@ class LazyContext(_Operators):
 
     def record(self, batch: Batch, inputs) -> list:
         """lt_op_many: records the operations of `batch` on `inputs` in one call; returns the results it keeps."""
-        pack, results, ops, n_ops, n_inputs, attrs = batch._c or batch._compiled()
+        pack, spare, array, ops, n_ops, n_inputs, attrs = batch._c or batch._compiled()
         handles = [t.handle for t in inputs]
         if len(handles) != batch._n_inputs:
             raise ValueError(f"the batch takes {batch._n_inputs} inputs, {len(handles)} given")
+        try:
+            results = spare.pop()
+        except IndexError:
+            results = array()
         st = _op_many(self._ctx, ops, n_ops, pack(*handles), n_inputs, attrs, results)
         if st:
             self._check(st)
-        if not batch._kept:
-            return []
-        return [LazyTensor(self, results[k]) for k in batch._kept]
+        kept = [LazyTensor(self, results[k]) for k in batch._kept] if batch._kept else []
+        spare.append(results)
+        return kept
 
     def release(self, t: LazyTensor) -> None:
         t.ctx = None

@@ -1,6 +1,7 @@
 """The transformer operators on a record-and-plan-only context: shapes, refusals, which launches a graph becomes, what is
 written in place, and the frequencies of rotary positions.  No GPU."""
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -293,6 +294,34 @@ def test_more_than_three_operands_in_a_batch(ctx):
     for bad in ([(app, (4, [0, 1, 2]), 3)], [(more, [3], 0)], [(more, [3], 0), (more, [3], 0), (app, (4, [0, 1, 2]), 3)], [(more, [3, 3], 0), (app, (4, [0, 1, 2]), 3)],
                 [(more, [9], 0), (app, (4, [0, 1, 2]), 3)], [(more, (4, [0, 1, 2]), 0), (app, (7, [0, 1, 2]), 3)], [(more, [3], 0), (lt.LT_BATCH_ASSIGN, [0, 0], 0)], [(more, [], 0), (app, [0, 1, 2], 3)]):
         assert run(bad) == lt.STATUS_NAMES.index("LT_ERR_INVALID_ARG"), bad
+
+
+def test_one_batch_on_several_threads(ctx):
+    """A batch may be recorded on several threads at once, each on a context of its own."""
+    b = lt.Batch()
+    i = b.input()
+    for _ in range(2000):
+        i = b.op("neg", i)
+    b.keep(i)
+    failed = []
+
+    def work(k):
+        c = lt.LazyContext(device=None)
+        try:
+            for j in range(20):
+                r, = c.record(b, [fake(c, (k + 1, j + 1))])
+                if r.shape != (k + 1, j + 1):
+                    failed.append((k, j, r.shape))
+                del r
+        except Exception as e:  # noqa: BLE001
+            failed.append((k, e))
+        finally:
+            c.close()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not failed, failed[:3]
 
 
 # ------------------------------------------------------------------------------------------------ frequencies
