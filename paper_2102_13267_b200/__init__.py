@@ -127,8 +127,8 @@ _lib.lt_version.argtypes = []
 _lib.lt_version.restype = ctypes.c_char_p
 
 # The recording call of a Batch, for arguments that are ctypes values already (made once per batch): converting them anew
-# costs more than the call.  It records and returns, so the interpreter lock is kept.
-_op_many = ctypes.PyDLL(str(LIB_PATH)).lt_op_many
+# costs more than the call.
+_op_many = ctypes.CDLL(str(LIB_PATH)).lt_op_many
 
 EXPORTED_SYMBOLS = sorted(list(_SIGNATURES) + ["lt_last_error", "lt_version"])
 

@@ -2,6 +2,7 @@
 written in place, and the frequencies of rotary positions.  No GPU."""
 import math
 import threading
+import time
 
 import numpy as np
 import pytest
@@ -294,6 +295,36 @@ def test_more_than_three_operands_in_a_batch(ctx):
     for bad in ([(app, (4, [0, 1, 2]), 3)], [(more, [3], 0)], [(more, [3], 0), (more, [3], 0), (app, (4, [0, 1, 2]), 3)], [(more, [3, 3], 0), (app, (4, [0, 1, 2]), 3)],
                 [(more, [9], 0), (app, (4, [0, 1, 2]), 3)], [(more, (4, [0, 1, 2]), 0), (app, (7, [0, 1, 2]), 3)], [(more, [3], 0), (lt.LT_BATCH_ASSIGN, [0, 0], 0)], [(more, [], 0), (app, [0, 1, 2], 3)]):
         assert run(bad) == lt.STATUS_NAMES.index("LT_ERR_INVALID_ARG"), bad
+
+
+def test_other_threads_run_while_a_batch_is_recorded(ctx):
+    """The recording call does not hold the interpreter lock: the clock is read on another thread in the middle of it."""
+    x = fake(ctx, (4, 4))
+    b = lt.Batch()
+    r = b.input()
+    for _ in range(300000):
+        r = b.op("neg", r)
+    ctx.record(b, [x])  # (compiles the batch)
+    reads, stop = [], threading.Event()
+
+    def watch():
+        while not stop.is_set():
+            reads.append(time.perf_counter())
+            time.sleep(0)
+
+    t = threading.Thread(target=watch)
+    t.start()
+    try:
+        while not reads:
+            time.sleep(0.001)
+        begin = time.perf_counter()
+        ctx.record(b, [x])
+        end = time.perf_counter()
+    finally:
+        stop.set()
+        t.join()
+    quarter = (end - begin) / 4
+    assert any(begin + quarter < at < end - quarter for at in reads), (begin, end, len(reads))
 
 
 def test_one_batch_on_several_threads(ctx):
