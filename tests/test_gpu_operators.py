@@ -680,6 +680,81 @@ def test_rms_norm_grad_slices_and_in_place(ctx):
         close(into, dg, bg + dg.abs() * ULP)
 
 
+# ------------------------------------------------------------------------------------------------ many rows
+# More rows than the blocks have at once, several times over: rows to come, their rings and what blocks keep from row to row.
+MANY = [(40000, 64), (8192, 4096), (3000, 8192), (1500, 16384), (8000, 999), (12000, 333), (30000, 131), (3000, 4095), (2500, 1400)]
+
+
+def near(got, want, bound, what):
+    """As close(), on the GPU."""
+    off = (got.double() - want).abs()
+    bad = ~(off <= bound)
+    if bool(bad.any()):
+        at = int(torch.argmax(torch.where(bad, off - bound, torch.zeros_like(off))))
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} too far; at {at}: {got.flatten()[at]} for {want.flatten()[at]}, bound {bound.flatten()[at]}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", MANY)
+def test_rms_norm_many_rows(ctx, dtype, rows, cols):
+    t, g = TYPES[dtype], gen(rows + cols)
+    gamma = 1 + normal(g, cols, std=0.2)
+    for residual, group in ((True, None), (False, None), (True, 0), (True, 128), (False, 64)):
+        x = normal(g, rows, cols, dtype=t)
+        r = normal(g, rows, cols, dtype=t, std=2.0) if residual else None
+        h = x.double() + (r.double() if residual else 0.0)
+        y = gamma.double() * h / torch.sqrt((h * h).mean(-1, keepdim=True) + 1e-6)
+        rel = (cols / 2 + 32) * ULP
+        lx, lg, lr = ctx.from_torch(x), ctx.from_torch(gamma), ctx.from_torch(r) if residual else None
+        if group is None:  # in place: y over x, the sum over the residual
+            ctx.rms_norm(lx, lg, residual=lr, out=(lx, lr) if residual else (lx,))
+        else:
+            width = group or cols
+            parts = y.split(width, -1)
+            top = torch.stack([p.abs().amax(-1) for p in parts], -1)
+            codes = torch.empty(rows, cols, dtype=torch.uint8, device="cuda")
+            scales = torch.empty(rows, len(parts), device="cuda")
+            kept = [ctx.from_torch(codes), ctx.from_torch(scales)] + ([lr] if residual else [])  # (named until the barrier)
+            ctx.rms_norm(lx, lg, residual=lr, eight_bit=True, group=group, out=kept)
+        ctx.barrier(blocking=True)
+        what = (residual, group)
+        if group is None:
+            assert ctx.device_ptr(lx) == x.data_ptr()
+            near(x, y, y.abs() * (rel + HALF[t]), what)
+        else:
+            near(scales, top / 448, top / 448 * rel, what)
+            value = torch.cat([p * (448 / top[:, i: i + 1]) for i, p in enumerate(parts)], -1)
+            near(codes.view(torch.float8_e4m3fn), value, (value.abs() * 2.0 ** -4).clamp(min=2.0 ** -10) + value.abs() * 2 * rel, what)
+        if residual:
+            assert ctx.device_ptr(lr) == r.data_ptr()
+            near(r, h, h.abs() * (ULP + HALF[t]), what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", MANY + [(16384, 1024)])
+def test_rms_norm_grad_many_rows(ctx, dtype, rows, cols):
+    t, g = TYPES[dtype], gen(rows + cols + 1)
+    gamma = 1 + normal(g, cols, std=0.2)
+    for direct in (True, False):
+        dy, h = normal(g, rows, cols, dtype=t), normal(g, rows, cols, dtype=t, std=2.0)
+        dh = normal(g, rows, cols, dtype=t) if direct else None
+        h64, d = h.double(), dy.double() * gamma.double()
+        inv = 1 / torch.sqrt((h64 * h64).mean(-1, keepdim=True) + 1e-6)
+        u = h64 * inv
+        e = dh.double() if direct else torch.zeros((), device="cuda", dtype=torch.float64)
+        dx = e + inv * (d - u * (d * u).mean(-1, keepdim=True))
+        size = inv * (d.abs() + u.abs() * (d * u).abs().mean(-1, keepdim=True)) + e.abs()
+        dgamma, total = (dy.double() * u).sum(0), (dy.double() * u).abs().sum(0)
+        into = torch.empty(cols, device="cuda")
+        lh, li = ctx.from_torch(h), ctx.from_torch(into)
+        ctx.rms_norm_grad(ctx.from_torch(dy), lh, ctx.from_torch(gamma), residual_grad=ctx.from_torch(dh) if direct else None, out=(lh, li))
+        ctx.barrier(blocking=True)
+        assert ctx.device_ptr(lh) == h.data_ptr()
+        near(h, dx, dx.abs() * HALF[t] + size * (2 * cols + 64) * ULP, ("dx", direct))
+        # u: a sum over the row; then the rows of a block one after the other (there are as many blocks as SMs at least), blocks in 64 bits
+        near(into, dgamma, total * (cols / 2 + 32 + rows / 148 + 16) * ULP, ("dgamma", direct))
+
+
 # ------------------------------------------------------------------------------------------------ together
 class Decoder:
     """One layer's operators of a decode step, as a program records them: norm in, rotation, append, attention, norm out."""
