@@ -1008,6 +1008,54 @@ def test_captured_barrier_without_allocator_callbacks(lt):
         c.close()
 
 
+@pytest.mark.parametrize("warm", [False, True])
+def test_results_of_a_captured_barrier_are_not_handed_out_again(lt, warm):
+    """Results without a buffer of the caller's, and what passes between a graph's kernels: neither is what a later flush gets."""
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        c, g = lt.LazyContext(device=0, stream=s.cuda_stream), gen(81)
+        x, gamma = normal(g, 64, 512), 1 + normal(g, 512, std=0.2)
+        lx, lg = c.from_torch(x), c.from_torch(gamma)
+
+        def step():
+            y, = c.rms_norm(lx, lg)
+            z, = c.rms_norm(y, lg)
+            del y
+            c.barrier()
+            return z
+
+        if warm:
+            z = step()
+            del z
+            c.barrier(blocking=True)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            z = step()
+
+        def want():
+            return ref.rms_norm(ref.rms_norm(x, gamma, None, 1e-6)[0], gamma, None, 1e-6)[0]
+
+        for _ in range(2):
+            x.copy_(normal(g, 64, 512))
+            graph.replay()
+            close(fetch(c, z), want(), want().abs() * 2000 * ULP)
+        taken = c.device_ptr(z)
+        del z
+        c.barrier(blocking=True)
+        later = [step() for _ in range(3)]
+        kept = [fetch(c, z) for z in later]
+        assert all(c.device_ptr(z) != taken for z in later)
+        x.copy_(normal(g, 64, 512))
+        graph.replay()
+        s.synchronize()
+        for z, k in zip(later, kept):
+            assert torch.equal(fetch(c, z), k)
+        del later, z
+        c.close()
+
+
 def test_bad_pages_in_a_replayed_graph_are_reported(lt):
     s = torch.cuda.Stream()
     torch.cuda.synchronize()
