@@ -141,8 +141,8 @@ typedef enum {
        PAGED_ATTENTION: inputs (q* [B, Hq, D], cache, page table i32 [B, M], lengths i32 [B], [out]), attrs
        {head_major, scale} -> [B, Hq, D]: softmax(scale q k) v of one query token per sequence and head over the first
        lengths[b] tokens, which lie in the pages the table's row b lists in order; Hq is a multiple of the cache's H, D at
-       most 256, and M pages hold at most 2^30 tokens.  An empty sequence gives zeros.  Entries of the table behind a
-       sequence's last page are not read.
+       most 256, and M pages hold at most 2^30 tokens.  An empty sequence gives zeros (and so does a
+       head whose scores are all minus infinity).  Entries of the table behind a sequence's last page are not read.
        A negative length counts as 0; one beyond M pages is cut there and, like a page number outside the cache (its
        tokens are left out), reported as LT_ERR_DEVICE_INDEX.
 
@@ -150,7 +150,8 @@ typedef enum {
        group, eps}.  h = x + residual, y = gamma h / sqrt(mean(h^2) + eps).  result 0: y; 1: h; 2: y in 8 bits, as the
        codes (u8) of float8 e4m3: round(y / scale); 3: the scales f32 [.., groups] = max|y| / 448 over each `group`
        columns (32, 64, 128, 256; 0: the whole row; the last group may be shorter).  A group of zeros has scale 0 and
-       codes 0.  Nodes that differ only in `result` (and [out]) are one launch.
+       codes 0.  mean(h^2) is a binary32 number: a row for which it is infinite or, with eps = 0, vanishes has no norm.
+       Nodes that differ only in `result` (and [out]) are one launch.
 
        RMS_NORM_GRAD: inputs (dy* [.., C], h* [.., C], gamma [C] [, dh* [.., C]], [out]), attrs {result, has dh, eps}.
        result 0: the gradient of h (of x and of the residual alike), plus dh, the gradient that reaches h past the

@@ -1,8 +1,10 @@
 // Attention of one query token per sequence over a paged key-value cache.
 //
 // For each sequence and query head: out = sum_i w_i v_i / sum_i w_i with w_i = exp(scale q k_i - m), m the running
-// maximum.  Every key and value is read once for all the query heads that share it; nothing else of size is read or
-// written, so the bound is the cache's bytes over the memory's rate.
+// maximum.  A block works on up to 8 (f32, and any type without 16-byte alignment), 16 (bf16 heads of more than 128 values)
+// or 32 (bf16) of the query heads that share a key, and reads its keys and values once for them; more of them are several
+// head blocks, each of which reads the cache.  Nothing else of size is read or written, so up to there the bound is the
+// cache's bytes over the memory's rate.
 //
 // Work split: the tokens of all sequences are cut into tiles of TILE; the list of (sequence, head block, tile) is divided
 // evenly over the thread blocks, whatever the sequences' lengths (which only the device knows).  Every (sequence, head
@@ -623,8 +625,10 @@ __device__ __forceinline__ void leave_stretch(const AttendArgs &a, const Share &
 // products: 40 us against 32 on 16 sequences of 16 heads of 64 values), and memory is slow enough for the others.  Two
 // lanes share a token's key, every other chunk each; the weights go through shared memory to all lanes, which have the
 // output's values between them, two neighbouring ones of every 64.  Warps, stages and joins as in lt_attend_tensor.
-// 28 sequences of 300 to 500 tokens, 32 heads of 128: 64 us, 5.7 TB/s; with 16 query heads per key head the products bound
-// it (28 of 1500 to 2000, 8 key heads of 64: 92 us, 2.2 TB/s; 106 when each head's maximum was followed at once).
+// 28 sequences of 300 to 500 tokens, 32 heads of 128: 64 us, 5.7 TB/s.  With 16 query heads per key head the cache is read by
+// two head blocks (28 of 1500 to 2000, 8 key heads of 64: 92 us, 2.2 TB/s of the cache's bytes counted once; 106 when each
+// head's maximum was followed at once), and every four products of a head wait for 16 bytes of its query out of shared memory,
+// with one stage that a warp cannot fill while it computes: a quarter of the products that the units could do.
 template <int DP, int NH, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_single(const AttendArgs a) {
     using S = Shape<float, DP, NH>;
@@ -760,7 +764,7 @@ __global__ void __launch_bounds__(THREADS, single_blocks(DP, NH)) lt_attend_sing
 // tokens along the columns of a register's pair: movmatrix turns them, as two bf16 parts (p and what its rounding left), which keeps
 // the weights to 2^-17 and costs one more product.  Each warp has steps and a copy pipeline of its own -- no barrier
 // in the loop -- and its own running maximum and sum; warps are joined once per stretch.  64 sequences of 17 to 4096
-// tokens, 32 heads on 8 key heads of 128: 92.6 us, 5.8 TB/s; issue slots are 34 % busy, the tensor units 13 %, what is left is
+// tokens, 32 heads on 8 key heads of 128: 95 us, 5.7 TB/s; issue slots are 34 % busy, the tensor units 13 %, what is left is
 // latency: beginning stretches, joining parts, and SMs that reach memory more slowly than others.
 template <int DP, int NT, bool WHOLE_STEPS>
 __global__ void __launch_bounds__(THREADS, tensor_blocks(DP, NT)) lt_attend_tensor(const AttendArgs a) {

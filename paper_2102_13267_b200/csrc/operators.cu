@@ -144,7 +144,7 @@ struct TurnShape {
 // unit and walks over tokens, so what it addresses is found once.  The bound is memory; the angles would not be free if
 // every head computed them (a sine and a cosine are some fifty instructions), so a block computes those of a batch of
 // tokens once, into shared memory, one batch ahead.  The chunks of the next batches are on their way meanwhile: each
-// thread copies its own ahead and reads them back, as in lt_norm_rows.  Rotary 8192 x 32 x 128 bf16: 24.1 us, 5.6 TB/s;
+// thread copies its own ahead and reads them back, as in lt_norm_rows.  Rotary 8192 x 32 x 128 bf16: 24.3 us, 5.5 TB/s;
 // append 8192 x 8 x 128 bf16: 14.5 us, 4.6 TB/s.
 // With 8 bytes, rotary 8192 x 32 x 80 bf16, 40 turned in halves of 20: 19.5 us, against 43 with lt_turn_any.
 template <class T, bool APPEND, bool INTER, int BYTES>
@@ -353,7 +353,10 @@ __device__ __forceinline__ float code_factor(float top) {
 }
 __device__ __forceinline__ float scale_of(float top) { return top * (1.f / 448.f); }
 
-// Any shape and alignment: a block per row, which is read once for its mean square, once more for each output.
+// Any shape and alignment: a block per row, which is read once for its mean square, once more for each output.  Taken by rows
+// of more than 1024 values that cannot be read in pieces of 16 bytes, of more than 16384 f32 or 32768 bf16 values, and, beyond
+// 1024 values, by groups of 256 in f32 (which 32 lanes of four values do not hold).  1000 x 20480 f32 with a residual: 165 us,
+// where 1000 x 16384 takes 47; 4096 x 4096 f32 to eight bits in groups of 256: 94 us, where groups of 128 take 39.
 template <class T>
 __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
     __shared__ float part[32];
@@ -406,8 +409,8 @@ __global__ void __launch_bounds__(256) lt_norm_any(const NormArgs a) {
 // or 128, the fewest that hold the row with eight values of each in registers -- values t, t + RT, ..), so that every value
 // is still read once.  The largest values of 32 columns each go through shared memory to whoever needs them.  Bound by its
 // instructions, one or two dozen per value; against lt_norm_any and lt_norm_grad_any, which read a row up to three times:
-// 8000 x 999 bf16 to eight bits 49 us against 55, the gradient of 8000 x 999 bf16 41 against 118, of 30000 x 131 f32 24
-// against 48.
+// 8000 x 999 bf16 to eight bits 50 us against 55, the gradient of 8000 x 999 bf16 42 against 118, of 30000 x 131 f32 23
+// against 48.  (Groups of 256 in f32 come here too: 8192 x 1024 to eight bits 40 us, where groups of 128 take 22.)
 constexpr int NARROW_COLS = 1024, NARROW_VALUES = 8, NARROW_BLOCKS = 4;  // blocks that share an SM
 constexpr int narrow_threads(uint64_t cols) { return cols <= 32 * NARROW_VALUES ? 32 : cols <= 64 * NARROW_VALUES ? 64 : 128; }
 
@@ -560,7 +563,7 @@ __host__ __device__ constexpr size_t norm_bytes(int rt, int ch) { return (size_t
 // result written once, so the bound is memory.  Threads keep their columns of gamma from row to row.  The rows to come
 // travel through shared memory ahead of their turn: a thread copies and reads back only its own chunks, so the ring
 // needs no barrier; registers alone kept too little on its way (8192 x 4096 bf16: 88 us with four chunks per thread and
-// the next row in registers, 52 us with one chunk per thread).  The same size with a residual, to eight bits: 41.6 us, 5.7
+// the next row in registers, 52 us with one chunk per thread).  The same size with a residual, to eight bits: 42.5 us, 5.5
 // TB/s.
 template <class T, int RT, int CH, bool EIGHT>
 __global__ void __launch_bounds__(norm_block(RT), norm_block(RT) == 1024 ? 1 : (CH == 1 ? 1536 : CH == 2 ? 1024 : 512) / norm_block(RT)) lt_norm_rows(const NormArgs a) {
@@ -713,7 +716,8 @@ __device__ __noinline__ float dot_again(const NormGradArgs &a, const T *dy, cons
 }
 
 // u = h / rms.  dx = dh + (gamma dy - u mean(gamma dy u)) / rms; a block adds up dy u over its rows in its own row of
-// `partial`.
+// `partial`.  Taken by rows of more than 1024 values that cannot be read in pieces of 16 bytes, and of more than 8192 f32 or
+// 16384 bf16 values: 1000 x 12288 f32 190 us, where 1000 x 8192 takes 28; 3000 x 4095 bf16 175 us, where 4096 takes 24.
 template <class T>
 __global__ void __launch_bounds__(256) lt_norm_grad_any(const NormGradArgs a) {
     __shared__ float part[32];
