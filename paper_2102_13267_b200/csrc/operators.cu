@@ -1226,7 +1226,10 @@ cudaError_t lt_operator_status_claim(LtOperatorStatus **out) {
     std::lock_guard<std::mutex> hold(g_lock);
     if (!g_status) {
         void *p = nullptr;
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;  // (the first context may be made while a stream is captured)
+        cudaThreadExchangeStreamCaptureMode(&mode);
         const cudaError_t e = cudaHostAlloc(&p, kStatusWords * sizeof(LtOperatorStatus), cudaHostAllocPortable | cudaHostAllocMapped);
+        cudaThreadExchangeStreamCaptureMode(&mode);
         if (e != cudaSuccess) return e;
         memset(p, 0, kStatusWords * sizeof(LtOperatorStatus));
         g_status = (LtOperatorStatus *)p;

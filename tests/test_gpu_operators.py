@@ -2,6 +2,9 @@
 entry points: types, head layouts, lengths from none to long, odd sizes, slices read in place, unaligned memory, results in
 place, padded batches, other streams, captured flushes, and a run of them together."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -1075,6 +1078,37 @@ def test_bad_pages_in_a_replayed_graph_are_reported(lt):
             table.copy_(good)
     handles.clear()
     c.close()
+
+
+FIRST_CONTEXT_UNDER_CAPTURE = """
+import torch
+import paper_2102_13267_b200 as lt
+
+s = torch.cuda.Stream()
+with torch.cuda.stream(s):
+    x = torch.ones(4, 2, 8, device="cuda")
+    pos = torch.zeros(4, dtype=torch.int32, device="cuda")
+    table = torch.from_numpy(lt.rotary_table(8).view("int32")).cuda()
+    out = torch.zeros_like(x)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        c = lt.LazyContext(device=0, stream=s.cuda_stream)
+        handles = [c.from_torch(x), c.from_torch(pos), c.from_torch(table, "u32"), c.from_torch(out)]
+        c.rotary(*handles[:3], out=handles[3])
+        c.barrier()
+    graph.replay()
+    s.synchronize()
+    assert torch.equal(out, x), out
+    handles.clear()
+    c.close()
+print("replayed")
+"""
+
+
+def test_first_context_of_a_process_is_made_under_capture():
+    done = subprocess.run([sys.executable, "-c", FIRST_CONTEXT_UNDER_CAPTURE], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "replayed" in done.stdout, done.stderr[-2000:]
 
 
 def test_replay(ctx, lt):
