@@ -991,6 +991,53 @@ def test_captured_barriers_share_nothing_and_outlive_their_contexts(lt):
         assert bool((t == 0x7fc07fc0).all())
 
 
+@pytest.mark.parametrize("allocator", ["torch", "none"])
+def test_two_graphs_of_one_context_replay_side_by_side(lt, allocator):
+    """Attention and the norm's gradient, whose blocks leave parts in temporaries; the context flushes between the replays."""
+    s, others = torch.cuda.Stream(), [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        c, g = lt.LazyContext(device=0, stream=s.cuda_stream, allocator=allocator), gen(82)
+        n = [7000, 900]
+        cache, table = paged(g, n, 16, 2, 64, False, torch.bfloat16)
+        ln, gamma = torch.tensor(n, dtype=torch.int32, device="cuda"), 1 + normal(g, 640, std=0.2)
+        dy = normal(g, 3000, 640)
+        data, graphs = [], []
+        for i in range(3):
+            q, h = normal(g, 2, 8, 64, dtype=torch.bfloat16), normal(g, 3000, 640)
+            outs = torch.zeros_like(q), torch.zeros_like(h), torch.zeros(640, device="cuda")
+            data.append((q, h, *outs, [c.from_torch(t) for t in (q, cache, table, ln, dy, h, gamma, *outs)]))
+
+        def step(i):
+            q, ca, tb, l, d, h, ga, att, dx, dg = data[i][5]
+            c.paged_attention(q, ca, tb, l, scale=0.125, out=att)
+            c.rms_norm_grad(d, h, ga, out=(dx, dg))
+            c.barrier()
+
+        step(2)
+        s.synchronize()
+        for i in range(2):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                step(i)
+            graphs.append(graph)
+        s.synchronize()
+    for _ in range(20):
+        for graph, o in zip(graphs, others):
+            with torch.cuda.stream(o):
+                graph.replay()
+        step(2)
+    torch.cuda.synchronize()
+    for q, h, att, dx, dg, _ in data:
+        close(att, *ref.attention(q, cache, table, n, 0.125, False))
+        a, b, e, f = ref.rms_norm_grad(dy, h, gamma, None, 1e-6)
+        close(dx, a, b)
+        close(dg, e, f + e.abs() * ULP)
+    for d in data:
+        d[5].clear()
+    c.close()
+
+
 def test_captured_barrier_without_allocator_callbacks(lt):
     s = torch.cuda.Stream()
     torch.cuda.synchronize()
