@@ -361,10 +361,10 @@ class Batch(_Operators):
         return _BatchRef(self, self._n_inputs - 1)
 
     def op(self, name: str, *inputs, **attrs) -> _BatchRef:
-        a = _attr_list(name, attrs)
-        if len(inputs) > 3:  # an entry has room for three: the others come in one ahead of it
-            self._ops.append((LT_BATCH_MORE, [r.index for r in inputs[3:]], 0, 0, 0))
-        self._ops.append((OPCODES[name], [r.index for r in inputs], len(self._attrs), len(a), 0))
+        code, a, ins = OPCODES[name], _attr_list(name, attrs), [r.index for r in inputs]
+        if len(ins) > 3:  # an entry has room for three: the others come in one ahead of it
+            self._ops.append((LT_BATCH_MORE, ins[3:], 0, 0, 0))
+        self._ops.append((code, ins, len(self._attrs), len(a), 0))
         self._attrs.extend(a)
         self._c = None
         return _BatchRef(self, -len(self._ops))

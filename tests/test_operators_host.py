@@ -275,6 +275,18 @@ def test_slices_are_read_in_place_only_where_rows_are_runs(ctx):
     del a, b, c, d, e, h, i
 
 
+def test_an_operation_that_a_batch_refuses_leaves_nothing_behind(ctx):
+    t = [fake(ctx, *s) for s in (CA, K, K, SL)]
+    b = lt.Batch()
+    i = [b.input() for _ in t]
+    for bad in (lambda: b.op("none such", *i), lambda: b.op("cache_append", i[0], None, i[2], i[3], **APP), lambda: b.op("cache_append", *i[:3], None, **APP)):
+        with pytest.raises((KeyError, AttributeError)):
+            bad()
+    b.cache_append(*i)
+    ctx.record(b, t)
+    assert "operator: cache_append" in plan(ctx)
+
+
 def test_more_than_three_operands_in_a_batch(ctx):
     import ctypes
 
