@@ -58,7 +58,7 @@ typedef enum {
                                  (lt_barrier with blocking set, lt_fetch) after a long-row kernel ran out
                                  of time waiting for a copy into shared memory, or for the partial results
                                  of the other thread blocks of its cluster                                */
-    LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes:
+    LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes, a token outside its table:
                                  reported by the context's first blocking call after the operator that met it, or
                                  after the replay of a graph that captured it (call once the replay is done); the
                                  operator left out what the index named and did the rest.  Up to 4095 contexts at
@@ -155,8 +155,27 @@ typedef enum {
 
        RMS_NORM_GRAD: inputs (dy* [.., C], h* [.., C], gamma [C] [, dh* [.., C]], [out]), attrs {result, has dh, eps}.
        result 0: the gradient of h (of x and of the residual alike), plus dh, the gradient that reaches h past the
-       norm; 1: the gradient of gamma, in gamma's dtype.  Also one launch for both. */
-    LT_OP_ROTARY = 70, LT_OP_CACHE_APPEND = 71, LT_OP_PAGED_ATTENTION = 72, LT_OP_RMS_NORM = 73, LT_OP_RMS_NORM_GRAD = 74
+       norm; 1: the gradient of gamma, in gamma's dtype.  Also one launch for both.
+
+       EMBEDDING: inputs (table* [V, C], ids i32 [..], [out]), attrs {scale} -> [.., C]: scale table[ids].  A negative id is
+       padding and gives zeros; so does one of V or more, which is reported as LT_ERR_DEVICE_INDEX.
+
+       EMBEDDING_GRAD: inputs (dy* [.., C], ids i32 [..] [, base [V, C] f32 or like dy], [out]), attrs {V, has base, scale}
+       -> [V, C] like base, or like dy: base + scale times the sum of the rows of dy whose id is v, for every row v; each sum
+       in binary32, always in the same order.  Ids as above; rows of dy without a token are not read.  lt_assign the result to the base
+       and only the rows that ids name are touched.
+
+       VOCABULARY_LOSS: inputs (x* [.., C], table* [V, C], targets i32 [..], [out]), attrs {result, scale} -> f32 [..].
+       With the scores z = scale x table^T, which are never kept: result 0: the loss lse - z[target]; 1: lse = log of the
+       sum of exp(z) over the vocabulary.  A token whose target is negative has loss 0, and so has one of V or more, which is
+       reported as LT_ERR_DEVICE_INDEX.  One launch for both.
+
+       VOCABULARY_LOSS_GRAD: inputs (x*, table*, targets, lse f32 [..], dloss f32 [..], [out]), attrs {result, scale}, lse
+       being the loss's result 1 on the same x and table.  With P = scale dloss (exp(z - lse) - (1 at the target)), zero for tokens without a
+       target (whose rows of x, lse and dloss do not count, whatever they hold): result 0: P table, the gradient of x; 1: P^T x, that of
+       the table.  One launch for both. */
+    LT_OP_ROTARY = 70, LT_OP_CACHE_APPEND = 71, LT_OP_PAGED_ATTENTION = 72, LT_OP_RMS_NORM = 73, LT_OP_RMS_NORM_GRAD = 74,
+    LT_OP_EMBEDDING = 80, LT_OP_EMBEDDING_GRAD = 81, LT_OP_VOCABULARY_LOSS = 82, LT_OP_VOCABULARY_LOSS_GRAD = 83
 } lt_opcode;
 
 /*

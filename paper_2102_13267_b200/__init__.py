@@ -42,6 +42,7 @@ OPCODES = {
     "col_sum": 53, "col_max": 54, "col_min": 55, "all_sum": 56, "all_max": 57, "all_min": 58,
     "reshape": 60, "narrow": 61, "permute": 62, "update_slice": 63,
     "rotary": 70, "cache_append": 71, "paged_attention": 72, "rms_norm": 73, "rms_norm_grad": 74,
+    "embedding": 80, "embedding_grad": 81, "vocabulary_loss": 82, "vocabulary_loss_grad": 83,
 }
 STATUS_NAMES = ["LT_OK", "LT_ERR_INVALID_ARG", "LT_ERR_SHAPE", "LT_ERR_DTYPE", "LT_ERR_DEVICE",
                 "LT_ERR_UNSUPPORTED", "LT_ERR_OOM", "LT_ERR_CUDA", "LT_ERR_DEVICE_TIMEOUT",
@@ -332,6 +333,38 @@ class _Operators:
         return tuple(made)
 
 
+    def embedding(self, table, ids, *, scale: float = 1.0, out=None):
+        """scale table[ids]: [.., columns] for ids [..]; a negative id is padding and gives zeros."""
+        return self._result("embedding", (table, ids), out, scale=scale)
+
+    def embedding_grad(self, dy, ids, rows: int, *, base=None, scale: float = 1.0, out=None):
+        """The gradient [rows, columns] of a table of `rows` rows from the gradient dy [.., columns] of embedding(table, ids),
+        added to `base` if there is one (assign the result to it: only the rows that ids name are touched)."""
+        inputs = (dy, ids) if base is None else (dy, ids, base)
+        return self._result("embedding_grad", inputs, out, rows=rows, base=base is not None, scale=scale)
+
+    def _results(self, name, inputs, out, **attrs) -> tuple:
+        """Both results of an operator that has two.  `out`: two buffers (or None in the place of one)."""
+        out = [None, None] if out is None else list(out)
+        if len(out) != 2:
+            raise ValueError(f"out: 2 results, {len(out)} buffers")
+        made = [self.op(name, *inputs, *(() if o is None else (o,)), result=w, **attrs) for w, o in enumerate(out)]
+        for t, o in zip(made, out):
+            if o is not None:
+                self.assign(o, t)
+        return tuple(made)
+
+    def vocabulary_loss(self, x, table, targets, *, scale: float = 1.0, out=None) -> tuple:
+        """(cross entropy of every token's target, log of the sum of exponentials) of the scores scale x table^T, which are
+        never kept; a negative target is not counted and has loss 0."""
+        return self._results("vocabulary_loss", (x, table, targets), out, scale=scale)
+
+    def vocabulary_loss_grad(self, x, table, targets, lse, dloss, *, scale: float = 1.0, out=None) -> tuple:
+        """(gradient of x, gradient of the table) of vocabulary_loss from the gradient dloss of its losses and its second
+        result `lse`."""
+        return self._results("vocabulary_loss_grad", (x, table, targets, lse, dloss), out, scale=scale)
+
+
 class _BatchRef:
     """An operand inside a Batch: one of its inputs (index >= 0) or the result of one of its entries (< 0)."""
     __slots__ = ("batch", "index")
@@ -420,6 +453,12 @@ def _attr_list(name: str, attrs: dict) -> list:
         return [int(attrs["result"]), int(bool(attrs["residual"])), int(attrs["group"]), _double_bits(attrs["eps"])]
     if name == "rms_norm_grad":
         return [int(attrs["result"]), int(bool(attrs["residual"])), _double_bits(attrs["eps"])]
+    if name == "embedding":
+        return [_double_bits(attrs["scale"])]
+    if name == "embedding_grad":
+        return [int(attrs["rows"]), int(bool(attrs["base"])), _double_bits(attrs["scale"])]
+    if name in ("vocabulary_loss", "vocabulary_loss_grad"):
+        return [int(attrs["result"]), _double_bits(attrs["scale"])]
     if name == "iota":
         shp = tuple(attrs["shape"])
         return [int(attrs["dim"]), len(shp), *shp]

@@ -12,7 +12,7 @@ OBJ = HERE / "_build"
 LIB = HERE / "liblazytensor.so"
 CUDA_HOME = Path(os.environ.get("CUDA_HOME", "/usr/local/cuda"))
 
-CU_SOURCES = ["kernels.cu", "compiled.cu", "static_scratch.cu", "reduce.cu", "views.cu", "operators.cu", "attention.cu"]
+CU_SOURCES = ["kernels.cu", "compiled.cu", "static_scratch.cu", "reduce.cu", "views.cu", "operators.cu", "attention.cu", "embedding.cu", "vocabulary_loss.cu"]
 CPP_SOURCES = ["engine.cpp", "canon.cpp", "planner.cpp", "executor.cpp", "jit.cpp", "operators.cpp"]
 HEADERS = ["engine.h", "vm.h", "launch.h", "vm_core.inc", "vm_ops.cuh", "compiled.h", "compiled_programs.inc", "pdl.cuh", "compiled_shells.cuh", "jit.h", "../../include/lazytensor.h"]
 
@@ -64,7 +64,7 @@ def _compile(src: str) -> Path:
     path = CSRC / src
     obj = OBJ / (src + ".o")
     deps = [path] + [CSRC / h for h in HEADERS]
-    if src.endswith(".cpp") or src in ("operators.cu", "attention.cu"):
+    if src.endswith(".cpp") or src in ("operators.cu", "attention.cu", "embedding.cu", "vocabulary_loss.cu"):
         deps += [CSRC / h for h in OPERATOR_HEADERS]
     if _stale(obj, deps):
         if src.endswith(".cu"):

@@ -237,9 +237,18 @@ lt_status sync_and_check(lt_ctx *c) {
     cudaError_t e = cudaStreamSynchronize(c->stream);
     if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("cudaStreamSynchronize: ") + cudaGetErrorString(e));
     const LtOperatorStatus found = lt_operator_status_take(c->operator_status);
-    if (found.attention || found.append)
-        return fail(c, LT_ERR_DEVICE_INDEX, std::string(found.attention ? "paged_attention: a page number or a length" : "") + (found.attention && found.append ? "; " : "") +
-                                                (found.append ? "cache_append: a slot number" : "") + " in device memory lies outside the cache; what it names was left out");
+    if (found.attention || found.append || found.embedding || found.loss) {
+        std::string what;
+        auto add = [&](unsigned there, const char *text) {
+            if (there) what += (what.empty() ? "" : "; ") + std::string(text);
+        };
+        if (found.attention || found.append)
+            add(1, ((found.attention ? std::string("paged_attention: a page number or a length") : std::string()) + (found.attention && found.append ? "; " : "") +
+                    (found.append ? "cache_append: a slot number" : "") + " in device memory lies outside the cache").c_str());
+        add(found.embedding, "embedding or embedding_grad: a token in device memory lies outside the table");
+        add(found.loss, "vocabulary_loss or its gradient: a target in device memory lies outside the table");
+        return fail(c, LT_ERR_DEVICE_INDEX, what + "; what it names was left out");
+    }
     if (c->status_pending) {
         c->status_pending = false;
         unsigned int word = 0;
@@ -305,6 +314,8 @@ const char *op_name(int op) {
     case LT_OP_ROTARY: return "rotary"; case LT_OP_CACHE_APPEND: return "cache_append";
     case LT_OP_PAGED_ATTENTION: return "paged_attention"; case LT_OP_RMS_NORM: return "rms_norm";
     case LT_OP_RMS_NORM_GRAD: return "rms_norm_grad";
+    case LT_OP_EMBEDDING: return "embedding"; case LT_OP_EMBEDDING_GRAD: return "embedding_grad";
+    case LT_OP_VOCABULARY_LOSS: return "vocabulary_loss"; case LT_OP_VOCABULARY_LOSS_GRAD: return "vocabulary_loss_grad";
     case N_DEVICE_DATA: return "device_data"; case N_SCALAR: return "constant";
     default: return "?";
     }

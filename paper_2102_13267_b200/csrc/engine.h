@@ -124,7 +124,7 @@ struct IoRef {
 };
 
 // K_RED: a reduction that runs as a kernel of its own (reduce.cu); K_VIEW: a shape operation (views.cu); K_OPERATOR: a
-// transformer operator, with all its results that the graph asks for (operators.cu, attention.cu)
+// transformer operator, with all its results that the graph asks for (operators.cu, attention.cu, embedding.cu, vocabulary_loss.cu)
 enum : uint8_t { K_EW = 0, K_ROW = 1, K_MULTI = 2, K_RED = 3, K_VIEW = 4, K_OPERATOR = 5 };
 
 struct Group {
@@ -485,7 +485,7 @@ std::string describe_plan(const Plan &plan);
 int broadcast_class(const int64_t *dims, int rank, uint64_t rows, uint64_t cols);
 
 // transformer operators (operators.cpp)
-inline bool is_operator(int op) { return op >= LT_OP_ROTARY && op <= LT_OP_RMS_NORM_GRAD; }
+inline bool is_operator(int op) { return (op >= LT_OP_ROTARY && op <= LT_OP_RMS_NORM_GRAD) || (op >= LT_OP_EMBEDDING && op <= LT_OP_VOCABULARY_LOSS_GRAD); }
 lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in, const int64_t *attrs, int n_attrs, int64_t *od, int *orank,
                          int *odtype);
 int operator_core_inputs(const CNode &n);

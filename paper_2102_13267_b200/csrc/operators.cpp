@@ -1,5 +1,6 @@
 // The transformer operators on the host side: checks of their operands, shapes of their results, what the planner and the
-// executor ask about them.  The kernels are in operators.cu (rotary, cache_append, norms) and attention.cu.
+// executor ask about them.  The kernels are in operators.cu (rotary, cache_append, norms), attention.cu, embedding.cu and
+// vocabulary_loss.cu.
 #include <cmath>
 #include <cstring>
 #include <string>
@@ -21,6 +22,17 @@ bool same_shape(const Node &a, const Node &b) {
 
 bool flag(int64_t v) { return v == 0 || v == 1; }
 
+// t is [.., n] for the shape [..] of `lead`
+bool leads(const Node &lead, const Node &t) {
+    if (lead.rank != t.rank - 1) return false;
+    for (int i = 0; i < lead.rank; ++i)
+        if (lead.dims[i] != t.dims[i]) return false;
+    return true;
+}
+
+// Do nodes of this operator that differ in their first attribute only belong to one launch?
+bool selects_result(int op) { return op == LT_OP_RMS_NORM || op == LT_OP_RMS_NORM_GRAD || op == LT_OP_VOCABULARY_LOSS || op == LT_OP_VOCABULARY_LOSS_GRAD; }
+
 }  // namespace
 
 // Shape and dtype of the result `opcode` gives on these operands, or why it gives none.
@@ -28,11 +40,12 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
                          int *odtype) {
     const std::string name = op_name(opcode);
     auto bad = [&](lt_status s, const std::string &why) { return fail(c, s, name + ": " + why); };
-    static const int want_attrs[] = {3, 3, 2, 4, 3};
-    if (n_attrs != want_attrs[opcode - LT_OP_ROTARY]) return bad(LT_ERR_INVALID_ARG, "wrong number of attributes");
+    static const int want_attrs[] = {3, 3, 2, 4, 3}, want_table_attrs[] = {1, 3, 2, 2};
+    if (n_attrs != (opcode >= LT_OP_EMBEDDING ? want_table_attrs[opcode - LT_OP_EMBEDDING] : want_attrs[opcode - LT_OP_ROTARY])) return bad(LT_ERR_INVALID_ARG, "wrong number of attributes");
     for (int i = 0; i < n_in; ++i)
         if (ops[i]->op == N_SCALAR) return bad(LT_ERR_INVALID_ARG, "operands are tensors, not constants");
     auto finite = [](int64_t bits) { return std::isfinite(lt_attr_double(bits)); };
+    auto finite32 = [](int64_t bits) { return std::isfinite((float)lt_attr_double(bits)); };
     auto result = [&](const Node &like, int dtype) {
         *orank = like.rank;
         for (int i = 0; i < like.rank; ++i) od[i] = like.dims[i];
@@ -44,6 +57,13 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         if (pos.dims[0] != tokens) return bad(LT_ERR_SHAPE, "one position per token is needed");
         if (freq.dtype != LT_U32 || freq.rank != 2 || freq.dims[1] != 2) return bad(LT_ERR_DTYPE, "frequencies are a u32 tensor [pairs, 2]");
         if (2 * freq.dims[0] > dim) return bad(LT_ERR_SHAPE, "more pairs than a head has");
+        return LT_OK;
+    };
+
+    auto check_table = [&](const Node &table) -> lt_status {
+        if (!is_float(table.dtype)) return bad(LT_ERR_DTYPE, "the table is f32 or bf16");
+        if (table.rank != 2) return bad(LT_ERR_SHAPE, "the table is [vocabulary, columns]");
+        if (table.dims[0] >= (1ll << 31) || table.dims[1] >= (1ll << 30)) return bad(LT_ERR_UNSUPPORTED, "more rows or columns than the kernel counts");
         return LT_OK;
     };
 
@@ -113,7 +133,7 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         if (cols >= (1ll << 30) || shape_numel(x.dims, x.rank) / cols >= (1ll << 31)) return bad(LT_ERR_UNSUPPORTED, "more rows or columns than the kernel counts");
         result(x, attrs[0] == 2 ? LT_U8 : attrs[0] == 3 ? LT_F32 : x.dtype);
         if (attrs[0] == 3) od[*orank - 1] = (int64_t)lt_row_groups((uint64_t)cols, attrs[2]);
-    } else {  // LT_OP_RMS_NORM_GRAD
+    } else if (opcode == LT_OP_RMS_NORM_GRAD) {
         if (!flag(attrs[1])) return bad(LT_ERR_INVALID_ARG, "attrs are {result, residual gradient, eps}");
         const int core = 3 + (int)attrs[1];
         if (n_in != core && n_in != core + 1)
@@ -131,6 +151,59 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         if (cols >= (1ll << 30) || shape_numel(h.dims, h.rank) / cols >= (1ll << 31)) return bad(LT_ERR_UNSUPPORTED, "more rows or columns than the kernel counts");
         if (attrs[0]) result(gamma, gamma.dtype);
         else result(h, h.dtype);
+    } else if (opcode == LT_OP_EMBEDDING) {
+        if (n_in != 2 && n_in != 3) return bad(LT_ERR_INVALID_ARG, "takes the table, tokens and optionally the result's buffer");
+        if (!finite32(attrs[0])) return bad(LT_ERR_INVALID_ARG, "attrs are {scale}");
+        const Node &table = *ops[0], &ids = *ops[1];
+        const lt_status s = check_table(table);
+        if (s) return s;
+        if (ids.dtype != LT_I32) return bad(LT_ERR_DTYPE, "tokens are i32");
+        if (ids.rank < 1 || ids.rank >= LT_MAX_RANK) return bad(LT_ERR_SHAPE, "tokens have one to five dimensions");
+        if (shape_numel(ids.dims, ids.rank) >= (1ll << 31)) return bad(LT_ERR_UNSUPPORTED, "more tokens than the kernel counts");
+        result(ids, table.dtype);
+        od[(*orank)++] = table.dims[1];
+    } else if (opcode == LT_OP_EMBEDDING_GRAD) {
+        if (!flag(attrs[1]) || !finite32(attrs[2])) return bad(LT_ERR_INVALID_ARG, "attrs are {rows of the table, base, scale}");
+        const int core = 2 + (int)attrs[1];
+        if (n_in != core && n_in != core + 1) return bad(LT_ERR_INVALID_ARG, "takes dy, tokens, the base if there is one and optionally the result's buffer");
+        const Node &dy = *ops[0], &ids = *ops[1];
+        if (!is_float(dy.dtype)) return bad(LT_ERR_DTYPE, "dy is f32 or bf16");
+        if (ids.dtype != LT_I32) return bad(LT_ERR_DTYPE, "tokens are i32");
+        if (dy.rank < 2 || !leads(ids, dy)) return bad(LT_ERR_SHAPE, "dy is [.., columns] for tokens [..]");
+        if (attrs[0] < 1) return bad(LT_ERR_INVALID_ARG, "the table has at least one row");
+        const int64_t cols = dy.dims[dy.rank - 1];
+        if (cols >= (1ll << 30) || attrs[0] >= (1ll << 31) || shape_numel(ids.dims, ids.rank) >= (1ll << 30)) return bad(LT_ERR_UNSUPPORTED, "more tokens, rows or columns than the kernel counts");
+        od[0] = attrs[0];
+        od[1] = cols;
+        *orank = 2;
+        *odtype = dy.dtype;
+        if (attrs[1]) {
+            const Node &base = *ops[2];
+            if (base.dtype != LT_F32 && base.dtype != dy.dtype) return bad(LT_ERR_DTYPE, "the base is f32 or like dy");
+            if (base.rank != 2 || base.dims[0] != attrs[0] || base.dims[1] != cols) return bad(LT_ERR_SHAPE, "the base is [rows, columns]");
+            *odtype = base.dtype;
+        }
+    } else {  // LT_OP_VOCABULARY_LOSS, LT_OP_VOCABULARY_LOSS_GRAD
+        const bool grad = opcode == LT_OP_VOCABULARY_LOSS_GRAD;
+        const int core = grad ? 5 : 3;
+        if (n_in != core && n_in != core + 1)
+            return bad(LT_ERR_INVALID_ARG, grad ? "takes x, the table, targets, lse, dloss and optionally the result's buffer" : "takes x, the table, targets and optionally the result's buffer");
+        if (!flag(attrs[0]) || !finite32(attrs[1]))
+            return bad(LT_ERR_INVALID_ARG, grad ? "attrs are {result: 0 (gradient of x) or 1 (of the table), scale}" : "attrs are {result: 0 (loss) or 1 (log of the sum of exponentials), scale}");
+        const Node &x = *ops[0], &table = *ops[1], &ids = *ops[2];
+        const lt_status s = check_table(table);
+        if (s) return s;
+        if (x.dtype != table.dtype) return bad(LT_ERR_DTYPE, "x and the table are both f32 or both bf16");
+        if (ids.dtype != LT_I32) return bad(LT_ERR_DTYPE, "targets are i32");
+        if (x.rank < 2 || x.dims[x.rank - 1] != table.dims[1] || !leads(ids, x)) return bad(LT_ERR_SHAPE, "x is [.., columns of the table] for targets [..]");
+        if (shape_numel(ids.dims, ids.rank) >= (1ll << 24) || table.dims[0] >= (1ll << 24) || table.dims[1] >= (1ll << 20))
+            return bad(LT_ERR_UNSUPPORTED, "more tokens, rows or columns than the kernel counts");
+        for (int k = 3; k < core; ++k) {
+            if (ops[k]->dtype != LT_F32) return bad(LT_ERR_DTYPE, "lse and dloss are f32");
+            if (!same_shape(*ops[k], ids)) return bad(LT_ERR_SHAPE, "lse and dloss have the shape of the targets");
+        }
+        if (!grad) result(ids, LT_F32);
+        else result(attrs[0] ? table : x, x.dtype);
     }
     const int core = operator_inputs(opcode, n_in, attrs);
     if (n_in > core) {
@@ -148,13 +221,12 @@ int operator_core_inputs(const CNode &n) {
 }
 
 // which of its operator's results a node is
-int operator_result(const CNode &n) { return n.op == LT_OP_RMS_NORM || n.op == LT_OP_RMS_NORM_GRAD ? (int)n.attr0 : 0; }
+int operator_result(const CNode &n) { return selects_result(n.op) ? (int)n.attr0 : 0; }
 
 // Two nodes that are results (the same or different ones) of one operator on the same operands.
 bool operator_same_launch(const CNode &a, const CNode &b) {
     if (a.op != b.op || a.attr1 != b.attr1 || a.attr2 != b.attr2 || a.attr3 != b.attr3) return false;
-    const bool selects = a.op == LT_OP_RMS_NORM || a.op == LT_OP_RMS_NORM_GRAD;
-    if (!selects && a.attr0 != b.attr0) return false;
+    if (!selects_result(a.op) && a.attr0 != b.attr0) return false;
     const int core = operator_core_inputs(a);
     if (core != operator_core_inputs(b)) return false;
     for (int k = 0; k < core; ++k)
@@ -171,6 +243,8 @@ uint64_t operator_operand_rows(const CNode &n, int k, const CNode &operand) {
     case LT_OP_ROTARY: case LT_OP_PAGED_ATTENTION: row_operand = k == 0; break;
     case LT_OP_CACHE_APPEND: row_operand = k == 1 || k == 2; break;
     case LT_OP_RMS_NORM: row_operand = k < core - 1; last_dim = true; break;
+    case LT_OP_EMBEDDING: case LT_OP_EMBEDDING_GRAD: row_operand = k == 0; last_dim = true; break;
+    case LT_OP_VOCABULARY_LOSS: case LT_OP_VOCABULARY_LOSS_GRAD: row_operand = k <= 1; last_dim = true; break;
     default: row_operand = k < core && k != 2; last_dim = true; break;
     }
     if (!row_operand) return 0;
@@ -187,6 +261,7 @@ bool operator_in_place(const CNode &n, int k) {
     case LT_OP_ROTARY: case LT_OP_CACHE_APPEND: return k == 0;
     case LT_OP_RMS_NORM: return (n.attr0 == 0 || n.attr0 == 1) && k < core - 1;
     case LT_OP_RMS_NORM_GRAD: return n.attr0 == 0 && k < core && k != 2;
+    case LT_OP_EMBEDDING_GRAD: return n.attr1 && k == 2;
     default: return false;
     }
 }
@@ -232,6 +307,20 @@ void operator_fill(const Canonical &cg, const CNode &n, LtOperator &o) {
         o.page = (uint32_t)(n.attr0 ? ca.dims[3] : ca.dims[2]);
         o.table_width = (uint32_t)cg.nodes[n.in[2]].dims[1];
         o.pitch[0] = inner(x, 1);
+    } else if (n.op == LT_OP_EMBEDDING) {
+        o.vocabulary = (uint64_t)x.dims[0];
+        o.cols = o.pitch[0] = (uint64_t)x.dims[1];
+        o.rows = inner(cg.nodes[n.in[1]], 0);
+    } else if (n.op == LT_OP_EMBEDDING_GRAD) {
+        o.vocabulary = (uint64_t)n.attr0;
+        o.cols = o.pitch[0] = (uint64_t)x.dims[x.rank - 1];
+        o.rows = inner(cg.nodes[n.in[1]], 0);
+        o.gamma_dtype = n.dtype;
+    } else if (n.op == LT_OP_VOCABULARY_LOSS || n.op == LT_OP_VOCABULARY_LOSS_GRAD) {
+        const CNode &table = cg.nodes[n.in[1]];
+        o.vocabulary = (uint64_t)table.dims[0];
+        o.cols = o.pitch[0] = o.pitch[1] = (uint64_t)table.dims[1];
+        o.rows = inner(x, 0) / o.cols;
     } else {
         const int gamma = n.op == LT_OP_RMS_NORM ? o.n_in - 1 : 2;
         o.cols = (uint64_t)x.dims[x.rank - 1];
@@ -259,6 +348,10 @@ uint64_t operator_bytes(const LtOperator &o) {
         if (o.wanted & 8u) b += 4 * o.rows * lt_row_groups(o.cols, o.attr[2]);
         return b + o.cols * dtype_size(o.gamma_dtype);
     }
+    case LT_OP_EMBEDDING: return 2 * o.rows * o.cols * es + 4 * o.rows;
+    case LT_OP_EMBEDDING_GRAD: return o.rows * o.cols * es + (uint64_t)(o.n_in - 1) * o.vocabulary * o.cols * dtype_size(o.gamma_dtype) + 4 * o.rows;
+    case LT_OP_VOCABULARY_LOSS: return (o.rows + o.vocabulary) * o.cols * es + 12 * o.rows;
+    case LT_OP_VOCABULARY_LOSS_GRAD: return (o.rows * (1 + (o.wanted & 1u)) + o.vocabulary * (1 + (o.wanted >> 1 & 1u))) * o.cols * es + 12 * o.rows;
     default: return (uint64_t)(o.n_in - 1 + (o.wanted & 1u)) * o.rows * o.cols * es + 2 * o.cols * dtype_size(o.gamma_dtype);
     }
 }

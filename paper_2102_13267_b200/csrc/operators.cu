@@ -1,6 +1,6 @@
 // Kernels of the transformer operators that move every value once: rotary positions, appending to a paged key-value
 // cache, the root-mean-square norm (with the residual's addition and an 8-bit output) and its gradient.  The attention
-// that reads the cache is in attention.cu.
+// that reads the cache is in attention.cu, what follows tokens into a table in embedding.cu and vocabulary_loss.cu.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -1205,6 +1205,9 @@ cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStrea
 size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count) {
     if (o.op == LT_OP_PAGED_ATTENTION) return lt_paged_attention_scratch(o, sm_count);
     if (o.op == LT_OP_RMS_NORM_GRAD) return lt_rms_norm_grad_scratch(o, sm_count);
+    if (o.op == LT_OP_EMBEDDING_GRAD) return lt_embedding_grad_scratch(o);
+    if (o.op == LT_OP_VOCABULARY_LOSS) return lt_vocabulary_loss_scratch(o, sm_count);
+    if (o.op == LT_OP_VOCABULARY_LOSS_GRAD) return lt_vocabulary_loss_grad_scratch(o, sm_count);
     return 0;
 }
 
@@ -1216,6 +1219,10 @@ cudaError_t lt_launch_operator(const LtOperator &o, int sm_count, cudaStream_t s
     case LT_OP_PAGED_ATTENTION: return lt_launch_paged_attention(o, sm_count, stream);
     case LT_OP_RMS_NORM: return lt_launch_rms_norm(o, sm_count, stream);
     case LT_OP_RMS_NORM_GRAD: return lt_launch_rms_norm_grad(o, sm_count, stream, launched);
+    case LT_OP_EMBEDDING: return lt_launch_embedding(o, sm_count, stream);
+    case LT_OP_EMBEDDING_GRAD: return lt_launch_embedding_grad(o, sm_count, stream, launched);
+    case LT_OP_VOCABULARY_LOSS: return lt_launch_vocabulary_loss(o, sm_count, stream, launched);
+    case LT_OP_VOCABULARY_LOSS_GRAD: return lt_launch_vocabulary_loss_grad(o, sm_count, stream, launched);
     default: return cudaErrorInvalidValue;
     }
 }
@@ -1252,5 +1259,7 @@ LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status) {
     LtOperatorStatus s;
     s.attention = __atomic_exchange_n(&status->attention, 0u, __ATOMIC_ACQ_REL);
     s.append = __atomic_exchange_n(&status->append, 0u, __ATOMIC_ACQ_REL);
+    s.embedding = __atomic_exchange_n(&status->embedding, 0u, __ATOMIC_ACQ_REL);
+    s.loss = __atomic_exchange_n(&status->loss, 0u, __ATOMIC_ACQ_REL);
     return s;
 }

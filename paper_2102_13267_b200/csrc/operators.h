@@ -11,14 +11,14 @@
 
 // Where a context's operators leave word that an index in device memory lay outside what it indexes.
 struct LtOperatorStatus {
-    unsigned int attention, append;
+    unsigned int attention, append, embedding, loss;
 };
 
 // One launch of an operator.  Everything but the addresses is known when the graph is planned.
 struct LtOperator {
     int op;
     int dtype;                             // of the data: x, the cache, ..
-    int gamma_dtype;                       // norms
+    int gamma_dtype;                       // norms; embedding_grad: of the result and the base
     int n_in;                              // operands that are read
     int64_t attr[4];                       // as passed to lt_op
     const void *in[LT_OPERATOR_INPUTS];
@@ -26,13 +26,14 @@ struct LtOperator {
     void *out[LT_OPERATOR_RESULTS];        // per result; null where the graph does not ask for it
     unsigned wanted;                       // bit k: result k is asked for
     void *scratch;
-    LtOperatorStatus *status;              // paged_attention, cache_append
+    LtOperatorStatus *status;              // operators that follow indices in device memory
     void *arrivals;                        // paged_attention: LT_ARRIVALS counters that are zero between launches
     // sizes (those that the operator has)
     uint64_t rows;                         // tokens, sequences or rows
     uint32_t heads, kv_heads, dim, pairs;  // pairs: rotated pairs of a head
     uint32_t pages, page, table_width;
     uint64_t cols;
+    uint64_t vocabulary;                   // rows of a table that tokens name
 };
 
 static inline double lt_attr_double(int64_t bits) {
@@ -51,6 +52,10 @@ static inline int operator_inputs(int op, int n_in, const int64_t *attrs) {
     case LT_OP_CACHE_APPEND: return n_in;
     case LT_OP_PAGED_ATTENTION: return 4;
     case LT_OP_RMS_NORM: return 2 + (attrs[1] ? 1 : 0);
+    case LT_OP_EMBEDDING: return 2;
+    case LT_OP_EMBEDDING_GRAD: return 2 + (attrs[1] ? 1 : 0);
+    case LT_OP_VOCABULARY_LOSS: return 3;
+    case LT_OP_VOCABULARY_LOSS_GRAD: return 5;
     default: return 3 + (attrs[1] ? 1 : 0);  // LT_OP_RMS_NORM_GRAD
     }
 }
@@ -77,3 +82,10 @@ size_t lt_paged_attention_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_rms_norm(const LtOperator &o, int sm_count, cudaStream_t stream);
 cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
 size_t lt_rms_norm_grad_scratch(const LtOperator &o, int sm_count);
+cudaError_t lt_launch_embedding(const LtOperator &o, int sm_count, cudaStream_t stream);
+cudaError_t lt_launch_embedding_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
+size_t lt_embedding_grad_scratch(const LtOperator &o);
+cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
+size_t lt_vocabulary_loss_scratch(const LtOperator &o, int sm_count);
+cudaError_t lt_launch_vocabulary_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
+size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int sm_count);
