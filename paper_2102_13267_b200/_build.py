@@ -17,7 +17,7 @@ CPP_SOURCES = ["engine.cpp", "canon.cpp", "planner.cpp", "executor.cpp", "jit.cp
 HEADERS = ["engine.h", "vm.h", "launch.h", "vm_core.inc", "vm_ops.cuh", "compiled.h", "compiled_programs.inc", "pdl.cuh", "compiled_shells.cuh", "jit.h", "../../include/lazytensor.h"]
 
 # read by the host runtime and the operators' kernels only
-OPERATOR_HEADERS = ["operators.h", "operator_device.cuh"]
+OPERATOR_HEADERS = ["operators.h", "operator_device.cuh", "tensor_device.cuh"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-diag-suppress", "177",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

@@ -237,6 +237,7 @@ lt_status sync_and_check(lt_ctx *c) {
     cudaError_t e = cudaStreamSynchronize(c->stream);
     if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("cudaStreamSynchronize: ") + cudaGetErrorString(e));
     const LtOperatorStatus found = lt_operator_status_take(c->operator_status);
+    if (found.timeout) return fail(c, LT_ERR_DEVICE_TIMEOUT, "a kernel gave up waiting for its operands or its products; results of that flush are incomplete");
     if (found.attention || found.append || found.embedding || found.loss) {
         std::string what;
         auto add = [&](unsigned there, const char *text) {

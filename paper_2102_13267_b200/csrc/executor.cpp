@@ -320,6 +320,7 @@ lt_status execute_plan(lt_ctx *c, Plan &plan, const Canonical &cg, bool *needs_s
                 o.scratch = g.scratch_temp >= 0 ? c->temp_ptr[g.scratch_temp] : nullptr;
                 o.arrivals = arrivals;
                 o.status = c->operator_status;
+                o.wait_ns = (uint64_t)c->wait_limit_ns;
                 if (ev0) cudaEventRecord(ev0, c->stream);
                 e = lt_launch_operator(o, c->sm_count, c->stream, &launched);
                 if (ev1) cudaEventRecord(ev1, c->stream);

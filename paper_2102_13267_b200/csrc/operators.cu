@@ -1205,7 +1205,7 @@ cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStrea
 size_t lt_operator_scratch_bytes(const LtOperator &o, int sm_count) {
     if (o.op == LT_OP_PAGED_ATTENTION) return lt_paged_attention_scratch(o, sm_count);
     if (o.op == LT_OP_RMS_NORM_GRAD) return lt_rms_norm_grad_scratch(o, sm_count);
-    if (o.op == LT_OP_EMBEDDING_GRAD) return lt_embedding_grad_scratch(o);
+    if (o.op == LT_OP_EMBEDDING_GRAD) return lt_embedding_grad_scratch(o, sm_count);
     if (o.op == LT_OP_VOCABULARY_LOSS) return lt_vocabulary_loss_scratch(o, sm_count);
     if (o.op == LT_OP_VOCABULARY_LOSS_GRAD) return lt_vocabulary_loss_grad_scratch(o, sm_count);
     return 0;
@@ -1261,5 +1261,6 @@ LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status) {
     s.append = __atomic_exchange_n(&status->append, 0u, __ATOMIC_ACQ_REL);
     s.embedding = __atomic_exchange_n(&status->embedding, 0u, __ATOMIC_ACQ_REL);
     s.loss = __atomic_exchange_n(&status->loss, 0u, __ATOMIC_ACQ_REL);
+    s.timeout = __atomic_exchange_n(&status->timeout, 0u, __ATOMIC_ACQ_REL);
     return s;
 }

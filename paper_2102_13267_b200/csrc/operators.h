@@ -12,6 +12,7 @@
 // Where a context's operators leave word that an index in device memory lay outside what it indexes.
 struct LtOperatorStatus {
     unsigned int attention, append, embedding, loss;
+    unsigned int timeout;                  // a wait inside a kernel ran out of time
 };
 
 // One launch of an operator.  Everything but the addresses is known when the graph is planned.
@@ -27,6 +28,7 @@ struct LtOperator {
     unsigned wanted;                       // bit k: result k is asked for
     void *scratch;
     LtOperatorStatus *status;              // operators that follow indices in device memory
+    uint64_t wait_ns;                      // how long a wait inside a kernel may last
     void *arrivals;                        // paged_attention: LT_ARRIVALS counters that are zero between launches
     // sizes (those that the operator has)
     uint64_t rows;                         // tokens, sequences or rows
@@ -84,7 +86,7 @@ cudaError_t lt_launch_rms_norm_grad(const LtOperator &o, int sm_count, cudaStrea
 size_t lt_rms_norm_grad_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_embedding(const LtOperator &o, int sm_count, cudaStream_t stream);
 cudaError_t lt_launch_embedding_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
-size_t lt_embedding_grad_scratch(const LtOperator &o);
+size_t lt_embedding_grad_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
 size_t lt_vocabulary_loss_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_vocabulary_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);

@@ -3,223 +3,909 @@
 // z = scale x table^T [tokens, vocabulary]; lse_n = log sum_v exp z_nv; loss_n = lse_n - z[n, target_n].
 // P = scale dloss_n (exp(z - lse_n) - [v = target_n]); dx = P table; dtable = P^T x.
 //
-// Scores are made a tile at a time.  The loss keeps of each tile the rows' maxima and sums of exponentials, which are joined in the
-// tiles' order; the gradient makes P for a piece of the vocabulary at a time and multiplies it from both sides.
+// Three matrix products, one kernel (lt_product) that differs in how its operands lie and in what it does with a tile of the
+// result.  Scores never reach memory: the loss keeps of each tile the rows' maxima and sums of exponentials, which
+// lt_loss_join adds up in the tiles' order.  The gradient makes P for a piece of the vocabulary at a time, in bf16, and
+// multiplies it from both sides while it is in the L2 cache.
+//
+// Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value, as much as storing
+// the gradients costs).  f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
+// parts the six largest are added: what is left out is below 2^-23 of each product.
 #include <algorithm>
 
-#include "operator_device.cuh"
+#include "tensor_device.cuh"
 
 using namespace ltop;
 
 namespace {
 
-constexpr int TILE = 64, DEPTH = 16, THREADS = 256;
+constexpr uint32_t ROWS = 128;      // of the left operand, per block
+constexpr uint32_t WIDTH = 256;     // columns of a tile
+constexpr uint32_t LEAST_WIDTH = 128;
+constexpr uint32_t DEPTH = 64;      // of K at a time: rows of 128 bytes
+constexpr int TAKERS = 8;           // warps that take the results: two for the 32 rows of tensor memory that a warp can read, half of the columns each
+constexpr uint32_t SIDE = WIDTH / 2;
+constexpr int THREADS = 128 + 32 * TAKERS;  // before them a warp that copies, one that multiplies, two that do nothing
+constexpr uint32_t STAGE_A = ROWS * DEPTH * 2;
 
-// A matrix in memory: element (i, k) at p + i * row + k * col.
-struct Matrix {
-    const void *p;
-    uint64_t row, col;
+template <int BLOCKS>
+struct Ring {
+    static constexpr uint32_t STAGE_B = WIDTH / BLOCKS * DEPTH * 2;
+    static constexpr uint32_t STAGE = STAGE_A + STAGE_B;
+    static constexpr int STAGES = BLOCKS == 1 ? 4 : 6;
+    static constexpr uint32_t BYTES = STAGES * STAGE + 1024;  // (to begin on a multiple of 1024)
 };
+
+enum { TO_LOSS, TO_P, TO_SUM, TO_F32, TO_BF16 };
 
 struct ProductArgs {
-    Matrix a, b;                // [m, depth], [n, depth]
-    uint32_t m, n, depth;
+    uint32_t m, n;              // of the result
+    uint32_t tiles_m, tiles_n, splits;
+    uint32_t width;             // columns of a tile, a multiple of 16 x BLOCKS up to WIDTH
+    uint32_t blocks_k;          // steps of K of one product
+    uint32_t part_a, part_b;    // columns from a part to the next
+    // TO_LOSS, TO_P
     const int *targets;
+    float scale, scale2;        // scale2: times log2(e), as exponentials are powers of two
+    float2 *tops;               // [halves of tiles of the vocabulary][tokens]: maximum and sum, base two
+    float *target_score;        // [tokens], base two
+    uint32_t first, first_tile, vocabulary;  // of the table's row that column 0 of the result is: its number, and that of its tile's first half
     const float *lse, *dloss;
-    float2 *tops;               // [tiles of n][m]
-    float *target_score;        // [m]
-    float *p;                   // [m][n]
-    float *sum;                 // [m][n] so far, or null
-    void *out;
-    uint32_t first, vocabulary; // first: row of the table that column 0 of the product is
-    float scale;
-    unsigned int *status;
-    int more;                   // more pieces follow: the sum goes back to `sum`
+    __nv_bfloat16 *p;
+    uint64_t p_pitch;
+    uint32_t p_part;
+    const uint8_t *odd_a, *odd_b;  // f32: which rows of the operands are not finite (1: infinities, 2: no numbers)
+    const float *plain_a, *plain_b;
+    uint64_t plain_pitch_a, plain_pitch_b;
+    uint32_t plain_cols;
+    // TO_SUM, TO_F32, TO_BF16
+    const float *before;        // [m][n] to be added, or null
+    void *out;                  // [m][n]; TO_SUM: [splits][m][n]
+    int wide;                   // rows of `out` begin on 16 bytes
+    unsigned int *bad_target, *timeout;
+    uint64_t limit_ns;
 };
 
-enum { TO_LOSS, TO_P, TO_RESULT };
+// (a, b) parts of the products of three by three that are kept, smallest first
+__device__ __forceinline__ uint32_t part_of_a(uint32_t i) { return (0x001120u >> (4 * i)) & 15; }
+__device__ __forceinline__ uint32_t part_of_b(uint32_t i) { return (0x010102u >> (4 * i)) & 15; }
 
-template <class TA, class TB, class R, int TO>
-__global__ void __launch_bounds__(THREADS) lt_product(const ProductArgs a) {
-    __shared__ float sa[DEPTH][TILE + 1], sb[DEPTH][TILE + 1];
-    pdl_release();
-    pdl_wait();
-    const uint32_t i0 = blockIdx.y * TILE, j0 = blockIdx.x * TILE, ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-    float c[4][4] = {};
-    for (uint32_t k0 = 0; k0 < a.depth; k0 += DEPTH) {
-        for (uint32_t x = threadIdx.x; x < TILE * DEPTH; x += THREADS) {
-            const uint32_t i = x / DEPTH, k = x % DEPTH;
-            const bool in = k0 + k < a.depth;
-            sa[k][i] = in && i0 + i < a.m ? to_float(((const TA *)a.a.p)[(i0 + i) * a.a.row + (k0 + k) * a.a.col]) : 0.f;
-            sb[k][i] = in && j0 + i < a.n ? to_float(((const TB *)a.b.p)[(j0 + i) * a.b.row + (k0 + k) * a.b.col]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < DEPTH; ++k)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) c[u][v] += sa[k][ti * 4 + u] * sb[k][tj * 4 + v];
-        __syncthreads();
+struct Tile {
+    uint32_t m, n, split;
+};
+// Tiles side by side in time share operands in the L2 cache: eight rows of tiles at a time.
+__device__ __forceinline__ Tile tile_of(const ProductArgs &a, uint32_t t) {
+    Tile r;
+    const uint32_t per = a.tiles_m * a.tiles_n;
+    r.split = t / per;
+    t -= r.split * per;
+    const uint32_t band = t / (8 * a.tiles_n), height = min(8u, a.tiles_m - 8 * band);
+    t -= band * 8 * a.tiles_n;
+    r.n = t / height;
+    r.m = 8 * band + t - r.n * height;
+    return r;
+}
+
+// The products of K steps [k0, k1) of a tile
+template <int PARTS>
+__device__ __forceinline__ void steps_of(const ProductArgs &a, uint32_t split, uint32_t *k0, uint32_t *k1) {
+    const uint32_t all = a.blocks_k * (PARTS == 1 ? 1 : 6);
+    *k0 = (uint32_t)((uint64_t)all * split / a.splits);
+    *k1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
+}
+
+// What a thread does with its row of a tile: `row` of the result, columns col .. col + 32 at a time.
+template <int TO, int PARTS>
+struct Epilogue;
+
+template <int PARTS>
+struct Epilogue<TO_LOSS, PARTS> {
+    const ProductArgs &a;
+    uint32_t row;
+    bool in;
+    int target;
+    float top, sum;
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_) : a(a_), row(row_), in(row_ < a_.m), top(-INFINITY), sum(0.f) {
+        target = in ? a.targets[row] : -1;
+        if (target >= 0 && (uint32_t)target >= a.vocabulary) report(a.bad_target);
     }
+    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t end) {
+        float t = top;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const uint32_t i = i0 + ti * 4 + u;
-        const int target = TO != TO_RESULT && i < a.m ? a.targets[i] : -1;
-        if (TO == TO_LOSS) {
-            if (target >= 0 && (uint32_t)target >= a.vocabulary && threadIdx.x % 16 == 0) report(a.status);
-            float top = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (j0 + tj * 4 + v < a.n) top = max_nan(top, c[u][v] * a.scale);
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (j0 + tj * 4 + v < a.n) {
-                    sum += expf(c[u][v] * a.scale - (top == -INFINITY ? 0.f : top));
-                    if (i < a.m && (int)(j0 + tj * 4 + v) == target) a.target_score[i] = c[u][v] * a.scale;
-                }
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (tj == 0 && i < a.m) a.tops[(uint64_t)blockIdx.x * a.m + i] = make_float2(top, sum);
-            continue;
+        for (int i = 0; i < 32; ++i) {
+            f[i] *= a.scale2;
+            if (col + 32 > end && col + i >= end) f[i] = -INFINITY;
+            t = max_nan(t, f[i]);
         }
-        if (i >= a.m) continue;
+        const float base = t == -INFINITY ? 0.f : t;
+        const uint32_t at = (uint32_t)target - a.first - col;
+        if (in && target >= 0 && at < 32 && col + at < end) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const uint32_t j = j0 + tj * 4 + v;
-            if (j >= a.n) continue;
-            const uint64_t at = (uint64_t)i * a.n + j;
-            if (TO == TO_P) {
-                const bool counts = target >= 0 && (uint32_t)target < a.vocabulary;
-                a.p[at] = counts ? (expf(c[u][v] * a.scale - a.lse[i]) - ((int)(a.first + j) == target ? 1.f : 0.f)) * a.dloss[i] * a.scale : 0.f;
+            for (int i = 0; i < 32; ++i)
+                if (at == (uint32_t)i) a.target_score[row] = f[i];
+        }
+        float s[4] = {sum * exp2f(top - base), 0.f, 0.f, 0.f};
+        if (top == -INFINITY) s[0] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float e;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f[i] - base));
+            s[i & 3] += e;
+        }
+        sum = (s[0] + s[1]) + (s[2] + s[3]);
+        top = t;
+    }
+    __device__ __forceinline__ void finish(const Tile &t, uint32_t side) {
+        if (in) a.tops[(uint64_t)(a.first_tile + 2 * t.n + side) * a.m + row] = make_float2(top, sum);
+    }
+};
+
+template <int PARTS>
+struct Epilogue<TO_P, PARTS> {
+    const ProductArgs &a;
+    uint32_t row;
+    bool in;
+    int target;
+    float lse2, factor;
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_) : a(a_), row(row_), in(row_ < a_.m) {
+        target = in ? a.targets[row] : -1;
+        if ((uint32_t)target >= a.vocabulary) target = -1;
+        lse2 = target >= 0 ? a.lse[row] * 1.44269504f : 0.f;
+        factor = target >= 0 ? a.dloss[row] * a.scale : 0.f;
+    }
+    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t) {
+        if (!in || col >= a.p_part) return;
+        const uint32_t at = (uint32_t)target - a.first - col;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float e;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(f[i], a.scale2, -lse2)));
+            if (at == (uint32_t)i) e -= 1.f;
+            f[i] = target >= 0 && col + i < a.n ? e * factor : 0.f;
+        }
+        __nv_bfloat16 *to = a.p + (uint64_t)row * a.p_pitch + col;
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                reinterpret_cast<uint4 *>(to)[i] =
+                    make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]), pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] -= __bfloat162float(__float2bfloat16_rn(f[i]));
+            to += a.p_part;
+        }
+    }
+    __device__ __forceinline__ void finish(const Tile &, uint32_t) {}
+};
+
+template <int TO, int PARTS>
+struct Epilogue {
+    const ProductArgs &a;
+    uint32_t row;
+    uint64_t at;
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_) : a(a_), row(row_), at(((TO == TO_SUM ? (uint64_t)t.split * a_.m : 0) + row_) * a_.n) {}
+    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t) {
+        if (row >= a.m || col >= a.n) return;
+        if (a.before) {
+            const float *b = a.before + at + col;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col + i < a.n) f[i] += b[i];
+        }
+        if (TO == TO_BF16) {
+            __nv_bfloat16 *to = (__nv_bfloat16 *)a.out + at + col;
+            if (a.wide && col + 32 <= a.n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    reinterpret_cast<uint4 *>(to)[i] =
+                        make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]), pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
             } else {
-                const float s = c[u][v] + (a.sum && a.first ? a.sum[at] : 0.f);
-                if (a.more) a.sum[at] = s;
-                else ((R *)a.out)[at] = from_float<R>(s);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + i < a.n) to[i] = __float2bfloat16_rn(f[i]);
+            }
+        } else {
+            float *to = (float *)a.out + at + col;
+            if (a.wide && col + 32 <= a.n) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) reinterpret_cast<float4 *>(to)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + i < a.n) to[i] = f[i];
             }
         }
     }
+    __device__ __forceinline__ void finish(const Tile &, uint32_t) {}
+};
+
+// The parts of an infinite f32 value are infinity and zeros, whose products with the parts of another value are no numbers where the
+// value's product is infinite.  Scores of rows that hold infinities are therefore made one by one.
+__device__ __noinline__ float score_of(const ProductArgs &a, uint32_t row, uint32_t col) {
+    const float *x = a.plain_a + row * a.plain_pitch_a, *w = a.plain_b + col * a.plain_pitch_b;
+    float s = 0.f;
+    for (uint32_t k = 0; k < a.plain_cols; ++k) s += x[k] * w[k];
+    return s;
+}
+__device__ __forceinline__ void mend_scores(const ProductArgs &a, float (&f)[32], uint32_t row, uint32_t col) {
+    const uint32_t lane = threadIdx.x & 31;
+    const int odd = row < a.m ? a.odd_a[row] : 0, other = col + lane < a.n ? a.odd_b[col + lane] : 0;
+    const uint32_t one = __ballot_sync(0xffffffffu, other == 1), two = __ballot_sync(0xffffffffu, other == 2);
+    if (!(odd | one | two) || row >= a.m) return;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        if (odd == 2 || (two >> i & 1)) f[i] = NAN;
+        else if ((odd == 1 || (one >> i & 1)) && col + i < a.n) f[i] = score_of(a, row, col + i);
+    }
 }
 
+// result = A B^T over a list of tiles of ROWS x BLOCKS by WIDTH; BLOCKS: blocks that share a tile, a cluster.  A_TURNED, B_TURNED: the operand
+// lies in memory with K down the rows.
+//
+// One warp copies operands ahead into a ring of stages, one thread multiplies them into an accumulator in tensor memory, four
+// warps take finished tiles from there while the next one is made in the other half.  All waits are bounded.
+//
+// The tensor cores cut the sum of what they add to off instead of rounding it (half a unit of 2^-23 each time on average, all in one
+// direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, STEPS steps of K at a time are
+// summed in tensor memory (0: all of them) and those sums added up in registers, by the warps that take them.
+__host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts) { return parts == 3 ? 8 : to != TO_LOSS ? 0 : blocks == 1 ? 4 : 16; }
+
+template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS>
+__global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs a) {
+    using R = Ring<BLOCKS>;
+    constexpr uint32_t STEPS = exact_steps(BLOCKS, TO, PARTS);
+    constexpr uint32_t WIDTH_B = WIDTH / BLOCKS;  // of B's rows, per block (at most)
+    extern __shared__ unsigned char product_mem[];
+    __shared__ __align__(8) uint64_t barriers[2 * R::STAGES + 4];
+    __shared__ uint32_t tensor_at, gave_up;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank = 0;
+    if constexpr (BLOCKS == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const uint32_t ring = (shared_address(product_mem) + 1023) & ~1023u;
+    const uint32_t bar = shared_address(barriers);
+    auto full = [&](uint32_t s) { return bar + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar + 8 * (R::STAGES + s); };
+    auto ready = [&](uint32_t b) { return bar + 8 * (2 * R::STAGES + b); };
+    auto taken = [&](uint32_t b) { return bar + 8 * (2 * R::STAGES + 2 + b); };
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int s = 0; s < R::STAGES; ++s) {
+            barrier_init(full(s), 1);
+            barrier_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            barrier_init(ready(b), 1);
+            barrier_init(taken(b), TAKERS * BLOCKS);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    if (warp == 1) tensor_alloc<BLOCKS>(shared_address(&tensor_at), 512);
+    tensor_fence_before();
+    __syncthreads();
+    if constexpr (BLOCKS == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    tensor_fence_after();
+    const uint32_t tensor = tensor_at;
+    const Waits waits{&gave_up, a.timeout, a.limit_ns};
+    const uint32_t tiles = a.tiles_m * a.tiles_n * a.splits, workers = gridDim.x / BLOCKS, worker = blockIdx.x / BLOCKS;
+    pdl_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t bytes = BLOCKS * (STAGE_A + (B_TURNED ? R::STAGE_B : a.width / BLOCKS * DEPTH * 2));
+            uint32_t stage = 0, phase = 0;
+            for (uint32_t i = worker; i < tiles; i += workers) {
+                const Tile t = tile_of(a, i);
+                uint32_t k0, k1;
+                steps_of<PARTS>(a, t.split, &k0, &k1);
+                const int row_a = (int)((t.m * BLOCKS + rank) * ROWS), row_b = (int)(t.n * a.width + rank * (a.width / BLOCKS));
+                uint32_t product = k0 / a.blocks_k, k = k0 - product * a.blocks_k;
+                for (uint32_t step = k0; step < k1; ++step) {
+                    if (!waits.wait(empty(stage), phase ^ 1)) goto done;
+                    const int at_a = PARTS == 1 ? 0 : (int)(part_of_a(product) * a.part_a), at_b = PARTS == 1 ? 0 : (int)(part_of_b(product) * a.part_b);
+                    const uint32_t to_a = ring + stage * R::STAGE, to_b = to_a + STAGE_A;
+                    uint32_t on = full(stage);
+                    if constexpr (BLOCKS == 2) on = shared_of(on, 0);
+                    if (rank == 0) barrier_expect(full(stage), bytes);
+                    if (A_TURNED) {
+#pragma unroll
+                        for (uint32_t c = 0; c < ROWS / 64; ++c) copy_tile<BLOCKS>(to_a + c * 64 * DEPTH * 2, &map_a, on, at_a + row_a + 64 * (int)c, (int)(k * DEPTH));
+                    } else {
+                        copy_tile<BLOCKS>(to_a, &map_a, on, at_a + (int)(k * DEPTH), row_a);
+                    }
+                    if (B_TURNED) {
+#pragma unroll
+                        for (uint32_t c = 0; c < WIDTH_B / 64; ++c) copy_tile<BLOCKS>(to_b + c * 64 * DEPTH * 2, &map_b, on, at_b + row_b + 64 * (int)c, (int)(k * DEPTH));
+                    } else {
+                        copy_tile<BLOCKS>(to_b, &map_b, on, at_b + (int)(k * DEPTH), row_b);
+                    }
+                    if (++stage == R::STAGES) stage = 0, phase ^= 1;
+                    if (++k == a.blocks_k) k = 0, ++product;
+                }
+            }
+            // the last commits arrive here, too, before the block may end
+            for (int s = 0; s < R::STAGES; ++s) {
+                if (!waits.wait(empty(stage), phase ^ 1)) break;
+                if (++stage == R::STAGES) stage = 0, phase ^= 1;
+            }
+        done:
+            pdl_release();
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t kind = product_kind(A_TURNED, B_TURNED, ROWS * BLOCKS, a.width);
+            uint32_t stage = 0, phase = 0, turn = 0;
+            bool ended = false;
+            for (uint32_t i = worker; i < tiles && !ended; i += workers) {
+                const Tile t = tile_of(a, i);
+                uint32_t k0, k1;
+                steps_of<PARTS>(a, t.split, &k0, &k1);
+                uint32_t step = k0;
+                do {
+                    const uint32_t half = turn & 1, to = tensor + half * WIDTH, from = step, end = STEPS ? min(k1, step + STEPS) : k1;
+                    if (!waits.wait(taken(half), ((turn >> 1) & 1) ^ 1)) {
+                        ended = true;
+                        break;
+                    }
+                    tensor_fence_after();
+                    for (; step < end; ++step) {
+                        if (!waits.wait(full(stage), phase)) {
+                            ended = true;
+                            break;
+                        }
+                        tensor_fence_after();
+                        const uint64_t da = operand(ring + stage * R::STAGE, A_TURNED, 64 * DEPTH * 2), db = operand(ring + stage * R::STAGE + STAGE_A, B_TURNED, 64 * DEPTH * 2);
+#pragma unroll
+                        for (uint32_t k = 0; k < DEPTH / 16; ++k)
+                            multiply_tiles<BLOCKS>(to, da + k * ((A_TURNED ? 16 * 128 : 32) >> 4), db + k * ((B_TURNED ? 16 * 128 : 32) >> 4), kind, step > from || k > 0);
+                        tensor_commit<BLOCKS>(empty(stage));
+                        if (++stage == R::STAGES) stage = 0, phase ^= 1;
+                    }
+                    if (ended) break;
+                    tensor_commit<BLOCKS>(ready(half));
+                    ++turn;
+                } while (step < k1);
+            }
+        }
+    } else if (warp >= 4) {
+        const uint32_t part = warp & 3, side = (warp - 4) >> 2, from = side * SIDE;
+        uint32_t turn = 0;
+        bool ended = false;
+        for (uint32_t i = worker; i < tiles; i += workers) {
+            const Tile t = tile_of(a, i);
+            uint32_t k0, k1;
+            steps_of<PARTS>(a, t.split, &k0, &k1);
+            Epilogue<TO, PARTS> to(a, t, (t.m * BLOCKS + rank) * ROWS + part * 32 + lane);
+            const uint32_t col = t.n * a.width + from, end = min(a.n, (t.n + 1) * a.width);
+            auto begin = [&]() {
+                if (!__all_sync(0xffffffffu, waits.wait(ready(turn & 1), (turn >> 1) & 1))) return false;
+                tensor_fence_after();
+                return true;
+            };
+            auto place = [&](uint32_t c) { return tensor + ((part * 32) << 16) + (turn & 1) * WIDTH + from + c; };
+            auto leave = [&]() {
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (BLOCKS == 2) barrier_arrive_at(shared_of(taken(turn & 1), 0));
+                    else barrier_arrive_at(taken(turn & 1));
+                }
+                ++turn;
+            };
+            auto take = [&](float (&f)[32], uint32_t c) {
+                if constexpr (TO == TO_LOSS || TO == TO_P) {
+                    if constexpr (PARTS == 3) mend_scores(a, f, to.row, c);
+                } else if (k0 == k1) {  // a split without a step of K
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) f[k] = 0.f;
+                }
+                to.take(f, c, end);
+            };
+            if constexpr (STEPS > 0) {
+                float sum[SIDE / 32][32];
+#pragma unroll
+                for (uint32_t c = 0; c < SIDE; ++c) sum[c / 32][c % 32] = 0.f;
+                uint32_t step = k0;
+                do {
+                    if (!begin()) {
+                        ended = true;
+                        break;
+                    }
+#pragma unroll
+                    for (uint32_t c = 0; c < SIDE / 16; ++c) {
+                        float f[16];
+                        tensor_read(place(c * 16), f);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) sum[c / 2][c % 2 * 16 + k] += f[k];
+                    }
+                    leave();
+                    step += STEPS;
+                } while (step < k1);
+                if (ended) break;
+#pragma unroll
+                for (uint32_t c = 0; c < SIDE / 32; ++c)
+                    if (from + c * 32 < a.width) {
+                        asm volatile("" ::: "memory");  // (one after the other: there are no registers for more at once)
+                        take(sum[c], col + c * 32);
+                    }
+            } else {
+                if (!begin()) break;
+#pragma unroll 1
+                for (uint32_t c = 0; c < SIDE && from + c < a.width; c += 32) {
+                    float f[32];
+                    tensor_read(place(c), f);
+                    take(f, col + c);
+                }
+                leave();
+            }
+            to.finish(t, side);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (gave_up) {  // copies and products that are still on their way end in far less than this
+        const uint64_t t0 = now_ns();
+        while (now_ns() - t0 < 1000000) __nanosleep(1000);
+    }
+    __syncwarp();
+    if constexpr (BLOCKS == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    if (warp == 1) {
+        tensor_fence_after();
+        tensor_free<BLOCKS>(tensor, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- around the products
+
+constexpr uint32_t LANES = 8;   // that share a token in lt_loss_join
+
+// lse and loss of every token from the tiles' maxima and sums, in the tiles' order.
 __global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const float *target_score, const int *targets, float *loss, float *lse, uint32_t tokens, uint32_t tiles, uint32_t vocabulary) {
     pdl_release();
     pdl_wait();
-    const uint32_t n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= tokens) return;
+    const uint32_t n = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
+    __shared__ float2 sums[LANES][32];
     float top = -INFINITY, sum = 0.f;
-    for (uint32_t t = 0; t < tiles; ++t) top = max_nan(top, tops[(uint64_t)t * tokens + n].x);
-    for (uint32_t t = 0; t < tiles; ++t) {
-        const float2 v = tops[(uint64_t)t * tokens + n];
-        if (v.x != -INFINITY) sum += v.y * expf(v.x - top);
+    if (n < tokens) {
+        const uint32_t run = (tiles + LANES - 1) / LANES, t1 = min(tiles, (g + 1) * run);
+#pragma unroll 4
+        for (uint32_t t = g * run; t < t1; ++t) {
+            const float2 v = tops[(uint64_t)t * tokens + n];
+            const float m = max_nan(top, v.x);
+            if (m != -INFINITY) sum = sum * (top == -INFINITY ? 0.f : exp2f(top - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
+            top = m;
+        }
     }
-    const float l = fabsf(top) == INFINITY ? top : top + logf(sum);
-    if (lse) lse[n] = l;
-    if (loss) loss[n] = targets[n] >= 0 && (uint32_t)targets[n] < vocabulary ? l - target_score[n] : 0.f;
+    sums[g][threadIdx.x & 31] = make_float2(top, sum);
+    __syncthreads();
+    if (g || n >= tokens) return;
+    for (uint32_t k = 1; k < LANES; ++k) {
+        const float2 v = sums[k][threadIdx.x];
+        const float m = max_nan(top, v.x);
+        if (m != -INFINITY) sum = sum * (top == -INFINITY ? 0.f : exp2f(top - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
+        top = m;
+    }
+    const bool there = (uint32_t)targets[n] < vocabulary;
+    const bool far = fabsf(top) == INFINITY;
+    const float l = far ? 0.f : log2f(sum);
+    if (lse) lse[n] = (top + l) * 0.693147181f;
+    // (the difference of the scores first: a target with nearly all the weight keeps its small loss)
+    if (loss) loss[n] = there ? ((top - target_score[n]) + l) * 0.693147181f : 0.f;
 }
 
-// x without the rows that have no target
+struct PackArgs {
+    const void *from;
+    uint64_t pitch;
+    const int *targets;         // rows without one become zeros; or null
+    __nv_bfloat16 *to;          // [rows][parts][padded]
+    uint8_t *odd;               // three parts: 1 for rows with infinities, 2 for rows with what is no number
+    uint32_t rows, cols, padded, parts, vocabulary;
+    unsigned int *bad_target;
+};
+
+// A matrix as the products take it: bf16, in three parts if it is f32, rows padded with zeros to whole steps of K.
 template <class T>
-__global__ void __launch_bounds__(256) lt_loss_rows(const T *x, uint64_t pitch, const int *targets, T *to, uint32_t tokens, uint32_t cols, uint32_t vocabulary, unsigned int *status) {
+__global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
     pdl_release();
     pdl_wait();
-    for (uint32_t n = blockIdx.x; n < tokens; n += gridDim.x) {
-        const bool counts = (uint32_t)targets[n] < vocabulary;
-        if (targets[n] >= 0 && !counts && threadIdx.x == 0) report(status);
-        for (uint32_t c = threadIdx.x; c < cols; c += 256) to[(uint64_t)n * cols + c] = counts ? x[n * pitch + c] : from_float<T>(0.f);
+    const uint32_t pairs = a.padded / 2;
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        bool there = true;
+        if (a.targets) {
+            there = (uint32_t)a.targets[r] < a.vocabulary;
+            if (!there && a.targets[r] >= 0 && threadIdx.x == 0 && blockIdx.y == 0) report(a.bad_target);
+        }
+        const T *from = (const T *)a.from + r * a.pitch;
+        uint32_t *to = reinterpret_cast<uint32_t *>(a.to + (uint64_t)r * a.parts * a.padded);
+        int odd = 0;
+        for (uint32_t c = blockIdx.y * 256 + threadIdx.x; c < pairs; c += gridDim.y * 256) {
+            float f[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f[i] = there && 2 * c + i < a.cols ? to_float(from[2 * c + i]) : 0.f;
+            odd |= (isinf(f[0]) || isinf(f[1])) | (isnan(f[0]) || isnan(f[1])) << 1;
+            for (uint32_t part = 0; part < a.parts; ++part) {
+                __nv_bfloat16 h[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    h[i] = __float2bfloat16_rn(f[i]);
+                    const float b = __bfloat162float(h[i]);
+                    if (isinf(b) && !isinf(f[i])) h[i] = __float2bfloat16_rz(f[i]);  // (the nearest would be infinite)
+                    f[i] = isfinite(f[i]) ? f[i] - __bfloat162float(h[i]) : 0.f;
+                }
+                to[part * pairs + c] = (uint32_t)__bfloat16_as_ushort(h[0]) | (uint32_t)__bfloat16_as_ushort(h[1]) << 16;
+            }
+        }
+        if (a.odd) {  // (a block has whole rows then)
+            const int no_number = __syncthreads_or(odd & 2), infinite = __syncthreads_or(odd & 1);
+            if (threadIdx.x == 0) a.odd[r] = no_number ? 2 : infinite ? 1 : 0;
+        }
     }
 }
 
-uint32_t tiles_of(uint64_t n) { return (uint32_t)((n + TILE - 1) / TILE); }
+// out = the sum of `splits` results, in order
+template <class R>
+__global__ void __launch_bounds__(256) lt_loss_sum(const float *sums, R *out, uint64_t count, uint32_t splits) {
+    pdl_release();
+    pdl_wait();
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (uint64_t)gridDim.x * 256) {
+        float s = 0.f;
+#pragma unroll 8
+        for (uint32_t k = 0; k < splits; ++k) s += sums[k * count + i];
+        out[i] = from_float<R>(s);
+    }
+}
 
-constexpr uint64_t PIECE_BYTES = 64 << 20;
+// ------------------------------------------------------------------------------------------- host
 
-struct GradScratch {
-    size_t rows, p, sum, bytes;
-    uint64_t piece;
-    explicit GradScratch(const LtOperator &o) {
-        auto up = [](uint64_t b) { return (size_t)((b + 255) & ~255ull); };
-        const uint64_t es = o.dtype == LT_BF16 ? 2 : 4;
-        piece = std::max<uint64_t>(TILE, PIECE_BYTES / (4 * o.rows) / TILE * TILE);
-        piece = std::min(piece, o.vocabulary);
-        rows = 0;
-        p = up(o.rows * o.cols * es);
-        sum = p + up(o.rows * piece * 4);
-        bytes = sum + up(o.rows * o.cols * 4);
+inline bool is_aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+inline uint64_t up_to(uint64_t n, uint64_t of) { return (n + of - 1) / of * of; }
+inline uint32_t count_of(uint64_t n, uint64_t of) { return (uint32_t)((n + of - 1) / of); }
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+cudaError_t encoder(EncodeTiled *out) {
+    static std::atomic<EncodeTiled> known{nullptr};
+    EncodeTiled f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) return e;
+        if (found != cudaDriverEntryPointSuccess || !p) return cudaErrorNotSupported;
+        f = (EncodeTiled)p;
+        known.store(f, std::memory_order_relaxed);
+    }
+    *out = f;
+    return cudaSuccess;
+}
+
+// bf16 rows in memory as an operand: `cols` a multiple of 8 with the pitch, or padded; tiles of 64 columns by `high` rows.
+struct Operand {
+    const void *p;
+    uint64_t pitch, rows, cols;
+    uint32_t part;              // columns from a part to the next
+    bool turned;
+};
+
+cudaError_t map_of(const Operand &o, uint32_t high, CUtensorMap *map) {
+    EncodeTiled encode;
+    const cudaError_t e = encoder(&encode);
+    if (e != cudaSuccess) return e;
+    const cuuint64_t dims[2] = {o.cols, o.rows}, strides[1] = {o.pitch * 2};
+    const cuuint32_t box[2] = {64, o.turned ? 64u : high}, steps[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS>
+cudaError_t launch_product_of(const Operand &x, const Operand &y, const ProductArgs &a, int sm_count, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    auto kernel = lt_product<BLOCKS, A_TURNED, B_TURNED, TO, PARTS>;
+    cudaError_t e = allow_shared(kernel, Ring<BLOCKS>::BYTES, ready);
+    CUtensorMap map_a, map_b;
+    if (e == cudaSuccess) e = map_of(x, ROWS, &map_a);
+    if (e == cudaSuccess) e = map_of(y, a.width / BLOCKS, &map_b);
+    if (e != cudaSuccess) return e;
+    const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n * a.splits;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(std::min<uint64_t>(tiles, (uint64_t)sm_count / BLOCKS) * BLOCKS));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Ring<BLOCKS>::BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = LT_PDL;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {BLOCKS, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = BLOCKS == 1 ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, a);
+}
+
+// How a product of m x n over k steps is cut: a pair of blocks per tile of 256 rows, single blocks where 128 rows are enough.
+struct Cut {
+    int blocks;
+    uint32_t tiles_m, tiles_n, splits = 1, width = WIDTH;
+    // `widths`: tiles may have fewer columns than WIDTH, by multiples of as many (0: no)
+    Cut(uint64_t m, uint64_t n, int sm_count, uint32_t widths) {
+        blocks = m <= ROWS ? 1 : 2;
+        tiles_m = count_of(m, (uint64_t)ROWS * blocks);
+        tiles_n = count_of(n, WIDTH);
+        // What a round of tiles takes: a pair of blocks brings 256 rows and its columns for each step, and is bound by that below WIDTH
+        // columns; a single one, which has few rows, by the columns.  Narrower tiles pay where the last round would be nearly empty:
+        // one token against 32000 rows of 4096, 143 tiles of 224 columns 49 us, 125 of 256 56.
+        auto cost = [&](uint32_t w) { return (uint64_t)count_of((uint64_t)tiles_m * count_of(n, w), (uint64_t)sm_count / blocks) * (w + (blocks == 1 ? 32 : 256)); };
+        for (uint32_t w = WIDTH; widths && w >= LEAST_WIDTH; w -= widths)
+            if (cost(w) < cost(width)) width = w;
+        tiles_n = count_of(n, width);
+    }
+    // few tiles: several workers to a tile, with four steps of K each at least
+    Cut &split(uint64_t steps, int sm_count) {
+        const uint64_t tiles = (uint64_t)tiles_m * tiles_n, workers = (uint64_t)sm_count / blocks;
+        if (2 * tiles <= workers) splits = (uint32_t)std::max<uint64_t>(1, std::min(workers / tiles, steps / 4));
+        return *this;
     }
 };
 
-template <class T>
-cudaError_t launch_loss(const LtOperator &o, cudaStream_t stream) {
-    ProductArgs a{};
-    a.a = Matrix{o.in[0], o.pitch[0], 1};
-    a.b = Matrix{o.in[1], o.pitch[1], 1};
-    a.m = (uint32_t)o.rows;
-    a.n = a.vocabulary = (uint32_t)o.vocabulary;
-    a.depth = (uint32_t)o.cols;
-    a.targets = (const int *)o.in[2];
-    a.target_score = (float *)o.scratch;
-    a.tops = (float2 *)((char *)o.scratch + ((o.rows * 4 + 255) & ~255ull));
-    a.status = &o.status->loss;
-    a.scale = (float)lt_attr_double(o.attr[1]);
-    const uint32_t tiles = tiles_of(a.n);
-    const cudaError_t e = launch_pdl_grid(lt_product<T, T, T, TO_LOSS>, dim3(tiles, tiles_of(a.m)), THREADS, stream, a);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(lt_loss_join, (a.m + 255) / 256, 256, (size_t)0, stream, (const float2 *)a.tops, (const float *)a.target_score, a.targets, (float *)o.out[0], (float *)o.out[1], a.m, tiles,
-                      a.vocabulary);
+template <bool A_TURNED, bool B_TURNED, int TO, int PARTS>
+cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, const Cut &cut, int sm_count, cudaStream_t stream) {
+    a.tiles_m = cut.tiles_m;
+    a.tiles_n = cut.tiles_n;
+    a.splits = cut.splits;
+    a.width = cut.width;
+    a.part_a = x.part;
+    a.part_b = y.part;
+    return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream);
 }
 
 template <class T>
-cudaError_t launch_loss_grad(const LtOperator &o, cudaStream_t stream, unsigned *launched) {
-    const GradScratch at(o);
+constexpr uint32_t parts_of() { return sizeof(T) == 4 ? 3 : 1; }
+
+template <class T>
+cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_t cols, const int *targets, uint32_t vocabulary, unsigned int *bad_target, void *to, void *odd, int sm_count,
+                        cudaStream_t stream) {
+    PackArgs p{};
+    p.from = from;
+    p.pitch = pitch;
+    p.targets = targets;
+    p.to = (__nv_bfloat16 *)to;
+    p.odd = sizeof(T) == 4 ? (uint8_t *)odd : nullptr;
+    p.rows = (uint32_t)rows;
+    p.cols = (uint32_t)cols;
+    p.padded = (uint32_t)up_to(cols, DEPTH);
+    p.parts = parts_of<T>();
+    p.vocabulary = vocabulary;
+    p.bad_target = bad_target;
+    const unsigned across = p.odd ? 1 : std::min(count_of(p.padded / 2, 256), 16u), most = (unsigned)sm_count * 8 / across + 1;
+    return launch_pdl_grid(lt_loss_pack<T>, dim3(std::min((unsigned)rows, most), across), 256, stream, p);
+}
+template <class T>
+Operand packed_operand(const void *p, uint64_t rows, uint64_t cols, bool turned) {
+    const uint64_t padded = up_to(cols, DEPTH);
+    return Operand{p, padded * parts_of<T>(), rows, padded * parts_of<T>(), (uint32_t)padded, turned};
+}
+inline size_t packed_bytes(int dtype, uint64_t rows, uint64_t cols) { return (size_t)up_to(rows * up_to(cols, DEPTH) * 2 * (dtype == LT_F32 ? 3 : 1), 256); }
+// May the matrix be an operand where it lies?
+inline bool lies_well(int dtype, const void *p, uint64_t pitch) { return dtype == LT_BF16 && is_aligned(p, 16) && pitch % 8 == 0; }
+
+constexpr uint64_t PIECE_BYTES = 96 << 20;  // of a piece of the vocabulary: its packed rows, and P
+
+// Rows of the table at a time (a multiple of a tile's columns), if a row takes `bytes`.
+uint64_t piece_of(uint64_t vocabulary, uint64_t bytes) {
+    const uint64_t most = std::max<uint64_t>(WIDTH, PIECE_BYTES / bytes / WIDTH * WIDTH), pieces = (vocabulary + most - 1) / most;
+    return up_to((vocabulary + pieces - 1) / pieces, WIDTH);
+}
+
+// Halves of tiles that the loss may leave maxima and sums of.
+uint64_t most_tops(uint64_t vocabulary, uint64_t piece) { return 2 * (count_of(vocabulary, LEAST_WIDTH) + (vocabulary + piece - 1) / piece); }
+
+// Addresses are not known when scratch is planned: room for packed operands is there whether they will need it or not, but
+// for bf16 sizes that never do it is not more than a piece.
+struct LossScratch {
+    size_t score, odd_x, odd_table, tops, x, table, bytes;
+    uint64_t piece;
+    explicit LossScratch(const LtOperator &o) {
+        piece = piece_of(o.vocabulary, packed_bytes(o.dtype, 1, o.cols));
+        score = 0;
+        odd_x = up_to(o.rows * 4, 256);
+        odd_table = odd_x + up_to(o.rows, 256);
+        tops = odd_table + up_to(piece, 256);
+        x = tops + up_to(most_tops(o.vocabulary, piece) * o.rows * sizeof(float2), 256);
+        table = x + packed_bytes(o.dtype, o.rows, o.cols);
+        bytes = table + packed_bytes(o.dtype, piece, o.cols);
+    }
+};
+
+struct GradScratch {
+    size_t x, odd_x, odd_table, table, p, sum_x, sum_table, bytes;
+    uint64_t piece;
+    uint32_t splits_table;
+    GradScratch(const LtOperator &o, int sm_count) {
+        const uint64_t parts = o.dtype == LT_F32 ? 3 : 1;
+        piece = piece_of(o.vocabulary, std::max<uint64_t>(packed_bytes(o.dtype, 1, o.cols), o.rows * 2 * parts));
+        const uint64_t steps = count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), steps_t = count_of(o.rows, DEPTH) * (parts == 1 ? 1 : 6);
+        const Cut cx = Cut(o.rows, o.cols, sm_count, 0).split(steps, sm_count), ct = Cut(piece, o.cols, sm_count, 0).split(steps_t, sm_count);
+        x = 0;
+        odd_x = x + packed_bytes(o.dtype, o.rows, o.cols);
+        odd_table = odd_x + up_to(o.rows, 256);
+        table = odd_table + up_to(piece, 256);
+        splits_table = ct.splits;
+        p = table + packed_bytes(o.dtype, piece, o.cols);
+        sum_x = p + up_to(o.rows * piece * 2 * parts, 256);
+        sum_table = sum_x + (piece < o.vocabulary || cx.splits > 1 ? up_to(cx.splits * o.rows * o.cols * 4, 256) : 0);
+        bytes = sum_table + (ct.splits > 1 ? up_to(ct.splits * piece * o.cols * 4, 256) : 0);
+    }
+};
+
+void common_args(const LtOperator &o, ProductArgs &a) {
+    a.targets = (const int *)o.in[2];
+    a.vocabulary = (uint32_t)o.vocabulary;
+    a.scale = (float)lt_attr_double(o.attr[1]);
+    a.scale2 = (float)(lt_attr_double(o.attr[1]) * 1.4426950408889634);
+    a.bad_target = &o.status->loss;
+    a.timeout = &o.status->timeout;
+    a.limit_ns = o.wait_ns;
+}
+
+// f32: the operands of the scores themselves
+void plain_args(const LtOperator &o, ProductArgs &a, const void *odd_x, const void *odd_table, const void *table) {
+    if (o.dtype != LT_F32) return;
+    a.odd_a = (const uint8_t *)odd_x;
+    a.odd_b = (const uint8_t *)odd_table;
+    a.plain_a = (const float *)o.in[0];
+    a.plain_b = (const float *)table;
+    a.plain_pitch_a = o.pitch[0];
+    a.plain_pitch_b = o.pitch[1];
+    a.plain_cols = (uint32_t)o.cols;
+}
+
+template <class T>
+cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
+    const LossScratch at(o);
     char *room = (char *)o.scratch;
-    const uint32_t tokens = (uint32_t)o.rows, cols = (uint32_t)o.cols, vocabulary = (uint32_t)o.vocabulary;
-    const int *targets = (const int *)o.in[2];
-    T *rows = (T *)(room + at.rows);
-    cudaError_t e = launch_pdl(lt_loss_rows<T>, std::min(tokens, 4096u), 256, (size_t)0, stream, (const T *)o.in[0], o.pitch[0], targets, rows, tokens, cols, vocabulary, &o.status->loss);
-    *launched = 1;
-    for (uint32_t v0 = 0; v0 < vocabulary && e == cudaSuccess; v0 += (uint32_t)at.piece) {
-        const uint32_t n = std::min((uint32_t)at.piece, vocabulary - v0);
-        const T *table = (const T *)o.in[1] + v0 * o.pitch[1];
-        ProductArgs a{};
-        a.a = Matrix{rows, cols, 1};
-        a.b = Matrix{table, o.pitch[1], 1};
-        a.m = tokens;
-        a.n = n;
-        a.depth = cols;
-        a.targets = targets;
-        a.lse = (const float *)o.in[3];
-        a.dloss = (const float *)o.in[4];
-        a.p = (float *)(room + at.p);
-        a.first = v0;
-        a.vocabulary = vocabulary;
-        a.scale = (float)lt_attr_double(o.attr[1]);
-        e = launch_pdl_grid(lt_product<T, T, T, TO_P>, dim3(tiles_of(n), tiles_of(tokens)), THREADS, stream, a);
+    const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]), table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
+    cudaError_t e = cudaSuccess;
+    *launched = 0;
+    Operand x{o.in[0], o.pitch[0], o.rows, o.cols, 0, false};
+    if (!x_well) {
+        e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, nullptr, 0, nullptr, room + at.x, room + at.odd_x, sm_count, stream);
+        x = packed_operand<T>(room + at.x, o.rows, o.cols, false);
         ++*launched;
-        if (o.out[0] && e == cudaSuccess) {
-            ProductArgs d{};
-            d.a = Matrix{a.p, n, 1};
-            d.b = Matrix{table, 1, o.pitch[1]};
-            d.m = tokens;
-            d.n = cols;
-            d.depth = n;
-            d.sum = (float *)(room + at.sum);
-            d.first = v0;
-            d.out = o.out[0];
-            d.more = v0 + n < vocabulary;
-            e = launch_pdl_grid(lt_product<float, T, T, TO_RESULT>, dim3(tiles_of(cols), tiles_of(tokens)), THREADS, stream, d);
+    }
+    const uint64_t piece = table_well ? o.vocabulary : at.piece;
+    ProductArgs a{};
+    common_args(o, a);
+    a.m = (uint32_t)o.rows;
+    a.blocks_k = count_of(o.cols, DEPTH);
+    a.target_score = (float *)(room + at.score);
+    a.tops = (float2 *)(room + at.tops);
+    for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
+        const uint64_t n = std::min(piece, o.vocabulary - v0);
+        const void *rows = (const T *)o.in[1] + v0 * o.pitch[1];
+        Operand table{rows, o.pitch[1], n, o.cols, 0, false};
+        if (!table_well) {
+            e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+            if (e != cudaSuccess) return e;
+            table = packed_operand<T>(room + at.table, n, o.cols, false);
             ++*launched;
         }
-        if (o.out[1] && e == cudaSuccess) {
+        a.n = (uint32_t)n;
+        a.first = (uint32_t)v0;
+        plain_args(o, a, room + at.odd_x, room + at.odd_table, rows);
+        const Cut cut(o.rows, n, sm_count, 32);
+        e = launch_product<false, false, TO_LOSS, (int)parts_of<T>()>(x, table, a, cut, sm_count, stream);
+        a.first_tile += 2 * cut.tiles_n;
+        ++*launched;
+    }
+    if (e != cudaSuccess) return e;
+    ++*launched;
+    return launch_pdl(lt_loss_join, count_of(o.rows, 32), 256, (size_t)0, stream, (const float2 *)a.tops, (const float *)a.target_score, a.targets, (float *)o.out[0], (float *)o.out[1], a.m,
+                      a.first_tile, a.vocabulary);
+}
+
+template <class T>
+cudaError_t launch_sum(const float *sums, void *out, uint64_t count, uint32_t splits, int sm_count, cudaStream_t stream) {
+    return launch_pdl(lt_loss_sum<T>, (unsigned)std::min<uint64_t>((count + 255) / 256, (uint64_t)sm_count * 8), 256, (size_t)0, stream, sums, (T *)out, count, splits);
+}
+
+template <class T>
+cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
+    constexpr int PARTS = parts_of<T>();
+    constexpr int TO_T = sizeof(T) == 4 ? TO_F32 : TO_BF16;
+    const GradScratch at(o, sm_count);
+    char *room = (char *)o.scratch;
+    const bool table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
+    const uint64_t parts = parts_of<T>();
+    // (x always: rows without a target, which may hold anything, are left out of the table's gradient)
+    cudaError_t e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, (const int *)o.in[2], (uint32_t)o.vocabulary, &o.status->loss, room + at.x, room + at.odd_x, sm_count, stream);
+    *launched = 1;
+    for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += at.piece) {
+        const uint64_t n = std::min(at.piece, o.vocabulary - v0), padded = up_to(n, WIDTH);
+        const bool last = v0 + n == o.vocabulary;
+        const void *rows = (const T *)o.in[1] + v0 * o.pitch[1];
+        Operand table{rows, o.pitch[1], n, o.cols, 0, false};
+        if (!table_well) {
+            e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+            if (e != cudaSuccess) return e;
+            table = packed_operand<T>(room + at.table, n, o.cols, false);
+            ++*launched;
+        }
+        ProductArgs a{};
+        common_args(o, a);
+        a.m = (uint32_t)o.rows;
+        a.n = (uint32_t)n;
+        a.blocks_k = count_of(o.cols, DEPTH);
+        a.first = (uint32_t)v0;
+        a.lse = (const float *)o.in[3];
+        a.dloss = (const float *)o.in[4];
+        a.p = (__nv_bfloat16 *)(room + at.p);
+        a.p_pitch = padded * parts;
+        a.p_part = (uint32_t)padded;
+        plain_args(o, a, room + at.odd_x, room + at.odd_table, rows);
+        e = launch_product<false, false, TO_P, PARTS>(packed_operand<T>(room + at.x, o.rows, o.cols, false), table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
+        if (e != cudaSuccess) return e;
+        ++*launched;
+        Operand p{a.p, padded * parts, o.rows, padded * parts, (uint32_t)padded, false};
+        if (o.out[0]) {
             ProductArgs d{};
-            d.a = Matrix{a.p, 1, n};
-            d.b = Matrix{rows, 1, cols};
-            d.m = n;
-            d.n = cols;
-            d.depth = tokens;
-            d.out = (T *)o.out[1] + (uint64_t)v0 * cols;
-            e = launch_pdl_grid(lt_product<float, T, T, TO_RESULT>, dim3(tiles_of(cols), tiles_of(n)), THREADS, stream, d);
+            common_args(o, d);
+            d.m = (uint32_t)o.rows;
+            d.n = (uint32_t)o.cols;
+            d.blocks_k = count_of(n, DEPTH);
+            // (as many splits for every piece, the last and shorter one too)
+            const Cut cut = Cut(o.rows, o.cols, sm_count, 0).split(count_of(at.piece, DEPTH) * (parts == 1 ? 1 : 6), sm_count);
+            float *sum = (float *)(room + at.sum_x);
+            table.turned = true;
+            if (last && cut.splits == 1) {
+                d.before = v0 ? sum : nullptr;
+                d.out = o.out[0];
+                d.wide = is_aligned(d.out, 16) && o.cols * sizeof(T) % 16 == 0;
+                e = launch_product<false, true, TO_T, PARTS>(p, table, d, cut, sm_count, stream);
+            } else {
+                d.before = v0 ? sum : nullptr;
+                d.out = sum;
+                d.wide = o.cols % 4 == 0;
+                e = launch_product<false, true, TO_SUM, PARTS>(p, table, d, cut, sm_count, stream);
+                if (e == cudaSuccess && last) {
+                    e = launch_sum<T>(sum, o.out[0], o.rows * o.cols, cut.splits, sm_count, stream);
+                    ++*launched;
+                }
+            }
+            if (e != cudaSuccess) return e;
+            ++*launched;
+        }
+        if (o.out[1]) {
+            ProductArgs d{};
+            common_args(o, d);
+            d.m = (uint32_t)n;
+            d.n = (uint32_t)o.cols;
+            d.blocks_k = count_of(o.rows, DEPTH);
+            Cut cut = Cut(n, o.cols, sm_count, 0).split(d.blocks_k * (parts == 1 ? 1 : 6), sm_count);
+            cut.splits = std::min(cut.splits, at.splits_table);  // (the last piece is shorter: what the scratch memory holds)
+            void *out = (T *)o.out[1] + v0 * o.cols;
+            p.turned = true;
+            const Operand x = packed_operand<T>(room + at.x, o.rows, o.cols, true);
+            if (cut.splits == 1) {
+                d.out = out;
+                d.wide = is_aligned(out, 16) && o.cols * sizeof(T) % 16 == 0;
+                e = launch_product<true, true, TO_T, PARTS>(p, x, d, cut, sm_count, stream);
+            } else {
+                d.out = room + at.sum_table;
+                d.wide = o.cols % 4 == 0;
+                e = launch_product<true, true, TO_SUM, PARTS>(p, x, d, cut, sm_count, stream);
+                if (e == cudaSuccess) e = launch_sum<T>((const float *)d.out, out, n * o.cols, cut.splits, sm_count, stream);
+                ++*launched;
+            }
+            if (e != cudaSuccess) return e;
             ++*launched;
         }
     }
@@ -228,14 +914,13 @@ cudaError_t launch_loss_grad(const LtOperator &o, cudaStream_t stream, unsigned 
 
 }  // namespace
 
-size_t lt_vocabulary_loss_scratch(const LtOperator &o, int) { return ((o.rows * 4 + 255) & ~255ull) + (size_t)tiles_of(o.vocabulary) * o.rows * sizeof(float2); }
-size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int) { return GradScratch(o).bytes; }
+size_t lt_vocabulary_loss_scratch(const LtOperator &o, int) { return LossScratch(o).bytes; }
+size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int sm_count) { return GradScratch(o, sm_count).bytes; }
 
-cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int, cudaStream_t stream, unsigned *launched) {
-    *launched = 2;
-    return o.dtype == LT_BF16 ? launch_loss<__nv_bfloat16>(o, stream) : launch_loss<float>(o, stream);
+cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
+    return o.dtype == LT_BF16 ? launch_loss<__nv_bfloat16>(o, sm_count, stream, launched) : launch_loss<float>(o, sm_count, stream, launched);
 }
 
-cudaError_t lt_launch_vocabulary_loss_grad(const LtOperator &o, int, cudaStream_t stream, unsigned *launched) {
-    return o.dtype == LT_BF16 ? launch_loss_grad<__nv_bfloat16>(o, stream, launched) : launch_loss_grad<float>(o, stream, launched);
+cudaError_t lt_launch_vocabulary_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
+    return o.dtype == LT_BF16 ? launch_loss_grad<__nv_bfloat16>(o, sm_count, stream, launched) : launch_loss_grad<float>(o, sm_count, stream, launched);
 }
