@@ -463,40 +463,153 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
 
 // ------------------------------------------------------------------------------------------- around the products
 
-constexpr uint32_t LANES = 8;   // that share a token in lt_loss_join
+// Two maxima and sums (of powers of two) as one
+__device__ __forceinline__ float2 joined(float2 a, float2 b) {
+    const float m = max_nan(a.x, b.x);
+    if (m == -INFINITY) return make_float2(m, 0.f);
+    return make_float2(m, (a.x == -INFINITY ? 0.f : a.y * exp2f(a.x - m)) + (b.x == -INFINITY ? 0.f : b.y * exp2f(b.x - m)));
+}
 
-// lse and loss of every token from the tiles' maxima and sums, in the tiles' order.
+// lse and loss of every token from what the tiles left, always in the same order: 32 / ACROSS lanes and the block's eight warps
+// have tiles of ACROSS tokens each (few tokens: one across, so that all lanes have work).
+template <uint32_t ACROSS>
 __global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const float *target_score, const int *targets, float *loss, float *lse, uint32_t tokens, uint32_t tiles, uint32_t vocabulary) {
+    constexpr uint32_t SHARES = 256 / ACROSS;
     pdl_release();
     pdl_wait();
-    const uint32_t n = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
-    __shared__ float2 sums[LANES][32];
-    float top = -INFINITY, sum = 0.f;
+    const uint32_t n = blockIdx.x * ACROSS + threadIdx.x % ACROSS, share = threadIdx.x / ACROSS;
+    __shared__ float2 sums[8][32];
+    float2 s = make_float2(-INFINITY, 0.f);
     if (n < tokens) {
-        const uint32_t run = (tiles + LANES - 1) / LANES, t1 = min(tiles, (g + 1) * run);
-#pragma unroll 4
-        for (uint32_t t = g * run; t < t1; ++t) {
-            const float2 v = tops[(uint64_t)t * tokens + n];
-            const float m = max_nan(top, v.x);
-            if (m != -INFINITY) sum = sum * (top == -INFINITY ? 0.f : exp2f(top - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
-            top = m;
+        uint32_t t = share;
+        for (; t + 3 * SHARES < tiles; t += 4 * SHARES) {
+            float2 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = tops[(uint64_t)(t + k * SHARES) * tokens + n];
+            s = joined(s, joined(joined(v[0], v[1]), joined(v[2], v[3])));
         }
+        for (; t < tiles; t += SHARES) s = joined(s, tops[(uint64_t)t * tokens + n]);
     }
-    sums[g][threadIdx.x & 31] = make_float2(top, sum);
+#pragma unroll
+    for (int d = 16; d >= (int)ACROSS; d >>= 1) s = joined(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, d), __shfl_xor_sync(0xffffffffu, s.y, d)));
+    sums[threadIdx.x >> 5][threadIdx.x & 31] = s;
     __syncthreads();
-    if (g || n >= tokens) return;
-    for (uint32_t k = 1; k < LANES; ++k) {
-        const float2 v = sums[k][threadIdx.x];
-        const float m = max_nan(top, v.x);
-        if (m != -INFINITY) sum = sum * (top == -INFINITY ? 0.f : exp2f(top - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2f(v.x - m));
-        top = m;
-    }
-    const bool there = (uint32_t)targets[n] < vocabulary;
-    const bool far = fabsf(top) == INFINITY;
-    const float l = far ? 0.f : log2f(sum);
-    if (lse) lse[n] = (top + l) * 0.693147181f;
+    if (threadIdx.x >= ACROSS || n >= tokens) return;
+    for (int k = 1; k < 8; ++k) s = joined(s, sums[k][threadIdx.x]);
+    const float l = fabsf(s.x) == INFINITY ? 0.f : log2f(s.y);
+    if (lse) lse[n] = (s.x + l) * 0.693147181f;
     // (the difference of the scores first: a target with nearly all the weight keeps its small loss)
-    if (loss) loss[n] = there ? ((top - target_score[n]) + l) * 0.693147181f : 0.f;
+    if (loss) loss[n] = (uint32_t)targets[n] < vocabulary ? ((s.x - target_score[n]) + l) * 0.693147181f : 0.f;
+}
+
+cudaError_t launch_join(const ProductArgs &a, uint32_t tiles, float *loss, float *lse, cudaStream_t stream) {
+    const float2 *tops = a.tops;
+    const float *score = a.target_score;
+    if (a.m <= 64) return launch_pdl(lt_loss_join<1>, a.m, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, tiles, a.vocabulary);
+    return launch_pdl(lt_loss_join<8>, (a.m + 7) / 8, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, tiles, a.vocabulary);
+}
+
+// ------------------------------------------------------------------------------------------- few tokens
+
+// One to FEW tokens: the table is read once, at the memory's rate, by warps that have FEW_ROWS of its rows at a time, 16 bytes of each per lane;
+// products and sums in binary32.  (A tile of the tensor cores would be nearly all padding, and f32 rows would have to be taken apart first.)
+constexpr int FEW = 4, FEW_ROWS = 2, FEW_THREADS = 256;
+
+struct FewArgs {
+    const void *x, *table;
+    const int *targets;
+    float2 *tops;               // [blocks][tokens]
+    float *target_score;
+    uint64_t x_pitch, table_pitch;
+    uint32_t vocabulary, cols;
+    float scale2;
+    unsigned int *bad_target;
+};
+
+template <class T, int N, int TOKENS>
+__global__ void __launch_bounds__(FEW_THREADS, 3) lt_loss_few(const FewArgs a) {
+    constexpr int WARPS = FEW_THREADS / 32, AHEAD = 4;
+    extern __shared__ uint4 few_mem[];  // x: [tokens][columns], as it lies in memory (N > 1), in pieces of 16 bytes
+    T *const xs = reinterpret_cast<T *>(few_mem);
+    __shared__ float2 sums[WARPS][TOKENS];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = (a.cols + 7) & ~7u;
+    pdl_release();
+    pdl_wait();
+    for (int t = 0; t < TOKENS; ++t)
+        for (uint32_t c = threadIdx.x; c < a.cols; c += FEW_THREADS) xs[t * pitch + c] = ((const T *)a.x)[t * a.x_pitch + c];
+    int target[TOKENS];
+    float2 s[TOKENS];
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        target[t] = a.targets[t];
+        if (blockIdx.x == 0 && threadIdx.x == 0 && target[t] >= 0 && (uint32_t)target[t] >= a.vocabulary) report(a.bad_target);
+        s[t] = make_float2(-INFINITY, 0.f);
+    }
+    __syncthreads();
+    const uint32_t v0 = (uint32_t)((uint64_t)a.vocabulary * blockIdx.x / gridDim.x), v1 = (uint32_t)((uint64_t)a.vocabulary * (blockIdx.x + 1) / gridDim.x);
+    for (uint32_t v = v0 + warp * FEW_ROWS; v < v1; v += WARPS * FEW_ROWS) {
+        float dot[FEW_ROWS][TOKENS] = {};
+        const T *row[FEW_ROWS];
+#pragma unroll
+        for (int r = 0; r < FEW_ROWS; ++r) row[r] = (const T *)a.table + (uint64_t)min(v + r, v1 - 1) * a.table_pitch;
+        if constexpr (N == 1) {
+            for (uint32_t c = lane; c < a.cols; c += 32) {
+#pragma unroll
+                for (int r = 0; r < FEW_ROWS; ++r) {
+                    const float w = to_float(row[r][c]);
+#pragma unroll
+                    for (int t = 0; t < TOKENS; ++t) dot[r][t] += w * to_float(xs[t * pitch + c]);
+                }
+            }
+        } else {
+            for (uint32_t c0 = lane * N; c0 < a.cols; c0 += 32 * N * AHEAD) {
+                uint4 w[AHEAD][FEW_ROWS];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                    for (int r = 0; r < FEW_ROWS; ++r) {
+                        const uint32_t c = c0 + k * 32 * N;
+                        if (c < a.cols) w[k][r] = __ldcs(reinterpret_cast<const uint4 *>(row[r] + c));
+                    }
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const uint32_t c = c0 + k * 32 * N;
+                    if (c >= a.cols) break;
+                    float f[FEW_ROWS][N];
+#pragma unroll
+                    for (int r = 0; r < FEW_ROWS; ++r) unpack(w[k][r], f[r]);
+#pragma unroll
+                    for (int t = 0; t < TOKENS; ++t) {
+                        float x[N];
+                        unpack(*reinterpret_cast<const uint4 *>(xs + t * pitch + c), x);
+#pragma unroll
+                        for (int r = 0; r < FEW_ROWS; ++r)
+#pragma unroll
+                            for (int i = 0; i < N; ++i) dot[r][t] += f[r][i] * x[i];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < FEW_ROWS; ++r)
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                const float z = warp_sum(dot[r][t]) * a.scale2;
+                if (v + r >= v1) continue;
+                s[t] = joined(s[t], make_float2(z, 1.f));
+                if ((int)(v + r) == target[t] && lane == 0) a.target_score[t] = z;
+            }
+    }
+    if (lane == 0) {
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) sums[warp][t] = s[t];
+    }
+    __syncthreads();
+    if (threadIdx.x < TOKENS) {
+        float2 r = sums[0][threadIdx.x];
+        for (int w = 1; w < WARPS; ++w) r = joined(r, sums[w][threadIdx.x]);
+        a.tops[(uint64_t)blockIdx.x * TOKENS + threadIdx.x] = r;
+    }
 }
 
 struct PackArgs {
@@ -505,16 +618,18 @@ struct PackArgs {
     const int *targets;         // rows without one become zeros; or null
     __nv_bfloat16 *to;          // [rows][parts][padded]
     uint8_t *odd;               // three parts: 1 for rows with infinities, 2 for rows with what is no number
-    uint32_t rows, cols, padded, parts, vocabulary;
+    uint32_t rows, cols, padded, vocabulary;
     unsigned int *bad_target;
 };
 
-// A matrix as the products take it: bf16, in three parts if it is f32, rows padded with zeros to whole steps of K.
-template <class T>
+// A matrix as the products take it: bf16, in three parts if it is f32, rows padded with zeros to whole steps of K.  A thread has eight
+// columns.
+template <class T, bool WIDE>
 __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     pdl_release();
     pdl_wait();
-    const uint32_t pairs = a.padded / 2;
+    const uint32_t eights = a.padded / 8;
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         bool there = true;
         if (a.targets) {
@@ -522,42 +637,77 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
             if (!there && a.targets[r] >= 0 && threadIdx.x == 0 && blockIdx.y == 0) report(a.bad_target);
         }
         const T *from = (const T *)a.from + r * a.pitch;
-        uint32_t *to = reinterpret_cast<uint32_t *>(a.to + (uint64_t)r * a.parts * a.padded);
+        uint4 *to = reinterpret_cast<uint4 *>(a.to + (uint64_t)r * PARTS * a.padded);
         int odd = 0;
-        for (uint32_t c = blockIdx.y * 256 + threadIdx.x; c < pairs; c += gridDim.y * 256) {
-            float f[2];
+        for (uint32_t c = blockIdx.y * 256 + threadIdx.x; c < eights; c += gridDim.y * 256) {
+            float f[8];
+            if (WIDE && there && 8 * c + 8 <= a.cols) {
+                if constexpr (PARTS == 1) {
+                    to[c] = reinterpret_cast<const uint4 *>(from)[c];
+                    continue;
+                } else {
+                    float g[4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) f[i] = there && 2 * c + i < a.cols ? to_float(from[2 * c + i]) : 0.f;
-            odd |= (isinf(f[0]) || isinf(f[1])) | (isnan(f[0]) || isnan(f[1])) << 1;
-            for (uint32_t part = 0; part < a.parts; ++part) {
-                __nv_bfloat16 h[2];
+                    for (int h = 0; h < 2; ++h) {
+                        unpack(reinterpret_cast<const uint4 *>(from)[2 * c + h], g);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    h[i] = __float2bfloat16_rn(f[i]);
-                    const float b = __bfloat162float(h[i]);
-                    if (isinf(b) && !isinf(f[i])) h[i] = __float2bfloat16_rz(f[i]);  // (the nearest would be infinite)
-                    f[i] = isfinite(f[i]) ? f[i] - __bfloat162float(h[i]) : 0.f;
+                        for (int i = 0; i < 4; ++i) f[4 * h + i] = g[i];
+                    }
                 }
-                to[part * pairs + c] = (uint32_t)__bfloat16_as_ushort(h[0]) | (uint32_t)__bfloat16_as_ushort(h[1]) << 16;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = there && 8 * c + i < a.cols ? to_float(from[8 * c + i]) : 0.f;
+            }
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    __nv_bfloat16 h = __float2bfloat16_rn(f[i]);
+                    if constexpr (PARTS == 3) {
+                        if (part == 0) {
+                            if (!(fabsf(f[i]) <= 3.38953139e38f)) {  // (the largest bf16)
+                                odd |= isinf(f[i]) ? 1 : isnan(f[i]) ? 2 : 0;
+                                if (!isinf(f[i])) h = __float2bfloat16_rz(f[i]);  // (the nearest might be infinite)
+                            }
+                        }
+                        f[i] = isfinite(f[i]) ? f[i] - __bfloat162float(h) : 0.f;
+                    }
+                    const uint32_t bits = __bfloat16_as_ushort(h);
+                    w[i / 2] = i & 1 ? w[i / 2] | bits << 16 : bits;
+                }
+                to[part * eights + c] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
-        if (a.odd) {  // (a block has whole rows then)
+        if constexpr (PARTS == 3) {  // (a block has whole rows)
             const int no_number = __syncthreads_or(odd & 2), infinite = __syncthreads_or(odd & 1);
             if (threadIdx.x == 0) a.odd[r] = no_number ? 2 : infinite ? 1 : 0;
         }
     }
 }
 
-// out = the sum of `splits` results, in order
-template <class R>
+// out = the sum of `splits` results of `count` values, in order; N (4 or 1) values of a thread at a time
+template <class R, int N>
 __global__ void __launch_bounds__(256) lt_loss_sum(const float *sums, R *out, uint64_t count, uint32_t splits) {
     pdl_release();
     pdl_wait();
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (uint64_t)gridDim.x * 256) {
-        float s = 0.f;
+    for (uint64_t i = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * N; i < count; i += (uint64_t)gridDim.x * 256 * N) {
+        float s[N] = {};
 #pragma unroll 8
-        for (uint32_t k = 0; k < splits; ++k) s += sums[k * count + i];
-        out[i] = from_float<R>(s);
+        for (uint32_t k = 0; k < splits; ++k) {
+            if constexpr (N == 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(sums + k * count + i);
+                s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+            } else {
+                s[0] += sums[k * count + i];
+            }
+        }
+        if constexpr (N == 4) {
+            if constexpr (sizeof(R) == 4) *reinterpret_cast<float4 *>(out + i) = make_float4(s[0], s[1], s[2], s[3]);
+            else *reinterpret_cast<uint2 *>(out + i) = make_uint2(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]));
+        } else {
+            out[i] = from_float<R>(s[0]);
+        }
     }
 }
 
@@ -682,11 +832,11 @@ cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_
     p.rows = (uint32_t)rows;
     p.cols = (uint32_t)cols;
     p.padded = (uint32_t)up_to(cols, DEPTH);
-    p.parts = parts_of<T>();
     p.vocabulary = vocabulary;
     p.bad_target = bad_target;
-    const unsigned across = p.odd ? 1 : std::min(count_of(p.padded / 2, 256), 16u), most = (unsigned)sm_count * 8 / across + 1;
-    return launch_pdl_grid(lt_loss_pack<T>, dim3(std::min((unsigned)rows, most), across), 256, stream, p);
+    const unsigned across = p.odd ? 1 : std::min(count_of(p.padded / 8, 256), 16u), most = (unsigned)sm_count * 16 / across + 1;
+    const dim3 grid(std::min((unsigned)rows, most), across);
+    return is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0 ? launch_pdl_grid(lt_loss_pack<T, true>, grid, 256, stream, p) : launch_pdl_grid(lt_loss_pack<T, false>, grid, 256, stream, p);
 }
 template <class T>
 Operand packed_operand(const void *p, uint64_t rows, uint64_t cols, bool turned) {
@@ -705,6 +855,10 @@ uint64_t piece_of(uint64_t vocabulary, uint64_t bytes) {
     return up_to((vocabulary + pieces - 1) / pieces, WIDTH);
 }
 
+constexpr size_t FEW_BYTES = 72 << 10;  // of x: three blocks to an SM
+inline bool few_tokens(const LtOperator &o) { return o.rows <= FEW && o.rows * up_to(o.cols, 8) * (o.dtype == LT_BF16 ? 2 : 4) <= FEW_BYTES; }
+inline unsigned few_blocks(const LtOperator &o, int sm_count) { return (unsigned)std::min<uint64_t>(3ull * sm_count, count_of(o.vocabulary, FEW_THREADS / 32 * FEW_ROWS)); }
+
 // Halves of tiles that the loss may leave maxima and sums of.
 uint64_t most_tops(uint64_t vocabulary, uint64_t piece) { return 2 * (count_of(vocabulary, LEAST_WIDTH) + (vocabulary + piece - 1) / piece); }
 
@@ -713,12 +867,16 @@ uint64_t most_tops(uint64_t vocabulary, uint64_t piece) { return 2 * (count_of(v
 struct LossScratch {
     size_t score, odd_x, odd_table, tops, x, table, bytes;
     uint64_t piece;
-    explicit LossScratch(const LtOperator &o) {
+    LossScratch(const LtOperator &o, int sm_count) {
         piece = piece_of(o.vocabulary, packed_bytes(o.dtype, 1, o.cols));
         score = 0;
         odd_x = up_to(o.rows * 4, 256);
         odd_table = odd_x + up_to(o.rows, 256);
         tops = odd_table + up_to(piece, 256);
+        if (few_tokens(o)) {
+            bytes = tops + up_to(few_blocks(o, sm_count) * o.rows * sizeof(float2), 256);
+            return;
+        }
         x = tops + up_to(most_tops(o.vocabulary, piece) * o.rows * sizeof(float2), 256);
         table = x + packed_bytes(o.dtype, o.rows, o.cols);
         bytes = table + packed_bytes(o.dtype, piece, o.cols);
@@ -768,10 +926,39 @@ void plain_args(const LtOperator &o, ProductArgs &a, const void *odd_x, const vo
     a.plain_cols = (uint32_t)o.cols;
 }
 
+template <class T, int N, int TOKENS>
+cudaError_t launch_few_of(const FewArgs &a, unsigned blocks, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(lt_loss_few<T, N, TOKENS>, FEW_BYTES, ready);
+    return e != cudaSuccess ? e : launch_pdl(lt_loss_few<T, N, TOKENS>, blocks, FEW_THREADS, TOKENS * up_to(a.cols, 8) * sizeof(T), stream, a);
+}
+template <class T, int N>
+cudaError_t launch_few(const FewArgs &a, uint64_t tokens, unsigned blocks, cudaStream_t stream) {
+    static_assert(FEW == 4, "");
+    return tokens == 1 ? launch_few_of<T, N, 1>(a, blocks, stream)
+         : tokens == 2 ? launch_few_of<T, N, 2>(a, blocks, stream)
+         : tokens == 3 ? launch_few_of<T, N, 3>(a, blocks, stream)
+                       : launch_few_of<T, N, 4>(a, blocks, stream);
+}
+
 template <class T>
 cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
-    const LossScratch at(o);
+    const LossScratch at(o, sm_count);
     char *room = (char *)o.scratch;
+    if (few_tokens(o)) {
+        ProductArgs a{};
+        common_args(o, a);
+        a.m = (uint32_t)o.rows;
+        a.target_score = (float *)(room + at.score);
+        a.tops = (float2 *)(room + at.tops);
+        constexpr int N = 16 / (int)sizeof(T);
+        const FewArgs f{o.in[0], o.in[1], a.targets, a.tops, a.target_score, o.pitch[0], o.pitch[1], a.vocabulary, (uint32_t)o.cols, a.scale2, a.bad_target};
+        const bool wide = o.cols % N == 0 && o.pitch[1] % N == 0 && is_aligned(o.in[1], 16);
+        const unsigned blocks = few_blocks(o, sm_count);
+        const cudaError_t e = wide ? launch_few<T, N>(f, o.rows, blocks, stream) : launch_few<T, 1>(f, o.rows, blocks, stream);
+        *launched = 2;
+        return e != cudaSuccess ? e : launch_join(a, blocks, (float *)o.out[0], (float *)o.out[1], stream);
+    }
     const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]), table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
     cudaError_t e = cudaSuccess;
     *launched = 0;
@@ -808,13 +995,15 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
     }
     if (e != cudaSuccess) return e;
     ++*launched;
-    return launch_pdl(lt_loss_join, count_of(o.rows, 32), 256, (size_t)0, stream, (const float2 *)a.tops, (const float *)a.target_score, a.targets, (float *)o.out[0], (float *)o.out[1], a.m,
-                      a.first_tile, a.vocabulary);
+    return launch_join(a, a.first_tile, (float *)o.out[0], (float *)o.out[1], stream);
 }
 
 template <class T>
 cudaError_t launch_sum(const float *sums, void *out, uint64_t count, uint32_t splits, int sm_count, cudaStream_t stream) {
-    return launch_pdl(lt_loss_sum<T>, (unsigned)std::min<uint64_t>((count + 255) / 256, (uint64_t)sm_count * 8), 256, (size_t)0, stream, sums, (T *)out, count, splits);
+    const bool wide = count % 4 == 0 && is_aligned(out, 4 * sizeof(T));
+    const unsigned grid = (unsigned)std::min<uint64_t>((count / (wide ? 4 : 1) + 255) / 256, (uint64_t)sm_count * 16);
+    return wide ? launch_pdl(lt_loss_sum<T, 4>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits)
+                : launch_pdl(lt_loss_sum<T, 1>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits);
 }
 
 template <class T>
@@ -914,7 +1103,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
 
 }  // namespace
 
-size_t lt_vocabulary_loss_scratch(const LtOperator &o, int) { return LossScratch(o).bytes; }
+size_t lt_vocabulary_loss_scratch(const LtOperator &o, int sm_count) { return LossScratch(o, sm_count).bytes; }
 size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int sm_count) { return GradScratch(o, sm_count).bytes; }
 
 cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
