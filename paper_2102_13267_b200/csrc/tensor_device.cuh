@@ -25,7 +25,7 @@ __device__ __forceinline__ void barrier_arrive_at(uint32_t cluster_bar) { asm vo
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
-        "{.reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        "{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
 __device__ __forceinline__ uint64_t now_ns() {
