@@ -33,7 +33,7 @@ struct Ring {
     static constexpr uint32_t STAGE_B = WIDTH / BLOCKS * DEPTH * 2;
     static constexpr uint32_t STAGE = STAGE_A + STAGE_B;
     static constexpr int STAGES = BLOCKS == 1 ? 4 : 6;
-    static constexpr uint32_t BYTES = STAGES * STAGE + 1024;  // (to begin on a multiple of 1024)
+    static constexpr uint32_t BYTES = STAGES * STAGE + TAKERS * 32 * 128 + 1024;  // (to begin on a multiple of 1024)
 };
 
 enum { TO_LOSS, TO_P, TO_SUM, TO_F32, TO_BF16 };
@@ -61,7 +61,7 @@ struct ProductArgs {
     // TO_SUM, TO_F32, TO_BF16
     const float *before;        // [m][n] to be added, or null
     void *out;                  // [m][n]; TO_SUM: [splits][m][n]
-    int wide;                   // rows of `out` begin on 16 bytes
+    int wide;                   // columns of `out` come in fours, aligned as such
     unsigned int *bad_target, *timeout;
     uint64_t limit_ns;
 };
@@ -96,7 +96,25 @@ __device__ __forceinline__ void steps_of(const ProductArgs &a, uint32_t split, u
     *k1 = (uint32_t)((uint64_t)all * (split + 1) / a.splits);
 }
 
-// What a thread does with its row of a tile: `row` of the result, columns col .. col + 32 at a time.
+// What a warp does with its part of a tile: 32 rows of the result, a row per lane, 32 columns at a time.
+//
+// Rows of the result lie far apart in memory, and 32 of them at once would be 32 requests for 16 bytes each (5.5 us a tile of sums): values
+// go through shared memory first, from where eight lanes have a row.
+constexpr uint32_t ROOM = 32 * 128;  // of a warp
+
+__device__ __forceinline__ void put_rows(unsigned char *room, const float (&f)[32]) {
+    const uint32_t lane = threadIdx.x & 31;
+    __syncwarp();  // what was there has been read
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(room + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    __syncwarp();
+}
+// Row 4 i + lane / 8, columns 4 (lane % 8) on
+__device__ __forceinline__ float4 get_row(const unsigned char *room, uint32_t i) {
+    const uint32_t lane = threadIdx.x & 31, r = 4 * i + (lane >> 3);
+    return *reinterpret_cast<const float4 *>(room + r * 128 + (((lane ^ r) & 7) << 4));
+}
+
 template <int TO, int PARTS>
 struct Epilogue;
 
@@ -106,57 +124,65 @@ struct Epilogue<TO_LOSS, PARTS> {
     uint32_t row;
     bool in;
     int target;
-    float top, sum;
-    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_) : a(a_), row(row_), in(row_ < a_.m), top(-INFINITY), sum(0.f) {
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_, unsigned char *) : a(a_), row(row_ + (threadIdx.x & 31)), in(row < a_.m) {
         target = in ? a.targets[row] : -1;
         if (target >= 0 && (uint32_t)target >= a.vocabulary) report(a.bad_target);
     }
-    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t end) {
-        float t = top;
+    // half a row of a tile: columns col .. end
+    __device__ __forceinline__ void take_half(float (&f)[SIDE / 32][32], uint32_t col, uint32_t end, const Tile &t, uint32_t side) {
+        constexpr int C = SIDE / 32;
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sums[4] = {};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            f[i] *= a.scale2;
-            if (col + 32 > end && col + i >= end) f[i] = -INFINITY;
-            t = max_nan(t, f[i]);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[c][i] *= a.scale2;
+        if (col + SIDE > end) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + 32 * c + i >= end) f[c][i] = -INFINITY;
         }
-        const float base = t == -INFINITY ? 0.f : t;
         const uint32_t at = (uint32_t)target - a.first - col;
-        if (in && target >= 0 && at < 32 && col + at < end) {
+        if (in && target >= 0 && at < SIDE && col + at < end) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (at == (uint32_t)i) a.target_score[row] = f[i];
-        }
-        float s[4] = {sum * exp2f(top - base), 0.f, 0.f, 0.f};
-        if (top == -INFINITY) s[0] = 0.f;
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f[i] - base));
-            s[i & 3] += e;
+                for (int i = 0; i < 32; ++i)
+                    if (at == (uint32_t)(32 * c + i)) a.target_score[row] = f[c][i];
         }
-        sum = (s[0] + s[1]) + (s[2] + s[3]);
-        top = t;
-    }
-    __device__ __forceinline__ void finish(const Tile &t, uint32_t side) {
-        if (in) a.tops[(uint64_t)(a.first_tile + 2 * t.n + side) * a.m + row] = make_float2(top, sum);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(tops[i / 2 % 4]) : "f"(f[c][i]), "f"(f[c][i + 1]));
+        const float top = max_nan(max_nan(tops[0], tops[1]), max_nan(tops[2], tops[3])), base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float e;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f[c][i] - base));
+                sums[i % 4] += e;
+            }
+        if (in) a.tops[(uint64_t)(a.first_tile + 2 * t.n + side) * a.m + row] = make_float2(top, (sums[0] + sums[1]) + (sums[2] + sums[3]));
     }
 };
 
 template <int PARTS>
 struct Epilogue<TO_P, PARTS> {
     const ProductArgs &a;
-    uint32_t row;
-    bool in;
+    unsigned char *room;
+    uint32_t row0, row;
     int target;
     float lse2, factor;
-    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_) : a(a_), row(row_), in(row_ < a_.m) {
-        target = in ? a.targets[row] : -1;
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_, unsigned char *room_) : a(a_), room(room_), row0(row_), row(row_ + (threadIdx.x & 31)) {
+        target = row < a.m ? a.targets[row] : -1;
         if ((uint32_t)target >= a.vocabulary) target = -1;
         lse2 = target >= 0 ? a.lse[row] * 1.44269504f : 0.f;
         factor = target >= 0 ? a.dloss[row] * a.scale : 0.f;
     }
-    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t) {
-        if (!in || col >= a.p_part) return;
+    __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
+        if (col >= a.p_part) return;
         const uint32_t at = (uint32_t)target - a.first - col;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -165,60 +191,71 @@ struct Epilogue<TO_P, PARTS> {
             if (at == (uint32_t)i) e -= 1.f;
             f[i] = target >= 0 && col + i < a.n ? e * factor : 0.f;
         }
-        __nv_bfloat16 *to = a.p + (uint64_t)row * a.p_pitch + col;
+        put_rows(room, f);
+        const uint32_t lane = threadIdx.x & 31, r0 = row0 + (lane >> 3);
+        __nv_bfloat16 *to = a.p + (uint64_t)r0 * a.p_pitch + col + 4 * (lane & 7);
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
+        for (uint32_t i = 0; i < 8; ++i, to += 4 * a.p_pitch) {
+            float4 v = get_row(room, i);
+            if (r0 + 4 * i >= a.m) break;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                reinterpret_cast<uint4 *>(to)[i] =
-                    make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]), pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
-#pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] -= __bfloat162float(__float2bfloat16_rn(f[i]));
-            to += a.p_part;
+            for (int part = 0; part < PARTS; ++part) {
+                const uint2 w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                *reinterpret_cast<uint2 *>(to + part * a.p_part) = w;
+                v.x -= __uint_as_float(w.x << 16);
+                v.y -= __uint_as_float(w.x & 0xffff0000u);
+                v.z -= __uint_as_float(w.y << 16);
+                v.w -= __uint_as_float(w.y & 0xffff0000u);
+            }
         }
     }
-    __device__ __forceinline__ void finish(const Tile &, uint32_t) {}
 };
 
 template <int TO, int PARTS>
 struct Epilogue {
     const ProductArgs &a;
-    uint32_t row;
-    uint64_t at;
-    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_) : a(a_), row(row_), at(((TO == TO_SUM ? (uint64_t)t.split * a_.m : 0) + row_) * a_.n) {}
-    __device__ __forceinline__ void take(float (&f)[32], uint32_t col, uint32_t) {
-        if (row >= a.m || col >= a.n) return;
-        if (a.before) {
-            const float *b = a.before + at + col;
+    unsigned char *room;
+    uint32_t row0;
+    uint64_t first;  // of the split's result
+    __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_, unsigned char *room_)
+        : a(a_), room(room_), row0(row_), first(TO == TO_SUM ? (uint64_t)t.split * a_.m * a_.n : 0) {}
+    __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
+        if (col >= a.n || row0 >= a.m) return;
+        put_rows(room, f);
+        const uint32_t lane = threadIdx.x & 31, r0 = row0 + (lane >> 3), c = col + 4 * (lane & 7);
+        uint64_t at = first + (uint64_t)r0 * a.n + c;
+        if (a.wide) {  // (columns come in fours)
+            if (c >= a.n) return;
+            float4 b[8];
+            if (a.before) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (col + i < a.n) f[i] += b[i];
-        }
-        if (TO == TO_BF16) {
-            __nv_bfloat16 *to = (__nv_bfloat16 *)a.out + at + col;
-            if (a.wide && col + 32 <= a.n) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    reinterpret_cast<uint4 *>(to)[i] =
-                        make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]), pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (col + i < a.n) to[i] = __float2bfloat16_rn(f[i]);
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (r0 + 4 * i < a.m) b[i] = *reinterpret_cast<const float4 *>(a.before + at + (uint64_t)(4 * i) * a.n);
             }
-        } else {
-            float *to = (float *)a.out + at + col;
-            if (a.wide && col + 32 <= a.n) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) reinterpret_cast<float4 *>(to)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-            } else {
+            for (uint32_t i = 0; i < 8; ++i, at += 4ull * a.n) {
+                if (r0 + 4 * i >= a.m) break;
+                float4 v = get_row(room, i);
+                if (a.before) v.x += b[i].x, v.y += b[i].y, v.z += b[i].z, v.w += b[i].w;
+                if (TO == TO_BF16) *reinterpret_cast<uint2 *>((__nv_bfloat16 *)a.out + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                else *reinterpret_cast<float4 *>((float *)a.out + at) = v;
+            }
+            return;
+        }
+#pragma unroll 1
+        for (uint32_t i = 0; i < 8; ++i, at += 4ull * a.n) {
+            if (r0 + 4 * i >= a.m) break;
+            const float4 v = get_row(room, i);
+            const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (col + i < a.n) to[i] = f[i];
+            for (uint32_t k = 0; k < 4; ++k) {
+                if (c + k >= a.n) break;
+                const float y = x[k] + (a.before ? a.before[at + k] : 0.f);
+                if (TO == TO_BF16) ((__nv_bfloat16 *)a.out)[at + k] = __float2bfloat16_rn(y);
+                else ((float *)a.out)[at + k] = y;
             }
         }
     }
-    __device__ __forceinline__ void finish(const Tile &, uint32_t) {}
 };
 
 // The parts of an infinite f32 value are infinity and zeros, whose products with the parts of another value are no numbers where the
@@ -379,13 +416,14 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
         }
     } else if (warp >= 4) {
         const uint32_t part = warp & 3, side = (warp - 4) >> 2, from = side * SIDE;
+        unsigned char *const room = product_mem + (ring - shared_address(product_mem)) + R::STAGES * R::STAGE + (warp - 4) * ROOM;
         uint32_t turn = 0;
         bool ended = false;
         for (uint32_t i = worker; i < tiles; i += workers) {
             const Tile t = tile_of(a, i);
             uint32_t k0, k1;
             steps_of<PARTS>(a, t.split, &k0, &k1);
-            Epilogue<TO, PARTS> to(a, t, (t.m * BLOCKS + rank) * ROWS + part * 32 + lane);
+            Epilogue<TO, PARTS> to(a, t, (t.m * BLOCKS + rank) * ROWS + part * 32, room);
             const uint32_t col = t.n * a.width + from, end = min(a.n, (t.n + 1) * a.width);
             auto begin = [&]() {
                 if (!__all_sync(0xffffffffu, waits.wait(ready(turn & 1), (turn >> 1) & 1))) return false;
@@ -403,13 +441,14 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                 ++turn;
             };
             auto take = [&](float (&f)[32], uint32_t c) {
-                if constexpr (TO == TO_LOSS || TO == TO_P) {
+                if constexpr (TO == TO_P) {
                     if constexpr (PARTS == 3) mend_scores(a, f, to.row, c);
                 } else if (k0 == k1) {  // a split without a step of K
 #pragma unroll
                     for (int k = 0; k < 32; ++k) f[k] = 0.f;
                 }
-                to.take(f, c, end);
+                if constexpr (TO != TO_LOSS) to.take(f, c);
+                __syncwarp();
             };
             if constexpr (STEPS > 0) {
                 float sum[SIDE / 32][32];
@@ -432,12 +471,20 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                     step += STEPS;
                 } while (step < k1);
                 if (ended) break;
+                if constexpr (TO == TO_LOSS) {
+                    if constexpr (PARTS == 3) {
 #pragma unroll
-                for (uint32_t c = 0; c < SIDE / 32; ++c)
-                    if (from + c * 32 < a.width) {
-                        asm volatile("" ::: "memory");  // (one after the other: there are no registers for more at once)
-                        take(sum[c], col + c * 32);
+                        for (uint32_t c = 0; c < SIDE / 32; ++c) mend_scores(a, sum[c], to.row, col + c * 32);
                     }
+                    to.take_half(sum, col, end, t, side);
+                } else {
+#pragma unroll
+                    for (uint32_t c = 0; c < SIDE / 32; ++c)
+                        if (from + c * 32 < a.width) {
+                            asm volatile("" ::: "memory");  // (one after the other: there are no registers for more at once)
+                            take(sum[c], col + c * 32);
+                        }
+                }
             } else {
                 if (!begin()) break;
 #pragma unroll 1
@@ -448,7 +495,6 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                 }
                 leave();
             }
-            to.finish(t, side);
         }
     }
     __syncwarp();
@@ -1064,7 +1110,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             if (last && cut.splits == 1) {
                 d.before = v0 ? sum : nullptr;
                 d.out = o.out[0];
-                d.wide = is_aligned(d.out, 16) && o.cols * sizeof(T) % 16 == 0;
+                d.wide = is_aligned(d.out, 4 * sizeof(T)) && o.cols % 4 == 0;
                 e = launch_product<false, true, TO_T, PARTS>(p, table, d, cut, sm_count, stream);
             } else {
                 d.before = v0 ? sum : nullptr;
@@ -1092,7 +1138,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             const Operand x = packed_operand<T>(room + at.x, o.rows, o.cols, true);
             if (cut.splits == 1) {
                 d.out = out;
-                d.wide = is_aligned(out, 16) && o.cols * sizeof(T) % 16 == 0;
+                d.wide = is_aligned(out, 4 * sizeof(T)) && o.cols % 4 == 0;
                 e = launch_product<true, true, TO_T, PARTS>(p, x, d, cut, sm_count, stream);
             } else {
                 d.out = room + at.sum_table;
