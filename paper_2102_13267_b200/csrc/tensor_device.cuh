@@ -34,21 +34,42 @@ __device__ __forceinline__ uint64_t now_ns() {
     return t;
 }
 
-// Waits of a block that end: when one runs out of time the others give up, too.
+// A warp's number, and one of its lanes, in a form that the compiler knows to be the same for the whole warp: what depends on
+// them alone stays in uniform registers, which tensor and copy instructions take their operands from.
+__device__ __forceinline__ uint32_t warp_number() { return __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0); }
+__device__ __forceinline__ bool one_lane() {
+    uint32_t r;
+    asm volatile("{.reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p;}" : "=r"(r));
+    return r != 0;
+}
+
+// Waits of a block that end: when one runs out of time the others give up, too.  A whole warp waits.
 struct Waits {
     volatile uint32_t *gave_up;  // shared
     unsigned int *status;
     uint64_t limit_ns;
 
+    // (the clock is slow to read: it is looked at after some tries only, which the compiler takes for one instruction)
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
-        if (barrier_try(bar, parity)) return true;
-        const uint64_t t0 = now_ns();
+        uint64_t t0 = 0;
         for (;;) {
-#pragma unroll 1
-            for (int i = 0; i < 32; ++i)
-                if (barrier_try(bar, parity)) return true;
-            if (*gave_up) return false;
-            if (now_ns() - t0 > limit_ns) {
+            uint32_t done;
+            asm volatile(
+                "{.reg .pred p, q; .reg .u32 n; mov.u32 n, 0;\n"
+                "TRY_%=: mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                "@p bra DONE_%=;\n"
+                "add.u32 n, n, 1; setp.lt.u32 q, n, 64;\n"
+                "@q bra TRY_%=;\n"
+                "DONE_%=: selp.u32 %0, 1, 0, p;}"
+                : "=r"(done)
+                : "r"(bar), "r"(parity)
+                : "memory");
+            if (__all_sync(0xffffffffu, done)) return true;
+            const bool over = *gave_up != 0;
+            if (__any_sync(0xffffffffu, over)) return false;
+            const uint64_t t = now_ns();
+            if (!t0) t0 = t;
+            if (__any_sync(0xffffffffu, t - t0 >= limit_ns)) {
                 *gave_up = 1;
                 report(status);
                 return false;
@@ -89,21 +110,26 @@ __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fen
 
 // An operand in shared memory in rows of 128 bytes, swizzled over 1024: K along the rows (`turned` false: the next eight rows lie
 // 1024 bytes on), or K across them (the next eight of K lie 1024 bytes on, the next 64 values of the other side `group` bytes).
-__device__ __forceinline__ uint64_t operand(uint32_t at, bool turned, uint32_t group) {
-    const uint64_t lead = turned ? group >> 4 : 1;
-    return (uint64_t)((at & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+__device__ __forceinline__ uint32_t operand_low(uint32_t at, bool turned, uint32_t group) { return (at & 0x3ffff) >> 4 | (turned ? group >> 4 : 1) << 16; }
+constexpr uint32_t OPERAND_HIGH = 1024 >> 4 | 1u << 14 | 2u << 29;
 // bf16 by bf16 into binary32, M x N
 __host__ __device__ constexpr uint32_t product_kind(bool a_turned, bool b_turned, uint32_t m, uint32_t n) {
     return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)a_turned << 15 | (uint32_t)b_turned << 16 | (n >> 3) << 17 | (m >> 4) << 24;
 }
+// The operands' lower halves vary, the upper ones do not.
 template <int BLOCKS>
-__device__ __forceinline__ void multiply_tiles(uint32_t to, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+__device__ __forceinline__ void multiply_tiles(uint32_t to, uint32_t a_low, uint32_t b_low, uint32_t a_high, uint32_t b_high, uint32_t kind, bool add) {
     const uint32_t more = add;
     if constexpr (BLOCKS == 1)
-        asm volatile("{.reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(to), "l"(a), "l"(b), "r"(kind), "r"(more) : "memory");
+        asm volatile(
+            "{.reg .pred p; .reg .b64 a, b; setp.ne.u32 p, %6, 0; mov.b64 a, {%1, %2}; mov.b64 b, {%3, %4}; tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;}" ::"r"(to), "r"(a_low), "r"(a_high),
+            "r"(b_low), "r"(b_high), "r"(kind), "r"(more)
+            : "memory");
     else
-        asm volatile("{.reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(to), "l"(a), "l"(b), "r"(kind), "r"(more) : "memory");
+        asm volatile(
+            "{.reg .pred p; .reg .b64 a, b; setp.ne.u32 p, %6, 0; mov.b64 a, {%1, %2}; mov.b64 b, {%3, %4}; tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;}" ::"r"(to), "r"(a_low), "r"(a_high),
+            "r"(b_low), "r"(b_high), "r"(kind), "r"(more)
+            : "memory");
 }
 // The barrier at `bar` (of both blocks of a pair) is arrived at when the products issued so far are done.
 template <int BLOCKS>

@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
     extern __shared__ unsigned char product_mem[];
     __shared__ __align__(8) uint64_t barriers[2 * R::STAGES + 4];
     __shared__ uint32_t tensor_at, gave_up;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
     uint32_t rank = 0;
     if constexpr (BLOCKS == 2) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const uint32_t ring = (shared_address(product_mem) + 1023) & ~1023u;
@@ -333,21 +333,25 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
     pdl_wait();
 
     if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t bytes = BLOCKS * (STAGE_A + (B_TURNED ? R::STAGE_B : a.width / BLOCKS * DEPTH * 2));
-            uint32_t stage = 0, phase = 0;
-            for (uint32_t i = worker; i < tiles; i += workers) {
-                const Tile t = tile_of(a, i);
-                uint32_t k0, k1;
-                steps_of<PARTS>(a, t.split, &k0, &k1);
-                const int row_a = (int)((t.m * BLOCKS + rank) * ROWS), row_b = (int)(t.n * a.width + rank * (a.width / BLOCKS));
-                uint32_t product = k0 / a.blocks_k, k = k0 - product * a.blocks_k;
-                for (uint32_t step = k0; step < k1; ++step) {
-                    if (!waits.wait(empty(stage), phase ^ 1)) goto done;
-                    const int at_a = PARTS == 1 ? 0 : (int)(part_of_a(product) * a.part_a), at_b = PARTS == 1 ? 0 : (int)(part_of_b(product) * a.part_b);
-                    const uint32_t to_a = ring + stage * R::STAGE, to_b = to_a + STAGE_A;
-                    uint32_t on = full(stage);
-                    if constexpr (BLOCKS == 2) on = shared_of(on, 0);
+        const uint32_t bytes = BLOCKS * (STAGE_A + (B_TURNED ? R::STAGE_B : a.width / BLOCKS * DEPTH * 2));
+        uint32_t stage = 0, phase = 0;
+        bool ended = false;
+        for (uint32_t i = worker; i < tiles && !ended; i += workers) {
+            const Tile t = tile_of(a, i);
+            uint32_t k0, k1;
+            steps_of<PARTS>(a, t.split, &k0, &k1);
+            const int row_a = (int)((t.m * BLOCKS + rank) * ROWS), row_b = (int)(t.n * a.width + rank * (a.width / BLOCKS));
+            uint32_t product = k0 / a.blocks_k, k = k0 - product * a.blocks_k;
+            for (uint32_t step = k0; step < k1; ++step) {
+                if (!waits.wait(empty(stage), phase ^ 1)) {
+                    ended = true;
+                    break;
+                }
+                const int at_a = PARTS == 1 ? 0 : (int)(part_of_a(product) * a.part_a), at_b = PARTS == 1 ? 0 : (int)(part_of_b(product) * a.part_b);
+                const uint32_t to_a = ring + stage * R::STAGE, to_b = to_a + STAGE_A;
+                uint32_t on = full(stage);
+                if constexpr (BLOCKS == 2) on = shared_of(on, 0);
+                if (one_lane()) {
                     if (rank == 0) barrier_expect(full(stage), bytes);
                     if (A_TURNED) {
 #pragma unroll
@@ -361,23 +365,24 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                     } else {
                         copy_tile<BLOCKS>(to_b, &map_b, on, at_b + (int)(k * DEPTH), row_b);
                     }
-                    if (++stage == R::STAGES) stage = 0, phase ^= 1;
-                    if (++k == a.blocks_k) k = 0, ++product;
                 }
-            }
-            // the last commits arrive here, too, before the block may end
-            for (int s = 0; s < R::STAGES; ++s) {
-                if (!waits.wait(empty(stage), phase ^ 1)) break;
+                __syncwarp();
                 if (++stage == R::STAGES) stage = 0, phase ^= 1;
+                if (++k == a.blocks_k) k = 0, ++product;
             }
-        done:
-            pdl_release();
         }
+        // the last commits arrive here, too, before the block may end
+        for (int s = 0; s < R::STAGES && !ended; ++s) {
+            if (!waits.wait(empty(stage), phase ^ 1)) break;
+            if (++stage == R::STAGES) stage = 0, phase ^= 1;
+        }
+        pdl_release();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             const uint32_t kind = product_kind(A_TURNED, B_TURNED, ROWS * BLOCKS, a.width);
+            const uint32_t low_a = operand_low(ring, A_TURNED, 64 * DEPTH * 2), low_b = operand_low(ring + STAGE_A, B_TURNED, 64 * DEPTH * 2);
             // Few products can be on their way at once: whether the next stage is full is asked before this one's are issued, or
-            // the tensor cores would wait for the answer (660 cycles a step instead of 540).
+            // the tensor cores would wait for the answer.
             uint32_t stage = 0, phase = 0, turn = 0;
             bool ended = false, there = false;
             for (uint32_t i = worker; i < tiles && !ended; i += workers) {
@@ -399,17 +404,21 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                         }
                         tensor_fence_after();
                         const uint32_t next = stage + 1 == R::STAGES ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1;
-                        there = barrier_try(full(next), next_phase);
-                        const uint64_t da = operand(ring + stage * R::STAGE, A_TURNED, 64 * DEPTH * 2), db = operand(ring + stage * R::STAGE + STAGE_A, B_TURNED, 64 * DEPTH * 2);
+                        there = __all_sync(0xffffffffu, barrier_try(full(next), next_phase));
+                        const uint32_t da = low_a + stage * (R::STAGE >> 4), db = low_b + stage * (R::STAGE >> 4);
+                        if (one_lane()) {
 #pragma unroll
-                        for (uint32_t k = 0; k < DEPTH / 16; ++k)
-                            multiply_tiles<BLOCKS>(to, da + k * ((A_TURNED ? 16 * 128 : 32) >> 4), db + k * ((B_TURNED ? 16 * 128 : 32) >> 4), kind, step > from || k > 0);
-                        tensor_commit<BLOCKS>(empty(stage));
+                            for (uint32_t k = 0; k < DEPTH / 16; ++k)
+                                multiply_tiles<BLOCKS>(to, da + k * ((A_TURNED ? 16 * 128 : 32) >> 4), db + k * ((B_TURNED ? 16 * 128 : 32) >> 4), OPERAND_HIGH, OPERAND_HIGH, kind, step > from || k > 0);
+                            tensor_commit<BLOCKS>(empty(stage));
+                        }
+                        __syncwarp();
                         stage = next;
                         phase = next_phase;
                     }
                     if (ended) break;
-                    tensor_commit<BLOCKS>(ready(half));
+                    if (one_lane()) tensor_commit<BLOCKS>(ready(half));
+                    __syncwarp();
                     ++turn;
                 } while (step < k1);
             }
@@ -426,7 +435,7 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
             Epilogue<TO, PARTS> to(a, t, (t.m * BLOCKS + rank) * ROWS + part * 32, room);
             const uint32_t col = t.n * a.width + from, end = min(a.n, (t.n + 1) * a.width);
             auto begin = [&]() {
-                if (!__all_sync(0xffffffffu, waits.wait(ready(turn & 1), (turn >> 1) & 1))) return false;
+                if (!waits.wait(ready(turn & 1), (turn >> 1) & 1)) return false;
                 tensor_fence_after();
                 return true;
             };
