@@ -22,10 +22,10 @@ __device__ __forceinline__ uint32_t shared_of(uint32_t at, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void barrier_arrive_at(uint32_t cluster_bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory"); }
-__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+// (asks only; the form that waits for a while holds a warp up that has something to do: 1300 cycles a step where stages come in late)
+__device__ __forceinline__ bool barrier_done(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    asm volatile(
-        "{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{.reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
 __device__ __forceinline__ uint64_t now_ns() {

@@ -266,15 +266,28 @@ __device__ __noinline__ float score_of(const ProductArgs &a, uint32_t row, uint3
     for (uint32_t k = 0; k < a.plain_cols; ++k) s += x[k] * w[k];
     return s;
 }
-__device__ __forceinline__ void mend_scores(const ProductArgs &a, float (&f)[32], uint32_t row, uint32_t col) {
+// Which rows of the table, under half a tile's columns, and which tokens are not finite
+struct Odd {
+    int row, column;            // of the lane's token; of the lane's four columns of half a tile, a byte each
+    bool any;
+};
+__device__ __forceinline__ Odd odd_ones(const ProductArgs &a, uint32_t row, uint32_t col) {
     const uint32_t lane = threadIdx.x & 31;
-    const int odd = row < a.m ? a.odd_a[row] : 0, other = col + lane < a.n ? a.odd_b[col + lane] : 0;
-    const uint32_t one = __ballot_sync(0xffffffffu, other == 1), two = __ballot_sync(0xffffffffu, other == 2);
-    if (!(odd | one | two) || row >= a.m) return;
+    Odd o{row < a.m ? a.odd_a[row] : 0, 0, false};
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k)
+        if (col + 4 * lane + k < a.n) o.column |= a.odd_b[col + 4 * lane + k] << (8 * k);
+    o.any = __any_sync(0xffffffffu, (o.row | o.column) != 0);
+    return o;
+}
+// columns 32 c .. of the half
+__device__ __forceinline__ void mend_scores(const ProductArgs &a, const Odd &o, float (&f)[32], uint32_t row, uint32_t col, uint32_t c) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        if (odd == 2 || (two >> i & 1)) f[i] = NAN;
-        else if ((odd == 1 || (one >> i & 1)) && col + i < a.n) f[i] = score_of(a, row, col + i);
+        const int other = __shfl_sync(0xffffffffu, o.column, 8 * c + i / 4) >> (8 * (i % 4)) & 255;
+        if (row >= a.m) continue;
+        if (o.row == 2 || other == 2) f[i] = NAN;
+        else if ((o.row == 1 || other == 1) && col + i < a.n) f[i] = score_of(a, row, col + i);
     }
 }
 
@@ -285,9 +298,17 @@ __device__ __forceinline__ void mend_scores(const ProductArgs &a, float (&f)[32]
 // warps take finished tiles from there while the next one is made in the other half.  All waits are bounded.
 //
 // The tensor cores cut the sum of what they add to off instead of rounding it (half a unit of 2^-23 each time on average, all in one
-// direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, STEPS steps of K at a time are
-// summed in tensor memory (0: all of them) and those sums added up in registers, by the warps that take them.
+// direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, exact_steps steps of K at a time are
+// summed in tensor memory (0: all of them) and those sums added up in registers, by the warps that take them.  Of the six products
+// of parts the first five are 2^-8 of the last one or less, and so is what is cut off them: they are summed in one go.
 __host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts) { return parts == 3 ? 8 : to != TO_LOSS ? 0 : blocks == 1 ? 4 : 16; }
+template <int PARTS, uint32_t STEPS>
+__device__ __forceinline__ uint32_t chunk_end(const ProductArgs &a, uint32_t step, uint32_t k1) {
+    if constexpr (STEPS == 0) return k1;
+    if constexpr (PARTS == 3)
+        if (step < 5 * a.blocks_k) return min(k1, 5 * a.blocks_k);
+    return min(k1, step + STEPS);
+}
 
 template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS>
 __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs a) {
@@ -391,7 +412,7 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                 steps_of<PARTS>(a, t.split, &k0, &k1);
                 uint32_t step = k0;
                 do {
-                    const uint32_t half = turn & 1, to = tensor + half * WIDTH, from = step, end = STEPS ? min(k1, step + STEPS) : k1;
+                    const uint32_t half = turn & 1, to = tensor + half * WIDTH, from = step, end = chunk_end<PARTS, STEPS>(a, step, k1);
                     if (!waits.wait(taken(half), ((turn >> 1) & 1) ^ 1)) {
                         ended = true;
                         break;
@@ -404,7 +425,7 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                         }
                         tensor_fence_after();
                         const uint32_t next = stage + 1 == R::STAGES ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1;
-                        there = __all_sync(0xffffffffu, barrier_try(full(next), next_phase));
+                        there = __all_sync(0xffffffffu, barrier_done(full(next), next_phase));
                         const uint32_t da = low_a + stage * (R::STAGE >> 4), db = low_b + stage * (R::STAGE >> 4);
                         if (one_lane()) {
 #pragma unroll
@@ -449,9 +470,12 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                 }
                 ++turn;
             };
+            Odd odd{};
+            if constexpr (PARTS == 3 && (TO == TO_LOSS || TO == TO_P)) odd = odd_ones(a, to.row, col);
             auto take = [&](float (&f)[32], uint32_t c) {
                 if constexpr (TO == TO_P) {
-                    if constexpr (PARTS == 3) mend_scores(a, f, to.row, c);
+                    if constexpr (PARTS == 3)
+                        if (odd.any) mend_scores(a, odd, f, to.row, c, (c - col) / 32);
                 } else if (k0 == k1) {  // a split without a step of K
 #pragma unroll
                     for (int k = 0; k < 32; ++k) f[k] = 0.f;
@@ -477,14 +501,15 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                         for (int k = 0; k < 16; ++k) sum[c / 2][c % 2 * 16 + k] += f[k];
                     }
                     leave();
-                    step += STEPS;
+                    step = chunk_end<PARTS, STEPS>(a, step, k1);
                 } while (step < k1);
                 if (ended) break;
                 if constexpr (TO == TO_LOSS) {
-                    if constexpr (PARTS == 3) {
+                    if constexpr (PARTS == 3)
+                        if (odd.any) {
 #pragma unroll
-                        for (uint32_t c = 0; c < SIDE / 32; ++c) mend_scores(a, sum[c], to.row, col + c * 32);
-                    }
+                            for (uint32_t c = 0; c < SIDE / 32; ++c) mend_scores(a, odd, sum[c], to.row, col + c * 32, c);
+                        }
                     to.take_half(sum, col, end, t, side);
                 } else {
 #pragma unroll
