@@ -198,6 +198,7 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         if (x.rank < 2 || x.dims[x.rank - 1] != table.dims[1] || !leads(ids, x)) return bad(LT_ERR_SHAPE, "x is [.., columns of the table] for targets [..]");
         if (shape_numel(ids.dims, ids.rank) >= (1ll << 24) || table.dims[0] >= (1ll << 24) || table.dims[1] >= (1ll << 20))
             return bad(LT_ERR_UNSUPPORTED, "more tokens, rows or columns than the kernel counts");
+        if (shape_numel(ids.dims, ids.rank) * table.dims[0] >= (1ll << 44)) return bad(LT_ERR_UNSUPPORTED, "more scores than the kernel counts");  // (2^30 tiles of at least 128 x 128)
         for (int k = 3; k < core; ++k) {
             if (ops[k]->dtype != LT_F32) return bad(LT_ERR_DTYPE, "lse and dloss are f32");
             if (!same_shape(*ops[k], ids)) return bad(LT_ERR_SHAPE, "lse and dloss have the shape of the targets");

@@ -47,7 +47,8 @@ struct ProductArgs {
     // TO_LOSS, TO_P
     const int *targets;
     float scale, scale2;        // scale2: times log2(e), as exponentials are powers of two
-    float2 *tops;               // [halves of tiles of the vocabulary][tokens]: maximum and sum, base two
+    float2 *tops;               // [halves of tiles of the vocabulary][tops_pitch tokens]: maximum and sum, base two
+    uint32_t tops_pitch;
     float *target_score;        // [tokens], base two
     uint32_t first, first_tile, vocabulary;  // of the table's row that column 0 of the result is: its number, and that of its tile's first half
     const float *lse, *dloss;
@@ -164,7 +165,7 @@ struct Epilogue<TO_LOSS, PARTS> {
                 asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f[c][i] - base));
                 sums[i % 4] += e;
             }
-        if (in) a.tops[(uint64_t)(a.first_tile + 2 * t.n + side) * a.m + row] = make_float2(top, (sums[0] + sums[1]) + (sums[2] + sums[3]));
+        if (in) a.tops[(uint64_t)(a.first_tile + 2 * t.n + side) * a.tops_pitch + row] = make_float2(top, (sums[0] + sums[1]) + (sums[2] + sums[3]));
     }
 };
 
@@ -560,7 +561,7 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b) {
 // lse and loss of every token from what the tiles left, always in the same order: 32 / ACROSS lanes and the block's eight warps
 // have tiles of ACROSS tokens each (few tokens: one across, so that all lanes have work).
 template <uint32_t ACROSS>
-__global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const float *target_score, const int *targets, float *loss, float *lse, uint32_t tokens, uint32_t tiles, uint32_t vocabulary) {
+__global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const float *target_score, const int *targets, float *loss, float *lse, uint32_t tokens, uint32_t pitch, uint32_t tiles, uint32_t vocabulary) {
     constexpr uint32_t SHARES = 256 / ACROSS;
     pdl_release();
     pdl_wait();
@@ -572,10 +573,10 @@ __global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const fl
         for (; t + 3 * SHARES < tiles; t += 4 * SHARES) {
             float2 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = tops[(uint64_t)(t + k * SHARES) * tokens + n];
+            for (int k = 0; k < 4; ++k) v[k] = tops[(uint64_t)(t + k * SHARES) * pitch + n];
             s = joined(s, joined(joined(v[0], v[1]), joined(v[2], v[3])));
         }
-        for (; t < tiles; t += SHARES) s = joined(s, tops[(uint64_t)t * tokens + n]);
+        for (; t < tiles; t += SHARES) s = joined(s, tops[(uint64_t)t * pitch + n]);
     }
 #pragma unroll
     for (int d = 16; d >= (int)ACROSS; d >>= 1) s = joined(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, d), __shfl_xor_sync(0xffffffffu, s.y, d)));
@@ -592,8 +593,8 @@ __global__ void __launch_bounds__(256) lt_loss_join(const float2 *tops, const fl
 cudaError_t launch_join(const ProductArgs &a, uint32_t tiles, float *loss, float *lse, cudaStream_t stream) {
     const float2 *tops = a.tops;
     const float *score = a.target_score;
-    if (a.m <= 64) return launch_pdl(lt_loss_join<1>, a.m, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, tiles, a.vocabulary);
-    return launch_pdl(lt_loss_join<8>, (a.m + 7) / 8, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, tiles, a.vocabulary);
+    if (a.m <= 64) return launch_pdl(lt_loss_join<1>, a.m, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, a.tops_pitch, tiles, a.vocabulary);
+    return launch_pdl(lt_loss_join<8>, (a.m + 7) / 8, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, a.tops_pitch, tiles, a.vocabulary);
 }
 
 // ------------------------------------------------------------------------------------------- few tokens
@@ -710,23 +711,26 @@ struct PackArgs {
 };
 
 // A matrix as the products take it: bf16, in three parts if it is f32, rows padded with zeros to whole steps of K.  A thread has eight
-// columns.
-template <class T, bool WIDE>
+// columns at a time, ACROSS threads (a warp, or the block where rows are long) a row.
+template <class T, bool WIDE, uint32_t ACROSS>
 __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    constexpr uint32_t BESIDE = 256 / ACROSS;
     pdl_release();
     pdl_wait();
-    const uint32_t eights = a.padded / 8;
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const uint32_t eights = a.padded / 8, lane = threadIdx.x % ACROSS;
+    for (uint32_t r = blockIdx.x * BESIDE + threadIdx.x / ACROSS; r < a.rows; r += gridDim.x * BESIDE) {
         bool there = true;
         if (a.targets) {
-            there = (uint32_t)a.targets[r] < a.vocabulary;
-            if (!there && a.targets[r] >= 0 && threadIdx.x == 0 && blockIdx.y == 0) report(a.bad_target);
+            const int target = a.targets[r];
+            there = (uint32_t)target < a.vocabulary;
+            if (!there && target >= 0 && lane == 0) report(a.bad_target);
         }
         const T *from = (const T *)a.from + r * a.pitch;
         uint4 *to = reinterpret_cast<uint4 *>(a.to + (uint64_t)r * PARTS * a.padded);
         int odd = 0;
-        for (uint32_t c = blockIdx.y * 256 + threadIdx.x; c < eights; c += gridDim.y * 256) {
+#pragma unroll 2
+        for (uint32_t c = lane; c < eights; c += ACROSS) {
             float f[8];
             if (WIDE && there && 8 * c + 8 <= a.cols) {
                 if constexpr (PARTS == 1) {
@@ -766,9 +770,15 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
                 to[part * eights + c] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
-        if constexpr (PARTS == 3) {  // (a block has whole rows)
-            const int no_number = __syncthreads_or(odd & 2), infinite = __syncthreads_or(odd & 1);
-            if (threadIdx.x == 0) a.odd[r] = no_number ? 2 : infinite ? 1 : 0;
+        if constexpr (PARTS == 3) {
+            int infinite, no_number;
+            if constexpr (ACROSS == 32) {
+                __syncwarp();
+                no_number = __any_sync(0xffffffffu, odd & 2), infinite = __any_sync(0xffffffffu, odd & 1);
+            } else {
+                no_number = __syncthreads_or(odd & 2), infinite = __syncthreads_or(odd & 1);
+            }
+            if (lane == 0) a.odd[r] = no_number ? 2 : infinite ? 1 : 0;
         }
     }
 }
@@ -853,6 +863,7 @@ cudaError_t launch_product_of(const Operand &x, const Operand &y, const ProductA
     if (e == cudaSuccess) e = map_of(y, a.width / BLOCKS, &map_b);
     if (e != cudaSuccess) return e;
     const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n * a.splits;
+    if (tiles >= 1ull << 31) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(std::min<uint64_t>(tiles, (uint64_t)sm_count / BLOCKS) * BLOCKS));
     cfg.blockDim = dim3(THREADS);
@@ -921,9 +932,10 @@ cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_
     p.padded = (uint32_t)up_to(cols, DEPTH);
     p.vocabulary = vocabulary;
     p.bad_target = bad_target;
-    const unsigned across = p.odd ? 1 : std::min(count_of(p.padded / 8, 256), 16u), most = (unsigned)sm_count * 16 / across + 1;
-    const dim3 grid(std::min((unsigned)rows, most), across);
-    return is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0 ? launch_pdl_grid(lt_loss_pack<T, true>, grid, 256, stream, p) : launch_pdl_grid(lt_loss_pack<T, false>, grid, 256, stream, p);
+    const bool wide = is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0, long_rows = p.padded > 8192 || (p.padded >= 512 && rows < 8 * (uint64_t)sm_count);
+    const unsigned grid = std::min(count_of(rows, long_rows ? 1 : 8), (unsigned)sm_count * 8);
+    if (long_rows) return wide ? launch_pdl(lt_loss_pack<T, true, 256>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 256>, grid, 256, (size_t)0, stream, p);
+    return wide ? launch_pdl(lt_loss_pack<T, true, 32>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 32>, grid, 256, (size_t)0, stream, p);
 }
 template <class T>
 Operand packed_operand(const void *p, uint64_t rows, uint64_t cols, bool turned) {
@@ -934,28 +946,42 @@ inline size_t packed_bytes(int dtype, uint64_t rows, uint64_t cols) { return (si
 // May the matrix be an operand where it lies?
 inline bool lies_well(int dtype, const void *p, uint64_t pitch) { return dtype == LT_BF16 && is_aligned(p, 16) && pitch % 8 == 0; }
 
-constexpr uint64_t PIECE_BYTES = 256 << 20;  // of a piece of the vocabulary: its packed rows, and P
+// Pieces of the vocabulary (or of the tokens): P of one, and what a packed piece of the table takes.  Larger pieces of P are fewer sums of
+// dx to bring back (loss and gradients of 8192 x 2048 against 32000 rows: 3.62 ms with 256 MB, 3.90 with 160, 4.08 with 96);
+// packed f32 rows are read from the L2 cache if there is not much more of them than fits.
+constexpr uint64_t P_BYTES = 256 << 20, PACK_BYTES = 96 << 20, SPARE_BYTES = 8 << 20;
 
-// Rows of the table at a time (a multiple of a tile's columns), if a row takes `bytes`.
-uint64_t piece_of(uint64_t vocabulary, uint64_t bytes) {
-    const uint64_t most = std::max<uint64_t>(WIDTH, PIECE_BYTES / bytes / WIDTH * WIDTH), pieces = (vocabulary + most - 1) / most;
-    return up_to((vocabulary + pieces - 1) / pieces, WIDTH);
+// Rows at a time (a multiple of a tile's columns, pieces of about one size), if a row takes `bytes` and a piece `most`.
+uint64_t piece_of(uint64_t rows, uint64_t bytes, uint64_t most) {
+    most = std::max<uint64_t>(WIDTH, most / bytes / WIDTH * WIDTH);
+    const uint64_t pieces = (rows + most - 1) / most;
+    return up_to((rows + pieces - 1) / pieces, WIDTH);
+}
+// Addresses are not known when scratch is planned: bf16 rows whose distance fits lie well unless they begin in an unusual place, for
+// which there is some room, too.
+inline uint64_t pack_piece(const LtOperator &o, int k, uint64_t rows) {
+    return piece_of(rows, packed_bytes(o.dtype, 1, o.cols), o.dtype == LT_BF16 && o.pitch[k] % 8 == 0 ? SPARE_BYTES : PACK_BYTES);
 }
 
 constexpr size_t FEW_BYTES = 72 << 10;  // of x: three blocks to an SM
 inline bool few_tokens(const LtOperator &o) { return o.rows <= FEW && o.rows * up_to(o.cols, 8) * (o.dtype == LT_BF16 ? 2 : 4) <= FEW_BYTES; }
 inline unsigned few_blocks(const LtOperator &o, int sm_count) { return (unsigned)std::min<uint64_t>(3ull * sm_count, count_of(o.vocabulary, FEW_THREADS / 32 * FEW_ROWS)); }
 
-// Halves of tiles that the loss may leave maxima and sums of.
-uint64_t most_tops(uint64_t vocabulary, uint64_t piece) { return 2 * (count_of(vocabulary, LEAST_WIDTH) + (vocabulary + piece - 1) / piece); }
-
-// Addresses are not known when scratch is planned: room for packed operands is there whether they will need it or not, but
-// for bf16 sizes that never do it is not more than a piece.
 struct LossScratch {
     size_t score, odd_x, odd_table, tops, x, table, bytes;
-    uint64_t piece;
+    uint64_t piece, x_piece;    // rows that are packed at a time
     LossScratch(const LtOperator &o, int sm_count) {
-        piece = piece_of(o.vocabulary, packed_bytes(o.dtype, 1, o.cols));
+        piece = pack_piece(o, 1, o.vocabulary);
+        x_piece = o.dtype == LT_F32 ? o.rows : std::min(o.rows, pack_piece(o, 0, o.rows));
+        // halves of tiles that maxima and sums are left of: of the whole vocabulary, or of pieces
+        uint64_t halves = 0;
+        for (uint64_t m : {o.rows, x_piece, o.rows % x_piece}) {
+            if (!m) continue;
+            const uint64_t rest = o.vocabulary % piece;
+            uint64_t some = 2ull * Cut(m, std::min(piece, o.vocabulary), sm_count, 32).tiles_n * (o.vocabulary / piece);
+            if (rest) some += 2ull * Cut(m, rest, sm_count, 32).tiles_n;
+            halves = std::max({halves, some, (uint64_t)2 * Cut(m, o.vocabulary, sm_count, 32).tiles_n});
+        }
         score = 0;
         odd_x = up_to(o.rows * 4, 256);
         odd_table = odd_x + up_to(o.rows, 256);
@@ -964,19 +990,21 @@ struct LossScratch {
             bytes = tops + up_to(few_blocks(o, sm_count) * o.rows * sizeof(float2), 256);
             return;
         }
-        x = tops + up_to(most_tops(o.vocabulary, piece) * o.rows * sizeof(float2), 256);
-        table = x + packed_bytes(o.dtype, o.rows, o.cols);
+        x = tops + up_to(halves * o.rows * sizeof(float2), 256);
+        table = x + packed_bytes(o.dtype, x_piece, o.cols);
         bytes = table + packed_bytes(o.dtype, piece, o.cols);
     }
 };
 
 struct GradScratch {
     size_t x, odd_x, odd_table, table, p, sum_x, sum_table, bytes;
-    uint64_t piece;
+    uint64_t piece, packed_piece;  // the latter where the table does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
         const uint64_t parts = o.dtype == LT_F32 ? 3 : 1;
-        piece = piece_of(o.vocabulary, std::max<uint64_t>(packed_bytes(o.dtype, 1, o.cols), o.rows * 2 * parts));
+        piece = piece_of(o.vocabulary, o.rows * 2 * parts, P_BYTES);
+        packed_piece = std::min(piece, pack_piece(o, 1, o.vocabulary));
+        if (o.dtype == LT_F32 || o.pitch[1] % 8) piece = packed_piece;
         const uint64_t steps = count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), steps_t = count_of(o.rows, DEPTH) * (parts == 1 ? 1 : 6);
         const Cut cx = Cut(o.rows, o.cols, sm_count, 0).split(steps, sm_count), ct = Cut(piece, o.cols, sm_count, 0).split(steps_t, sm_count);
         x = 0;
@@ -984,9 +1012,9 @@ struct GradScratch {
         odd_table = odd_x + up_to(o.rows, 256);
         table = odd_table + up_to(piece, 256);
         splits_table = ct.splits;
-        p = table + packed_bytes(o.dtype, piece, o.cols);
+        p = table + packed_bytes(o.dtype, packed_piece, o.cols);
         sum_x = p + up_to(o.rows * piece * 2 * parts, 256);
-        sum_table = sum_x + (piece < o.vocabulary || cx.splits > 1 ? up_to(cx.splits * o.rows * o.cols * 4, 256) : 0);
+        sum_table = sum_x + (packed_piece < o.vocabulary || cx.splits > 1 ? up_to(cx.splits * o.rows * o.cols * 4, 256) : 0);
         bytes = sum_table + (ct.splits > 1 ? up_to(ct.splits * piece * o.cols * 4, 256) : 0);
     }
 };
@@ -1002,11 +1030,11 @@ void common_args(const LtOperator &o, ProductArgs &a) {
 }
 
 // f32: the operands of the scores themselves
-void plain_args(const LtOperator &o, ProductArgs &a, const void *odd_x, const void *odd_table, const void *table) {
+void plain_args(const LtOperator &o, ProductArgs &a, const void *x, const void *odd_x, const void *odd_table, const void *table) {
     if (o.dtype != LT_F32) return;
     a.odd_a = (const uint8_t *)odd_x;
     a.odd_b = (const uint8_t *)odd_table;
-    a.plain_a = (const float *)o.in[0];
+    a.plain_a = (const float *)x;
     a.plain_b = (const float *)table;
     a.plain_pitch_a = o.pitch[0];
     a.plain_pitch_b = o.pitch[1];
@@ -1038,6 +1066,7 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
         a.m = (uint32_t)o.rows;
         a.target_score = (float *)(room + at.score);
         a.tops = (float2 *)(room + at.tops);
+        a.tops_pitch = a.m;
         constexpr int N = 16 / (int)sizeof(T);
         const FewArgs f{o.in[0], o.in[1], a.targets, a.tops, a.target_score, o.pitch[0], o.pitch[1], a.vocabulary, (uint32_t)o.cols, a.scale2, a.bad_target};
         const bool wide = o.cols % N == 0 && o.pitch[1] % N == 0 && is_aligned(o.in[1], 16);
@@ -1049,40 +1078,49 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
     const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]), table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
     cudaError_t e = cudaSuccess;
     *launched = 0;
-    Operand x{o.in[0], o.pitch[0], o.rows, o.cols, 0, false};
-    if (!x_well) {
-        e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, nullptr, 0, nullptr, room + at.x, room + at.odd_x, sm_count, stream);
-        x = packed_operand<T>(room + at.x, o.rows, o.cols, false);
-        ++*launched;
-    }
-    const uint64_t piece = table_well ? o.vocabulary : at.piece;
-    ProductArgs a{};
-    common_args(o, a);
-    a.m = (uint32_t)o.rows;
-    a.blocks_k = count_of(o.cols, DEPTH);
-    a.target_score = (float *)(room + at.score);
-    a.tops = (float2 *)(room + at.tops);
-    for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
-        const uint64_t n = std::min(piece, o.vocabulary - v0);
-        const void *rows = (const T *)o.in[1] + v0 * o.pitch[1];
-        Operand table{rows, o.pitch[1], n, o.cols, 0, false};
-        if (!table_well) {
-            e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+    const uint64_t piece = table_well ? o.vocabulary : at.piece, x_piece = x_well ? o.rows : at.x_piece;
+    for (uint64_t r0 = 0; r0 < o.rows; r0 += x_piece) {
+        const uint64_t m = std::min(x_piece, o.rows - r0);
+        ProductArgs a{};
+        common_args(o, a);
+        a.m = (uint32_t)m;
+        a.targets += r0;
+        a.blocks_k = count_of(o.cols, DEPTH);
+        a.target_score = (float *)(room + at.score) + r0;
+        a.tops = (float2 *)(room + at.tops) + r0;
+        a.tops_pitch = (uint32_t)o.rows;
+        const T *tokens = (const T *)o.in[0] + r0 * o.pitch[0];
+        Operand x{tokens, o.pitch[0], m, o.cols, 0, false};
+        if (!x_well) {
+            e = launch_pack<T>(tokens, o.pitch[0], m, o.cols, nullptr, 0, nullptr, room + at.x, room + at.odd_x, sm_count, stream);
             if (e != cudaSuccess) return e;
-            table = packed_operand<T>(room + at.table, n, o.cols, false);
+            x = packed_operand<T>(room + at.x, m, o.cols, false);
             ++*launched;
         }
-        a.n = (uint32_t)n;
-        a.first = (uint32_t)v0;
-        plain_args(o, a, room + at.odd_x, room + at.odd_table, rows);
-        const Cut cut(o.rows, n, sm_count, 32);
-        e = launch_product<false, false, TO_LOSS, (int)parts_of<T>()>(x, table, a, cut, sm_count, stream);
-        a.first_tile += 2 * cut.tiles_n;
+        for (uint64_t v0 = 0; v0 < o.vocabulary; v0 += piece) {
+            const uint64_t n = std::min(piece, o.vocabulary - v0);
+            const T *rows = (const T *)o.in[1] + v0 * o.pitch[1];
+            Operand table{rows, o.pitch[1], n, o.cols, 0, false};
+            if (!table_well) {
+                e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+                if (e != cudaSuccess) return e;
+                table = packed_operand<T>(room + at.table, n, o.cols, false);
+                ++*launched;
+            }
+            a.n = (uint32_t)n;
+            a.first = (uint32_t)v0;
+            plain_args(o, a, tokens, room + at.odd_x, room + at.odd_table, rows);
+            const Cut cut(m, n, sm_count, 32);
+            e = launch_product<false, false, TO_LOSS, (int)parts_of<T>()>(x, table, a, cut, sm_count, stream);
+            if (e != cudaSuccess) return e;
+            a.first_tile += 2 * cut.tiles_n;
+            ++*launched;
+        }
         ++*launched;
+        e = launch_join(a, a.first_tile, o.out[0] ? (float *)o.out[0] + r0 : nullptr, o.out[1] ? (float *)o.out[1] + r0 : nullptr, stream);
+        if (e != cudaSuccess) return e;
     }
-    if (e != cudaSuccess) return e;
-    ++*launched;
-    return launch_join(a, a.first_tile, (float *)o.out[0], (float *)o.out[1], stream);
+    return e;
 }
 
 template <class T>
@@ -1104,8 +1142,9 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
     // (x always: rows without a target, which may hold anything, are left out of the table's gradient)
     cudaError_t e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, (const int *)o.in[2], (uint32_t)o.vocabulary, &o.status->loss, room + at.x, room + at.odd_x, sm_count, stream);
     *launched = 1;
-    for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += at.piece) {
-        const uint64_t n = std::min(at.piece, o.vocabulary - v0), padded = up_to(n, WIDTH);
+    const uint64_t piece = table_well ? at.piece : at.packed_piece;
+    for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
+        const uint64_t n = std::min(piece, o.vocabulary - v0), padded = up_to(n, WIDTH);
         const bool last = v0 + n == o.vocabulary;
         const void *rows = (const T *)o.in[1] + v0 * o.pitch[1];
         Operand table{rows, o.pitch[1], n, o.cols, 0, false};
@@ -1126,7 +1165,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         a.p = (__nv_bfloat16 *)(room + at.p);
         a.p_pitch = padded * parts;
         a.p_part = (uint32_t)padded;
-        plain_args(o, a, room + at.odd_x, room + at.odd_table, rows);
+        plain_args(o, a, o.in[0], room + at.odd_x, room + at.odd_table, rows);
         e = launch_product<false, false, TO_P, PARTS>(packed_operand<T>(room + at.x, o.rows, o.cols, false), table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
         if (e != cudaSuccess) return e;
         ++*launched;
@@ -1138,7 +1177,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             d.n = (uint32_t)o.cols;
             d.blocks_k = count_of(n, DEPTH);
             // (as many splits for every piece, the last and shorter one too)
-            const Cut cut = Cut(o.rows, o.cols, sm_count, 0).split(count_of(at.piece, DEPTH) * (parts == 1 ? 1 : 6), sm_count);
+            const Cut cut = Cut(o.rows, o.cols, sm_count, 0).split(count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), sm_count);
             float *sum = (float *)(room + at.sum_x);
             table.turned = true;
             if (last && cut.splits == 1) {
