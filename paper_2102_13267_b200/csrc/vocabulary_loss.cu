@@ -62,7 +62,7 @@ struct ProductArgs {
     // TO_SUM, TO_F32, TO_BF16
     const float *before;        // [m][n] to be added, or null
     void *out;                  // [m][n]; TO_SUM: [splits][m][n]
-    int wide;                   // columns of `out` come in fours, aligned as such
+    int wide;                   // columns of `out` come in fours (4) or eights (8), aligned as such
     unsigned int *bad_target, *timeout;
     uint64_t limit_ns;
 };
@@ -114,6 +114,31 @@ __device__ __forceinline__ void put_rows(unsigned char *room, const float (&f)[3
 __device__ __forceinline__ float4 get_row(const unsigned char *room, uint32_t i) {
     const uint32_t lane = threadIdx.x & 31, r = 4 * i + (lane >> 3);
     return *reinterpret_cast<const float4 *>(room + r * 128 + (((lane ^ r) & 7) << 4));
+}
+
+// The same for bf16: 64 columns, half of them at a time; row 4 i + lane / 8, columns 8 (lane % 8) on
+__device__ __forceinline__ void put_half_rows(unsigned char *room, const float (&f)[32], uint32_t half) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (half == 0) __syncwarp();  // what was there has been read
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4 *>(room + lane * 128 + (((4 * half + i) ^ (lane & 7)) << 4)) =
+            make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]), pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
+    if (half == 1) __syncwarp();
+}
+__device__ __forceinline__ uint4 get_eight(const unsigned char *room, uint32_t i) {
+    const uint32_t lane = threadIdx.x & 31, r = 4 * i + (lane >> 3);
+    return *reinterpret_cast<const uint4 *>(room + r * 128 + (((lane ^ r) & 7) << 4));
+}
+// 64 columns of 32 rows to memory, rows `pitch` apart; `end`: behind the last column that is there, `rows`: how many rows are
+__device__ __forceinline__ void store_eights(const unsigned char *room, __nv_bfloat16 *to, uint64_t pitch, uint32_t col, uint32_t end, uint32_t rows) {
+    const uint32_t lane = threadIdx.x & 31, r0 = lane >> 3, c = 8 * (lane & 7);
+    to += r0 * pitch + col + c;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        const uint4 v = get_eight(room, i);
+        if (r0 + 4 * i < rows && col + c < end) *reinterpret_cast<uint4 *>(to + 4 * i * pitch) = v;
+    }
 }
 
 template <int TO, int PARTS>
@@ -192,6 +217,12 @@ struct Epilogue<TO_P, PARTS> {
             if (at == (uint32_t)i) e -= 1.f;
             f[i] = target >= 0 && col + i < a.n ? e * factor : 0.f;
         }
+        if constexpr (PARTS == 1) {  // (columns come in 64s)
+            const uint32_t half = col >> 5 & 1;
+            put_half_rows(room, f, half);
+            if (half && row0 < a.m) store_eights(room, a.p + (uint64_t)row0 * a.p_pitch, a.p_pitch, col - 32, a.p_part, a.m - row0);
+            return;
+        }
         put_rows(room, f);
         const uint32_t lane = threadIdx.x & 31, r0 = row0 + (lane >> 3);
         __nv_bfloat16 *to = a.p + (uint64_t)r0 * a.p_pitch + col + 4 * (lane & 7);
@@ -221,6 +252,13 @@ struct Epilogue {
     __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_, unsigned char *room_)
         : a(a_), room(room_), row0(row_), first(TO == TO_SUM ? (uint64_t)t.split * a_.m * a_.n : 0) {}
     __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
+        if (TO == TO_BF16 && a.wide == 8 && !a.before) {
+            const uint32_t half = col >> 5 & 1;
+            if (col - 32 * half >= a.n || row0 >= a.m) return;
+            put_half_rows(room, f, half);
+            if (half) store_eights(room, (__nv_bfloat16 *)a.out + (uint64_t)row0 * a.n, a.n, col - 32, a.n, a.m - row0);
+            return;
+        }
         if (col >= a.n || row0 >= a.m) return;
         put_rows(room, f);
         const uint32_t lane = threadIdx.x & 31, r0 = row0 + (lane >> 3), c = col + 4 * (lane & 7);
@@ -1131,6 +1169,9 @@ cudaError_t launch_sum(const float *sums, void *out, uint64_t count, uint32_t sp
                 : launch_pdl(lt_loss_sum<T, 1>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits);
 }
 
+// How many columns of a result can be stored at once: 8, 4 or 0 (one)
+inline int width_of(const void *out, uint64_t cols, size_t size) { return size == 2 && cols % 8 == 0 && is_aligned(out, 16) ? 8 : cols % 4 == 0 && is_aligned(out, 4 * size) ? 4 : 0; }
+
 template <class T>
 cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
     constexpr int PARTS = parts_of<T>();
@@ -1183,12 +1224,12 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             if (last && cut.splits == 1) {
                 d.before = v0 ? sum : nullptr;
                 d.out = o.out[0];
-                d.wide = is_aligned(d.out, 4 * sizeof(T)) && o.cols % 4 == 0;
+                d.wide = width_of(d.out, o.cols, sizeof(T));
                 e = launch_product<false, true, TO_T, PARTS>(p, table, d, cut, sm_count, stream);
             } else {
                 d.before = v0 ? sum : nullptr;
                 d.out = sum;
-                d.wide = o.cols % 4 == 0;
+                d.wide = width_of(d.out, o.cols, 4);
                 e = launch_product<false, true, TO_SUM, PARTS>(p, table, d, cut, sm_count, stream);
                 if (e == cudaSuccess && last) {
                     e = launch_sum<T>(sum, o.out[0], o.rows * o.cols, cut.splits, sm_count, stream);
@@ -1211,11 +1252,11 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             const Operand x = packed_operand<T>(room + at.x, o.rows, o.cols, true);
             if (cut.splits == 1) {
                 d.out = out;
-                d.wide = is_aligned(out, 4 * sizeof(T)) && o.cols % 4 == 0;
+                d.wide = width_of(out, o.cols, sizeof(T));
                 e = launch_product<true, true, TO_T, PARTS>(p, x, d, cut, sm_count, stream);
             } else {
                 d.out = room + at.sum_table;
-                d.wide = o.cols % 4 == 0;
+                d.wide = width_of(d.out, o.cols, 4);
                 e = launch_product<true, true, TO_SUM, PARTS>(p, x, d, cut, sm_count, stream);
                 if (e == cudaSuccess) e = launch_sum<T>((const float *)d.out, out, n * o.cols, cut.splits, sm_count, stream);
                 ++*launched;
