@@ -54,7 +54,7 @@ struct ProductArgs {
     const float *lse, *dloss;
     __nv_bfloat16 *p;
     uint64_t p_pitch;
-    uint32_t p_part;
+    uint32_t p_part, p_rows;    // p_rows: those that are written, zeros behind the tokens
     const uint8_t *odd_a, *odd_b;  // f32: which rows of the operands are not finite (1: infinities, 2: no numbers)
     const float *plain_a, *plain_b;
     uint64_t plain_pitch_a, plain_pitch_b;
@@ -220,7 +220,7 @@ struct Epilogue<TO_P, PARTS> {
         if constexpr (PARTS == 1) {  // (columns come in 64s)
             const uint32_t half = col >> 5 & 1;
             put_half_rows(room, f, half);
-            if (half && row0 < a.m) store_eights(room, a.p + (uint64_t)row0 * a.p_pitch, a.p_pitch, col - 32, a.p_part, a.m - row0);
+            if (half && row0 < a.p_rows) store_eights(room, a.p + (uint64_t)row0 * a.p_pitch, a.p_pitch, col - 32, a.p_part, a.p_rows - row0);
             return;
         }
         put_rows(room, f);
@@ -229,7 +229,7 @@ struct Epilogue<TO_P, PARTS> {
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i, to += 4 * a.p_pitch) {
             float4 v = get_row(room, i);
-            if (r0 + 4 * i >= a.m) break;
+            if (r0 + 4 * i >= a.p_rows) break;
 #pragma unroll
             for (int part = 0; part < PARTS; ++part) {
                 const uint2 w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
@@ -637,9 +637,9 @@ cudaError_t launch_join(const ProductArgs &a, uint32_t tiles, float *loss, float
 
 // ------------------------------------------------------------------------------------------- few tokens
 
-// One to FEW tokens: the table is read once, at the memory's rate, by warps that have FEW_ROWS of its rows at a time, 16 bytes of each per lane;
+// One or two tokens: the table is read once, at the memory's rate, by warps that have FEW_ROWS of its rows at a time, 16 bytes of each per lane;
 // products and sums in binary32.  (A tile of the tensor cores would be nearly all padding, and f32 rows would have to be taken apart first.)
-constexpr int FEW = 4, FEW_ROWS = 2, FEW_THREADS = 256;
+constexpr int FEW_ROWS = 2, FEW_THREADS = 256, SOME_THREADS = 512;
 
 struct FewArgs {
     const void *x, *table;
@@ -647,9 +647,27 @@ struct FewArgs {
     float2 *tops;               // [blocks][tokens]
     float *target_score;
     uint64_t x_pitch, table_pitch;
-    uint32_t vocabulary, cols;
+    uint32_t tokens, vocabulary, cols;
     float scale2;
     unsigned int *bad_target;
+};
+
+// N values of T that lie side by side: 16 bytes, or one
+template <class T, int N>
+struct Loaded {
+    uint4 v;
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (N == 1) v.x = __float_as_uint(to_float(*p));
+        else v = __ldcs(reinterpret_cast<const uint4 *>(p));
+    }
+    __device__ __forceinline__ void load_shared(const T *p) {
+        if constexpr (N == 1) v.x = __float_as_uint(to_float(*p));
+        else v = *reinterpret_cast<const uint4 *>(p);
+    }
+    __device__ __forceinline__ void values(float (&f)[N]) const {
+        if constexpr (N == 1) f[0] = __uint_as_float(v.x);
+        else unpack(v, f);
+    }
 };
 
 template <class T, int N, int TOKENS>
@@ -738,13 +756,105 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) lt_loss_few(const FewArgs a) {
     }
 }
 
+// The same for TOKENS tokens at a time, ROWS of the table's rows to a warp, so that what is read from shared memory serves several rows.
+// The warp's ROWS x TOKENS sums over its lanes are made by halving: each lane sends half of its values and keeps the sums of the other half,
+// and is left with one or two, of one row.
+template <class T, int N, int TOKENS>
+__global__ void __launch_bounds__(SOME_THREADS, 1) lt_loss_some(const FewArgs a) {
+    constexpr int ROWS_AT_ONCE = TOKENS < 8 ? 32 / TOKENS : 4, VALUES = ROWS_AT_ONCE * TOKENS, EACH = VALUES / 32, WARPS = SOME_THREADS / 32, AHEAD = 8 / ROWS_AT_ONCE;
+    extern __shared__ uint4 few_mem[];  // x: [TOKENS][columns], as it lies in memory
+    T *const xs = reinterpret_cast<T *>(few_mem);
+    __shared__ float2 sums[WARPS][TOKENS];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = (a.cols + 7) & ~7u, first = blockIdx.y * TOKENS, tokens = min((uint32_t)TOKENS, a.tokens - first);
+    pdl_release();
+    pdl_wait();
+    for (uint32_t t = 0; t < TOKENS; ++t)
+        for (uint32_t c = threadIdx.x; c < pitch; c += SOME_THREADS) xs[t * pitch + c] = t < tokens && c < a.cols ? ((const T *)a.x)[(first + t) * a.x_pitch + c] : from_float<T>(0.f);
+    // the lane's values: of row `mine` of those at once, tokens from `token` on
+    const uint32_t value = lane * EACH, mine = value / TOKENS, token = value % TOKENS;
+    int target[EACH];
+    float2 s[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        target[e] = token + e < tokens ? a.targets[first + token + e] : -1;
+        if (blockIdx.x == 0 && warp == 0 && mine == 0 && target[e] >= 0 && (uint32_t)target[e] >= a.vocabulary) report(a.bad_target);
+        s[e] = make_float2(-INFINITY, 0.f);
+    }
+    __syncthreads();
+    const uint32_t v0 = (uint32_t)((uint64_t)a.vocabulary * blockIdx.x / gridDim.x), v1 = (uint32_t)((uint64_t)a.vocabulary * (blockIdx.x + 1) / gridDim.x);
+    for (uint32_t v = v0 + warp * ROWS_AT_ONCE; v < v1; v += WARPS * ROWS_AT_ONCE) {
+        float dot[VALUES] = {};
+        const T *row[ROWS_AT_ONCE];
+#pragma unroll
+        for (int r = 0; r < ROWS_AT_ONCE; ++r) row[r] = (const T *)a.table + (uint64_t)min(v + r, v1 - 1) * a.table_pitch;
+        for (uint32_t c0 = lane * N; c0 < a.cols; c0 += 32 * N * AHEAD) {
+            Loaded<T, N> w[AHEAD][ROWS_AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int r = 0; r < ROWS_AT_ONCE; ++r)
+                    if (c0 + k * 32 * N < a.cols) w[k][r].load(row[r] + c0 + k * 32 * N);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const uint32_t c = c0 + k * 32 * N;
+                if (c >= a.cols) break;
+                float f[ROWS_AT_ONCE][N];
+#pragma unroll
+                for (int r = 0; r < ROWS_AT_ONCE; ++r) w[k][r].values(f[r]);
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) {
+                    float x[N];
+                    Loaded<T, N> l;
+                    l.load_shared(xs + t * pitch + c);
+                    l.values(x);
+#pragma unroll
+                    for (int r = 0; r < ROWS_AT_ONCE; ++r)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) dot[r * TOKENS + t] += f[r][i] * x[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 16, n = VALUES / 2; d >= 1; d >>= 1, n >>= 1) {
+            const bool upper = lane & d;
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const float keep = upper ? dot[i + n] : dot[i], send = upper ? dot[i] : dot[i + n];
+                dot[i] = keep + __shfl_xor_sync(0xffffffffu, send, d);
+            }
+        }
+        if (v + mine < v1) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const float z = dot[e] * a.scale2;
+                s[e] = joined(s[e], make_float2(z, 1.f));
+                if ((int)(v + mine) == target[e]) a.target_score[first + token + e] = z;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+#pragma unroll
+        for (int d = TOKENS / EACH; d < 32; d <<= 1) s[e] = joined(s[e], make_float2(__shfl_xor_sync(0xffffffffu, s[e].x, d), __shfl_xor_sync(0xffffffffu, s[e].y, d)));
+    if (mine == 0) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) sums[warp][token + e] = s[e];
+    }
+    __syncthreads();
+    if (threadIdx.x < tokens) {
+        float2 r = sums[0][threadIdx.x];
+        for (int w = 1; w < WARPS; ++w) r = joined(r, sums[w][threadIdx.x]);
+        a.tops[(uint64_t)blockIdx.x * a.tokens + first + threadIdx.x] = r;
+    }
+}
+
 struct PackArgs {
     const void *from;
     uint64_t pitch;
     const int *targets;         // rows without one become zeros; or null
     __nv_bfloat16 *to;          // [rows][parts][padded]
     uint8_t *odd;               // three parts: 1 for rows with infinities, 2 for rows with what is no number
-    uint32_t rows, cols, padded, vocabulary;
+    uint32_t rows, present, cols, padded, vocabulary;  // present: rows that there are; zeros behind them
     unsigned int *bad_target;
 };
 
@@ -758,8 +868,8 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
     pdl_wait();
     const uint32_t eights = a.padded / 8, lane = threadIdx.x % ACROSS;
     for (uint32_t r = blockIdx.x * BESIDE + threadIdx.x / ACROSS; r < a.rows; r += gridDim.x * BESIDE) {
-        bool there = true;
-        if (a.targets) {
+        bool there = r < a.present;
+        if (a.targets && there) {
             const int target = a.targets[r];
             there = (uint32_t)target < a.vocabulary;
             if (!there && target >= 0 && lane == 0) report(a.bad_target);
@@ -953,6 +1063,10 @@ cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, co
     return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream);
 }
 
+// A packed operand has at least so many rows (zeros): of a tile that holds fewer, copies are slower (5 tokens against 32000 rows of 4096: 73
+// us, 16 of them 51).
+constexpr uint64_t LEAST_ROWS = 16;
+
 template <class T>
 constexpr uint32_t parts_of() { return sizeof(T) == 4 ? 3 : 1; }
 
@@ -965,22 +1079,24 @@ cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_
     p.targets = targets;
     p.to = (__nv_bfloat16 *)to;
     p.odd = sizeof(T) == 4 ? (uint8_t *)odd : nullptr;
-    p.rows = (uint32_t)rows;
+    p.rows = (uint32_t)std::max<uint64_t>(rows, LEAST_ROWS);
+    p.present = (uint32_t)rows;
     p.cols = (uint32_t)cols;
     p.padded = (uint32_t)up_to(cols, DEPTH);
     p.vocabulary = vocabulary;
     p.bad_target = bad_target;
     const bool wide = is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0, long_rows = p.padded > 8192 || (p.padded >= 512 && rows < 8 * (uint64_t)sm_count);
-    const unsigned grid = std::min(count_of(rows, long_rows ? 1 : 8), (unsigned)sm_count * 8);
+    const unsigned grid = std::min(count_of(p.rows, long_rows ? 1 : 8), (unsigned)sm_count * 8);
     if (long_rows) return wide ? launch_pdl(lt_loss_pack<T, true, 256>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 256>, grid, 256, (size_t)0, stream, p);
     return wide ? launch_pdl(lt_loss_pack<T, true, 32>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 32>, grid, 256, (size_t)0, stream, p);
 }
 template <class T>
 Operand packed_operand(const void *p, uint64_t rows, uint64_t cols, bool turned) {
     const uint64_t padded = up_to(cols, DEPTH);
-    return Operand{p, padded * parts_of<T>(), rows, padded * parts_of<T>(), (uint32_t)padded, turned};
+    return Operand{p, padded * parts_of<T>(), std::max<uint64_t>(rows, LEAST_ROWS), padded * parts_of<T>(), (uint32_t)padded, turned};
 }
-inline size_t packed_bytes(int dtype, uint64_t rows, uint64_t cols) { return (size_t)up_to(rows * up_to(cols, DEPTH) * 2 * (dtype == LT_F32 ? 3 : 1), 256); }
+inline size_t packed_row(int dtype, uint64_t cols) { return (size_t)up_to(up_to(cols, DEPTH) * 2 * (dtype == LT_F32 ? 3 : 1), 256); }
+inline size_t packed_bytes(int dtype, uint64_t rows, uint64_t cols) { return (size_t)up_to(std::max<uint64_t>(rows, LEAST_ROWS) * up_to(cols, DEPTH) * 2 * (dtype == LT_F32 ? 3 : 1), 256); }
 // May the matrix be an operand where it lies?
 inline bool lies_well(int dtype, const void *p, uint64_t pitch) { return dtype == LT_BF16 && is_aligned(p, 16) && pitch % 8 == 0; }
 
@@ -998,12 +1114,24 @@ uint64_t piece_of(uint64_t rows, uint64_t bytes, uint64_t most) {
 // Addresses are not known when scratch is planned: bf16 rows whose distance fits lie well unless they begin in an unusual place, for
 // which there is some room, too.
 inline uint64_t pack_piece(const LtOperator &o, int k, uint64_t rows) {
-    return piece_of(rows, packed_bytes(o.dtype, 1, o.cols), o.dtype == LT_BF16 && o.pitch[k] % 8 == 0 ? SPARE_BYTES : PACK_BYTES);
+    return piece_of(rows, packed_row(o.dtype, o.cols), o.dtype == LT_BF16 && o.pitch[k] % 8 == 0 ? SPARE_BYTES : PACK_BYTES);
 }
 
-constexpr size_t FEW_BYTES = 72 << 10;  // of x: three blocks to an SM
-inline bool few_tokens(const LtOperator &o) { return o.rows <= FEW && o.rows * up_to(o.cols, 8) * (o.dtype == LT_BF16 ? 2 : 4) <= FEW_BYTES; }
-inline unsigned few_blocks(const LtOperator &o, int sm_count) { return (unsigned)std::min<uint64_t>(3ull * sm_count, count_of(o.vocabulary, FEW_THREADS / 32 * FEW_ROWS)); }
+// Tokens that are scored by plain loads, at a time (0: on the tensor cores), and by how many blocks.  bf16: up to two (one token against
+// 32000 rows of 4096: 46 us, two 47.5; three 57 so, 54 on the tensor cores).  f32, which takes six products there: up to 64, 16 at a time
+// (against 32000 rows of 2048: 5 tokens 54 us, 658 on the tensor cores; 16 88, 382; 64 331, 386).
+constexpr size_t FEW_BYTES = 72 << 10, SOME_BYTES = 208 << 10;  // of x in shared memory
+struct Few {
+    uint32_t at_once = 0, blocks = 0;
+    Few(const LtOperator &o, int sm_count) {
+        const uint64_t row = up_to(o.cols, 8) * (o.dtype == LT_BF16 ? 2 : 4);
+        if (o.rows > (o.dtype == LT_BF16 ? 2 : 64)) return;
+        at_once = o.rows <= 2 ? (uint32_t)o.rows : o.rows <= 4 ? 4 : o.rows <= 8 ? 8 : 16;
+        if (at_once * row > (at_once <= 2 ? FEW_BYTES : SOME_BYTES)) at_once = 0;
+        const uint32_t rows = at_once <= 2 ? FEW_THREADS / 32 * FEW_ROWS : SOME_THREADS / 32 * 4;
+        blocks = (uint32_t)std::min<uint64_t>((at_once <= 2 ? 3 : 1) * (uint64_t)sm_count, count_of(o.vocabulary, rows));
+    }
+};
 
 struct LossScratch {
     size_t score, odd_x, odd_table, tops, x, table, bytes;
@@ -1023,9 +1151,10 @@ struct LossScratch {
         score = 0;
         odd_x = up_to(o.rows * 4, 256);
         odd_table = odd_x + up_to(o.rows, 256);
-        tops = odd_table + up_to(piece, 256);
-        if (few_tokens(o)) {
-            bytes = tops + up_to(few_blocks(o, sm_count) * o.rows * sizeof(float2), 256);
+        tops = odd_table + up_to(piece + LEAST_ROWS, 256);
+        const Few few(o, sm_count);
+        if (few.at_once) {
+            bytes = tops + up_to(few.blocks * o.rows * sizeof(float2), 256);
             return;
         }
         x = tops + up_to(halves * o.rows * sizeof(float2), 256);
@@ -1048,10 +1177,10 @@ struct GradScratch {
         x = 0;
         odd_x = x + packed_bytes(o.dtype, o.rows, o.cols);
         odd_table = odd_x + up_to(o.rows, 256);
-        table = odd_table + up_to(piece, 256);
+        table = odd_table + up_to(piece + LEAST_ROWS, 256);
         splits_table = ct.splits;
         p = table + packed_bytes(o.dtype, packed_piece, o.cols);
-        sum_x = p + up_to(o.rows * piece * 2 * parts, 256);
+        sum_x = p + up_to(std::max<uint64_t>(o.rows, LEAST_ROWS) * piece * 2 * parts, 256);
         sum_table = sum_x + (packed_piece < o.vocabulary || cx.splits > 1 ? up_to(cx.splits * o.rows * o.cols * 4, 256) : 0);
         bytes = sum_table + (ct.splits > 1 ? up_to(ct.splits * piece * o.cols * 4, 256) : 0);
     }
@@ -1082,23 +1211,31 @@ void plain_args(const LtOperator &o, ProductArgs &a, const void *x, const void *
 template <class T, int N, int TOKENS>
 cudaError_t launch_few_of(const FewArgs &a, unsigned blocks, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(lt_loss_few<T, N, TOKENS>, FEW_BYTES, ready);
-    return e != cudaSuccess ? e : launch_pdl(lt_loss_few<T, N, TOKENS>, blocks, FEW_THREADS, TOKENS * up_to(a.cols, 8) * sizeof(T), stream, a);
+    const size_t bytes = TOKENS * up_to(a.cols, 8) * sizeof(T);
+    if constexpr (TOKENS <= 2) {
+        const cudaError_t e = allow_shared(lt_loss_few<T, N, TOKENS>, FEW_BYTES, ready);
+        return e != cudaSuccess ? e : launch_pdl(lt_loss_few<T, N, TOKENS>, blocks, FEW_THREADS, bytes, stream, a);
+    } else {
+        const cudaError_t e = allow_shared(lt_loss_some<T, N, TOKENS>, SOME_BYTES, ready);
+        return e != cudaSuccess ? e : launch_pdl_shared(lt_loss_some<T, N, TOKENS>, dim3(blocks, count_of(a.tokens, TOKENS)), SOME_THREADS, bytes, stream, a);
+    }
 }
 template <class T, int N>
-cudaError_t launch_few(const FewArgs &a, uint64_t tokens, unsigned blocks, cudaStream_t stream) {
-    static_assert(FEW == 4, "");
-    return tokens == 1 ? launch_few_of<T, N, 1>(a, blocks, stream)
-         : tokens == 2 ? launch_few_of<T, N, 2>(a, blocks, stream)
-         : tokens == 3 ? launch_few_of<T, N, 3>(a, blocks, stream)
-                       : launch_few_of<T, N, 4>(a, blocks, stream);
+cudaError_t launch_few(const FewArgs &a, const Few &few, cudaStream_t stream) {
+    if constexpr (sizeof(T) == 4) {
+        if (few.at_once == 16) return launch_few_of<T, N, 16>(a, few.blocks, stream);
+        if (few.at_once == 8) return launch_few_of<T, N, 8>(a, few.blocks, stream);
+        if (few.at_once == 4) return launch_few_of<T, N, 4>(a, few.blocks, stream);
+    }
+    return few.at_once == 1 ? launch_few_of<T, N, 1>(a, few.blocks, stream) : launch_few_of<T, N, 2>(a, few.blocks, stream);
 }
 
 template <class T>
 cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
     const LossScratch at(o, sm_count);
     char *room = (char *)o.scratch;
-    if (few_tokens(o)) {
+    const Few few(o, sm_count);
+    if (few.at_once) {
         ProductArgs a{};
         common_args(o, a);
         a.m = (uint32_t)o.rows;
@@ -1106,12 +1243,11 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
         a.tops = (float2 *)(room + at.tops);
         a.tops_pitch = a.m;
         constexpr int N = 16 / (int)sizeof(T);
-        const FewArgs f{o.in[0], o.in[1], a.targets, a.tops, a.target_score, o.pitch[0], o.pitch[1], a.vocabulary, (uint32_t)o.cols, a.scale2, a.bad_target};
+        const FewArgs f{o.in[0], o.in[1], a.targets, a.tops, a.target_score, o.pitch[0], o.pitch[1], a.m, a.vocabulary, (uint32_t)o.cols, a.scale2, a.bad_target};
         const bool wide = o.cols % N == 0 && o.pitch[1] % N == 0 && is_aligned(o.in[1], 16);
-        const unsigned blocks = few_blocks(o, sm_count);
-        const cudaError_t e = wide ? launch_few<T, N>(f, o.rows, blocks, stream) : launch_few<T, 1>(f, o.rows, blocks, stream);
+        const cudaError_t e = wide ? launch_few<T, N>(f, few, stream) : launch_few<T, 1>(f, few, stream);
         *launched = 2;
-        return e != cudaSuccess ? e : launch_join(a, blocks, (float *)o.out[0], (float *)o.out[1], stream);
+        return e != cudaSuccess ? e : launch_join(a, few.blocks, (float *)o.out[0], (float *)o.out[1], stream);
     }
     const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]), table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
     cudaError_t e = cudaSuccess;
@@ -1129,7 +1265,7 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
         a.tops_pitch = (uint32_t)o.rows;
         const T *tokens = (const T *)o.in[0] + r0 * o.pitch[0];
         Operand x{tokens, o.pitch[0], m, o.cols, 0, false};
-        if (!x_well) {
+        if (!x_well || m < LEAST_ROWS) {
             e = launch_pack<T>(tokens, o.pitch[0], m, o.cols, nullptr, 0, nullptr, room + at.x, room + at.odd_x, sm_count, stream);
             if (e != cudaSuccess) return e;
             x = packed_operand<T>(room + at.x, m, o.cols, false);
@@ -1206,11 +1342,12 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         a.p = (__nv_bfloat16 *)(room + at.p);
         a.p_pitch = padded * parts;
         a.p_part = (uint32_t)padded;
+        a.p_rows = (uint32_t)std::max<uint64_t>(o.rows, LEAST_ROWS);
         plain_args(o, a, o.in[0], room + at.odd_x, room + at.odd_table, rows);
         e = launch_product<false, false, TO_P, PARTS>(packed_operand<T>(room + at.x, o.rows, o.cols, false), table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
         if (e != cudaSuccess) return e;
         ++*launched;
-        Operand p{a.p, padded * parts, o.rows, padded * parts, (uint32_t)padded, false};
+        Operand p{a.p, padded * parts, a.p_rows, padded * parts, (uint32_t)padded, false};
         if (o.out[0]) {
             ProductArgs d{};
             common_args(o, d);
