@@ -357,6 +357,87 @@ def test_vocabulary_loss_gradient_against_differences(ctx):  # noqa: F811
     assert abs((up - down) / (2 * h) - want) < 60 * h * h * 40 ** 3 + 1000 * ULP * size
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 8, 9, 15, 16, 17, 33, 64, 65, 128])
+@pytest.mark.parametrize("vocab,cols", [(3, 64), (1003, 264), (5003, 72), (777, 33)])
+def test_vocabulary_loss_of_few_tokens(ctx, dtype, tokens, vocab, cols):  # noqa: F811
+    g, t = gen(tokens + vocab), TYPES[dtype]
+    x, table, ids = normal(g, tokens, cols, dtype=t, std=2.0), normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab)
+    ids[-1] = vocab - 1
+    if tokens > 2:
+        ids[1] = -3
+    check_loss(ctx, x, table, ids, scale=1.5, dloss=normal(g, tokens))
+
+
+def test_few_infinite_scores(ctx):  # noqa: F811
+    """As in test_infinite_scores, for each way in which few and many tokens are scored."""
+    g = gen(24)
+    for tokens in (1, 4, 7, 16, 70, 200):
+        x, table = normal(g, tokens, 24).abs() + 0.5, normal(g, 900, 24)
+        table[[0, 255, 256, 700, 899]] = -math.inf
+        ids = torch.full((tokens,), 300, dtype=torch.int32, device="cuda")
+        keep = torch.isfinite(table[:, 0])
+        loss, lse = (fetch(ctx, r) for r in ctx.vocabulary_loss(ctx.from_torch(x), ctx.from_torch(table), ctx.from_torch(ids)))
+        a, b, c, d = ref.loss(x, table[keep], ids - 3)
+        close(loss, a, b)
+        close(lse, c, d)
+        table[300] = math.inf  # the target itself: everything else vanishes beside it
+        loss, lse = (fetch(ctx, r) for r in ctx.vocabulary_loss(ctx.from_torch(x), ctx.from_torch(table), ctx.from_torch(ids)))
+        assert bool((lse == math.inf).all()) and bool(torch.isnan(loss).all())
+        x[-1, 3] = math.nan
+        lse = fetch(ctx, ctx.vocabulary_loss(ctx.from_torch(x), ctx.from_torch(table), ctx.from_torch(ids))[1])
+        assert bool(torch.isnan(lse[-1])) and bool((lse[:-1] == math.inf).all())
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab,cols,where", [("f32", 70, 3, 8210, None), ("f32", 300, 20011, 1000, None), ("bf16", 300, 5001, 1000, "table"), ("bf16", 4500, 300, 1000, "x"),
+                                                           ("bf16", 5, 40, 8210, "table")])
+def test_vocabulary_loss_in_pieces(ctx, dtype, tokens, vocab, cols, where):  # noqa: F811
+    """More than one piece of a packed table, of packed tokens, and long rows; bf16 rows are packed where they begin at odd places."""
+    g, t = gen(tokens), TYPES[dtype]
+    x, table, ids, d = normal(g, tokens, cols, dtype=t), normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab), normal(g, tokens)
+    ids[::5] = -1
+    lx, lw = (unaligned(ctx, v, dtype) if where == n else ctx.from_torch(v) for n, v in (("x", x), ("table", table)))
+    loss, lse = ctx.vocabulary_loss(lx, lw, ctx.from_torch(ids))
+    dx, dw = ctx.vocabulary_loss_grad(lx, lw, ctx.from_torch(ids), lse, ctx.from_torch(d))
+    a, b, c, e = ref.loss(x, table, ids)
+    got = fetch(ctx, lse)
+    close(got, c, e)
+    close(fetch(ctx, loss), a, b)
+    a, b, c, e = ref.loss_grad(x, table, ids, got, d)
+    close(fetch(ctx, dx), a, b)
+    close(fetch(ctx, dw), c, e)
+
+
+@pytest.fixture()
+def on_the_gpu(monkeypatch):
+    monkeypatch.setattr(ref, "WHERE", ["cuda"])
+
+
+def test_vocabulary_loss_of_so_many_scores_that_p_is_made_in_pieces(ctx, on_the_gpu):  # noqa: F811
+    g, t = gen(25), torch.bfloat16
+    x, table, ids, d = normal(g, 9001, 72, dtype=t), normal(g, 20001, 72, dtype=t, std=0.1), tokens_of(g, 9001, 20001), normal(g, 9001)
+    ids[::5] = -1
+    check_loss(ctx, x, table, ids, dloss=d)
+
+
+@pytest.mark.parametrize("tokens,vocab,cols,tied", [(20000, 3000, 1032, True), (20000, 300, 2056, False), (40001, 5000, 2048, True), (70001, 40, 1024, False)])
+def test_embedding_grad_of_large_windows(ctx, on_the_gpu, tokens, vocab, cols, tied):  # noqa: F811
+    """So many tokens that windows of 16, 32 and 64 of them are summed, and that they are sorted in several steps."""
+    g, t = gen(tokens), torch.bfloat16
+    dy, ids = normal(g, tokens, cols, dtype=t), tokens_of(g, tokens, vocab)
+    ids[:: 7] = -1
+    check_grad(ctx, dy, ids, vocab, normal(g, vocab, cols, dtype=t) if tied else None)
+
+
+@pytest.mark.parametrize("tokens", [33000, 100000])
+def test_embedding_grad_where_one_token_is_most_of_them(ctx, on_the_gpu, tokens):  # noqa: F811
+    g = gen(tokens)
+    dy, ids = normal(g, tokens, 40), tokens_of(g, tokens, 1000)
+    ids[torch.rand(tokens, generator=g, device="cuda") < 0.6] = 128 * 3 + 5
+    ids[torch.rand(tokens, generator=g, device="cuda") < 0.1] = 128 * 4 + 5  # (of the same class)
+    check_grad(ctx, dy, ids, 1000)
+
+
 # ------------------------------------------------------------------------------------------------ together, on streams, captured
 def step(c, t, out):
     """Both ends of a model on one table: lookup, (a norm stands for the model), loss, gradients, all into the table's."""
