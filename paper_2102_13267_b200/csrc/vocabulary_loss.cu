@@ -1,15 +1,17 @@
 // The cross entropy of hidden states against a table of rows, and its gradient, without keeping the scores.
 //
 // z = scale x table^T [tokens, vocabulary]; lse_n = log sum_v exp z_nv; loss_n = lse_n - z[n, target_n].
-// P = scale dloss_n (exp(z - lse_n) - [v = target_n]); dx = P table; dtable = P^T x.
+// P = exp(z - lse_n) - [v = target_n], 0 for tokens without a target; dx = scale dloss_n P table; dtable = P^T (scale dloss_n x).
 //
 // Three matrix products, one kernel (lt_product) that differs in how its operands lie and in what it does with a tile of the
 // result.  Scores never reach memory: the loss keeps of each tile the rows' maxima and sums of exponentials, which
 // lt_loss_join adds up in the tiles' order.  The gradient makes P for a piece of the vocabulary at a time, in bf16, and
 // multiplies it from both sides while it is in the L2 cache.
 //
-// Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value, as much as storing
-// the gradients costs).  f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
+// Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value at most, as much as storing
+// the gradients costs; P is near -1 at most targets and rounded little there, which it would not be with dloss in it).  So is x dloss_n where dloss
+// differs from token to token: it is divided by that of the first tokens and dtable multiplied by it, and stays x where they are all alike.
+//  f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
 // parts the six largest are added: what is left out is below 2^-23 of each product.
 #include <algorithm>
 
@@ -51,7 +53,7 @@ struct ProductArgs {
     uint32_t tops_pitch;
     float *target_score;        // [tokens], base two
     uint32_t first, first_tile, vocabulary;  // of the table's row that column 0 of the result is: its number, and that of its tile's first half
-    const float *lse, *dloss;
+    const float *lse;
     __nv_bfloat16 *p;
     uint64_t p_pitch;
     uint32_t p_part, p_rows;    // p_rows: those that are written, zeros behind the tokens
@@ -60,6 +62,7 @@ struct ProductArgs {
     uint64_t plain_pitch_a, plain_pitch_b;
     uint32_t plain_cols;
     // TO_SUM, TO_F32, TO_BF16
+    const float *factors, *unit;  // of each row, or of all
     const float *before;        // [m][n] to be added, or null
     void *out;                  // [m][n]; TO_SUM: [splits][m][n]
     int wide;                   // columns of `out` come in fours (4) or eights (8), aligned as such
@@ -200,12 +203,11 @@ struct Epilogue<TO_P, PARTS> {
     unsigned char *room;
     uint32_t row0, row;
     int target;
-    float lse2, factor;
+    float lse2;
     __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &, uint32_t row_, unsigned char *room_) : a(a_), room(room_), row0(row_), row(row_ + (threadIdx.x & 31)) {
         target = row < a.m ? a.targets[row] : -1;
         if ((uint32_t)target >= a.vocabulary) target = -1;
         lse2 = target >= 0 ? a.lse[row] * 1.44269504f : 0.f;
-        factor = target >= 0 ? a.dloss[row] * a.scale : 0.f;
     }
     __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
         if (col >= a.p_part) return;
@@ -215,7 +217,7 @@ struct Epilogue<TO_P, PARTS> {
             float e;
             asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(f[i], a.scale2, -lse2)));
             if (at == (uint32_t)i) e -= 1.f;
-            f[i] = target >= 0 && col + i < a.n ? e * factor : 0.f;
+            f[i] = target >= 0 && col + i < a.n ? e : 0.f;
         }
         if constexpr (PARTS == 1) {  // (columns come in 64s)
             const uint32_t half = col >> 5 & 1;
@@ -249,9 +251,15 @@ struct Epilogue {
     unsigned char *room;
     uint32_t row0;
     uint64_t first;  // of the split's result
+    float factor;
     __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_, unsigned char *room_)
-        : a(a_), room(room_), row0(row_), first(TO == TO_SUM ? (uint64_t)t.split * a_.m * a_.n : 0) {}
+        : a(a_), room(room_), row0(row_), first(TO == TO_SUM ? (uint64_t)t.split * a_.m * a_.n : 0) {
+        const uint32_t row = row0 + (threadIdx.x & 31);
+        factor = !a.factors ? *a.unit : row < a.m ? a.factors[row] : 0.f;
+    }
     __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) f[i] = factor == 0.f ? 0.f : f[i] * factor;  // (rows of tokens without a target: zeros, whatever the table holds)
         if (TO == TO_BF16 && a.wide == 8 && !a.before) {
             const uint32_t half = col >> 5 & 1;
             if (col - 32 * half >= a.n || row0 >= a.m) return;
@@ -851,12 +859,61 @@ __global__ void __launch_bounds__(SOME_THREADS, 1) lt_loss_some(const FewArgs a)
 struct PackArgs {
     const void *from;
     uint64_t pitch;
-    const int *targets;         // rows without one become zeros; or null
-    __nv_bfloat16 *to;          // [rows][parts][padded]
+    __nv_bfloat16 *to;          // [rows][parts][padded]; or null
     uint8_t *odd;               // three parts: 1 for rows with infinities, 2 for rows with what is no number
-    uint32_t rows, present, cols, padded, vocabulary;  // present: rows that there are; zeros behind them
+    uint32_t rows, present, cols, padded;  // present: rows that there are; zeros behind them
+    // x for the gradient of the table: `scaled`, rows without a target zeros, the others times dloss / unit; rows' factors scale dloss
+    __nv_bfloat16 *scaled;
+    const int *targets;
+    const float *dloss;
+    float *factors, *unit;      // *unit: times scale
+    float scale;
+    uint32_t vocabulary;
     unsigned int *bad_target;
 };
+
+// |dloss| of the first of the first thousand tokens that has a target and a dloss of ordinary size; 1 if there is none. By a whole block.
+__device__ __forceinline__ float unit_of(const PackArgs &a) {
+    __shared__ uint32_t first;
+    if (threadIdx.x == 0) first = 0xffffffffu;
+    __syncthreads();
+    for (uint32_t n = threadIdx.x; n < min(a.present, 1024u); n += blockDim.x) {
+        const float d = fabsf(a.dloss[n]);
+        if ((uint32_t)a.targets[n] < a.vocabulary && d >= 0x1p-60f && d <= 0x1p60f) {
+            atomicMin(&first, n);
+            break;
+        }
+    }
+    __syncthreads();
+    return first == 0xffffffffu ? 1.f : fabsf(a.dloss[first]);
+}
+
+// Eight values in bf16 parts; returns what is not finite among them (1: infinities, 2: no numbers).
+template <int PARTS>
+__device__ __forceinline__ int pack_eight(float (&f)[8], uint4 *to, uint32_t apart) {
+    int odd = 0;
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __nv_bfloat16 h = __float2bfloat16_rn(f[i]);
+            if constexpr (PARTS == 3) {
+                if (part == 0) {
+                    if (!(fabsf(f[i]) <= 3.38953139e38f)) {  // (the largest bf16)
+                        odd |= isinf(f[i]) ? 1 : isnan(f[i]) ? 2 : 0;
+                        if (!isinf(f[i])) h = __float2bfloat16_rz(f[i]);  // (the nearest might be infinite)
+                    }
+                }
+                f[i] = isfinite(f[i]) ? f[i] - __bfloat162float(h) : 0.f;
+            }
+            const uint32_t bits = __bfloat16_as_ushort(h);
+            w[i / 2] = i & 1 ? w[i / 2] | bits << 16 : bits;
+        }
+        to[part * apart] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return odd;
+}
 
 // A matrix as the products take it: bf16, in three parts if it is f32, rows padded with zeros to whole steps of K.  A thread has eight
 // columns at a time, ACROSS threads (a warp, or the block where rows are long) a row.
@@ -867,23 +924,35 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
     pdl_release();
     pdl_wait();
     const uint32_t eights = a.padded / 8, lane = threadIdx.x % ACROSS;
+    float unit = 1.f;
+    if (a.scaled) {
+        unit = unit_of(a);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.unit = unit * a.scale;
+    }
     for (uint32_t r = blockIdx.x * BESIDE + threadIdx.x / ACROSS; r < a.rows; r += gridDim.x * BESIDE) {
-        bool there = r < a.present;
-        if (a.targets && there) {
+        const bool there = r < a.present;
+        float factor = 0.f;
+        bool counts = true;
+        if (a.scaled && there) {
             const int target = a.targets[r];
-            there = (uint32_t)target < a.vocabulary;
-            if (!there && target >= 0 && lane == 0) report(a.bad_target);
+            counts = (uint32_t)target < a.vocabulary;
+            const float d = counts ? a.dloss[r] : 0.f;
+            factor = d / unit;
+            if (lane == 0) {
+                if (!counts && target >= 0) report(a.bad_target);
+                a.factors[r] = d * a.scale;
+            }
         }
         const T *from = (const T *)a.from + r * a.pitch;
-        uint4 *to = reinterpret_cast<uint4 *>(a.to + (uint64_t)r * PARTS * a.padded);
+        uint4 *to = reinterpret_cast<uint4 *>(a.to + (uint64_t)r * PARTS * a.padded), *scaled = reinterpret_cast<uint4 *>(a.scaled + (uint64_t)r * PARTS * a.padded);
         int odd = 0;
 #pragma unroll 2
         for (uint32_t c = lane; c < eights; c += ACROSS) {
             float f[8];
             if (WIDE && there && 8 * c + 8 <= a.cols) {
                 if constexpr (PARTS == 1) {
-                    to[c] = reinterpret_cast<const uint4 *>(from)[c];
-                    continue;
+                    const uint4 v = reinterpret_cast<const uint4 *>(from)[c];
+                    unpack(v, f);
                 } else {
                     float g[4];
 #pragma unroll
@@ -897,28 +966,15 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = there && 8 * c + i < a.cols ? to_float(from[8 * c + i]) : 0.f;
             }
+            if (a.scaled) {
+                float x[8];
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    __nv_bfloat16 h = __float2bfloat16_rn(f[i]);
-                    if constexpr (PARTS == 3) {
-                        if (part == 0) {
-                            if (!(fabsf(f[i]) <= 3.38953139e38f)) {  // (the largest bf16)
-                                odd |= isinf(f[i]) ? 1 : isnan(f[i]) ? 2 : 0;
-                                if (!isinf(f[i])) h = __float2bfloat16_rz(f[i]);  // (the nearest might be infinite)
-                            }
-                        }
-                        f[i] = isfinite(f[i]) ? f[i] - __bfloat162float(h) : 0.f;
-                    }
-                    const uint32_t bits = __bfloat16_as_ushort(h);
-                    w[i / 2] = i & 1 ? w[i / 2] | bits << 16 : bits;
-                }
-                to[part * eights + c] = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int i = 0; i < 8; ++i) x[i] = factor == 0.f ? 0.f : f[i] * factor;
+                pack_eight<PARTS>(x, scaled + c, eights);
             }
+            if (a.to) odd |= pack_eight<PARTS>(f, to + c, eights);
         }
-        if constexpr (PARTS == 3) {
+        if (PARTS == 3 && a.to) {
             int infinite, no_number;
             if constexpr (ACROSS == 32) {
                 __syncwarp();
@@ -926,7 +982,7 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
             } else {
                 no_number = __syncthreads_or(odd & 2), infinite = __syncthreads_or(odd & 1);
             }
-            if (lane == 0) a.odd[r] = no_number ? 2 : infinite ? 1 : 0;
+            if (lane == 0) a.odd[r] = !counts ? 0 : no_number ? 2 : infinite ? 1 : 0;  // (what does not count is not looked at)
         }
     }
 }
@@ -1070,21 +1126,20 @@ constexpr uint64_t LEAST_ROWS = 16;
 template <class T>
 constexpr uint32_t parts_of() { return sizeof(T) == 4 ? 3 : 1; }
 
+// The gradient's part of PackArgs
+struct Scaled {
+    void *to = nullptr;
+    const int *targets = nullptr;
+    const float *dloss = nullptr;
+    float *factors = nullptr, *unit = nullptr;
+    float scale = 1.f;
+    uint32_t vocabulary = 0;
+    unsigned int *bad_target = nullptr;
+};
 template <class T>
-cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_t cols, const int *targets, uint32_t vocabulary, unsigned int *bad_target, void *to, void *odd, int sm_count,
-                        cudaStream_t stream) {
-    PackArgs p{};
-    p.from = from;
-    p.pitch = pitch;
-    p.targets = targets;
-    p.to = (__nv_bfloat16 *)to;
-    p.odd = sizeof(T) == 4 ? (uint8_t *)odd : nullptr;
-    p.rows = (uint32_t)std::max<uint64_t>(rows, LEAST_ROWS);
-    p.present = (uint32_t)rows;
-    p.cols = (uint32_t)cols;
-    p.padded = (uint32_t)up_to(cols, DEPTH);
-    p.vocabulary = vocabulary;
-    p.bad_target = bad_target;
+cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_t cols, void *to, void *odd, const Scaled &scaled, int sm_count, cudaStream_t stream) {
+    const PackArgs p{from,          pitch,           (__nv_bfloat16 *)to, (uint8_t *)odd, (uint32_t)std::max<uint64_t>(rows, LEAST_ROWS), (uint32_t)rows, (uint32_t)cols, (uint32_t)up_to(cols, DEPTH),
+                     (__nv_bfloat16 *)scaled.to, scaled.targets,  scaled.dloss,        scaled.factors, scaled.unit, scaled.scale, scaled.vocabulary, scaled.bad_target};
     const bool wide = is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0, long_rows = p.padded > 8192 || (p.padded >= 512 && rows < 8 * (uint64_t)sm_count);
     const unsigned grid = std::min(count_of(p.rows, long_rows ? 1 : 8), (unsigned)sm_count * 8);
     if (long_rows) return wide ? launch_pdl(lt_loss_pack<T, true, 256>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 256>, grid, 256, (size_t)0, stream, p);
@@ -1150,7 +1205,7 @@ struct LossScratch {
         }
         score = 0;
         odd_x = up_to(o.rows * 4, 256);
-        odd_table = odd_x + up_to(o.rows, 256);
+        odd_table = odd_x + up_to(o.rows + LEAST_ROWS, 256);
         tops = odd_table + up_to(piece + LEAST_ROWS, 256);
         const Few few(o, sm_count);
         if (few.at_once) {
@@ -1164,7 +1219,7 @@ struct LossScratch {
 };
 
 struct GradScratch {
-    size_t x, odd_x, odd_table, table, p, sum_x, sum_table, bytes;
+    size_t unit, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, bytes;
     uint64_t piece, packed_piece;  // the latter where the table does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
@@ -1174,9 +1229,12 @@ struct GradScratch {
         if (o.dtype == LT_F32 || o.pitch[1] % 8) piece = packed_piece;
         const uint64_t steps = count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), steps_t = count_of(o.rows, DEPTH) * (parts == 1 ? 1 : 6);
         const Cut cx = Cut(o.rows, o.cols, sm_count, 0).split(steps, sm_count), ct = Cut(piece, o.cols, sm_count, 0).split(steps_t, sm_count);
-        x = 0;
+        unit = 0;
+        factors = 256;
+        scaled = factors + up_to(o.rows * 4, 256);
+        x = scaled + packed_bytes(o.dtype, o.rows, o.cols);
         odd_x = x + packed_bytes(o.dtype, o.rows, o.cols);
-        odd_table = odd_x + up_to(o.rows, 256);
+        odd_table = odd_x + up_to(o.rows + LEAST_ROWS, 256);
         table = odd_table + up_to(piece + LEAST_ROWS, 256);
         splits_table = ct.splits;
         p = table + packed_bytes(o.dtype, packed_piece, o.cols);
@@ -1266,7 +1324,7 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
         const T *tokens = (const T *)o.in[0] + r0 * o.pitch[0];
         Operand x{tokens, o.pitch[0], m, o.cols, 0, false};
         if (!x_well || m < LEAST_ROWS) {
-            e = launch_pack<T>(tokens, o.pitch[0], m, o.cols, nullptr, 0, nullptr, room + at.x, room + at.odd_x, sm_count, stream);
+            e = launch_pack<T>(tokens, o.pitch[0], m, o.cols, room + at.x, room + at.odd_x, Scaled{}, sm_count, stream);
             if (e != cudaSuccess) return e;
             x = packed_operand<T>(room + at.x, m, o.cols, false);
             ++*launched;
@@ -1276,7 +1334,7 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
             const T *rows = (const T *)o.in[1] + v0 * o.pitch[1];
             Operand table{rows, o.pitch[1], n, o.cols, 0, false};
             if (!table_well) {
-                e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+                e = launch_pack<T>(rows, o.pitch[1], n, o.cols, room + at.table, room + at.odd_table, Scaled{}, sm_count, stream);
                 if (e != cudaSuccess) return e;
                 table = packed_operand<T>(room + at.table, n, o.cols, false);
                 ++*launched;
@@ -1316,8 +1374,12 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
     char *room = (char *)o.scratch;
     const bool table_well = lies_well(o.dtype, o.in[1], o.pitch[1]);
     const uint64_t parts = parts_of<T>();
-    // (x always: rows without a target, which may hold anything, are left out of the table's gradient)
-    cudaError_t e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, (const int *)o.in[2], (uint32_t)o.vocabulary, &o.status->loss, room + at.x, room + at.odd_x, sm_count, stream);
+    float *factors = (float *)(room + at.factors), *unit = (float *)(room + at.unit);
+    // (x is scaled and rows without a target, which may hold anything, left out for the gradient of the table alone)
+    const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]) && o.rows >= LEAST_ROWS;
+    const Scaled scaled{room + at.scaled, (const int *)o.in[2], (const float *)o.in[4], factors, unit, (float)lt_attr_double(o.attr[1]), (uint32_t)o.vocabulary, &o.status->loss};
+    cudaError_t e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, x_well ? nullptr : room + at.x, room + at.odd_x, scaled, sm_count, stream);
+    const Operand x = x_well ? Operand{o.in[0], o.pitch[0], o.rows, o.cols, 0, false} : packed_operand<T>(room + at.x, o.rows, o.cols, false);
     *launched = 1;
     const uint64_t piece = table_well ? at.piece : at.packed_piece;
     for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
@@ -1326,7 +1388,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         const void *rows = (const T *)o.in[1] + v0 * o.pitch[1];
         Operand table{rows, o.pitch[1], n, o.cols, 0, false};
         if (!table_well) {
-            e = launch_pack<T>(rows, o.pitch[1], n, o.cols, nullptr, 0, nullptr, room + at.table, room + at.odd_table, sm_count, stream);
+            e = launch_pack<T>(rows, o.pitch[1], n, o.cols, room + at.table, room + at.odd_table, Scaled{}, sm_count, stream);
             if (e != cudaSuccess) return e;
             table = packed_operand<T>(room + at.table, n, o.cols, false);
             ++*launched;
@@ -1338,13 +1400,12 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         a.blocks_k = count_of(o.cols, DEPTH);
         a.first = (uint32_t)v0;
         a.lse = (const float *)o.in[3];
-        a.dloss = (const float *)o.in[4];
         a.p = (__nv_bfloat16 *)(room + at.p);
         a.p_pitch = padded * parts;
         a.p_part = (uint32_t)padded;
         a.p_rows = (uint32_t)std::max<uint64_t>(o.rows, LEAST_ROWS);
         plain_args(o, a, o.in[0], room + at.odd_x, room + at.odd_table, rows);
-        e = launch_product<false, false, TO_P, PARTS>(packed_operand<T>(room + at.x, o.rows, o.cols, false), table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
+        e = launch_product<false, false, TO_P, PARTS>(x, table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
         if (e != cudaSuccess) return e;
         ++*launched;
         Operand p{a.p, padded * parts, a.p_rows, padded * parts, (uint32_t)padded, false};
@@ -1354,6 +1415,7 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             d.m = (uint32_t)o.rows;
             d.n = (uint32_t)o.cols;
             d.blocks_k = count_of(n, DEPTH);
+            d.factors = factors;
             // (as many splits for every piece, the last and shorter one too)
             const Cut cut = Cut(o.rows, o.cols, sm_count, 0).split(count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), sm_count);
             float *sum = (float *)(room + at.sum_x);
@@ -1382,19 +1444,20 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
             d.m = (uint32_t)n;
             d.n = (uint32_t)o.cols;
             d.blocks_k = count_of(o.rows, DEPTH);
+            d.unit = unit;
             Cut cut = Cut(n, o.cols, sm_count, 0).split(d.blocks_k * (parts == 1 ? 1 : 6), sm_count);
             cut.splits = std::min(cut.splits, at.splits_table);  // (the last piece is shorter: what the scratch memory holds)
             void *out = (T *)o.out[1] + v0 * o.cols;
             p.turned = true;
-            const Operand x = packed_operand<T>(room + at.x, o.rows, o.cols, true);
+            const Operand scaled_x = packed_operand<T>(room + at.scaled, o.rows, o.cols, true);
             if (cut.splits == 1) {
                 d.out = out;
                 d.wide = width_of(out, o.cols, sizeof(T));
-                e = launch_product<true, true, TO_T, PARTS>(p, x, d, cut, sm_count, stream);
+                e = launch_product<true, true, TO_T, PARTS>(p, scaled_x, d, cut, sm_count, stream);
             } else {
                 d.out = room + at.sum_table;
                 d.wide = width_of(d.out, o.cols, 4);
-                e = launch_product<true, true, TO_SUM, PARTS>(p, x, d, cut, sm_count, stream);
+                e = launch_product<true, true, TO_SUM, PARTS>(p, scaled_x, d, cut, sm_count, stream);
                 if (e == cudaSuccess) e = launch_sum<T>((const float *)d.out, out, n * o.cols, cut.splits, sm_count, stream);
                 ++*launched;
             }

@@ -55,7 +55,7 @@ def loss(x, table, targets, scale=1.0):
 
 
 def loss_grad(x, table, targets, lse, dloss, scale=1.0):
-    """(dx, bound, dtable, bound): for bf16, P goes into the products rounded to bf16; for f32 as three parts."""
+    """(dx, bound, dtable, bound): for bf16, P and x dloss go into the products rounded to bf16; for f32 as three parts."""
     z, dz = _scores(x, table, scale)
     t = targets.to(WHERE[0]).long().flatten()
     there = (t >= 0) & (t < table.shape[0])
@@ -71,5 +71,6 @@ def loss_grad(x, table, targets, lse, dloss, scale=1.0):
     x64, w = torch.where(there[:, None], _64(x).reshape(-1, x.shape[-1]), 0.0), _64(table)
     n, v = p.shape
     dx, dtable = p @ w, p.T @ x64
+    more = p.abs().T @ x64.abs() * (HALF[torch.bfloat16] if x.dtype == torch.bfloat16 else 4 * ULP)
     return (dx, dp @ w.abs() + 2 * (v + 64) * ULP * (p.abs() @ w.abs()) + dx.abs() * HALF[x.dtype] + TINY,
-            dtable, dp.T @ x64.abs() + 2 * (n + 64) * ULP * (p.abs().T @ x64.abs()) + dtable.abs() * HALF[x.dtype] + TINY)
+            dtable, dp.T @ x64.abs() + more + 2 * (n + 64) * ULP * (p.abs().T @ x64.abs()) + dtable.abs() * HALF[x.dtype] + TINY)
