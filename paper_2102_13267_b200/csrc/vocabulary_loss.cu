@@ -38,7 +38,7 @@ struct Ring {
     static constexpr uint32_t BYTES = STAGES * STAGE + TAKERS * 32 * 128 + 1024;  // (to begin on a multiple of 1024)
 };
 
-enum { TO_LOSS, TO_P, TO_SUM, TO_F32, TO_BF16 };
+enum { TO_LOSS, TO_P, TO_SUM, TO_F32, TO_BF16, TO_SCORES };  // TO_SUM, TO_SCORES: binary32, each split its own
 
 struct ProductArgs {
     uint32_t m, n;              // of the result
@@ -253,13 +253,13 @@ struct Epilogue {
     uint64_t first;  // of the split's result
     float factor;
     __device__ __forceinline__ Epilogue(const ProductArgs &a_, const Tile &t, uint32_t row_, unsigned char *room_)
-        : a(a_), room(room_), row0(row_), first(TO == TO_SUM ? (uint64_t)t.split * a_.m * a_.n : 0) {
+        : a(a_), room(room_), row0(row_), first(TO == TO_SUM || TO == TO_SCORES ? (uint64_t)t.split * a_.m * a_.n : 0), factor(1.f) {
         const uint32_t row = row0 + (threadIdx.x & 31);
-        factor = !a.factors ? *a.unit : row < a.m ? a.factors[row] : 0.f;
+        if (TO != TO_SCORES) factor = !a.factors ? *a.unit : row < a.m ? a.factors[row] : 0.f;
     }
     __device__ __forceinline__ void take(float (&f)[32], uint32_t col) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = factor == 0.f ? 0.f : f[i] * factor;  // (rows of tokens without a target: zeros, whatever the table holds)
+        for (int i = 0; i < 32 && TO != TO_SCORES; ++i) f[i] = factor == 0.f ? 0.f : f[i] * factor;  // (rows of tokens without a target: zeros, whatever the table holds)
         if (TO == TO_BF16 && a.wide == 8 && !a.before) {
             const uint32_t half = col >> 5 & 1;
             if (col - 32 * half >= a.n || row0 >= a.m) return;
@@ -348,7 +348,7 @@ __device__ __forceinline__ void mend_scores(const ProductArgs &a, const Odd &o, 
 // direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, exact_steps steps of K at a time are
 // summed in tensor memory (0: all of them) and those sums added up in registers, by the warps that take them.  Of the six products
 // of parts the first five are 2^-8 of the last one or less, and so is what is cut off them: they are summed in one go.
-__host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts) { return parts == 3 ? 8 : to != TO_LOSS ? 0 : blocks == 1 ? 4 : 16; }
+__host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts) { return parts == 3 ? 8 : to != TO_LOSS && to != TO_SCORES ? 0 : blocks == 1 ? 4 : 16; }
 template <int PARTS, uint32_t STEPS>
 __device__ __forceinline__ uint32_t chunk_end(const ProductArgs &a, uint32_t step, uint32_t k1) {
     if constexpr (STEPS == 0) return k1;
@@ -641,6 +641,63 @@ cudaError_t launch_join(const ProductArgs &a, uint32_t tiles, float *loss, float
     const float *score = a.target_score;
     if (a.m <= 64) return launch_pdl(lt_loss_join<1>, a.m, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, a.tops_pitch, tiles, a.vocabulary);
     return launch_pdl(lt_loss_join<8>, (a.m + 7) / 8, 256, (size_t)0, stream, tops, score, a.targets, loss, lse, a.m, a.tops_pitch, tiles, a.vocabulary);
+}
+
+// Few scores: one tile after the other would leave most of the GPU idle for the length of K, so that several workers have a tile, for a
+// part of K each, and leave sums of scores (see cut_of_scores).  A block adds up those of a token, and makes its loss and
+// lse, or its row of P, of them.
+template <bool GRAD, int PARTS>
+__global__ void __launch_bounds__(256) lt_loss_finish(const ProductArgs a, const float *scores, uint32_t splits, float *loss, float *lse) {
+    __shared__ float2 sums[8];
+    __shared__ float at_target;
+    pdl_release();
+    pdl_wait();
+    const uint32_t row = blockIdx.x;
+    const bool there = row < a.m;
+    int target = there ? a.targets[row] : -1;
+    if (!GRAD && target >= 0 && (uint32_t)target >= a.vocabulary && threadIdx.x == 0) report(a.bad_target);
+    if ((uint32_t)target >= a.vocabulary) target = -1;
+    auto score = [&](uint32_t c) {
+        float z = 0.f;
+        const float *from = scores + (uint64_t)row * a.n + c;
+#pragma unroll 8
+        for (uint32_t k = 0; k < splits; ++k) z += from[(uint64_t)k * a.m * a.n];
+        if constexpr (PARTS == 3) {
+            const int odd = a.odd_a[row], other = a.odd_b[c];
+            if (odd | other) z = odd == 2 || other == 2 ? NAN : score_of(a, row, c);
+        }
+        return z * a.scale2;
+    };
+    if constexpr (GRAD) {
+        const float lse2 = target >= 0 ? a.lse[row] * 1.44269504f : 0.f;
+        __nv_bfloat16 *to = a.p + (uint64_t)row * a.p_pitch;
+        for (uint32_t c = threadIdx.x; c < a.p_part; c += 256) {
+            float v = 0.f;
+            if (target >= 0 && c < a.n) v = exp2f(score(c) - lse2) - (a.first + c == (uint32_t)target ? 1.f : 0.f);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                const __nv_bfloat16 h = __float2bfloat16_rn(v);
+                to[part * a.p_part + c] = h;
+                v -= __bfloat162float(h);
+            }
+        }
+    } else {
+        float2 s = make_float2(-INFINITY, 0.f);
+        for (uint32_t c = threadIdx.x; c < a.n; c += 256) {
+            const float z = score(c);
+            if ((int)c == target) at_target = z;
+            s = joined(s, make_float2(z, 1.f));
+        }
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) s = joined(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, d), __shfl_xor_sync(0xffffffffu, s.y, d)));
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+        __syncthreads();
+        if (threadIdx.x) return;
+        for (int k = 1; k < 8; ++k) s = joined(s, sums[k]);
+        const float l = fabsf(s.x) == INFINITY ? 0.f : log2f(s.y);
+        if (lse) lse[row] = (s.x + l) * 0.693147181f;
+        if (loss) loss[row] = target >= 0 ? ((s.x - at_target) + l) * 0.693147181f : 0.f;
+    }
 }
 
 // ------------------------------------------------------------------------------------------- few tokens
@@ -1015,6 +1072,8 @@ __global__ void __launch_bounds__(256) lt_loss_sum(const float *sums, R *out, ui
 // ------------------------------------------------------------------------------------------- host
 
 inline bool is_aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+// How many columns of a result can be stored at once: 8, 4 or 0 (one)
+inline int width_of(const void *out, uint64_t cols, size_t size) { return size == 2 && cols % 8 == 0 && is_aligned(out, 16) ? 8 : cols % 4 == 0 && is_aligned(out, 4 * size) ? 4 : 0; }
 inline uint64_t up_to(uint64_t n, uint64_t of) { return (n + of - 1) / of * of; }
 inline uint32_t count_of(uint64_t n, uint64_t of) { return (uint32_t)((n + of - 1) / of); }
 
@@ -1123,6 +1182,16 @@ cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, co
 // us, 16 of them 51).
 constexpr uint64_t LEAST_ROWS = 16;
 
+// How the scores of m tokens and n rows are cut: a worker to a tile and no scores in memory, or, where workers would be few and K is long,
+// several (splits > 1).  300 x 4096 bf16 against 1000 rows, 64 steps: 20.4 us whole, 21.4 split; 174 x 3944 f32 against 252, 372 steps: 82 and
+// 29; loss and gradients of 100 x 1024 f32 against 1000, 96 steps: 113 and 78.
+inline Cut cut_of_scores(uint64_t m, uint64_t n, uint64_t cols, int dtype, int sm_count, uint32_t widths) {
+    const uint64_t steps = count_of(cols, DEPTH) * (dtype == LT_F32 ? 6 : 1);
+    const Cut whole = Cut(m, n, sm_count, 0).split(steps, sm_count);
+    return whole.splits > 1 && steps >= 96 ? whole : Cut(m, n, sm_count, widths);
+}
+inline size_t score_bytes(const Cut &cut, uint64_t m, uint64_t n) { return cut.splits > 1 ? (size_t)up_to(cut.splits * m * n * 4, 256) : 0; }
+
 template <class T>
 constexpr uint32_t parts_of() { return sizeof(T) == 4 ? 3 : 1; }
 
@@ -1189,7 +1258,7 @@ struct Few {
 };
 
 struct LossScratch {
-    size_t score, odd_x, odd_table, tops, x, table, bytes;
+    size_t score, odd_x, odd_table, tops, scores, x, table, bytes;
     uint64_t piece, x_piece;    // rows that are packed at a time
     LossScratch(const LtOperator &o, int sm_count) {
         piece = pack_piece(o, 1, o.vocabulary);
@@ -1212,14 +1281,15 @@ struct LossScratch {
             bytes = tops + up_to(few.blocks * o.rows * sizeof(float2), 256);
             return;
         }
-        x = tops + up_to(halves * o.rows * sizeof(float2), 256);
+        scores = tops + up_to(halves * o.rows * sizeof(float2), 256);
+        x = scores + score_bytes(cut_of_scores(o.rows, o.vocabulary, o.cols, o.dtype, sm_count, 32), o.rows, o.vocabulary);
         table = x + packed_bytes(o.dtype, x_piece, o.cols);
         bytes = table + packed_bytes(o.dtype, piece, o.cols);
     }
 };
 
 struct GradScratch {
-    size_t unit, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, bytes;
+    size_t unit, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, scores, bytes;
     uint64_t piece, packed_piece;  // the latter where the table does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
@@ -1240,7 +1310,8 @@ struct GradScratch {
         p = table + packed_bytes(o.dtype, packed_piece, o.cols);
         sum_x = p + up_to(std::max<uint64_t>(o.rows, LEAST_ROWS) * piece * 2 * parts, 256);
         sum_table = sum_x + (packed_piece < o.vocabulary || cx.splits > 1 ? up_to(cx.splits * o.rows * o.cols * 4, 256) : 0);
-        bytes = sum_table + (ct.splits > 1 ? up_to(ct.splits * piece * o.cols * 4, 256) : 0);
+        scores = sum_table + (ct.splits > 1 ? up_to(ct.splits * piece * o.cols * 4, 256) : 0);
+        bytes = scores + (piece >= o.vocabulary ? score_bytes(cut_of_scores(o.rows, o.vocabulary, o.cols, o.dtype, sm_count, 64), o.rows, o.vocabulary) : 0);
     }
 };
 
@@ -1342,7 +1413,15 @@ cudaError_t launch_loss(const LtOperator &o, int sm_count, cudaStream_t stream, 
             a.n = (uint32_t)n;
             a.first = (uint32_t)v0;
             plain_args(o, a, tokens, room + at.odd_x, room + at.odd_table, rows);
-            const Cut cut(m, n, sm_count, 32);
+            const Cut cut = n == o.vocabulary && m == o.rows ? cut_of_scores(m, n, o.cols, o.dtype, sm_count, 32) : Cut(m, n, sm_count, 32);
+            if (cut.splits > 1) {
+                a.out = room + at.scores;
+                a.wide = width_of(a.out, n, 4);
+                e = launch_product<false, false, TO_SCORES, (int)parts_of<T>()>(x, table, a, cut, sm_count, stream);
+                *launched += 2;
+                return e != cudaSuccess ? e
+                                        : launch_pdl(lt_loss_finish<false, (int)parts_of<T>()>, a.m, 256, (size_t)0, stream, a, (const float *)a.out, cut.splits, (float *)o.out[0], (float *)o.out[1]);
+            }
             e = launch_product<false, false, TO_LOSS, (int)parts_of<T>()>(x, table, a, cut, sm_count, stream);
             if (e != cudaSuccess) return e;
             a.first_tile += 2 * cut.tiles_n;
@@ -1362,9 +1441,6 @@ cudaError_t launch_sum(const float *sums, void *out, uint64_t count, uint32_t sp
     return wide ? launch_pdl(lt_loss_sum<T, 4>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits)
                 : launch_pdl(lt_loss_sum<T, 1>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits);
 }
-
-// How many columns of a result can be stored at once: 8, 4 or 0 (one)
-inline int width_of(const void *out, uint64_t cols, size_t size) { return size == 2 && cols % 8 == 0 && is_aligned(out, 16) ? 8 : cols % 4 == 0 && is_aligned(out, 4 * size) ? 4 : 0; }
 
 template <class T>
 cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
@@ -1405,7 +1481,16 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         a.p_part = (uint32_t)padded;
         a.p_rows = (uint32_t)std::max<uint64_t>(o.rows, LEAST_ROWS);
         plain_args(o, a, o.in[0], room + at.odd_x, room + at.odd_table, rows);
-        e = launch_product<false, false, TO_P, PARTS>(x, table, a, Cut(o.rows, n, sm_count, 64), sm_count, stream);
+        const Cut of_scores = n == o.vocabulary ? cut_of_scores(o.rows, n, o.cols, o.dtype, sm_count, 64) : Cut(o.rows, n, sm_count, 64);
+        if (of_scores.splits > 1) {
+            a.out = room + at.scores;
+            a.wide = width_of(a.out, n, 4);
+            e = launch_product<false, false, TO_SCORES, PARTS>(x, table, a, of_scores, sm_count, stream);
+            if (e == cudaSuccess) e = launch_pdl(lt_loss_finish<true, PARTS>, a.p_rows, 256, (size_t)0, stream, a, (const float *)a.out, of_scores.splits, (float *)nullptr, (float *)nullptr);
+            ++*launched;
+        } else {
+            e = launch_product<false, false, TO_P, PARTS>(x, table, a, of_scores, sm_count, stream);
+        }
         if (e != cudaSuccess) return e;
         ++*launched;
         Operand p{a.p, padded * parts, a.p_rows, padded * parts, (uint32_t)padded, false};

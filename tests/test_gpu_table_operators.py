@@ -369,11 +369,22 @@ def test_vocabulary_loss_of_few_tokens(ctx, dtype, tokens, vocab, cols):  # noqa
     check_loss(ctx, x, table, ids, scale=1.5, dloss=normal(g, tokens))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,cols", [(5, 3, 2504), (129, 90, 2504), (200, 300, 6200), (260, 255, 6145), (17, 1500, 2100), (1000, 600, 2051)])
+def test_vocabulary_loss_of_few_scores(ctx, dtype, tokens, vocab, cols):  # noqa: F811
+    """Long rows and few tiles: several workers have one, for a part of the columns each."""
+    g, t = gen(tokens + vocab), TYPES[dtype]
+    x, table, ids = normal(g, tokens, cols, dtype=t, std=2.0), normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab)
+    ids[1::3] = -1
+    check_loss(ctx, x, table, ids, scale=0.75, dloss=normal(g, tokens))
+    check_loss(ctx, x, table, ids)
+
+
 def test_few_infinite_scores(ctx):  # noqa: F811
     """As in test_infinite_scores, for each way in which few and many tokens are scored."""
     g = gen(24)
-    for tokens in (1, 4, 7, 16, 70, 200):
-        x, table = normal(g, tokens, 24).abs() + 0.5, normal(g, 900, 24)
+    for tokens, cols in ((1, 24), (4, 24), (7, 24), (16, 24), (70, 24), (200, 24), (200, 500), (200, 1030)):
+        x, table = normal(g, tokens, cols).abs() + 0.5, normal(g, 900, cols) * cols ** -0.5
         table[[0, 255, 256, 700, 899]] = -math.inf
         ids = torch.full((tokens,), 300, dtype=torch.int32, device="cuda")
         keep = torch.isfinite(table[:, 0])
