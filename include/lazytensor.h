@@ -57,7 +57,8 @@ typedef enum {
     LT_ERR_DEVICE_TIMEOUT = 8, /* a bounded device-side wait gave up: reported by the first blocking call
                                  (lt_barrier with blocking set, lt_fetch) after a long-row kernel ran out
                                  of time waiting for a copy into shared memory, or for the partial results
-                                 of the other thread blocks of its cluster                                */
+                                 of the other thread blocks of its cluster, or a matrix product of
+                                 VOCABULARY_LOSS or its gradient for its operands or its tiles             */
     LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes, a token outside its table:
                                  reported by the context's first blocking call after the operator that met it, or
                                  after the replay of a graph that captured it (call once the replay is done); the
@@ -173,7 +174,13 @@ typedef enum {
        VOCABULARY_LOSS_GRAD: inputs (x*, table*, targets, lse f32 [..], dloss f32 [..], [out]), attrs {result, scale}, lse
        being the loss's result 1 on the same x and table.  With P = scale dloss (exp(z - lse) - (1 at the target)), zero for tokens without a
        target (whose rows of x, lse and dloss do not count, whatever they hold): result 0: P table, the gradient of x; 1: P^T x, that of
-       the table.  One launch for both. */
+       the table.  One launch for both.
+
+       Both take fewer than 2^24 tokens and rows and 2^20 columns, and fewer than 2^44 scores.  Scores beyond 2.3e38 count as infinite.
+       bf16 is multiplied as it is and summed in binary32; f32 in three bf16 parts, to 2^-23 of each product.  Temporaries: the loss
+       16 bytes per token and 256 rows of the table, the gradient up to 256 MB of P and, where dx is a sum of several pieces of
+       it, 4 bytes a value; f32 and rows that are not a multiple of 16 bytes apart are packed piece by piece, up to 96 MB (x as a whole
+       in f32: 6 bytes a value, in the gradient 12). */
     LT_OP_ROTARY = 70, LT_OP_CACHE_APPEND = 71, LT_OP_PAGED_ATTENTION = 72, LT_OP_RMS_NORM = 73, LT_OP_RMS_NORM_GRAD = 74,
     LT_OP_EMBEDDING = 80, LT_OP_EMBEDDING_GRAD = 81, LT_OP_VOCABULARY_LOSS = 82, LT_OP_VOCABULARY_LOSS_GRAD = 83
 } lt_opcode;
@@ -276,7 +283,8 @@ lt_status lt_ctx_destroy(lt_ctx *ctx);
  * "log" (0 default; 1 = one line on stderr for every graph that is planned, i.e. every cache miss; 2 = also one
  * line per flush and per replay; preset by the environment variable LT_LOG),
  * "wait_limit_ms" (2000 default: how long a long-row kernel waits for one of its asynchronous copies into shared
- * memory, or for the other thread blocks of its cluster, before it gives up, see LT_ERR_DEVICE_TIMEOUT),
+ * memory, or for the other thread blocks of its cluster, before it gives up, see LT_ERR_DEVICE_TIMEOUT; the products of
+ * VOCABULARY_LOSS and its gradient wait that long beside what a tile's work takes),
  * "pool_bytes" (4 GiB default: device blocks the library has released are kept, up to this total, and reused
  * by later flushes before the allocator is asked; 0 = return every block at once).
  * fusion, fast_math, horizontal and ieee are part of the cache key; the others act at launch time.

@@ -188,7 +188,7 @@ lt_status operator_infer(lt_ctx *c, int opcode, const Node *const *ops, int n_in
         const int core = grad ? 5 : 3;
         if (n_in != core && n_in != core + 1)
             return bad(LT_ERR_INVALID_ARG, grad ? "takes x, the table, targets, lse, dloss and optionally the result's buffer" : "takes x, the table, targets and optionally the result's buffer");
-        if (!flag(attrs[0]) || !finite32(attrs[1]))
+        if (!flag(attrs[0]) || !std::isfinite((float)(lt_attr_double(attrs[1]) * 1.4426950408889634)))  // (scores are made base two)
             return bad(LT_ERR_INVALID_ARG, grad ? "attrs are {result: 0 (gradient of x) or 1 (of the table), scale}" : "attrs are {result: 0 (loss) or 1 (log of the sum of exponentials), scale}");
         const Node &x = *ops[0], &table = *ops[1], &ids = *ops[2];
         const lt_status s = check_table(table);

@@ -77,8 +77,8 @@ __device__ __forceinline__ uint32_t part_of_b(uint32_t i) { return (0x010102u >>
 struct Tile {
     uint32_t m, n, split;
 };
-// Tiles side by side in time share operands in the L2 cache: BAND rows of tiles at a time (8192 x 4096 against 32000 rows: 1684 us with 16,
-// 1750 with 8, 1835 with 4).
+// Tiles side by side in time share operands in the L2 cache: BAND rows of tiles at a time (8192 x 4096 against 32000 rows: 1.52 ms with 16,
+// 1.56 with 9 or 12).
 constexpr uint32_t BAND = 16;
 __device__ __forceinline__ Tile tile_of(const ProductArgs &a, uint32_t t) {
     Tile r;
@@ -341,8 +341,13 @@ __device__ __forceinline__ void mend_scores(const ProductArgs &a, const Odd &o, 
 // result = A B^T over a list of tiles of ROWS x BLOCKS by WIDTH; BLOCKS: blocks that share a tile, a cluster.  A_TURNED, B_TURNED: the operand
 // lies in memory with K down the rows.
 //
-// One warp copies operands ahead into a ring of stages, one thread multiplies them into an accumulator in tensor memory, four
-// warps take finished tiles from there while the next one is made in the other half.  All waits are bounded.
+// One warp copies operands ahead into a ring of stages, one multiplies them into an accumulator in tensor memory, eight take
+// finished tiles from there while the next one is made in the other half.  All waits are bounded.
+//
+// Bound by the tensor cores: the scores of 8192 x 4096 bf16 against 32000 rows take 1.52 ms with everything around them, 1.41 PFLOP/s (a long
+// run of products alone sustains 1.36 on the same machines, which lower their clocks to hold their power).  A pair of blocks has 256 x 256,
+// so that each brings only half of the columns' operand: with 128 x 256 to a block shared memory is the bound.  Counters of one
+// launch (8192 x 2048): tensor cores busy 94 % of the time in scores, 89 in P, 80 in dx (4 rounds of 74 tiles where 3.46 would do), 90 in dtable.
 //
 // The tensor cores cut the sum of what they add to off instead of rounding it (half a unit of 2^-23 each time on average, all in one
 // direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, exact_steps steps of K at a time are
@@ -1175,6 +1180,8 @@ cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, co
     a.width = cut.width;
     a.part_a = x.part;
     a.part_b = y.part;
+    // Beside the limit, a wait may last as long as the work of a tile: its steps (0.4 us each), and scores that are made one by one.
+    a.limit_ns += (uint64_t)a.blocks_k * (PARTS == 1 ? 1 : 6) * 4000 + (uint64_t)a.plain_cols * SIDE * 200;
     return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream);
 }
 

@@ -273,6 +273,20 @@ def main() -> None:
         generic("rms_norm_grad", 4 * 2 * 16384 * 1024,
                 lambda c: [c.from_torch(bf16((16384, 1024))), c.from_torch(bf16((16384, 1024))), c.from_torch(torch.ones(1024, device=dev)), c.from_torch(bf16((16384, 1024)))],
                 lambda c, s_: c.rms_norm_grad(*s_[:3], residual_grad=s_[3]))
+        # a table's two ends; the products are bound by operations: their rate is printed as bytes of the operands
+        vocab, width = 32000, 4096
+        ids = torch.randint(0, vocab, (tokens,), dtype=torch.int32, device=dev)
+        generic("embedding 16384x4096", 2 * 2 * 2 * tokens * width, lambda c: [c.from_torch(bf16((vocab, width))), c.from_torch(torch.cat([ids, ids.flip(0)]))],
+                lambda c, s_: c.embedding(*s_, scale=0.5))
+        generic("embedding_grad 16384x4096", 2 * (2 * tokens + vocab) * width, lambda c: [c.from_torch(bf16((2 * tokens, width))), c.from_torch(torch.cat([ids, ids.flip(0)]))],
+                lambda c, s_: c.embedding_grad(*s_, vocab))
+        for name, n, c_ in (("vocabulary_loss 1x4096", 1, 4096), ("vocabulary_loss 8192x4096", tokens, 4096)):
+            generic(name, 2 * (n + vocab) * c_, lambda c, n=n, c_=c_: [c.from_torch(bf16((n, c_))), c.from_torch(bf16((vocab, c_))), c.from_torch(ids[:n])],
+                    lambda c, s_: c.vocabulary_loss(*s_, scale=c_ ** -0.5))
+        generic("vocabulary_loss_grad 8192x2048", 4 * (tokens + vocab) * 2048,
+                lambda c: [c.from_torch(bf16((tokens, 2048))), c.from_torch(bf16((vocab, 2048))), c.from_torch(ids), c.from_torch(torch.full((tokens,), 50.0, device=dev)),
+                           c.from_torch(torch.ones(tokens, device=dev))],
+                lambda c, s_: c.vocabulary_loss_grad(*s_))
     if "c5" in which:
         shapes = parameter_shapes()
         ctx = context()

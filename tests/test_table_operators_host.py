@@ -150,3 +150,11 @@ def test_a_batch_records_the_same(ctx):  # noqa: F811
     ctx.barrier()
     assert len(kept) == 1 and kept[0].shape == (5,) and ctx.stats()["compiles"] == compiles
     del loss
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -3e38, 1e39])
+def test_a_scale_that_is_infinite_base_two_is_refused(ctx, scale):  # noqa: F811
+    refused(ctx, "INVALID_ARG", "vocabulary_loss", [DY, TAB, IDS], result=0, scale=scale)
+    refused(ctx, "INVALID_ARG", "vocabulary_loss_grad", [DY, TAB, IDS, VEC, VEC], result=0, scale=scale)
+    x, table, ids = fake(ctx, (5, 16), "bf16"), fake(ctx, (50, 16), "bf16"), fake(ctx, (5,), "i32")
+    ctx.vocabulary_loss(x, table, ids, scale=2.3e38)
