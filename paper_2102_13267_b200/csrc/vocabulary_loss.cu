@@ -34,7 +34,7 @@ template <int BLOCKS>
 struct Ring {
     static constexpr uint32_t STAGE_B = WIDTH / BLOCKS * DEPTH * 2;
     static constexpr uint32_t STAGE = STAGE_A + STAGE_B;
-    static constexpr int STAGES = BLOCKS == 1 ? 4 : 6;
+    static constexpr int STAGES = BLOCKS == 1 ? 4 : 6, MOST = BLOCKS == 1 ? 8 : STAGES;  // MOST: of narrower tiles
     static constexpr uint32_t BYTES = STAGES * STAGE + TAKERS * 32 * 128 + 1024;  // (to begin on a multiple of 1024)
 };
 
@@ -45,6 +45,7 @@ struct ProductArgs {
     uint32_t tiles_m, tiles_n, splits;
     uint32_t width;             // columns of a tile, a multiple of 16 x BLOCKS up to WIDTH
     uint32_t blocks_k;          // steps of K of one product
+    uint32_t stages, stage_bytes;  // single blocks
     uint32_t part_a, part_b;    // columns from a part to the next
     // TO_LOSS, TO_P
     const int *targets;
@@ -367,8 +368,9 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
     using R = Ring<BLOCKS>;
     constexpr uint32_t STEPS = exact_steps(BLOCKS, TO, PARTS);
     constexpr uint32_t WIDTH_B = WIDTH / BLOCKS;  // of B's rows, per block (at most)
+    const uint32_t stages = BLOCKS == 1 ? a.stages : R::STAGES, stage_bytes = BLOCKS == 1 ? a.stage_bytes : R::STAGE;
     extern __shared__ unsigned char product_mem[];
-    __shared__ __align__(8) uint64_t barriers[2 * R::STAGES + 4];
+    __shared__ __align__(8) uint64_t barriers[2 * R::MOST + 4];
     __shared__ uint32_t tensor_at, gave_up;
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
     uint32_t rank = 0;
@@ -376,12 +378,12 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
     const uint32_t ring = (shared_address(product_mem) + 1023) & ~1023u;
     const uint32_t bar = shared_address(barriers);
     auto full = [&](uint32_t s) { return bar + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar + 8 * (R::STAGES + s); };
-    auto ready = [&](uint32_t b) { return bar + 8 * (2 * R::STAGES + b); };
-    auto taken = [&](uint32_t b) { return bar + 8 * (2 * R::STAGES + 2 + b); };
+    auto empty = [&](uint32_t s) { return bar + 8 * (R::MOST + s); };
+    auto ready = [&](uint32_t b) { return bar + 8 * (2 * R::MOST + b); };
+    auto taken = [&](uint32_t b) { return bar + 8 * (2 * R::MOST + 2 + b); };
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (int s = 0; s < R::STAGES; ++s) {
+        for (uint32_t s = 0; s < stages; ++s) {
             barrier_init(full(s), 1);
             barrier_init(empty(s), 1);
         }
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                     break;
                 }
                 const int at_a = PARTS == 1 ? 0 : (int)(part_of_a(product) * a.part_a), at_b = PARTS == 1 ? 0 : (int)(part_of_b(product) * a.part_b);
-                const uint32_t to_a = ring + stage * R::STAGE, to_b = to_a + STAGE_A;
+                const uint32_t to_a = ring + stage * stage_bytes, to_b = to_a + STAGE_A;
                 uint32_t on = full(stage);
                 if constexpr (BLOCKS == 2) on = shared_of(on, 0);
                 if (one_lane()) {
@@ -440,14 +442,14 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                     }
                 }
                 __syncwarp();
-                if (++stage == R::STAGES) stage = 0, phase ^= 1;
+                if (++stage == stages) stage = 0, phase ^= 1;
                 if (++k == a.blocks_k) k = 0, ++product;
             }
         }
         // the last commits arrive here, too, before the block may end
-        for (int s = 0; s < R::STAGES && !ended; ++s) {
+        for (uint32_t s = 0; s < stages && !ended; ++s) {
             if (!waits.wait(empty(stage), phase ^ 1)) break;
-            if (++stage == R::STAGES) stage = 0, phase ^= 1;
+            if (++stage == stages) stage = 0, phase ^= 1;
         }
         pdl_release();
     } else if (warp == 1) {
@@ -476,9 +478,9 @@ __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__
                             break;
                         }
                         tensor_fence_after();
-                        const uint32_t next = stage + 1 == R::STAGES ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1;
+                        const uint32_t next = stage + 1 == stages ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1;
                         there = __all_sync(0xffffffffu, barrier_done(full(next), next_phase));
-                        const uint32_t da = low_a + stage * (R::STAGE >> 4), db = low_b + stage * (R::STAGE >> 4);
+                        const uint32_t da = low_a + stage * (stage_bytes >> 4), db = low_b + stage * (stage_bytes >> 4);
                         if (one_lane()) {
 #pragma unroll
                             for (uint32_t k = 0; k < DEPTH / 16; ++k)
@@ -918,6 +920,198 @@ __global__ void __launch_bounds__(SOME_THREADS, 1) lt_loss_some(const FewArgs a)
     }
 }
 
+// The gradients of few tokens, TOKENS at a time: a block has whole rows of the table, eight columns to a thread, and with them in registers
+// makes the scores (its threads' sums joined by the warps and then through shared memory), the rows of dtable, and its share of dx, which
+// lt_loss_few_join adds up.  The table is read once and dtable written once; the rows to come are on their way meanwhile.
+constexpr uint32_t FEW_GRAD_THREADS = 512, FEW_GRAD_COLS = 8;
+
+struct FewGradArgs {
+    const void *x, *table;
+    const int *targets;
+    const float *lse, *dloss;
+    void *dtable;               // or null
+    float *dx;                  // [blocks][tokens][cols], or null
+    uint64_t x_pitch, table_pitch;
+    uint32_t tokens, vocabulary, cols;
+    float scale, scale2;
+    int add;                    // to what dtable holds of the tokens before
+    unsigned int *bad_target;
+};
+
+// sum += q f, two values an instruction
+template <int N>
+__device__ __forceinline__ void add_scaled(float (&sum)[N], float q, const float (&f)[N]) {
+    if constexpr (N == 1) {
+        sum[0] += q * f[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            asm("{.reg .b64 s, f, q; mov.b64 s, {%0, %1}; mov.b64 f, {%2, %3}; mov.b64 q, {%4, %4}; fma.rn.f32x2 s, q, f, s; mov.b64 {%0, %1}, s;}"
+                : "+f"(sum[i]), "+f"(sum[i + 1])
+                : "f"(f[i]), "f"(f[i + 1]), "f"(q));
+    }
+}
+
+template <class T, int N, int TOKENS>
+__global__ void __launch_bounds__(FEW_GRAD_THREADS, 1) lt_loss_few_grad(const FewGradArgs a) {
+    constexpr int ROWS_AT_ONCE = sizeof(T) == 2 ? 4 : 2, PIECES = FEW_GRAD_COLS / N, VALUES = ROWS_AT_ONCE * TOKENS, LANES = 32 / VALUES, WARPS = FEW_GRAD_THREADS / 32;
+    static_assert(VALUES <= 32, "a lane for each score at least");
+    extern __shared__ uint4 few_mem[];  // x: [TOKENS][columns], zeros for tokens that do not count
+    T *const xs = reinterpret_cast<T *>(few_mem);
+    __shared__ float part[2][WARPS][VALUES];
+    __shared__ __align__(16) float weights[WARPS][VALUES];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, pitch = (a.cols + 7) & ~7u;
+    // the lane's score of those at once: of row `mine`, token `token`
+    const uint32_t value = lane / LANES, mine = value / TOKENS, token = value % TOKENS;
+    pdl_release();
+    pdl_wait();
+    for (uint32_t t = 0; t < TOKENS; ++t) {
+        const bool counts = t < a.tokens && (uint32_t)a.targets[t] < a.vocabulary;
+        for (uint32_t c = threadIdx.x; c < pitch; c += blockDim.x) xs[t * pitch + c] = counts && c < a.cols ? ((const T *)a.x)[t * a.x_pitch + c] : from_float<T>(0.f);
+    }
+    int target = token < a.tokens ? a.targets[token] : -1;
+    if (blockIdx.x == 0 && warp == 0 && target >= 0 && (uint32_t)target >= a.vocabulary) report(a.bad_target);
+    if ((uint32_t)target >= a.vocabulary) target = -1;
+    const float lse2 = target >= 0 ? a.lse[token] * 1.44269504f : 0.f, factor = target >= 0 ? a.dloss[token] * a.scale : 0.f;
+    __syncthreads();
+    const uint32_t v0 = (uint32_t)((uint64_t)a.vocabulary * blockIdx.x / gridDim.x), v1 = (uint32_t)((uint64_t)a.vocabulary * (blockIdx.x + 1) / gridDim.x);
+    auto col = [&](int k) { return (k * blockDim.x + threadIdx.x) * N; };
+    Loaded<T, N> w[PIECES][ROWS_AT_ONCE], next[PIECES][ROWS_AT_ONCE];
+    auto load = [&](Loaded<T, N> (&to)[PIECES][ROWS_AT_ONCE], uint32_t v) {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int r = 0; r < ROWS_AT_ONCE; ++r) {
+                to[k][r].v = make_uint4(0, 0, 0, 0);
+                if (v + r < v1 && col(k) < a.cols) to[k][r].load((const T *)a.table + (uint64_t)(v + r) * a.table_pitch + col(k));
+            }
+    };
+    float dx[TOKENS][PIECES][N] = {};
+    load(w, v0);
+    uint32_t turn = 0;
+    for (uint32_t v = v0; v < v1; v += ROWS_AT_ONCE, turn ^= 1) {
+        load(next, v + ROWS_AT_ONCE);
+        float dot[VALUES] = {};
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            if (col(k) >= a.cols) break;
+            float f[ROWS_AT_ONCE][N];
+#pragma unroll
+            for (int r = 0; r < ROWS_AT_ONCE; ++r) w[k][r].values(f[r]);
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                float x[N];
+                Loaded<T, N> l;
+                l.load_shared(xs + t * pitch + col(k));
+                l.values(x);
+#pragma unroll
+                for (int r = 0; r < ROWS_AT_ONCE; ++r)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) dot[r * TOKENS + t] += f[r][i] * x[i];
+            }
+        }
+        __syncwarp();
+        // as lt_loss_some does it, and the last values between all lanes that have them
+#pragma unroll
+        for (int d = 16, n = VALUES / 2; d >= 1; d >>= 1, n >>= 1) {
+            if (n > 0) {
+                const bool upper = lane & d;
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const float keep = upper ? dot[i + n] : dot[i], send = upper ? dot[i] : dot[i + n];
+                    dot[i] = keep + __shfl_xor_sync(0xffffffffu, send, d);
+                }
+            } else {
+                dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], d);
+            }
+        }
+        if (lane % LANES == 0) part[turn][warp][value] = dot[0];
+        __syncthreads();
+        float z = 0.f;
+#pragma unroll 4
+        for (uint32_t k = 0; k < warps; ++k) z += part[turn][k][value];
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(z, a.scale2, -lse2)));
+        if (v + mine == (uint32_t)target) e -= 1.f;
+        if (lane % LANES == 0) weights[warp][value] = target >= 0 ? e * factor : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            if (col(k) >= a.cols) break;
+            float f[ROWS_AT_ONCE][N], out[ROWS_AT_ONCE][N] = {};
+#pragma unroll
+            for (int r = 0; r < ROWS_AT_ONCE; ++r) w[k][r].values(f[r]);
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                float x[N];
+                Loaded<T, N> l;
+                l.load_shared(xs + t * pitch + col(k));
+                l.values(x);
+#pragma unroll
+                for (int r = 0; r < ROWS_AT_ONCE; ++r) {
+                    const float q = weights[warp][r * TOKENS + t];
+                    if (v + r >= v1) continue;  // (its scores are not any row's)
+                    add_scaled(out[r], q, x);
+                    add_scaled(dx[t][k], q, f[r]);
+                }
+            }
+            if (!a.dtable) continue;
+#pragma unroll
+            for (int r = 0; r < ROWS_AT_ONCE; ++r) {
+                if (v + r >= v1) continue;
+                T *to = (T *)a.dtable + (uint64_t)(v + r) * a.cols + col(k);
+                if (a.add) {
+                    Loaded<T, N> before;
+                    float b[N];
+                    before.load(to);
+                    before.values(b);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) out[r][i] += b[i];
+                }
+                if constexpr (N == 1) *to = from_float<T>(out[r][0]);
+                else *reinterpret_cast<uint4 *>(to) = pack(out[r]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int r = 0; r < ROWS_AT_ONCE; ++r) w[k][r] = next[k][r];
+    }
+    if (!a.dx) return;
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        if (t >= a.tokens) break;
+        float *to = a.dx + ((uint64_t)blockIdx.x * a.tokens + t) * a.cols;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            if (col(k) >= a.cols) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i) to[col(k) + i] = dx[t][k][i];
+        }
+    }
+}
+
+// dx of few tokens: the blocks' shares, eight warps having an eighth of them each
+template <class T>
+__global__ void __launch_bounds__(256) lt_loss_few_join(const float *shares, T *dx, const int *targets, const float *dloss, float scale, uint32_t tokens, uint32_t cols, uint32_t blocks, uint32_t vocabulary) {
+    __shared__ float sums[8][32];
+    pdl_release();
+    pdl_wait();
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, count = tokens * cols, at = blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (at < count) {
+        const uint32_t k1 = (uint32_t)((uint64_t)blocks * (warp + 1) / 8);
+#pragma unroll 16
+        for (uint32_t k = (uint32_t)((uint64_t)blocks * warp / 8); k < k1; ++k) s += shares[(uint64_t)k * count + at];
+    }
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp || at >= count) return;
+    for (int k = 1; k < 8; ++k) s += sums[k][lane];
+    const uint32_t t = at / cols;
+    dx[at] = from_float<T>((uint32_t)targets[t] < vocabulary && dloss[t] * scale != 0.f ? s : 0.f);
+}
+
 struct PackArgs {
     const void *from;
     uint64_t pitch;
@@ -1160,7 +1354,7 @@ struct Cut {
         // columns; a single one, which has few rows, by the columns.  Narrower tiles pay where the last round would be nearly empty:
         // one token against 32000 rows of 4096, 143 tiles of 224 columns 49 us, 125 of 256 56.
         auto cost = [&](uint32_t w) { return (uint64_t)count_of((uint64_t)tiles_m * count_of(n, w), (uint64_t)sm_count / blocks) * (w + (blocks == 1 ? 32 : 256)); };
-        for (uint32_t w = WIDTH; widths && w >= LEAST_WIDTH; w -= widths)
+        for (uint32_t w = WIDTH; widths && w >= (blocks == 1 ? LEAST_WIDTH / 2 : LEAST_WIDTH); w -= widths)
             if (cost(w) < cost(width)) width = w;
         tiles_n = count_of(n, width);
     }
@@ -1180,6 +1374,10 @@ cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, co
     a.width = cut.width;
     a.part_a = x.part;
     a.part_b = y.part;
+    // (narrow tiles have more stages, which cover the way to memory by their number: loss and gradients of 128 x 2048 f32 against 32000 rows,
+    // tiles of 64 columns, 990 us with eight, 1076 with four, 1104 with 128 columns)
+    a.stage_bytes = STAGE_A + (B_TURNED ? WIDTH : cut.width) * DEPTH * 2;
+    a.stages = std::min<uint32_t>(Ring<1>::MOST, Ring<1>::STAGES * Ring<1>::STAGE / a.stage_bytes);
     // Beside the limit, a wait may last as long as the work of a tile: its steps (0.4 us each), and scores that are made one by one.
     a.limit_ns += (uint64_t)a.blocks_k * (PARTS == 1 ? 1 : 6) * 4000 + (uint64_t)a.plain_cols * SIDE * 200;
     return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream);
@@ -1264,6 +1462,19 @@ struct Few {
     }
 };
 
+// Tokens whose gradients are made by plain loads, at a time (0: on the tensor cores).  bf16: up to two; f32: up to 16, every eight of them once
+// through the table.  Loss and gradients against 32000 rows of 4096 bf16: one token 150 us, two 169, four 263 (by tiles 255 all of them);
+// of 2048 f32: 1 token 144, 4 160, 8 216, 16 523, 32 1150 (by tiles 705, 704, 714, 753, 796).
+struct FewGrad {
+    uint32_t at_once = 0, blocks = 0, threads = 0;
+    FewGrad(const LtOperator &o, int sm_count) {
+        if (o.rows > (o.dtype == LT_BF16 ? 2 : 16) || o.cols > FEW_GRAD_THREADS * FEW_GRAD_COLS) return;
+        at_once = o.rows <= 2 ? (uint32_t)o.rows : o.rows <= 4 ? 4 : 8;
+        threads = (uint32_t)up_to(count_of(o.cols, FEW_GRAD_COLS), 32);
+        blocks = (uint32_t)std::min<uint64_t>((uint64_t)sm_count * std::min(8u, FEW_GRAD_THREADS / threads), count_of(o.vocabulary, 4));
+    }
+};
+
 struct LossScratch {
     size_t score, odd_x, odd_table, tops, scores, x, table, bytes;
     uint64_t piece, x_piece;    // rows that are packed at a time
@@ -1300,6 +1511,11 @@ struct GradScratch {
     uint64_t piece, packed_piece;  // the latter where the table does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
+        const FewGrad few(o, sm_count);
+        if (few.at_once) {
+            bytes = few.blocks * few.at_once * o.cols * 4;
+            return;
+        }
         const uint64_t parts = o.dtype == LT_F32 ? 3 : 1;
         piece = piece_of(o.vocabulary, o.rows * 2 * parts, P_BYTES);
         packed_piece = std::min(piece, pack_piece(o, 1, o.vocabulary));
@@ -1449,8 +1665,45 @@ cudaError_t launch_sum(const float *sums, void *out, uint64_t count, uint32_t sp
                 : launch_pdl(lt_loss_sum<T, 1>, grid, 256, (size_t)0, stream, sums, (T *)out, count, splits);
 }
 
+template <class T, int N, int TOKENS>
+cudaError_t launch_few_grad_of(const FewGradArgs &a, const FewGrad &few, cudaStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(lt_loss_few_grad<T, N, TOKENS>, TOKENS * FEW_GRAD_THREADS * FEW_GRAD_COLS * sizeof(T), ready);
+    return e != cudaSuccess ? e : launch_pdl_shared(lt_loss_few_grad<T, N, TOKENS>, dim3(few.blocks), few.threads, (size_t)TOKENS * up_to(a.cols, 8) * sizeof(T), stream, a);
+}
+template <class T, int N>
+cudaError_t launch_few_grad_of(const FewGradArgs &a, const FewGrad &few, cudaStream_t stream) {
+    if constexpr (sizeof(T) == 4) {
+        if (few.at_once == 8) return launch_few_grad_of<T, N, 8>(a, few, stream);
+        if (few.at_once == 4) return launch_few_grad_of<T, N, 4>(a, few, stream);
+    }
+    return few.at_once == 1 ? launch_few_grad_of<T, N, 1>(a, few, stream) : launch_few_grad_of<T, N, 2>(a, few, stream);
+}
+template <class T>
+cudaError_t launch_few_grad(const LtOperator &o, const FewGrad &few, cudaStream_t stream, unsigned *launched) {
+    constexpr int N = 16 / (int)sizeof(T);
+    const bool wide = o.cols % N == 0 && o.pitch[1] % N == 0 && is_aligned(o.in[1], 16) && is_aligned(o.out[1], 16);
+    const float scale = (float)lt_attr_double(o.attr[1]);
+    cudaError_t e = cudaSuccess;
+    *launched = 0;
+    for (uint64_t r0 = 0; r0 < o.rows && e == cudaSuccess; r0 += few.at_once) {
+        const uint32_t tokens = (uint32_t)std::min<uint64_t>(few.at_once, o.rows - r0);
+        const FewGradArgs a{(const T *)o.in[0] + r0 * o.pitch[0], o.in[1], (const int *)o.in[2] + r0, (const float *)o.in[3] + r0, (const float *)o.in[4] + r0, o.out[1], o.out[0] ? (float *)o.scratch : nullptr,
+                            o.pitch[0], o.pitch[1], tokens, (uint32_t)o.vocabulary, (uint32_t)o.cols, scale, (float)(lt_attr_double(o.attr[1]) * 1.4426950408889634), r0 > 0, &o.status->loss};
+        e = wide ? launch_few_grad_of<T, N>(a, few, stream) : launch_few_grad_of<T, 1>(a, few, stream);
+        ++*launched;
+        if (e != cudaSuccess || !o.out[0]) continue;
+        e = launch_pdl(lt_loss_few_join<T>, count_of((uint64_t)tokens * o.cols, 32), 256, (size_t)0, stream, (const float *)a.dx, (T *)o.out[0] + r0 * o.cols, a.targets, a.dloss, scale, tokens, a.cols, few.blocks,
+                       a.vocabulary);
+        ++*launched;
+    }
+    return e;
+}
+
 template <class T>
 cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched) {
+    const FewGrad few(o, sm_count);
+    if (few.at_once) return launch_few_grad<T>(o, few, stream, launched);
     constexpr int PARTS = parts_of<T>();
     constexpr int TO_T = sizeof(T) == 4 ? TO_F32 : TO_BF16;
     const GradScratch at(o, sm_count);

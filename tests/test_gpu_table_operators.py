@@ -565,3 +565,56 @@ def test_two_contexts_on_two_streams_at_once(lt):  # noqa: F811
         c.barrier(blocking=True)
         check_step(s, out)
         c.close()
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab,cols", [("bf16", 1, 700, 4096), ("bf16", 2, 3, 8), ("bf16", 2, 1201, 333), ("bf16", 1, 2000, 4104), ("f32", 1, 1, 1), ("f32", 2, 901, 2048), ("f32", 3, 1500, 4096),
+                                                     ("f32", 4, 5, 36), ("f32", 7, 2001, 260), ("f32", 9, 800, 516), ("f32", 13, 1003, 77), ("f32", 16, 3001, 1024), ("f32", 16, 300, 4100), ("f32", 17, 900, 512)])
+def test_gradients_of_few_tokens(ctx, dtype, tokens, vocab, cols):  # noqa: F811
+    g, t = gen(tokens + vocab + cols), TYPES[dtype]
+    x, table, ids = normal(g, tokens, cols, dtype=t, std=2.0), normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab)
+    ids[-1] = vocab - 1
+    check_loss(ctx, x, table, ids, dloss=normal(g, tokens))
+    odd = torch.empty(table.numel() + 1, device="cuda", dtype=t)[1:].view(vocab, cols)  # (begins behind a 16-byte boundary)
+    odd.copy_(table)
+    check_loss(ctx, x, odd, ids, scale=-0.75)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_few_tokens_report_a_target_outside_the_table(ctx, lt, dtype):  # noqa: F811
+    g, t = gen(3), TYPES[dtype]
+    x, table, ids = normal(g, 2, 64, dtype=t), normal(g, 30, 64, dtype=t), torch.tensor([30, 29], dtype=torch.int32, device="cuda")
+    lse, d = torch.logsumexp(x.double() @ table.double().T, -1).float(), normal(g, 2)
+    got, r = ctx.vocabulary_loss_grad(*(ctx.from_torch(v) for v in (x, table, ids, lse, d))), ref.loss_grad(x, table, ids, lse, d)
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE_INDEX.*vocabulary_loss"):
+        ctx.barrier(blocking=True)
+    for a, b in zip(got, (r[:2], r[2:])):
+        close(fetch(ctx, a), *b)
+
+
+@pytest.mark.parametrize("dtype,tokens", [("bf16", 2), ("f32", 2), ("f32", 16)])
+def test_gradients_of_few_tokens_that_do_not_count_and_one_alone(ctx, dtype, tokens):  # noqa: F811
+    """Rows without a target hold NaN; each gradient is the same when it is asked for alone."""
+    g, t = gen(tokens), TYPES[dtype]
+    x, table, targets, dloss = normal(g, tokens, 260, dtype=t), normal(g, 501, 260, dtype=t), tokens_of(g, tokens, 501), normal(g, tokens)
+    targets[0] = -1
+    tt = [ctx.from_torch(v) for v in (x, table, targets, dloss)]
+    lse = ctx.vocabulary_loss(*tt[:3])[1]
+    ctx.barrier()
+    out = [torch.full_like(x, 7.0), torch.full_like(table, 7.0)]
+    buffers = [ctx.from_torch(o) for o in out]
+    ctx.vocabulary_loss_grad(*tt[:3], lse, tt[3], out=buffers)
+    ctx.barrier()
+    torch.cuda.synchronize()
+    x2, dloss2 = x.clone(), dloss.clone()
+    x2[0], dloss2[0] = math.nan, math.nan
+    hurt = ctx.from_torch(x2), ctx.from_torch(dloss2)
+    for which in (0, 1):
+        alone = torch.full_like(out[which], 7.0)
+        buffers = [None, None]
+        buffers[which] = ctx.from_torch(alone)
+        results = ctx.vocabulary_loss_grad(hurt[0], *tt[1:3], lse, hurt[1], out=buffers)
+        ctx.release(results[1 - which])
+        ctx.barrier()
+        torch.cuda.synchronize()
+        assert torch.equal(alone, out[which])
+    assert bool((out[0][0] == 0).all()) and bool(torch.isfinite(out[1].float()).all())
