@@ -6,12 +6,14 @@
 // Three matrix products, one kernel (lt_product) that differs in how its operands lie and in what it does with a tile of the
 // result.  Scores never reach memory: the loss keeps of each tile the rows' maxima and sums of exponentials, which
 // lt_loss_join adds up in the tiles' order.  The gradient makes P for a piece of the vocabulary at a time, in bf16, and
-// multiplies it from both sides while it is in the L2 cache.
+// multiplies it from both sides.
+//
+// Few tokens are scored, and their gradients made, by plain loads and products in binary32 (lt_loss_few, lt_loss_some, lt_loss_few_grad).
 //
 // Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value at most, as much as storing
 // the gradients costs; P is near -1 at most targets and rounded little there, which it would not be with dloss in it).  So is x dloss_n where dloss
 // differs from token to token: it is divided by that of the first tokens and dtable multiplied by it, and stays x where they are all alike.
-//  f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
+// f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
 // parts the six largest are added: what is left out is below 2^-23 of each product.
 #include <algorithm>
 
@@ -920,9 +922,10 @@ __global__ void __launch_bounds__(SOME_THREADS, 1) lt_loss_some(const FewArgs a)
     }
 }
 
-// The gradients of few tokens, TOKENS at a time: a block has whole rows of the table, eight columns to a thread, and with them in registers
+// The gradients of few tokens, TOKENS at a time (through tiles of 128 tokens most of the work would be padding; figures at FewGrad): a block has whole rows of the table, eight columns to a thread, and with them in registers
 // makes the scores (its threads' sums joined by the warps and then through shared memory), the rows of dtable, and its share of dx, which
-// lt_loss_few_join adds up.  The table is read once and dtable written once; the rows to come are on their way meanwhile.
+// lt_loss_few_join adds up.  The table is read once and dtable written once; the rows to come are on their way meanwhile.  One token of 4096 bf16
+// against 32000 rows: 98 us, 4.7 TB/s, a barrier per four rows; eight of 2048 f32 174, half of them issue slots.
 constexpr uint32_t FEW_GRAD_THREADS = 512, FEW_GRAD_COLS = 8;
 
 struct FewGradArgs {
