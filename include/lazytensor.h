@@ -512,12 +512,19 @@ lt_status lt_dump_plan(lt_ctx *ctx, char *buf, size_t cap, size_t *need);
 lt_status lt_debug_bounds_violations(lt_ctx *ctx, uint64_t *out);
 
 /*
- * Exercises the one device-side wait the library has, without touching any tensor: enqueues a one-warp kernel
+ * Exercises the device-side wait of the long-row kernels, without touching any tensor: enqueues a one-warp kernel
  * that waits at most `limit_ns` nanoseconds for a completion nothing delivers, gives up and raises the device
  * status word.  The next blocking call on the context (lt_barrier with blocking set, lt_fetch) then returns
  * LT_ERR_DEVICE_TIMEOUT and clears the word; the context stays usable.
  */
 lt_status lt_debug_wait_probe(lt_ctx *ctx, uint64_t limit_ns);
+
+/*
+ * The same for the wait of the matrix products of VOCABULARY_LOSS and its gradient: two warps of one block wait for a
+ * completion nothing delivers, one at most `limit_ns` nanoseconds (up to a second), the other fifty times as long unless the
+ * first gives up, as it does.
+ */
+lt_status lt_debug_product_wait_probe(lt_ctx *ctx, uint64_t limit_ns);
 
 const char *lt_last_error(lt_ctx *ctx);
 const char *lt_version(void);

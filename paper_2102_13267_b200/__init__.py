@@ -103,6 +103,7 @@ _SIGNATURES = {
     "lt_barrier_static_scratch": [_vp, _int, _int],
     "lt_debug_bounds_violations": [_vp, _P(_u64)],
     "lt_debug_wait_probe": [_vp, _u64],
+    "lt_debug_product_wait_probe": [_vp, _u64],
     "lt_replay": [_vp, _int],
     "lt_scalar_set": [_vp, _u64, ctypes.c_double],
     "lt_replay_slots": [_vp, _P(ctypes.c_uint32)],
@@ -654,6 +655,10 @@ class LazyContext(_Operators):
     def debug_wait_probe(self, limit_ns: int) -> None:
         """lt_debug_wait_probe: enqueue a kernel whose bounded wait runs out (see LT_ERR_DEVICE_TIMEOUT)."""
         self._check(_lib.lt_debug_wait_probe(self._ctx, int(limit_ns)))
+
+    def debug_product_wait_probe(self, limit_ns: int) -> None:
+        """lt_debug_product_wait_probe: the same for the wait of the vocabulary loss's matrix products."""
+        self._check(_lib.lt_debug_product_wait_probe(self._ctx, int(limit_ns)))
 
     def replay(self, blocking: bool = False) -> None:
         """lt_replay: run the previously flushed graph again on the same tensors, without recording it."""

@@ -2264,6 +2264,16 @@ lt_status lt_debug_wait_probe(lt_ctx *c, uint64_t limit_ns) {
     return LT_OK;
 }
 
+lt_status lt_debug_product_wait_probe(lt_ctx *c, uint64_t limit_ns) {
+    if (!c) return LT_ERR_INVALID_ARG;
+    if (c->device == LT_DEVICE_NONE) return fail(c, LT_ERR_DEVICE, "lt_debug_product_wait_probe needs a context on a CUDA device");
+    if (limit_ns > 1000000000ull) return fail(c, LT_ERR_INVALID_ARG, "lt_debug_product_wait_probe: at most a second");
+    DeviceScope on_device(c->device);
+    cudaError_t e = lt_launch_product_wait_probe(c->operator_status, limit_ns, c->stream);
+    if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("probe launch: ") + cudaGetErrorString(e));
+    return LT_OK;
+}
+
 lt_status lt_fetch(lt_ctx *c, lt_tensor t, void *host_dst, size_t nbytes) {
     if (!c) return LT_ERR_INVALID_ARG;
     uint32_t slot;

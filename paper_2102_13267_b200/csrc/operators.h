@@ -91,3 +91,5 @@ cudaError_t lt_launch_vocabulary_loss(const LtOperator &o, int sm_count, cudaStr
 size_t lt_vocabulary_loss_scratch(const LtOperator &o, int sm_count);
 cudaError_t lt_launch_vocabulary_loss_grad(const LtOperator &o, int sm_count, cudaStream_t stream, unsigned *launched);
 size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int sm_count);
+// A kernel whose bounded wait, that of the matrix products, runs out after `limit_ns`.
+cudaError_t lt_launch_product_wait_probe(LtOperatorStatus *status, uint64_t limit_ns, cudaStream_t stream);

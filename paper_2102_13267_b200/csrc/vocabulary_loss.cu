@@ -1816,7 +1816,30 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
     return e;
 }
 
+// The bounded wait of lt_product on a barrier that nobody arrives at, with no copy or product on its way.  The first warp's
+// limit is `limit_ns`, the second's fifty times that: it ends when the first gives up.
+__global__ void lt_product_wait_probe(unsigned int *timeout, uint64_t limit_ns) {
+    __shared__ __align__(8) uint64_t barriers[2];
+    __shared__ uint32_t gave_up;
+    const uint32_t arrived = shared_address(&barriers[0]), never = shared_address(&barriers[1]);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        barrier_init(arrived, 1);
+        barrier_init(never, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        barrier_arrive_at(arrived);
+    }
+    __syncthreads();
+    const Waits waits{&gave_up, timeout, warp_number() ? 50 * limit_ns : limit_ns};
+    if (waits.wait(arrived, 0)) waits.wait(never, 0);
+}
+
 }  // namespace
+
+cudaError_t lt_launch_product_wait_probe(LtOperatorStatus *status, uint64_t limit_ns, cudaStream_t stream) {
+    lt_product_wait_probe<<<1, 64, 0, stream>>>(&status->timeout, limit_ns);
+    return cudaGetLastError();
+}
 
 size_t lt_vocabulary_loss_scratch(const LtOperator &o, int sm_count) { return LossScratch(o, sm_count).bytes; }
 size_t lt_vocabulary_loss_grad_scratch(const LtOperator &o, int sm_count) { return GradScratch(o, sm_count).bytes; }

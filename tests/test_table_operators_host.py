@@ -158,3 +158,8 @@ def test_a_scale_that_is_infinite_base_two_is_refused(ctx, scale):  # noqa: F811
     refused(ctx, "INVALID_ARG", "vocabulary_loss_grad", [DY, TAB, IDS, VEC, VEC], result=0, scale=scale)
     x, table, ids = fake(ctx, (5, 16), "bf16"), fake(ctx, (50, 16), "bf16"), fake(ctx, (5,), "i32")
     ctx.vocabulary_loss(x, table, ids, scale=2.3e38)
+
+
+def test_the_products_wait_probe_needs_a_device(ctx):  # noqa: F811
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE"):
+        ctx.debug_product_wait_probe(1000)
