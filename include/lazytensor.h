@@ -62,7 +62,8 @@ typedef enum {
     LT_ERR_DEVICE_INDEX = 9   /* a slot, page number or length in device memory lay outside the cache it indexes, a token outside its table:
                                  reported by the context's first blocking call after the operator that met it, or
                                  after the replay of a graph that captured it (call once the replay is done); the
-                                 operator left out what the index named and did the rest.  Up to 4095 contexts at
+                                 operator left out what the index named and did the rest.  If that call reports
+                                 LT_ERR_DEVICE_TIMEOUT the next one reports this.  Up to 4095 contexts at
                                  a time look separately, any more together.                                */
 } lt_status;
 

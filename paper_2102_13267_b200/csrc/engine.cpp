@@ -236,8 +236,10 @@ void record_replay(lt_ctx *c, Plan *cached, Plan *plan, const Canonical &cg, con
 lt_status sync_and_check(lt_ctx *c) {
     cudaError_t e = cudaStreamSynchronize(c->stream);
     if (e != cudaSuccess) return fail(c, LT_ERR_CUDA, std::string("cudaStreamSynchronize: ") + cudaGetErrorString(e));
+    // (one finding for a call: what is known of indices beside a wait that ran out is said by the next one)
+    if (lt_operator_timeout_take(c->operator_status))
+        return fail(c, LT_ERR_DEVICE_TIMEOUT, "a kernel gave up waiting for its operands or its products; results of that flush are incomplete");
     const LtOperatorStatus found = lt_operator_status_take(c->operator_status);
-    if (found.timeout) return fail(c, LT_ERR_DEVICE_TIMEOUT, "a kernel gave up waiting for its operands or its products; results of that flush are incomplete");
     if (found.attention || found.append || found.embedding || found.loss) {
         std::string what;
         auto add = [&](unsigned there, const char *text) {

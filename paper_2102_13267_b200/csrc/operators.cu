@@ -1261,6 +1261,8 @@ LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status) {
     s.append = __atomic_exchange_n(&status->append, 0u, __ATOMIC_ACQ_REL);
     s.embedding = __atomic_exchange_n(&status->embedding, 0u, __ATOMIC_ACQ_REL);
     s.loss = __atomic_exchange_n(&status->loss, 0u, __ATOMIC_ACQ_REL);
-    s.timeout = __atomic_exchange_n(&status->timeout, 0u, __ATOMIC_ACQ_REL);
+    s.timeout = lt_operator_timeout_take(status);
     return s;
 }
+
+unsigned lt_operator_timeout_take(LtOperatorStatus *status) { return __atomic_exchange_n(&status->timeout, 0u, __ATOMIC_ACQ_REL); }

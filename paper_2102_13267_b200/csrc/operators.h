@@ -75,6 +75,8 @@ cudaError_t lt_operator_status_claim(LtOperatorStatus **out);
 void lt_operator_status_return(LtOperatorStatus *status);
 // What was left there since the last call (by kernels that have completed), and is from now on not.
 LtOperatorStatus lt_operator_status_take(LtOperatorStatus *status);
+// The same for a wait that ran out alone; words about indices stay.
+unsigned lt_operator_timeout_take(LtOperatorStatus *status);
 
 // the operators' own launchers
 cudaError_t lt_launch_rotary(const LtOperator &o, int sm_count, cudaStream_t stream);

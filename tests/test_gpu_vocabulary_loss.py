@@ -33,3 +33,26 @@ def test_the_products_bounded_wait_gives_up_and_is_reported(ctx, lt):  # noqa: F
 def test_the_probe_refuses_more_than_a_second(ctx, lt):  # noqa: F811
     with pytest.raises(lt.LazyTensorError, match="LT_ERR_INVALID_ARG"):
         ctx.debug_product_wait_probe(1_000_000_001)
+
+
+@pytest.mark.parametrize("op", ["embedding", "loss", "append"])
+def test_a_wait_that_gives_up_does_not_hide_an_index_outside(ctx, lt, op):  # noqa: F811
+    """Both in one flush: the first blocking call says the one, the next the other."""
+    g = gen(1)
+    table, ids = normal(g, 30, 16), torch.tensor([3, 30, 5], dtype=torch.int32, device="cuda")
+    if op == "embedding":
+        kept = ctx.embedding(ctx.from_torch(table), ctx.from_torch(ids))
+    elif op == "loss":
+        kept = ctx.vocabulary_loss(ctx.from_torch(normal(g, 3, 16)), ctx.from_torch(table), ctx.from_torch(ids))
+    else:
+        kept = ctx.from_torch(torch.zeros(2, 2, 4, 1, 16, device="cuda"))
+        k = ctx.from_torch(normal(g, 3, 1, 16))
+        ctx.cache_append(kept, k, k, ctx.from_torch(torch.tensor([1, 8, 2], dtype=torch.int32, device="cuda")))
+    ctx.barrier()
+    ctx.debug_product_wait_probe(1000)
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE_TIMEOUT"):
+        ctx.barrier(blocking=True)
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_DEVICE_INDEX.*" + dict(embedding="embedding", loss="vocabulary_loss", append="cache_append")[op]):
+        ctx.barrier(blocking=True)
+    ctx.barrier(blocking=True)
+    del kept
