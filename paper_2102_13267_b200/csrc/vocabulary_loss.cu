@@ -352,23 +352,28 @@ __device__ __forceinline__ void mend_scores(const ProductArgs &a, const Odd &o, 
 // so that each brings only half of the columns' operand: with 128 x 256 to a block shared memory is the bound.  Counters of one
 // launch (8192 x 2048): tensor cores busy 94 % of the time in scores, 89 in P, 80 in dx (4 rounds of 74 tiles where 3.46 would do), 90 in dtable.
 //
-// The tensor cores cut the sum of what they add to off instead of rounding it (half a unit of 2^-23 each time on average, all in one
-// direction): 256 additions, 4096 of K, left scores 7e-6 too small.  Where results are binary32, exact_steps steps of K at a time are
-// summed in tensor memory (0: all of them) and those sums added up in registers, by the warps that take them.  Of the six products
-// of parts the first five are 2^-8 of the last one or less, and so is what is cut off them: they are summed in one go.
-__host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts) { return parts == 3 ? 8 : to != TO_LOSS && to != TO_SCORES ? 0 : blocks == 1 ? 4 : 16; }
+// The tensor cores cut what they add off at a unit of the sum's 2^-23, each product of 16 by itself, instead of rounding: 256 additions,
+// 4096 of K, left scores 7e-6 too small, and since the sum grows meanwhile 64 times as many of one sign left them 7e-3 too small.  Where
+// results are binary32, exact_steps steps of K at a time are summed in tensor memory (0: all of them) and those sums added up in
+// registers, by the warps that take them.  Of the six products of parts the first five are 2^-8 of the last one or less, and so is what
+// is cut off them: ONE_GO steps of them are summed in one go.
+// Gradients in bf16, whose storing costs up to 2^-8, are summed in one go up to ONE_GO steps (8192 products, each cut by 2^-23 at most), and P, which
+// an error of the score multiplies, up to ONE_GO_P; longer ones are FAR: 64 steps at a time.  Taking sums out in between costs tiles of a
+// short K much (loss and gradients of 257 x 512 against 5003 rows: 45 us, 54 if all products did it), which is why they do not.
+constexpr uint32_t ONE_GO = 128, ONE_GO_P = 64;
+__host__ __device__ constexpr uint32_t exact_steps(int blocks, int to, int parts, bool far) { return parts == 3 ? 8 : to != TO_LOSS && to != TO_SCORES ? (far ? 64 : 0) : blocks == 1 ? 4 : 16; }
 template <int PARTS, uint32_t STEPS>
 __device__ __forceinline__ uint32_t chunk_end(const ProductArgs &a, uint32_t step, uint32_t k1) {
     if constexpr (STEPS == 0) return k1;
     if constexpr (PARTS == 3)
-        if (step < 5 * a.blocks_k) return min(k1, 5 * a.blocks_k);
+        if (step < 5 * a.blocks_k) return min(step + ONE_GO, min(k1, 5 * a.blocks_k));
     return min(k1, step + STEPS);
 }
 
-template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS>
+template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS, bool FAR>
 __global__ void __launch_bounds__(THREADS, 1) lt_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs a) {
     using R = Ring<BLOCKS>;
-    constexpr uint32_t STEPS = exact_steps(BLOCKS, TO, PARTS);
+    constexpr uint32_t STEPS = exact_steps(BLOCKS, TO, PARTS, FAR);
     constexpr uint32_t WIDTH_B = WIDTH / BLOCKS;  // of B's rows, per block (at most)
     const uint32_t stages = BLOCKS == 1 ? a.stages : R::STAGES, stage_bytes = BLOCKS == 1 ? a.stage_bytes : R::STAGE;
     extern __shared__ unsigned char product_mem[];
@@ -1318,10 +1323,10 @@ cudaError_t map_of(const Operand &o, uint32_t high, CUtensorMap *map) {
                : cudaErrorInvalidValue;
 }
 
-template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS>
+template <int BLOCKS, bool A_TURNED, bool B_TURNED, int TO, int PARTS, bool FAR>
 cudaError_t launch_product_of(const Operand &x, const Operand &y, const ProductArgs &a, int sm_count, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    auto kernel = lt_product<BLOCKS, A_TURNED, B_TURNED, TO, PARTS>;
+    auto kernel = lt_product<BLOCKS, A_TURNED, B_TURNED, TO, PARTS, FAR>;
     cudaError_t e = allow_shared(kernel, Ring<BLOCKS>::BYTES, ready);
     CUtensorMap map_a, map_b;
     if (e == cudaSuccess) e = map_of(x, ROWS, &map_a);
@@ -1383,7 +1388,10 @@ cudaError_t launch_product(const Operand &x, const Operand &y, ProductArgs a, co
     a.stages = std::min<uint32_t>(Ring<1>::MOST, Ring<1>::STAGES * Ring<1>::STAGE / a.stage_bytes);
     // Beside the limit, a wait may last as long as the work of a tile: its steps (0.4 us each), and scores that are made one by one.
     a.limit_ns += (uint64_t)a.blocks_k * (PARTS == 1 ? 1 : 6) * 4000 + (uint64_t)a.plain_cols * SIDE * 200;
-    return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS>(x, y, a, sm_count, stream);
+    if constexpr (PARTS == 1 && (TO == TO_P || TO == TO_SUM || TO == TO_BF16))
+        if (count_of(a.blocks_k, cut.splits) > (TO == TO_P ? ONE_GO_P : ONE_GO))
+            return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS, true>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS, true>(x, y, a, sm_count, stream);
+    return cut.blocks == 1 ? launch_product_of<1, A_TURNED, B_TURNED, TO, PARTS, false>(x, y, a, sm_count, stream) : launch_product_of<2, A_TURNED, B_TURNED, TO, PARTS, false>(x, y, a, sm_count, stream);
 }
 
 // A packed operand has at least so many rows (zeros): of a tile that holds fewer, copies are slower (5 tokens against 32000 rows of 4096: 73

@@ -56,3 +56,66 @@ def test_a_wait_that_gives_up_does_not_hide_an_index_outside(ctx, lt, op):  # no
         ctx.barrier(blocking=True)
     ctx.barrier(blocking=True)
     del kept
+
+
+# ------------------------------------------------------------------------------------------------ long sums
+# A tensor core's sum cuts each product that it adds off at a unit of 2^-23 of the sum; 64 steps of 64 are 4096 products, and sums
+# of so many are added up in binary32.
+CUT = 4096 * 2.0 ** -23
+
+
+@pytest.fixture()
+def on_the_gpu(monkeypatch):
+    monkeypatch.setattr(ref, "WHERE", ["cuda"])
+
+
+def test_the_tables_gradient_of_many_tokens_rounds_to_the_right_side(ctx):  # noqa: F811
+    """262144 tokens with one and the same P and row of x: a sum of equal terms, whose exact value is just above the middle
+    between two bf16 numbers in some columns.  In one sum, all of whose 262144 products are cut off, it would end below."""
+    tokens, vocab, cols = 1 << 18, 512, 4864
+    p, q = (128 + 69) / 1024, 1 + (torch.arange(cols, device="cuda") % 128).double() / 128
+    x = q.to(torch.bfloat16).expand(tokens, cols).contiguous()
+    table, ids = torch.zeros(vocab, cols, device="cuda", dtype=torch.bfloat16), torch.zeros(tokens, device="cuda", dtype=torch.int32)
+    lse, d, dtable = torch.full((tokens,), -math.log(p), device="cuda"), torch.ones(tokens, device="cuda"), torch.empty_like(table)
+    ctx.assign(lo := ctx.from_torch(dtable), ctx.op("vocabulary_loss_grad", *(ctx.from_torch(t) for t in (x, table, ids, lse, d)), lo, result=1, scale=1.0))
+    ctx.barrier(blocking=True)
+    want = tokens * p * q
+    bound = (CUT + (tokens / 4096 + 2) * ULP) * want
+    ulp = torch.exp2(torch.frexp(want)[1].double() - 8)
+    above = want - (torch.floor(want / ulp) + 0.5) * ulp  # of the middle
+    sure = above.abs() > bound
+    assert int((sure & (above > 0) & (above < 2e-3 * want)).sum()) >= 38  # (columns that the one sum, 5e-3 or more too small, would get wrong)
+    want = want.to(torch.bfloat16)
+    assert torch.equal(dtable[1:, sure], want[sure].expand(vocab - 1, -1))
+
+
+def test_gradients_of_rows_of_262144_columns(ctx, on_the_gpu, monkeypatch):  # noqa: F811
+    """Scores of tens, sums of terms of one sign: P is their exponential, so that what is cut off them counts tens of times."""
+    tokens, vocab, cols = 130, 300, 1 << 18
+    g = gen(40)
+    x, table = normal(g, tokens, cols).abs() + 0.5, normal(g, vocab, cols).abs() + 0.5
+    table *= (torch.linspace(30.0, 60.0, vocab, device="cuda") / (cols * 1.68))[:, None]
+    x, table, ids, d = x.to(torch.bfloat16), table.to(torch.bfloat16), tokens_of(g, tokens, vocab, False), normal(g, tokens)
+    monkeypatch.setattr(ref, "_scores", lambda x, w, scale: (lambda a, b: (scale * a @ b.T, abs(scale) * (CUT + (cols / 4096 + 2) * ULP) * (a.abs() @ b.abs().T)))(x.double(), w.double()))
+    lse = torch.logsumexp(x.double() @ table.double().T, -1).float()
+    # (a table that begins behind a 16-byte boundary is taken in pieces, so that no tile's columns are shared out)
+    got = ctx.vocabulary_loss_grad(ctx.from_torch(x), unaligned(ctx, table, "bf16"), *(ctx.from_torch(t) for t in (ids, lse, d)))
+    r = ref.loss_grad(x, table, ids, lse, d)
+    close(fetch(ctx, got[0]), *r[:2], "dx")
+    close(fetch(ctx, got[1]), *r[2:], "dtable")
+
+
+def test_f32_scores_of_524288_columns(ctx):  # noqa: F811
+    """x is 1 and a second bf16 part of one sign, the table powers of two times small numbers: the largest of the six products of parts is exact,
+    and what is seen is how the sums of the small ones, 2^-8 of it, are made: 128 steps at a time, 8192 products."""
+    tokens, vocab, cols = 70, 300, 1 << 19
+    g = gen(41)
+    x = 1 + 2.0 ** -8 * (0.9 + 0.09 * torch.rand(tokens, cols, device="cuda", generator=g))
+    table = (torch.arange(vocab, device="cuda") % 61 / cols).float()[:, None].expand(vocab, cols).contiguous()
+    ids = torch.zeros(tokens, device="cuda", dtype=torch.int32)
+    loss, lse = (fetch(ctx, t) for t in ctx.vocabulary_loss(*(ctx.from_torch(t) for t in (x, table, ids))))
+    z = (x.double().sum(-1)[:, None] * table[:, 0].double()[None]).cpu()
+    want = torch.logsumexp(z, -1)
+    far = (z * (8 * ULP + 2.0 ** -8 * (8192 * 2.0 ** -23 + cols / 8192 * ULP) + 4 * 2.0 ** -23)).amax(-1) + (vocab / 256 + 320) * ULP + want * 4 * ULP
+    close(lse, want, far)
+    close(loss, want, far + want * 4 * ULP)
