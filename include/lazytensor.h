@@ -175,7 +175,8 @@ typedef enum {
        VOCABULARY_LOSS_GRAD: inputs (x*, table*, targets, lse f32 [..], dloss f32 [..], [out]), attrs {result, scale}, lse
        being the loss's result 1 on the same x and table.  With P = scale dloss (exp(z - lse) - (1 at the target)), zero for tokens without a
        target (whose rows of x, lse and dloss do not count, whatever they hold): result 0: P table, the gradient of x; 1: P^T x, that of
-       the table.  One launch for both.
+       the table.  One launch for both.  The gradient of the table is made relative to the largest finite |dloss|: a weight times a value
+       of x below 2^-126 of that may be lost beside it.
 
        Both take fewer than 2^24 tokens and rows and 2^20 columns, and fewer than 2^44 scores.  Scores beyond 2.3e38 count as infinite.
        bf16 is multiplied as it is and summed in binary32; f32 in three bf16 parts, to 2^-23 of each product.  Temporaries: the loss

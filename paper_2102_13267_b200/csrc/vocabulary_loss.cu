@@ -12,7 +12,7 @@
 //
 // Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value at most, as much as storing
 // the gradients costs; P is near -1 at most targets and rounded little there, which it would not be with dloss in it).  So is x dloss_n where dloss
-// differs from token to token: it is divided by that of the first tokens and dtable multiplied by it, and stays x where they are all alike.
+// differs from token to token: it is divided by the largest |dloss| and dtable multiplied by it, and stays x where they are all alike.
 // f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
 // parts the six largest are added: what is left out is below 2^-23 of each product.
 #include <algorithm>
@@ -1134,22 +1134,28 @@ struct PackArgs {
     float scale;
     uint32_t vocabulary;
     unsigned int *bad_target;
+    const float *largest;       // [LARGEST_BLOCKS], or null
 };
 
-// |dloss| of the first of the first thousand tokens that has a target and a dloss of ordinary size; 1 if there is none. By a whole block.
-__device__ __forceinline__ float unit_of(const PackArgs &a) {
-    __shared__ uint32_t first;
-    if (threadIdx.x == 0) first = 0xffffffffu;
-    __syncthreads();
-    for (uint32_t n = threadIdx.x; n < min(a.present, 1024u); n += blockDim.x) {
-        const float d = fabsf(a.dloss[n]);
-        if ((uint32_t)a.targets[n] < a.vocabulary && d >= 0x1p-60f && d <= 0x1p60f) {
-            atomicMin(&first, n);
-            break;
-        }
+// The largest finite |dloss| of the tokens that have a target; 1 if there is none but zeros.  Relative to it no row of x becomes larger
+// than it is, and what becomes too small for binary32 is below 2^-126 of what the largest one adds.  By a whole block: of all tokens, or
+// of what lt_loss_largest has left of each of its blocks.
+__device__ __forceinline__ float largest_dloss(const float *dloss, const int *targets, uint32_t vocabulary, uint32_t first, uint32_t tokens, uint32_t step) {
+    __shared__ float part[32];
+    float most = 0.f;
+#pragma unroll 8
+    for (uint32_t n = first; n < tokens; n += step) {
+        const float d = fabsf(dloss[n]);
+        if ((!targets || (uint32_t)targets[n] < vocabulary) && d < INFINITY) most = fmaxf(most, d);
     }
-    __syncthreads();
-    return first == 0xffffffffu ? 1.f : fabsf(a.dloss[first]);
+    return block_reduce<true>(most, part);
+}
+constexpr uint32_t LARGEST_BLOCKS = 256, LARGEST_ALONE = 4096;  // up to so many tokens every block that needs it looks for it itself
+__global__ void __launch_bounds__(256) lt_loss_largest(const float *dloss, const int *targets, float *largest, uint32_t tokens, uint32_t vocabulary) {
+    pdl_release();
+    pdl_wait();
+    const float most = largest_dloss(dloss, targets, vocabulary, blockIdx.x * 256 + threadIdx.x, tokens, gridDim.x * 256);
+    if (threadIdx.x == 0) largest[blockIdx.x] = most;
 }
 
 // Eight values in bf16 parts; returns what is not finite among them (1: infinities, 2: no numbers).
@@ -1190,7 +1196,8 @@ __global__ void __launch_bounds__(256) lt_loss_pack(const PackArgs a) {
     const uint32_t eights = a.padded / 8, lane = threadIdx.x % ACROSS;
     float unit = 1.f;
     if (a.scaled) {
-        unit = unit_of(a);
+        unit = a.largest ? largest_dloss(a.largest, nullptr, 0, threadIdx.x, LARGEST_BLOCKS, 256) : largest_dloss(a.dloss, a.targets, a.vocabulary, threadIdx.x, a.present, 256);
+        if (unit == 0.f) unit = 1.f;
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.unit = unit * a.scale;
     }
     for (uint32_t r = blockIdx.x * BESIDE + threadIdx.x / ACROSS; r < a.rows; r += gridDim.x * BESIDE) {
@@ -1420,11 +1427,12 @@ struct Scaled {
     float scale = 1.f;
     uint32_t vocabulary = 0;
     unsigned int *bad_target = nullptr;
+    const float *largest = nullptr;
 };
 template <class T>
 cudaError_t launch_pack(const void *from, uint64_t pitch, uint64_t rows, uint64_t cols, void *to, void *odd, const Scaled &scaled, int sm_count, cudaStream_t stream) {
     const PackArgs p{from,          pitch,           (__nv_bfloat16 *)to, (uint8_t *)odd, (uint32_t)std::max<uint64_t>(rows, LEAST_ROWS), (uint32_t)rows, (uint32_t)cols, (uint32_t)up_to(cols, DEPTH),
-                     (__nv_bfloat16 *)scaled.to, scaled.targets,  scaled.dloss,        scaled.factors, scaled.unit, scaled.scale, scaled.vocabulary, scaled.bad_target};
+                     (__nv_bfloat16 *)scaled.to, scaled.targets,  scaled.dloss,        scaled.factors, scaled.unit, scaled.scale, scaled.vocabulary, scaled.bad_target, scaled.largest};
     const bool wide = is_aligned(from, 16) && pitch * sizeof(T) % 16 == 0, long_rows = p.padded > 8192 || (p.padded >= 512 && rows < 8 * (uint64_t)sm_count);
     const unsigned grid = std::min(count_of(p.rows, long_rows ? 1 : 8), (unsigned)sm_count * 8);
     if (long_rows) return wide ? launch_pdl(lt_loss_pack<T, true, 256>, grid, 256, (size_t)0, stream, p) : launch_pdl(lt_loss_pack<T, false, 256>, grid, 256, (size_t)0, stream, p);
@@ -1518,7 +1526,7 @@ struct LossScratch {
 };
 
 struct GradScratch {
-    size_t unit, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, scores, bytes;
+    size_t unit, largest, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, scores, bytes;
     uint64_t piece, packed_piece;  // the latter where the table does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
@@ -1534,7 +1542,8 @@ struct GradScratch {
         const uint64_t steps = count_of(piece, DEPTH) * (parts == 1 ? 1 : 6), steps_t = count_of(o.rows, DEPTH) * (parts == 1 ? 1 : 6);
         const Cut cx = Cut(o.rows, o.cols, sm_count, 0).split(steps, sm_count), ct = Cut(piece, o.cols, sm_count, 0).split(steps_t, sm_count);
         unit = 0;
-        factors = 256;
+        largest = 256;
+        factors = largest + LARGEST_BLOCKS * 4;
         scaled = factors + up_to(o.rows * 4, 256);
         x = scaled + packed_bytes(o.dtype, o.rows, o.cols);
         odd_x = x + packed_bytes(o.dtype, o.rows, o.cols);
@@ -1724,10 +1733,18 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
     float *factors = (float *)(room + at.factors), *unit = (float *)(room + at.unit);
     // (x is scaled and rows without a target, which may hold anything, left out for the gradient of the table alone)
     const bool x_well = lies_well(o.dtype, o.in[0], o.pitch[0]) && o.rows >= LEAST_ROWS;
-    const Scaled scaled{room + at.scaled, (const int *)o.in[2], (const float *)o.in[4], factors, unit, (float)lt_attr_double(o.attr[1]), (uint32_t)o.vocabulary, &o.status->loss};
-    cudaError_t e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, x_well ? nullptr : room + at.x, room + at.odd_x, scaled, sm_count, stream);
-    const Operand x = x_well ? Operand{o.in[0], o.pitch[0], o.rows, o.cols, 0, false} : packed_operand<T>(room + at.x, o.rows, o.cols, false);
+    Scaled scaled{room + at.scaled, (const int *)o.in[2], (const float *)o.in[4], factors, unit, (float)lt_attr_double(o.attr[1]), (uint32_t)o.vocabulary, &o.status->loss};
+    cudaError_t e = cudaSuccess;
     *launched = 1;
+    if (o.rows > LARGEST_ALONE) {
+        float *largest = (float *)(room + at.largest);
+        scaled.largest = largest;
+        e = launch_pdl(lt_loss_largest, LARGEST_BLOCKS, 256, (size_t)0, stream, scaled.dloss, scaled.targets, largest, (uint32_t)o.rows, scaled.vocabulary);
+        if (e != cudaSuccess) return e;
+        ++*launched;
+    }
+    e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, x_well ? nullptr : room + at.x, room + at.odd_x, scaled, sm_count, stream);
+    const Operand x = x_well ? Operand{o.in[0], o.pitch[0], o.rows, o.cols, 0, false} : packed_operand<T>(room + at.x, o.rows, o.cols, false);
     const uint64_t piece = table_well ? at.piece : at.packed_piece;
     for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
         const uint64_t n = std::min(piece, o.vocabulary - v0), padded = up_to(n, WIDTH);

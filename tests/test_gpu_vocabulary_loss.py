@@ -119,3 +119,33 @@ def test_f32_scores_of_524288_columns(ctx):  # noqa: F811
     far = (z * (8 * ULP + 2.0 ** -8 * (8192 * 2.0 ** -23 + cols / 8192 * ULP) + 4 * 2.0 ** -23)).amax(-1) + (vocab / 256 + 320) * ULP + want * 4 * ULP
     close(lse, want, far)
     close(loss, want, far + want * 4 * ULP)
+
+
+# ------------------------------------------------------------------------------------------------ weights of very different size
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [2, 40, 300, 4096, 4097, 9000])
+def test_losses_weighted_from_2_to_the_minus_60_to_2_to_the_60(ctx, on_the_gpu, dtype, tokens):  # noqa: F811
+    """No product of a gradient, which is 2^70 at most, leaves binary32 on the way, whichever token comes first."""
+    g, t = gen(tokens), TYPES[dtype]
+    x, table, ids = normal(g, tokens, 72, dtype=t, std=2.0 ** 10), normal(g, 200, 72, dtype=t, std=2.0 ** -13), tokens_of(g, tokens, 200)
+    for first, others in ((2.0 ** -60, 2.0 ** 60), (2.0 ** 60, 2.0 ** -60), (0.0, -2.0 ** 100), (math.inf, 3.0), (math.nan, 2.0 ** 90)):
+        d = torch.where(torch.rand(tokens, device="cuda", generator=g) < 0.5, others, 1.0)
+        d[0], d[-1] = first, others
+        ids[0] = 3 if math.isfinite(first) else -1  # (of a token without a target it does not count)
+        lse = torch.logsumexp(x.double() @ table.double().T, -1).float()
+        got = ctx.vocabulary_loss_grad(*(ctx.from_torch(v) for v in (x, table, ids, lse, d)))
+        r = ref.loss_grad(x, table, ids, lse, d)
+        close(fetch(ctx, got[0]), *r[:2], "dx")
+        close(fetch(ctx, got[1]), *r[2:], "dtable")
+
+
+@pytest.mark.parametrize("tokens", [300, 5000])
+def test_a_weight_that_all_tokens_share_leaves_x_as_it_is(ctx, tokens):  # noqa: F811
+    """Gradients of 0 and w for weights are w times those of 0 and 1, to the last bit where w is a power of two."""
+    g = gen(tokens)
+    x, table, ids = normal(g, tokens, 64, dtype=torch.bfloat16), normal(g, 700, 64, dtype=torch.bfloat16, std=0.2), tokens_of(g, tokens, 700)
+    mask = (torch.rand(tokens, device="cuda", generator=g) < 0.7).float()
+    mask[0] = 0.0
+    lse = torch.logsumexp(x.double() @ table.double().T, -1).float()
+    one, other = ([fetch(ctx, r).float() for r in ctx.vocabulary_loss_grad(*(ctx.from_torch(v) for v in (x, table, ids, lse, w * mask)))] for w in (1.0, -2.0 ** -13))
+    assert all(torch.equal(b, a * -2.0 ** -13) for a, b in zip(one, other))
