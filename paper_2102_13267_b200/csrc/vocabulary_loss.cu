@@ -1467,7 +1467,8 @@ inline uint64_t pack_piece(const LtOperator &o, int k, uint64_t rows) {
 
 // Tokens that are scored by plain loads, at a time (0: on the tensor cores), and by how many blocks.  bf16: up to two (one token against
 // 32000 rows of 4096: 46 us, two 47.5; three 57 so, 54 on the tensor cores).  f32, which takes six products there: up to 64, 16 at a time
-// (against 32000 rows of 2048: 5 tokens 54 us, 658 on the tensor cores; 16 88, 382; 64 331, 386).
+// (against 32000 rows of 2048: 5 tokens 54 us, 658 on the tensor cores; 16 88, 382; 64 331, 386), or 8 or 4 where rows are so long that no more
+// of them fit (from 3329 and 6657 columns on; 16 x 4096 190 us, 885 on the tensor cores; 64 757, 888; 16 x 8192 659, 2930; 64 2671, 2936).
 constexpr size_t FEW_BYTES = 72 << 10, SOME_BYTES = 208 << 10;  // of x in shared memory
 struct Few {
     uint32_t at_once = 0, blocks = 0;
@@ -1475,6 +1476,7 @@ struct Few {
         const uint64_t row = up_to(o.cols, 8) * (o.dtype == LT_BF16 ? 2 : 4);
         if (o.rows > (o.dtype == LT_BF16 ? 2 : 64)) return;
         at_once = o.rows <= 2 ? (uint32_t)o.rows : o.rows <= 4 ? 4 : o.rows <= 8 ? 8 : 16;
+        while (at_once > 4 && at_once * row > SOME_BYTES) at_once /= 2;
         if (at_once * row > (at_once <= 2 ? FEW_BYTES : SOME_BYTES)) at_once = 0;
         const uint32_t rows = at_once <= 2 ? FEW_THREADS / 32 * FEW_ROWS : SOME_THREADS / 32 * 4;
         blocks = (uint32_t)std::min<uint64_t>((at_once <= 2 ? 3 : 1) * (uint64_t)sm_count, count_of(o.vocabulary, rows));

@@ -149,3 +149,21 @@ def test_a_weight_that_all_tokens_share_leaves_x_as_it_is(ctx, tokens):  # noqa:
     lse = torch.logsumexp(x.double() @ table.double().T, -1).float()
     one, other = ([fetch(ctx, r).float() for r in ctx.vocabulary_loss_grad(*(ctx.from_torch(v) for v in (x, table, ids, lse, w * mask)))] for w in (1.0, -2.0 ** -13))
     assert all(torch.equal(b, a * -2.0 ** -13) for a, b in zip(one, other))
+
+
+# ------------------------------------------------------------------------------------------------ few tokens of long rows
+@pytest.mark.parametrize("tokens,cols,launches", [(16, 3328, 2), (9, 3329, 2), (16, 4100, 2), (64, 4096, 2), (33, 6656, 2), (8, 6657, 2), (5, 8200, 2), (64, 8193, 2), (3, 13312, 2), (17, 13312, 2),
+                                                  (4, 13313, None), (16, 13400, None)])
+def test_few_f32_tokens_are_scored_by_plain_loads_however_long_their_rows(ctx, tokens, cols, launches):  # noqa: F811
+    """Fewer of them at a time where not all fit in shared memory: two launches, none of which packs the table."""
+    g = gen(tokens + cols)
+    x, table, ids = normal(g, tokens, cols, std=2.0), normal(g, 300, cols, std=cols ** -0.5), tokens_of(g, tokens, 300)
+    ids[0], ids[-1] = -1, 299
+    before = ctx.stats()["kernels_launched"]
+    loss, lse = ctx.vocabulary_loss(*(ctx.from_torch(t) for t in (x, table, ids)))
+    ctx.barrier(blocking=True)
+    if launches:
+        assert ctx.stats()["kernels_launched"] - before == launches
+    a, b, c, d = ref.loss(x, table, ids)
+    close(fetch(ctx, loss), a, b, "loss")
+    close(fetch(ctx, lse), c, d, "lse")
