@@ -179,10 +179,11 @@ typedef enum {
        of x below 2^-126 of that may be lost beside it.
 
        Both take fewer than 2^24 tokens and rows and 2^20 columns, and fewer than 2^44 scores.  Scores beyond 2.3e38 count as infinite.
-       bf16 is multiplied as it is and summed in binary32; f32 in three bf16 parts, to 2^-23 of each product.  Temporaries: the loss
-       16 bytes per token and 256 rows of the table, the gradient up to 256 MB of P and, where dx is a sum of several pieces of
-       it, 4 bytes a value; f32 and rows that are not a multiple of 16 bytes apart are packed piece by piece, up to 96 MB (x as a whole
-       in f32: 6 bytes a value, in the gradient 12). */
+       bf16 is multiplied as it is and summed in binary32; f32 in three bf16 parts, to 2^-23 of each product.  Temporaries: the loss 16 bytes per token and tile of 64 to 256 rows of the table; the gradient P, up to 256 MB or, where that is more,
+       256 rows of the table for all tokens (2 bytes a score, in f32 6), x times dloss (2 bytes a value, in f32 6), dx in binary32 where it
+       is a sum of several pieces of P, and the sums of tiles that several workers share.  f32 and rows that are not a multiple of 16 bytes apart
+       are packed piece by piece, up to 96 MB or 256 rows (x as a whole in f32: 6 bytes a value); there is room for 8 MB, or 256 rows, of x
+       and of the table where other rows begin behind a 16-byte boundary. */
     LT_OP_ROTARY = 70, LT_OP_CACHE_APPEND = 71, LT_OP_PAGED_ATTENTION = 72, LT_OP_RMS_NORM = 73, LT_OP_RMS_NORM_GRAD = 74,
     LT_OP_EMBEDDING = 80, LT_OP_EMBEDDING_GRAD = 81, LT_OP_VOCABULARY_LOSS = 82, LT_OP_VOCABULARY_LOSS_GRAD = 83
 } lt_opcode;

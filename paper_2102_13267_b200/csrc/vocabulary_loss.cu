@@ -1530,6 +1530,7 @@ struct LossScratch {
 struct GradScratch {
     size_t unit, largest, factors, scaled, x, odd_x, odd_table, table, p, sum_x, sum_table, scores, bytes;
     uint64_t piece, packed_piece;  // the latter where the table does not lie well
+    uint64_t x_piece;           // rows of x that are packed at a time where it does not lie well
     uint32_t splits_table;
     GradScratch(const LtOperator &o, int sm_count) {
         const FewGrad few(o, sm_count);
@@ -1547,8 +1548,9 @@ struct GradScratch {
         largest = 256;
         factors = largest + LARGEST_BLOCKS * 4;
         scaled = factors + up_to(o.rows * 4, 256);
+        x_piece = o.dtype == LT_F32 || o.rows < LEAST_ROWS ? o.rows : std::min(o.rows, pack_piece(o, 0, o.rows));
         x = scaled + packed_bytes(o.dtype, o.rows, o.cols);
-        odd_x = x + packed_bytes(o.dtype, o.rows, o.cols);
+        odd_x = x + packed_bytes(o.dtype, x_piece, o.cols);
         odd_table = odd_x + up_to(o.rows + LEAST_ROWS, 256);
         table = odd_table + up_to(piece + LEAST_ROWS, 256);
         splits_table = ct.splits;
@@ -1745,8 +1747,10 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         if (e != cudaSuccess) return e;
         ++*launched;
     }
-    e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, x_well ? nullptr : room + at.x, room + at.odd_x, scaled, sm_count, stream);
-    const Operand x = x_well ? Operand{o.in[0], o.pitch[0], o.rows, o.cols, 0, false} : packed_operand<T>(room + at.x, o.rows, o.cols, false);
+    // (an x that does not lie well is packed as a whole here, or piece by piece for its scores)
+    const uint64_t x_piece = x_well ? o.rows : at.x_piece;
+    const bool x_whole = x_piece == o.rows;
+    e = launch_pack<T>(o.in[0], o.pitch[0], o.rows, o.cols, x_well || !x_whole ? nullptr : room + at.x, room + at.odd_x, scaled, sm_count, stream);
     const uint64_t piece = table_well ? at.piece : at.packed_piece;
     for (uint64_t v0 = 0; v0 < o.vocabulary && e == cudaSuccess; v0 += piece) {
         const uint64_t n = std::min(piece, o.vocabulary - v0), padded = up_to(n, WIDTH);
@@ -1771,18 +1775,37 @@ cudaError_t launch_loss_grad(const LtOperator &o, int sm_count, cudaStream_t str
         a.p_part = (uint32_t)padded;
         a.p_rows = (uint32_t)std::max<uint64_t>(o.rows, LEAST_ROWS);
         plain_args(o, a, o.in[0], room + at.odd_x, room + at.odd_table, rows);
-        const Cut of_scores = n == o.vocabulary ? cut_of_scores(o.rows, n, o.cols, o.dtype, sm_count, 64) : Cut(o.rows, n, sm_count, 64);
-        if (of_scores.splits > 1) {
-            a.out = room + at.scores;
-            a.wide = width_of(a.out, n, 4);
-            e = launch_product<false, false, TO_SCORES, PARTS>(x, table, a, of_scores, sm_count, stream);
-            if (e == cudaSuccess) e = launch_pdl(lt_loss_finish<true, PARTS>, a.p_rows, 256, (size_t)0, stream, a, (const float *)a.out, of_scores.splits, (float *)nullptr, (float *)nullptr);
+        for (uint64_t r0 = 0; r0 < o.rows; r0 += x_piece) {
+            const uint64_t m = std::min(x_piece, o.rows - r0);
+            const T *tokens = (const T *)o.in[0] + r0 * o.pitch[0];
+            Operand x{tokens, o.pitch[0], m, o.cols, 0, false};
+            if (!x_well) {
+                if (!x_whole) {
+                    e = launch_pack<T>(tokens, o.pitch[0], m, o.cols, room + at.x, room + at.odd_x, Scaled{}, sm_count, stream);
+                    if (e != cudaSuccess) return e;
+                    ++*launched;
+                }
+                x = packed_operand<T>(room + at.x, m, o.cols, false);
+            }
+            ProductArgs s = a;
+            s.m = (uint32_t)m;
+            s.targets += r0;
+            s.lse += r0;
+            s.p += r0 * s.p_pitch;
+            s.p_rows = x_whole ? a.p_rows : (uint32_t)m;
+            const Cut of_scores = n == o.vocabulary && x_whole ? cut_of_scores(m, n, o.cols, o.dtype, sm_count, 64) : Cut(m, n, sm_count, 64);
+            if (of_scores.splits > 1) {
+                s.out = room + at.scores;
+                s.wide = width_of(s.out, n, 4);
+                e = launch_product<false, false, TO_SCORES, PARTS>(x, table, s, of_scores, sm_count, stream);
+                if (e == cudaSuccess) e = launch_pdl(lt_loss_finish<true, PARTS>, s.p_rows, 256, (size_t)0, stream, s, (const float *)s.out, of_scores.splits, (float *)nullptr, (float *)nullptr);
+                ++*launched;
+            } else {
+                e = launch_product<false, false, TO_P, PARTS>(x, table, s, of_scores, sm_count, stream);
+            }
+            if (e != cudaSuccess) return e;
             ++*launched;
-        } else {
-            e = launch_product<false, false, TO_P, PARTS>(x, table, a, of_scores, sm_count, stream);
         }
-        if (e != cudaSuccess) return e;
-        ++*launched;
         Operand p{a.p, padded * parts, a.p_rows, padded * parts, (uint32_t)padded, false};
         if (o.out[0]) {
             ProductArgs d{};

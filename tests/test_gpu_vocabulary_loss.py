@@ -167,3 +167,43 @@ def test_few_f32_tokens_are_scored_by_plain_loads_however_long_their_rows(ctx, t
     a, b, c, d = ref.loss(x, table, ids)
     close(fetch(ctx, loss), a, b, "loss")
     close(fetch(ctx, lse), c, d, "lse")
+
+
+# ------------------------------------------------------------------------------------------------ memory
+def planned(c, lt, record):  # noqa: F811
+    """Bytes of temporaries that what `record` records takes, as a flush that may not allocate says when it refuses it."""
+    kept = record()
+    with pytest.raises(lt.LazyTensorError, match="LT_ERR_UNSUPPORTED.*bytes of temporaries") as err:
+        c.barrier_static_scratch()
+    c.barrier(blocking=True)
+    del kept
+    return int(str(err.value).split("the graph needs ")[1].split()[0])
+
+
+@pytest.mark.parametrize("tokens,vocab,cols", [(65536, 1000, 512), (16384, 3000, 1024)])
+def test_the_gradients_of_bf16_copy_x_once(ctx, lt, tokens, vocab, cols):  # noqa: F811
+    """P, x scaled, room for pieces of x and the table (8 MB each), and sums of dx and dtable in binary32."""
+    g, t = gen(1), torch.bfloat16
+    v = [normal(g, tokens, cols, dtype=t), normal(g, vocab, cols, dtype=t), tokens_of(g, tokens, vocab), torch.zeros(tokens, device="cuda"), torch.ones(tokens, device="cuda")]
+    h = [ctx.from_torch(x) for x in v]
+    out = [ctx.from_torch(torch.empty_like(x)) for x in v[:2]]
+    need = planned(ctx, lt, lambda: ctx.vocabulary_loss_grad(*h, out=out))
+    p = min(256 << 20, 2 * tokens * (vocab + 255))
+    splits = 4 * (148 // 2) * 256 * 256  # (of products with few tiles: at most a tile's sums for each pair of blocks)
+    assert need <= p + 2 * tokens * cols + (16 << 20) + 4 * tokens * cols * (2 * tokens * vocab > p) + 2 * splits + 16 * tokens
+
+
+@pytest.mark.parametrize("tokens,vocab,cols,where", [(773, 300, 16392, "begins"), (773, 300, 16392, "both"), (60000, 300, 1001, "lies"), (2100, 70000, 4096, "begins")])
+def test_gradients_where_x_is_packed_in_pieces(ctx, on_the_gpu, tokens, vocab, cols, where):  # noqa: F811
+    """bf16 rows that begin behind a 16-byte boundary (the last piece of few of them), and rows of odd length; pieces of P, too."""
+    g, t = gen(tokens), torch.bfloat16
+    x, table, ids, d = normal(g, tokens, cols, dtype=t), normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab), normal(g, tokens)
+    ids[::5] = -1
+    x[0], x[tokens - 1], ids[tokens - 1] = math.nan, math.inf, -1
+    lse = torch.where(ids >= 0, torch.logsumexp(x.double() @ table.double().T, -1), 0.0).float()
+    lx = ctx.from_torch(x) if where == "lies" else unaligned(ctx, x, "bf16")
+    lw = unaligned(ctx, table, "bf16") if where == "both" else ctx.from_torch(table)
+    got = ctx.vocabulary_loss_grad(lx, lw, *(ctx.from_torch(v) for v in (ids, lse, d)))
+    r = ref.loss_grad(x, table, ids, lse, d)
+    close(fetch(ctx, got[0]), *r[:2], "dx")
+    close(fetch(ctx, got[1]), *r[2:], "dtable")
