@@ -8,7 +8,7 @@ import torch
 import table_reference as ref
 from operator_reference import HALF, TYPES, ULP, close
 from test_gpu_operators import ctx, fetch, gen, lt, normal, unaligned  # noqa: F401
-from test_gpu_table_operators import tokens_of
+from test_gpu_table_operators import handles, make_step, step, step64, tokens_of
 
 pytestmark = pytest.mark.gpu
 
@@ -207,3 +207,89 @@ def test_gradients_where_x_is_packed_in_pieces(ctx, on_the_gpu, tokens, vocab, c
     r = ref.loss_grad(x, table, ids, lse, d)
     close(fetch(ctx, got[0]), *r[:2], "dx")
     close(fetch(ctx, got[1]), *r[2:], "dtable")
+
+
+# ------------------------------------------------------------------------------------------------ a training step
+def step64_bounds(s):
+    """The step of test_gpu_table_operators in 64 bits and, for every value, how far binary32 may be from it: the roundings of each
+    operator, and what those of the ones before it become in it."""
+    table, gamma, ids = s["table"].double().cpu(), s["gamma"].double().cpu(), s["ids"].long().cpu()
+    t, d = s["targets"].long().cpu(), s["dloss"].double().cpu()
+    n, (v, c) = ids.numel(), table.shape
+    e = 2.0 * table[ids]
+    r = torch.rsqrt((e * e).mean(-1, keepdim=True) + 1e-6)
+    x, dx_ = gamma * e * r, (gamma * e * r).abs() * (c + 8) * ULP
+    z = x @ table.T
+    dz = dx_ @ table.T.abs() + 2 * (c + 16) * ULP * (x.abs() @ table.T.abs())
+    lse = torch.logsumexp(z, -1)
+    far = (z.abs() * 8 * ULP + dz).amax(-1) + (v / 256 + 320) * ULP + lse.abs() * 4 * ULP
+    there, at = t >= 0, t.clamp(min=0)[:, None]
+    loss = torch.where(there, lse - z.gather(1, at)[:, 0], 0.0)
+    loss_off = torch.where(there, far + dz.gather(1, at)[:, 0] + (loss.abs() + z.gather(1, at)[:, 0].abs()) * 4 * ULP, 0.0)
+    hot = torch.zeros_like(z).scatter_(1, at, 1.0)
+    k = torch.where(there, d, 0.0)[:, None]
+    ez = torch.exp(z - lse[:, None])
+    p, dp = k * (ez - hot), k.abs() * (ez * (dz + far[:, None] + 8 * ULP * (z.abs() + lse.abs()[:, None] + 1)) + 8 * ULP * (ez + hot))
+    gx, gx_off = p @ table, dp @ table.abs() + 2 * (v + 64) * ULP * (p.abs() @ table.abs())
+    dw, dw_off = p.T @ x, dp.T @ x.abs() + p.abs().T @ dx_ + 2 * (n + 64) * ULP * (p.abs().T @ x.abs())
+    # the norm's gradient: r (gamma gx - e r^2 mean(gamma gx e)), and of gamma the sum of gx e r
+    q = (gamma * gx * e).mean(-1, keepdim=True)
+    q_off = ((gamma.abs() * gx_off * e.abs()).mean(-1, keepdim=True) + (c + 8) * ULP * (gamma * gx * e).abs().mean(-1, keepdim=True))
+    ge = r * (gamma * gx - e * r * r * q)
+    ge_off = r * (gamma.abs() * gx_off + (c + 16) * ULP * (gamma * gx).abs() + e.abs() * r * r * (q_off + (2 * c + 16) * ULP * q.abs()))
+    gg, gg_off = (gx * e * r).sum(0), ((gx_off + (c + n + 16) * ULP * gx.abs()) * (e * r).abs()).sum(0)
+    out = dw + 2.0 * torch.zeros_like(table).index_add_(0, ids, ge)
+    size = torch.zeros_like(table).index_add_(0, ids, 2 * ge.abs())
+    off = dw_off + torch.zeros_like(table).index_add_(0, ids, 2 * ge_off) + (n + 4) * ULP * size + 2 * ULP * out.abs()
+    return [(loss, loss_off), (out, off), (gg, gg_off)]
+
+
+def test_every_value_of_a_training_step(ctx):  # noqa: F811
+    """Rows of the table's gradient that few tokens touch are as near as their own terms are, and none is left out."""
+    s, out = make_step(21)
+    want = step64_bounds(s)
+    assert all(torch.allclose(a, b[0], rtol=1e-9, atol=1e-12) for a, b in zip(step64(s), want))
+    # (a bound that tells rows from nothing: nine in ten values of the table's gradient are more than ten bounds away from zero)
+    assert float((want[1][0].abs() > 10 * want[1][1]).double().mean()) > 0.9
+    t, lo = handles(ctx, s, out)
+    for _ in range(3):  # (planned, then matched)
+        for o in out:
+            o.fill_(math.nan)
+        step(ctx, t, lo)
+        ctx.barrier(blocking=True)
+        for got, w, name in zip(out, want, ("loss", "table", "gamma")):
+            close(got, *w, name)
+    for o in out:
+        o.fill_(math.nan)
+    ctx.replay(blocking=True)
+    for got, w, name in zip(out, want, ("loss", "table", "gamma")):
+        close(got, *w, name)
+
+
+def test_two_streams_at_once_give_the_bits_that_each_gives_alone(lt):  # noqa: F811
+    made = []
+    for k in range(2):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            s, out = make_step(50 + k, tokens=500 + 131 * k, vocab=3000 - 700 * k, cols=128)
+            c = lt.LazyContext(device=0, stream=stream.cuda_stream)
+            made.append([stream, out, c, handles(c, s, out), []])
+    torch.cuda.synchronize()
+    for stream, out, c, (t, lo), alone in made:
+        step(c, t, lo)
+        c.barrier(blocking=True)
+        alone += [o.clone() for o in out]
+        torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, out, c, (t, lo), alone in made:
+            with torch.cuda.stream(stream):
+                for o in out:
+                    o.fill_(math.nan)
+            step(c, t, lo)
+            c.barrier()
+        for stream, out, c, (t, lo), alone in made:
+            c.barrier(blocking=True)
+        for stream, out, c, (t, lo), alone in made:
+            assert all(torch.equal(a, b) for a, b in zip(alone, out))
+    for entry in made:
+        entry[2].close()
