@@ -286,6 +286,17 @@ class _Operators:
         self.assign(out, t)
         return t
 
+    def _results(self, name, inputs, out, **attrs) -> tuple:
+        """Both results of an operator that has two.  `out`: two buffers (or None in the place of one)."""
+        out = [None, None] if out is None else list(out)
+        if len(out) != 2:
+            raise ValueError(f"out: 2 results, {len(out)} buffers")
+        made = [self.op(name, *inputs, *(() if o is None else (o,)), result=w, **attrs) for w, o in enumerate(out)]
+        for t, o in zip(made, out):
+            if o is not None:
+                self.assign(o, t)
+        return tuple(made)
+
     def rotary(self, x, positions, frequencies, *, interleaved: bool = False, inverse: bool = False, scale: float = 1.0, out=None):
         """x [tokens, .., head size] with the first 2 P values of every head turned by position x frequency
         (`frequencies`: see rotary_table).  `inverse` gives the gradient of x from the gradient of the result."""
@@ -322,17 +333,8 @@ class _Operators:
     def rms_norm_grad(self, dy, h, gamma, *, residual_grad=None, eps: float = 1e-6, out=None) -> tuple:
         """(gradient of h, gradient of gamma) for y = rms_norm(h, gamma); `residual_grad`, the gradient that reaches h past the
         norm, is added to the first.  `out`: two buffers (or None in the place of one)."""
-        out = [None, None] if out is None else list(out)
-        if len(out) != 2:
-            raise ValueError(f"out: 2 results, {len(out)} buffers")
         inputs = (dy, h, gamma) if residual_grad is None else (dy, h, gamma, residual_grad)
-        made = [self.op("rms_norm_grad", *inputs, *(() if o is None else (o,)), result=w, residual=residual_grad is not None, eps=eps)
-                for w, o in enumerate(out)]
-        for t, o in zip(made, out):
-            if o is not None:
-                self.assign(o, t)
-        return tuple(made)
-
+        return self._results("rms_norm_grad", inputs, out, residual=residual_grad is not None, eps=eps)
 
     def embedding(self, table, ids, *, scale: float = 1.0, out=None):
         """scale table[ids]: [.., columns] for ids [..]; a negative id is padding and gives zeros."""
@@ -344,17 +346,6 @@ class _Operators:
         inputs = (dy, ids) if base is None else (dy, ids, base)
         return self._result("embedding_grad", inputs, out, rows=rows, base=base is not None, scale=scale)
 
-    def _results(self, name, inputs, out, **attrs) -> tuple:
-        """Both results of an operator that has two.  `out`: two buffers (or None in the place of one)."""
-        out = [None, None] if out is None else list(out)
-        if len(out) != 2:
-            raise ValueError(f"out: 2 results, {len(out)} buffers")
-        made = [self.op(name, *inputs, *(() if o is None else (o,)), result=w, **attrs) for w, o in enumerate(out)]
-        for t, o in zip(made, out):
-            if o is not None:
-                self.assign(o, t)
-        return tuple(made)
-
     def vocabulary_loss(self, x, table, targets, *, scale: float = 1.0, out=None) -> tuple:
         """(cross entropy of every token's target, log of the sum of exponentials) of the scores scale x table^T, which are
         never kept; a negative target is not counted and has loss 0."""
@@ -362,7 +353,8 @@ class _Operators:
 
     def vocabulary_loss_grad(self, x, table, targets, lse, dloss, *, scale: float = 1.0, out=None) -> tuple:
         """(gradient of x, gradient of the table) of vocabulary_loss from the gradient dloss of its losses and its second
-        result `lse`."""
+        result `lse`.  With bf16 operands exp(z - lse) - (1 at the target) is rounded to bf16 before it is multiplied, and x dloss
+        where dloss differs from token to token; f32 operands keep 24 bits."""
         return self._results("vocabulary_loss_grad", (x, table, targets, lse, dloss), out, scale=scale)
 
 

@@ -13,8 +13,10 @@
 // Types.  bf16 operands are multiplied as they are, with binary32 sums; P is rounded to bf16 (2^-8 of each value at most, as much as storing
 // the gradients costs; P is near -1 at most targets and rounded little there, which it would not be with dloss in it).  So is x dloss_n where dloss
 // differs from token to token: it is divided by the largest |dloss| and dtable multiplied by it, and stays x where they are all alike.
-// f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly), and of the nine products of
-// parts the six largest are added: what is left out is below 2^-23 of each product.
+// Gradients are 2.0e-3 off as a whole for that (257 x 512 against 5003 rows), the table's 2.6e-3 where every dloss is another; storing exact
+// ones costs 1.65e-3.
+// f32 operands, and P then, are taken as three bf16 parts each (24 bits, exactly, of values above 2^-110; below, the last part is
+// subnormal), and of the nine products of parts the six largest are added: what is left out is below 2^-23 of each product.
 #include <algorithm>
 
 #include "tensor_device.cuh"
@@ -927,10 +929,11 @@ __global__ void __launch_bounds__(SOME_THREADS, 1) lt_loss_some(const FewArgs a)
     }
 }
 
-// The gradients of few tokens, TOKENS at a time (through tiles of 128 tokens most of the work would be padding; figures at FewGrad): a block has whole rows of the table, eight columns to a thread, and with them in registers
-// makes the scores (its threads' sums joined by the warps and then through shared memory), the rows of dtable, and its share of dx, which
-// lt_loss_few_join adds up.  The table is read once and dtable written once; the rows to come are on their way meanwhile.  One token of 4096 bf16
-// against 32000 rows: 98 us, 4.7 TB/s, a barrier per four rows; eight of 2048 f32 174, half of them issue slots.
+// The gradients of few tokens, TOKENS at a time (through tiles of 128 tokens most of the work would be padding; figures at FewGrad):
+// a block has whole rows of the table, eight columns to a thread, and with them in registers makes the scores (its threads' sums
+// joined by the warps and then through shared memory), the rows of dtable, and its share of dx, which lt_loss_few_join adds up.
+// The table is read once and dtable written once; the rows to come are on their way meanwhile.  One token of 4096 bf16 against
+// 32000 rows: 98 us, 4.7 TB/s, a barrier per four rows; eight of 2048 f32 174, half of them issue slots.
 constexpr uint32_t FEW_GRAD_THREADS = 512, FEW_GRAD_COLS = 8;
 
 struct FewGradArgs {
@@ -1483,8 +1486,8 @@ struct Few {
     }
 };
 
-// Tokens whose gradients are made by plain loads, at a time (0: on the tensor cores).  bf16: up to two; f32: up to 16, every eight of them once
-// through the table.  Loss and gradients against 32000 rows of 4096 bf16: one token 150 us, two 169, four 263 (by tiles 255 all of them);
+// Tokens whose gradients are made by plain loads, at a time (0: on the tensor cores), of rows that a block's threads can hold, 4096 columns.
+// bf16: up to two; f32: up to 16, every eight of them once through the table.  Loss and gradients against 32000 rows of 4096 bf16: one token 150 us, two 169, four 263 (by tiles 255 all of them);
 // of 2048 f32: 1 token 144, 4 160, 8 216, 16 523, 32 1150 (by tiles 705, 704, 714, 753, 796).
 struct FewGrad {
     uint32_t at_once = 0, blocks = 0, threads = 0;
