@@ -179,7 +179,13 @@ typedef enum {
        of x below 2^-126 of that may be lost beside it.
 
        Both take fewer than 2^24 tokens and rows and 2^20 columns, and fewer than 2^44 scores.  Scores beyond 2.3e38 count as infinite.
-       bf16 is multiplied as it is and summed in binary32; f32 in three bf16 parts, to 2^-23 of each product.  Temporaries: the loss 16 bytes per token and tile of 64 to 256 rows of the table; the gradient P, up to 256 MB or, where that is more,
+       bf16 is multiplied as it is, f32 in three bf16 parts, to 2^-23 of each product of values above 2^-110.  Sums are binary32; the tensor
+       cores' part of them, up to 1024 products at a time (f32 512, bf16 gradients 8192, scores of P 4096), is cut off instead of rounded, by 2^-23 of the
+       sum for each product at most.  In the gradients of bf16 operands P is rounded to bf16 before it is multiplied (2^-8 of each value at
+       most), and so is x times dloss for the table's where dloss differs from token to token (not up to two tokens of 4096 columns): against 64 bits the gradients
+       are 2.0e-3 off as a whole, the table's 2.6e-3 where every token has another dloss; storing exact ones in bf16 costs 1.65e-3.  f32 operands keep 24 bits throughout.
+
+       Temporaries: the loss 16 bytes per token and tile of 64 to 256 rows of the table; the gradient P, up to 256 MB or, where that is more,
        256 rows of the table for all tokens (2 bytes a score, in f32 6), x times dloss (2 bytes a value, in f32 6), dx in binary32 where it
        is a sum of several pieces of P, and the sums of tiles that several workers share.  f32 and rows that are not a multiple of 16 bytes apart
        are packed piece by piece, up to 96 MB or 256 rows (x as a whole in f32: 6 bytes a value); there is room for 8 MB, or 256 rows, of x
