@@ -293,3 +293,42 @@ def test_two_streams_at_once_give_the_bits_that_each_gives_alone(lt):  # noqa: F
             assert all(torch.equal(a, b) for a, b in zip(alone, out))
     for entry in made:
         entry[2].close()
+
+
+def test_many_tokens_with_weights_of_their_own_captured_and_replayed(lt, on_the_gpu):  # noqa: F811
+    """More tokens than a block looks through for the largest weight, x in pieces; the graph is replayed on new weights, targets and rows of x."""
+    stream = torch.cuda.Stream()
+    g, t = gen(60), torch.bfloat16
+    tokens, vocab, cols = 5003, 300, 1024
+    room = torch.empty(tokens * cols + 64, device="cuda", dtype=t)
+    x = room[1: 1 + tokens * cols].view(tokens, cols)  # (begins behind a 16-byte boundary)
+    table, ids, lse, d = normal(g, vocab, cols, dtype=t, std=cols ** -0.5), tokens_of(g, tokens, vocab), torch.zeros(tokens, device="cuda"), normal(g, tokens)
+    x.copy_(normal(g, tokens, cols, dtype=t))
+    dx, dw = torch.empty(tokens, cols, device="cuda", dtype=t), torch.empty_like(table)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        c = lt.LazyContext(device=0, stream=stream.cuda_stream)
+        lx = c.from_device_ptr(x.data_ptr(), "bf16", tuple(x.shape), keep=room)
+        h = [lx, *(c.from_torch(v) for v in (table, ids, lse, d))]
+        out = [c.from_torch(v) for v in (dx, dw)]
+        c.vocabulary_loss_grad(*h, out=out)
+        c.barrier(blocking=True)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            c.vocabulary_loss_grad(*h, out=out)
+            c.barrier()
+        for size in (2.0 ** -40, 2.0 ** 40):
+            x.copy_(normal(g, tokens, cols, dtype=t))
+            ids.copy_(tokens_of(g, tokens, vocab))
+            ids[::11] = -1
+            d.copy_(normal(g, tokens) * size)
+            lse.copy_(torch.logsumexp(x.double() @ table.double().T, -1))
+            dx.fill_(math.nan), dw.fill_(math.nan)
+            graph.replay()
+            stream.synchronize()
+            r = ref.loss_grad(x, table, ids, lse, d)
+            close(dx, *r[:2], "dx")
+            close(dw, *r[2:], "dtable")
+        c.barrier(blocking=True)
+        del graph
+        c.close()
